@@ -261,6 +261,118 @@ PCPP_API int pcpp_tune_plan_order(const float *in_xyz, int64_t n_in, const float
                                   void *workspace, size_t workspace_bytes, int *best_plan_flags, float *ms_index_order,
                                   float *ms_spatial_order, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Activations in 8 bits, for a backward pass that needs them later.  A row of c channels becomes
+ *   q      [n, c] int8
+ *   codes  [n, pcpp_act_code_bytes(c)] uint8: one code for 32 channels of the row, in order; the rest of the row's
+ *          whole 32-bit words is zero
+ * and stands for the values q * 2^(code - 127).  code is the smallest with which no channel of the 32 rounds past
+ * +-127, at least 1; q is the channel over that power of two, rounded to nearest even.  The values are bf16 numbers
+ * exactly.  Code 255 (q = 0) marks channels of which one is Inf or NaN: they are read as NaN.
+ *   x  [n, c] dtype (PCPP_F32 or PCPP_BF16), row-major, 16-byte aligned, as is q; codes 4-byte aligned.
+ * Errors: INVALID_ARG, UNSUPPORTED (c outside 1..1024, n >= 2^31, dtype).
+ * ------------------------------------------------------------------------------------------- */
+PCPP_API size_t pcpp_act_code_bytes(int c);      /* per row: 4 * ceil(c / 128); 0 if c is outside 1..1024 */
+PCPP_API int pcpp_act_pack(const void *x, int dtype, int64_t n, int c, int8_t *q, uint8_t *codes, void *stream);
+PCPP_API int pcpp_act_unpack(const int8_t *q, const uint8_t *codes, int64_t n, int c, void *x, int dtype, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * pcpp_mvmr_bwd_weight with the layer's input kept in 8 bits (pcpp_act_pack):
+ *   dw[k] = sum_{(o,i,k) in T} dy[o, :] (outer) values(xq, xcodes)[i, :],   dw [K, c_out, c_in] always fp32.
+ *   dy [n_out, c_out] dy_dtype.  The 8-bit values enter the products as they are, dy as in pcpp_mvmr_bwd_weight.
+ * tri_* / seg_offsets as there.  plan may be NULL (with plan_bytes = 0 and plan_flags = 0) unless xq, dy or the
+ * triplet list takes 4 GiB or more.  A code of 255 is a non-finite feature (see the conventions above).
+ * workspace: pcpp_mvmr_packed_workspace_bytes(...) bytes, 256-byte aligned.
+ * Errors: as pcpp_mvmr_bwd_weight.
+ * ------------------------------------------------------------------------------------------- */
+PCPP_API size_t pcpp_mvmr_packed_workspace_bytes(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int K,
+                                                 int dy_dtype);
+PCPP_API int pcpp_mvmr_bwd_weight_packed(const int8_t *xq, const uint8_t *xcodes, const void *dy, float *dw, int dy_dtype,
+                                         int64_t n_in, int64_t n_out, int c_in, int c_out, int K,
+                                         const int32_t *tri_o, const int32_t *tri_i, const int32_t *tri_k,
+                                         const int64_t *seg_offsets, int64_t n_triplets,
+                                         const void *plan, size_t plan_bytes, int plan_flags,
+                                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * What lies between two blocks of a residual network, in one pass: the norm behind a block, its gate, the residual,
+ * and the norm in front of the next block.  Row by row, over c channels, with
+ *   n(v) = v (PCPP_NORM_NONE), v * rstd (PCPP_NORM_RMS) or (v - mean(v)) * rstd (PCPP_NORM_LAYER),
+ *   rstd = 1 / sqrt(mean((v - mean(v))^2) + eps), without the mean for PCPP_NORM_RMS:
+ *
+ *   r = residual_scale * x + sigmoid(gate) * (w_post * n_post(f))
+ *   h = w_pre * n_pre(r)
+ *
+ *   x, r     [n, c] stream_dtype: the residual stream before and behind the block
+ *   f        [n, c] dtype, row pitch ld_f elements: the block's output.  NULL: no block in front, r is x and is not
+ *            written (r NULL); only h is formed
+ *   gate     logits, dtype, row pitch ld_gate elements; gate_cols = 0 (NULL: factor 1), 1 (one for the row) or c
+ *   w_post, w_pre  [c] fp32, NULL: ones
+ *   h        [n, c] dtype: input of the next block; NULL exactly if pre_norm is PCPP_NORM_NONE
+ *   fq, fcodes / hq, hcodes   optional 8-bit copies of f and h (pcpp_act_pack) for the backward pass
+ * stream_dtype is dtype, or PCPP_F32 with dtype PCPP_BF16.  All arithmetic is fp32, each output is rounded once (h
+ * and its 8-bit copy from the unrounded r).  x, r, h and hq, fq are contiguous and 16-byte aligned; f and gate need
+ * only the alignment of an element.  Outputs may not overlap inputs.  A row with an Inf or NaN gives NaN in that row only.
+ *
+ * Gradients.  dr is what flows to r from behind (NULL: nothing), dh what flows to h:
+ *   y = w_pre * dh,  d = dr + rstd * (y - [mean(y)] - n(r) * mean(y * n(r)))          ([..]: PCPP_NORM_LAYER)
+ *   dx = residual_scale * d,  du = sigmoid(gate) * d,  dgate = du * (1 - sigmoid(gate)) * w_post * n(f), summed over
+ *   the row for gate_cols = 1,  df = gradient of n_post for w_post * du, as for h,
+ *   dw_pre = sum over rows of dh * n(r),  dw_post = sum over rows of du * n(f)
+ *   r        as the forward pass wrote it (x where f was NULL); NULL if pre_norm is PCPP_NORM_NONE, like dh
+ *   f, or fq with fcodes (then f is NULL); both may be NULL if there was no block (df NULL) or neither a post norm
+ *            nor a gate
+ *   dx [n, c] stream_dtype; NULL: not wanted.  df [n, c] dtype, dgate [n, gate_cols] dtype: contiguous
+ *   dw_post, dw_pre  [c] fp32; NULL: not wanted
+ *   workspace: pcpp_block_norm_workspace_bytes(n, c) bytes, 256-byte aligned (backward only)
+ * The sums over rows are taken in a fixed order: the same result each time.
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (c outside 1..1024, n >= 2^31, dtype combination).
+ * ------------------------------------------------------------------------------------------- */
+#define PCPP_NORM_NONE   0
+#define PCPP_NORM_RMS    1
+#define PCPP_NORM_LAYER  2
+
+PCPP_API int pcpp_block_norm_fwd(const void *x, const void *f, int64_t ld_f, const void *gate, int64_t ld_gate, int gate_cols,
+                                 const float *w_post, const float *w_pre, int post_norm, int pre_norm,
+                                 float residual_scale, float eps, int64_t n, int c, int stream_dtype, int dtype,
+                                 void *r, void *h, int8_t *fq, uint8_t *fcodes, int8_t *hq, uint8_t *hcodes, void *stream);
+PCPP_API size_t pcpp_block_norm_workspace_bytes(int64_t n, int c);
+PCPP_API int pcpp_block_norm_bwd(const void *dr, const void *dh, const void *r,
+                                 const void *f, int64_t ld_f, const int8_t *fq, const uint8_t *fcodes,
+                                 const void *gate, int64_t ld_gate, int gate_cols,
+                                 const float *w_post, const float *w_pre, int post_norm, int pre_norm,
+                                 float residual_scale, float eps, int64_t n, int c, int stream_dtype, int dtype,
+                                 void *dx, void *df, void *dgate, float *dw_post, float *dw_pre,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Log probabilities of a head's classes (tokens of a vocabulary, labels of points), row by row over v classes:
+ *   lse = log(sum_j exp(x_j)),  log_prob = x_label - lse,  entropy = -sum_j p_j log(p_j),  p_j = exp(x_j - lse),
+ *   and the n_top most probable classes in descending order, of equal logits the lowest index first.
+ *   logits  [n, v] dtype, row pitch ld elements, aligned to an element
+ *   labels  [n] int32; a label outside 0 .. v - 1 is none: log_prob is 0 and has no gradient.  NULL: no labels
+ *   log_prob, entropy  [n] fp32, max_log_sum [n, 2] fp32: max_j x_j and log(sum_j exp(x_j - max)), whose sum is lse;
+ *            each NULL if not wanted (the gradient needs max_log_sum, and entropy for d_entropy)
+ *   top_log_prob, top_index  [n, n_top] fp32, int32; 0 <= n_top <= min(v, PCPP_MAX_ALTERNATIVES)
+ * A class is masked by a logit of -Inf: its probability is 0.  A row in which all are has max_log_sum = (-Inf, 0),
+ * log_prob and top_log_prob -Inf, entropy 0, and no gradient.  A row with a NaN or +Inf has NaN in all floating outputs
+ * (but the maximum); among the classes a NaN ranks as -Inf.
+ *   workspace: pcpp_log_probs_workspace_bytes(...) bytes, 256-byte aligned (may be NULL if that is 0)
+ * Gradient of the logits, from what flows to log_prob and to entropy ([n] fp32, NULL: nothing):
+ *   d_logits_j = d_log_prob * (1[j = label] - p_j) - d_entropy * p_j * (log(p_j) + entropy)
+ *   d_logits  [n, v] dtype, row pitch ld_d; it may be the logits themselves (same pitch), otherwise no overlap.
+ * Errors: INVALID_ARG (also: pitch < v, n_top out of range), WORKSPACE, UNSUPPORTED (n or v >= 2^31, dtype).
+ * ------------------------------------------------------------------------------------------- */
+#define PCPP_MAX_ALTERNATIVES 64
+
+PCPP_API size_t pcpp_log_probs_workspace_bytes(int64_t n, int64_t v, int n_top);
+PCPP_API int pcpp_log_probs_fwd(const void *logits, int dtype, int64_t n, int64_t v, int64_t ld, const int32_t *labels,
+                                int n_top, float *log_prob, float *entropy, float *max_log_sum,
+                                float *top_log_prob, int32_t *top_index, void *workspace, size_t workspace_bytes, void *stream);
+PCPP_API int pcpp_log_probs_bwd(const void *logits, int dtype, int64_t n, int64_t v, int64_t ld, const int32_t *labels,
+                                const float *max_log_sum, const float *entropy, const float *d_log_prob,
+                                const float *d_entropy, void *d_logits, int64_t ld_d, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

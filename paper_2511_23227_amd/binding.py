@@ -15,13 +15,17 @@ PCPP_F32, PCPP_BF16 = 0, 1
 PLAN_FWD, PLAN_BWD_INPUT, PLAN_SPATIAL = 1, 2, 4
 BUILD_TEST_SHORT_LISTS, BUILD_TEST_WIDE_KEYS, BUILD_VOXEL = 0x100, 0x200, 0x400
 PLAN_MASK = PLAN_FWD | PLAN_BWD_INPUT | PLAN_SPATIAL
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ERR_CAPACITY = -2
 
 EXPORTS = ("pcpp_last_error", "pcpp_version", "pcpp_build_triplets_workspace_bytes",
            "pcpp_build_triplets_workspace_bytes_for", "pcpp_plan_bytes",
            "pcpp_build_triplets", "pcpp_mvmr_workspace_bytes", "pcpp_mvmr_fwd", "pcpp_mvmr_bwd_input",
            "pcpp_mvmr_bwd_weight", "pcpp_static_scratch_bytes", "pcpp_mvmr_fwd_static",
-           "pcpp_build_triplets_batched", "pcpp_voxel_subsample_workspace_bytes", "pcpp_voxel_subsample")
+           "pcpp_build_triplets_batched", "pcpp_voxel_subsample_workspace_bytes", "pcpp_voxel_subsample",
+           "pcpp_act_code_bytes", "pcpp_act_pack", "pcpp_act_unpack", "pcpp_mvmr_packed_workspace_bytes",
+           "pcpp_mvmr_bwd_weight_packed", "pcpp_block_norm_fwd", "pcpp_block_norm_workspace_bytes", "pcpp_block_norm_bwd",
+           "pcpp_log_probs_workspace_bytes", "pcpp_log_probs_fwd", "pcpp_log_probs_bwd")
 
 
 class PcppError(RuntimeError):
@@ -81,6 +85,29 @@ def library() -> ctypes.CDLL:
     L.pcpp_static_scratch_bytes.argtypes = []
     L.pcpp_mvmr_fwd_static.restype = i32
     L.pcpp_mvmr_fwd_static.argtypes = [vp, vp, vp, i32, i32] + head + [vp]
+    L.pcpp_act_code_bytes.restype = sz
+    L.pcpp_act_code_bytes.argtypes = [i32]
+    L.pcpp_act_pack.restype = i32
+    L.pcpp_act_pack.argtypes = [vp, i32, i64, i32, vp, vp, vp]
+    L.pcpp_act_unpack.restype = i32
+    L.pcpp_act_unpack.argtypes = [vp, vp, i64, i32, vp, i32, vp]
+    L.pcpp_mvmr_packed_workspace_bytes.restype = sz
+    L.pcpp_mvmr_packed_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32, i32]
+    L.pcpp_mvmr_bwd_weight_packed.restype = i32
+    L.pcpp_mvmr_bwd_weight_packed.argtypes = [vp, vp, vp, vp, i32] + tail
+    block = [vp, i64, i32, vp, vp, i32, i32, f32, f32, i64, i32, i32, i32]     # gate, weights, norms, sizes, types
+    L.pcpp_block_norm_fwd.restype = i32
+    L.pcpp_block_norm_fwd.argtypes = [vp, vp, i64] + block + [vp, vp, vp, vp, vp, vp, vp]
+    L.pcpp_block_norm_workspace_bytes.restype = sz
+    L.pcpp_block_norm_workspace_bytes.argtypes = [i64, i32]
+    L.pcpp_block_norm_bwd.restype = i32
+    L.pcpp_block_norm_bwd.argtypes = [vp, vp, vp, vp, i64, vp, vp] + block + [vp, vp, vp, vp, vp, vp, sz, vp]
+    L.pcpp_log_probs_workspace_bytes.restype = sz
+    L.pcpp_log_probs_workspace_bytes.argtypes = [i64, i64, i32]
+    L.pcpp_log_probs_fwd.restype = i32
+    L.pcpp_log_probs_fwd.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.pcpp_log_probs_bwd.restype = i32
+    L.pcpp_log_probs_bwd.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     _lib = L
     return L
 
@@ -338,3 +365,264 @@ def pcpp_mvmr_bwd_weight(x: torch.Tensor, dy: torch.Tensor, T: Triplets, dw: tor
                                   _ptr(T.tri_o), _ptr(T.tri_i), _ptr(T.tri_k), _ptr(T.seg_offsets), T.n_triplets,
                                   *_plan_args(T), _ptr(ws), ws.numel(), _stream()))
     return dw
+
+
+# ---- the operators around the convolution ------------------------------------------------------------------------
+
+@dataclass
+class Packed:
+    """Rows in 8 bits: values q * 2^(code - 127), one code for 32 channels (255: not finite)."""
+    q: torch.Tensor          # int8 [n, c]
+    codes: torch.Tensor      # uint8 [n, pcpp_act_code_bytes(c)]
+
+
+def _empty_packed(n: int, c: int, device) -> Packed:
+    return Packed(torch.empty((n, c), dtype=torch.int8, device=device),
+                  torch.empty((n, library().pcpp_act_code_bytes(c)), dtype=torch.uint8, device=device))
+
+
+def _check_packed(p: Packed):
+    assert p.q.is_cuda and p.codes.is_cuda and p.q.is_contiguous() and p.codes.is_contiguous()
+    assert p.q.dtype == torch.int8 and p.codes.dtype == torch.uint8
+    assert tuple(p.codes.shape) == (p.q.shape[0], library().pcpp_act_code_bytes(p.q.shape[1]))
+
+
+def _pitch(t: torch.Tensor) -> int:
+    """Row pitch of a [n, c] tensor whose rows are contiguous, in elements."""
+    n, c = t.shape
+    assert c <= 1 or t.stride(1) == 1, "the channels of a row must lie side by side"
+    if n <= 1:
+        return c
+    assert t.stride(0) >= c, "rows must not overlap"
+    return t.stride(0)
+
+
+def pcpp_act_pack(x: torch.Tensor, out: Packed | None = None) -> Packed:
+    """Activations in 8 bits for a later backward pass: blocks of 32 channels of a row share a power of two."""
+    L = library()
+    assert x.is_cuda and x.is_contiguous() and x.dim() == 2
+    n, c = x.shape
+    if out is None:
+        out = _empty_packed(n, c, x.device)
+    _check_packed(out)
+    assert out.q.shape == x.shape
+    _check(L.pcpp_act_pack(_ptr(x), _dtype_code(x), n, c, _ptr(out.q), _ptr(out.codes), _stream()))
+    return out
+
+
+def pcpp_act_unpack(p: Packed, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values of rows in 8 bits; bfloat16 holds them exactly."""
+    L = library()
+    _check_packed(p)
+    n, c = p.q.shape
+    if out is None:
+        out = torch.empty((n, c), dtype=dtype, device=p.q.device)
+    assert out.is_cuda and out.is_contiguous() and out.shape == p.q.shape
+    _check(L.pcpp_act_unpack(_ptr(p.q), _ptr(p.codes), n, c, _ptr(out), _dtype_code(out), _stream()))
+    return out
+
+
+def pcpp_mvmr_bwd_weight_packed(x: Packed, dy: torch.Tensor, T: Triplets, dw: torch.Tensor | None = None,
+                                workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """pcpp_mvmr_bwd_weight from an input that was kept in 8 bits: dW[k] = sum dy[o] (outer) x[i].  T.plan may be None."""
+    L = library()
+    _check_packed(x)
+    assert dy.is_cuda and dy.is_contiguous()
+    c_in, c_out = x.q.shape[1], dy.shape[1]
+    assert x.q.shape[0] == T.n_in and dy.shape[0] == T.n_out
+    if dw is None:
+        dw = torch.empty((T.K, c_out, c_in), dtype=torch.float32, device=dy.device)
+    assert dw.is_cuda and dw.is_contiguous() and dw.dtype == torch.float32 and tuple(dw.shape) == (T.K, c_out, c_in)
+    code = _dtype_code(dy)
+    need = L.pcpp_mvmr_packed_workspace_bytes(T.n_in, T.n_out, T.n_triplets, c_in, c_out, T.K, code)
+    if workspace is None or workspace.numel() < need:
+        workspace = _bytes(need, dy.device)
+    _check(L.pcpp_mvmr_bwd_weight_packed(_ptr(x.q), _ptr(x.codes), _ptr(dy), _ptr(dw), code, T.n_in, T.n_out, c_in, c_out,
+                                         T.K, _ptr(T.tri_o), _ptr(T.tri_i), _ptr(T.tri_k), _ptr(T.seg_offsets),
+                                         T.n_triplets, *_plan_args(T), _ptr(workspace), workspace.numel(), _stream()))
+    return dw
+
+
+@dataclass
+class BlockNorm:
+    """Result of pcpp_block_norm_fwd: the residual stream behind the block, the next block's input, 8-bit copies."""
+    r: torch.Tensor | None
+    h: torch.Tensor | None
+    f_packed: Packed | None = None
+    h_packed: Packed | None = None
+
+
+@dataclass
+class BlockNormGrads:
+    """Result of pcpp_block_norm_bwd; what does not apply is None."""
+    dx: torch.Tensor
+    df: torch.Tensor | None
+    dgate: torch.Tensor | None
+    dw_post: torch.Tensor | None
+    dw_pre: torch.Tensor | None
+
+
+def _weights(w, c):
+    if w is not None:
+        assert w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and tuple(w.shape) == (c,)
+    return _ptr(w)
+
+
+def _gate_args(gate, n, c, dtype):
+    if gate is None:
+        return None, 0, 0
+    assert gate.is_cuda and gate.dtype == dtype and gate.dim() == 2 and gate.shape[0] == n and gate.shape[1] in (1, c)
+    return _ptr(gate), _pitch(gate), int(gate.shape[1])
+
+
+def pcpp_block_norm_fwd(x: torch.Tensor, f: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                        w_post: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, *,
+                        post_norm: int = NORM_RMS, pre_norm: int = NORM_RMS, residual_scale: float = 1.0,
+                        eps: float = 1e-6, dtype: torch.dtype | None = None, pack_f: bool = False,
+                        pack_h: bool = False) -> BlockNorm:
+    """Between two blocks: r = residual_scale x + sigmoid(gate) w_post norm(f),  h = w_pre norm(r).
+
+    x [n, c]: the residual stream, f [n, c]: the block's output (None: r is x, only h is formed), gate [n, c] or [n, 1]:
+    logits; f and gate may be column slices.  post_norm / pre_norm: NORM_NONE, NORM_RMS or NORM_LAYER (pre_norm
+    NORM_NONE: no h).  dtype: type of h where there is no f.  pack_f, pack_h: copies in 8 bits for the backward pass.
+    """
+    L = library()
+    assert x.is_cuda and x.is_contiguous() and x.dim() == 2
+    n, c = x.shape
+    if f is not None:
+        assert f.is_cuda and f.shape == x.shape
+        dtype = f.dtype
+    elif dtype is None:
+        dtype = x.dtype
+    code = {torch.float32: PCPP_F32, torch.bfloat16: PCPP_BF16}.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    r = torch.empty_like(x) if f is not None else None
+    h = torch.empty((n, c), dtype=dtype, device=x.device) if pre_norm != NORM_NONE else None
+    out = BlockNorm(x if f is None else r, h, _empty_packed(n, c, x.device) if pack_f else None,
+                    _empty_packed(n, c, x.device) if pack_h else None)
+    fp, hp = out.f_packed, out.h_packed
+    _check(L.pcpp_block_norm_fwd(_ptr(x), _ptr(f), _pitch(f) if f is not None else c, *_gate_args(gate, n, c, dtype),
+                                 _weights(w_post, c), _weights(w_pre, c), post_norm, pre_norm, float(residual_scale),
+                                 float(eps), n, c, _dtype_code(x), code, _ptr(r), _ptr(h),
+                                 _ptr(fp.q) if fp else None, _ptr(fp.codes) if fp else None,
+                                 _ptr(hp.q) if hp else None, _ptr(hp.codes) if hp else None, _stream()))
+    return out
+
+
+def pcpp_block_norm_bwd(dr: torch.Tensor | None, dh: torch.Tensor | None, r: torch.Tensor | None,
+                        f: torch.Tensor | Packed | None = None, gate: torch.Tensor | None = None,
+                        w_post: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, *,
+                        post_norm: int = NORM_RMS, pre_norm: int = NORM_RMS, residual_scale: float = 1.0,
+                        eps: float = 1e-6, dtype: torch.dtype | None = None, block: bool | None = None,
+                        workspace: torch.Tensor | None = None) -> BlockNormGrads:
+    """Gradients of pcpp_block_norm_fwd.  dr (None: zero) and dh flow to its r and h; r is what it wrote, f what it was
+    given or its copy in 8 bits.  `block`: there was a block, though nothing of f is needed (neither post norm nor gate;
+    default: f is not None).  dtype: type of the block's tensors where neither dh nor f says it."""
+    L = library()
+    packed = isinstance(f, Packed)
+    some = dr if dr is not None else dh
+    assert some is not None and some.is_cuda, "neither dr nor dh"
+    n, c = some.shape
+    for t in (dr, dh, r):
+        assert t is None or (t.is_cuda and t.is_contiguous() and tuple(t.shape) == (n, c))
+    if dh is not None:
+        dtype = dh.dtype
+    elif f is not None and not packed:
+        dtype = f.dtype
+    elif gate is not None:
+        dtype = gate.dtype
+    stream_dtype = r.dtype if r is not None else dr.dtype
+    assert dr is None or dr.dtype == stream_dtype
+    if dtype is None:
+        dtype = stream_dtype
+    code = {torch.float32: PCPP_F32, torch.bfloat16: PCPP_BF16}.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    if packed:
+        _check_packed(f)
+        assert tuple(f.q.shape) == (n, c)
+        f_args = (None, c, _ptr(f.q), _ptr(f.codes))
+    elif f is not None:
+        assert f.is_cuda and tuple(f.shape) == (n, c) and f.dtype == dtype
+        f_args = (_ptr(f), _pitch(f), None, None)
+    else:
+        f_args = (None, c, None, None)
+    if block is None:
+        block = f is not None
+    dev = some.device
+    dx = torch.empty((n, c), dtype=stream_dtype, device=dev)
+    df = torch.empty((n, c), dtype=dtype, device=dev) if block else None
+    dgate = torch.empty(tuple(gate.shape), dtype=dtype, device=dev) if gate is not None else None
+    new = lambda wanted: torch.empty(c, dtype=torch.float32, device=dev) if wanted else None  # noqa: E731
+    dw_post, dw_pre = new(block and post_norm != NORM_NONE), new(pre_norm != NORM_NONE)
+    need = L.pcpp_block_norm_workspace_bytes(n, c)
+    if workspace is None or workspace.numel() < need:
+        workspace = _bytes(need, dev)
+    _check(L.pcpp_block_norm_bwd(_ptr(dr), _ptr(dh), _ptr(r), *f_args, *_gate_args(gate, n, c, dtype),
+                                 _weights(w_post, c), _weights(w_pre, c), post_norm, pre_norm, float(residual_scale),
+                                 float(eps), n, c, PCPP_F32 if stream_dtype == torch.float32 else PCPP_BF16, code,
+                                 _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(workspace),
+                                 workspace.numel(), _stream()))
+    return BlockNormGrads(dx, df, dgate, dw_post, dw_pre)
+
+
+@dataclass
+class LogProbs:
+    """Result of pcpp_log_probs_fwd, fp32 [n]; max_log_sum [n, 2]: the row's maximum and the logarithm of its sum of exp(x - maximum);
+    top_* [n, n_top], the most probable classes in descending order."""
+    log_prob: torch.Tensor | None
+    entropy: torch.Tensor
+    max_log_sum: torch.Tensor
+    top_log_prob: torch.Tensor
+    top_index: torch.Tensor
+
+    @property
+    def lse(self) -> torch.Tensor:
+        return self.max_log_sum.sum(1)
+
+
+def _labels(labels, n):
+    if labels is not None:
+        assert labels.is_cuda and labels.is_contiguous() and labels.dtype == torch.int32 and tuple(labels.shape) == (n,)
+    return _ptr(labels)
+
+
+def pcpp_log_probs_fwd(logits: torch.Tensor, labels: torch.Tensor | None = None, n_top: int = 0,
+                       workspace: torch.Tensor | None = None) -> LogProbs:
+    """Log probability of every row's label (a label outside 0 .. v - 1: none, 0), the entropy, and the n_top most probable
+    classes.  logits [n, v], rows may be a slice of wider ones; labels int32 [n]."""
+    L = library()
+    assert logits.is_cuda and logits.dim() == 2
+    n, v = logits.shape
+    dev = logits.device
+    code, ld = _dtype_code(logits), _pitch(logits)
+    word = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)  # noqa: E731
+    out = LogProbs(word(n) if labels is not None else None, word(n), word(n, 2), word(n, n_top), word(n, n_top, dtype=torch.int32))
+    need = L.pcpp_log_probs_workspace_bytes(n, v, n_top)
+    if need and (workspace is None or workspace.numel() < need):
+        workspace = _bytes(need, dev)
+    _check(L.pcpp_log_probs_fwd(_ptr(logits), code, n, v, ld, _labels(labels, n), n_top, _ptr(out.log_prob),
+                                _ptr(out.entropy), _ptr(out.max_log_sum), _ptr(out.top_log_prob), _ptr(out.top_index),
+                                _ptr(workspace) if need else None, workspace.numel() if need else 0, _stream()))
+    return out
+
+
+def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forward: LogProbs,
+                       d_log_prob: torch.Tensor | None = None, d_entropy: torch.Tensor | None = None,
+                       out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of the logits from what flows to log_prob and to entropy (fp32 [n]).  out: where it goes, by default a new
+    tensor; it may be the logits."""
+    L = library()
+    assert logits.is_cuda and logits.dim() == 2
+    n, v = logits.shape
+    assert forward.max_log_sum.is_cuda and forward.max_log_sum.is_contiguous() and tuple(forward.max_log_sum.shape) == (n, 2)
+    for t in (d_log_prob, d_entropy, forward.entropy):
+        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and tuple(t.shape) == (n,))
+    if out is None:
+        out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
+    assert out.is_cuda and out.dtype == logits.dtype and out.shape == logits.shape
+    _check(L.pcpp_log_probs_bwd(_ptr(logits), _dtype_code(logits), n, v, _pitch(logits), _labels(labels, n),
+                                _ptr(forward.max_log_sum), _ptr(forward.entropy), _ptr(d_log_prob), _ptr(d_entropy), _ptr(out),
+                                _pitch(out), _stream()))
+    return out

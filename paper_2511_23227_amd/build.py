@@ -26,6 +26,10 @@ SOURCES = {
     "mvmr_rows_tile.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "mvmr_rows_pc.hip": [],
     "tune.hip": [],
+    "act_pack.hip": [],
+    "block_norm.hip": [],
+    "log_probs.hip": [],
+    "rows_api.hip": [],
 }
 
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", "-Wno-unused-function",

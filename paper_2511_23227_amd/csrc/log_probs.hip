@@ -1,0 +1,438 @@
+// Log probabilities of given classes, entropy and the most probable classes of every row of logits, and the gradient of the logits.
+//
+//   m = max x, S = sum exp(x - m), T = sum exp(x - m) (x - m)        one pass over the row, in 32 bits; when the maximum grows by g,
+//                                                                     S and T become S exp(-g) and exp(-g) (T - g S)
+//   log p_j = (x_j - m) - log S,  entropy = log S - T / S             (m and log S apart: their sum would lose log S beside a large m)
+//   d_j = d_log_prob (1[j = label] - p_j) - d_entropy p_j (log p_j + entropy)
+//
+// A masked class has x = -inf (or the type's lowest value): its terms are zero.  A row without any class has log probabilities -inf,
+// entropy 0 and no gradient.  A row that holds a NaN or +inf has NaN everywhere but in its indices.
+//
+// Bound by memory, and in bf16 nearly as much by the exponentials.  Rows of up to 512 classes lie in the registers of a few lanes;
+// longer ones are walked by a thread block, or, where there are few rows, by several, whose sums a second kernel joins.
+// The most probable classes are kept as a list, sorted over the lanes of a wave, of 64-bit keys: the value in an order-preserving
+// form above the complement of the index, so that of equal values the lowest index is the largest key.  Hardly any element of a long
+// row passes the list's last entry, and only one that does costs more than the comparison.
+
+#include "log_probs.h"
+#include "row_ops.h"
+
+namespace pcpp {
+
+namespace {
+
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int64_t MAX_BLOCKS = 1 << 22;                            // (a grid has fewer than 2^32 threads)
+constexpr int SMALL = 512;                                        // classes of the rows that lie in registers
+constexpr float LOG2E = 1.44269504f;
+typedef unsigned long long key_t64;
+
+__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+// A logarithm of a probability beside the probability, in products of the two: below -104 the probability is zero, and so has the product to
+// be, for -inf too.
+__device__ inline float bounded(float log_p) { return fmaxf(log_p, -1e4f); }
+
+__device__ inline uint32_t ordered(float x)                       // same order as the values; -0 is 0, a NaN is -inf
+{
+    const uint32_t b = __float_as_uint(x != x ? -__builtin_inff() : x + 0.f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ inline float from_ordered(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o ^ 0x80000000u : ~o); }
+__device__ inline key_t64 key_of(float x, uint32_t index) { return (key_t64)ordered(x) << 32 | (uint32_t)~index; }
+__device__ inline uint32_t key_index(key_t64 k) { return ~(uint32_t)k; }
+__device__ inline float key_value(key_t64 k) { return from_ordered((uint32_t)(k >> 32)); }
+
+__device__ inline key_t64 lane_of(key_t64 k, int lane)
+{
+    return (key_t64)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
+}
+
+// The largest keys seen by a wave: lane j holds the (j + 1)-th, 0 where there are fewer.
+struct TopList {
+    key_t64 mine = 0, last = 0;                                   // last: lane n_top - 1's, the one to pass
+    int n_top;
+    __device__ inline void insert(key_t64 k, int lane)            // k: the same in all lanes, larger than `last`
+    {
+        const int at = __popcll(__ballot(mine > k));
+        const key_t64 before = __shfl_up(mine, 1);
+        mine = lane < at ? mine : (lane == at ? k : before);
+        last = lane_of(mine, n_top - 1);
+    }
+    __device__ inline void offer(key_t64 k, int lane)             // every lane's own, 0: none
+    {
+        key_t64 left = __ballot(k > last);
+        while (left) {
+            const int from = __ffsll((long long)left) - 1;
+            left &= left - 1;
+            const key_t64 c = lane_of(k, from);
+            if (c > last) insert(c, lane);
+        }
+    }
+};
+
+// sums of a part of a row
+struct Sums {
+    float m, s, t;
+    __device__ inline void join(float om, float os, float ot)
+    {
+        const float nm = fmaxf(m, om);
+        if (nm == -__builtin_inff()) {                            // no class on either side (a NaN is kept)
+            s += os;
+            return;
+        }
+        const float a = bounded(m - nm), b = bounded(om - nm), ea = exp_of(a), eb = exp_of(b);
+        t = ea * (t + a * s) + eb * (ot + b * os);
+        s = ea * s + eb * os;
+        m = nm;
+    }
+};
+__device__ inline Sums join_lanes(Sums v, int lanes)
+{
+    for (int d = 1; d < lanes; d <<= 1) {
+        const float om = __shfl_xor(v.m, d), os = __shfl_xor(v.s, d), ot = __shfl_xor(v.t, d);
+        v.join(om, os, ot);
+    }
+    return v;
+}
+
+// what a row's sums say; NaN in S reaches everything
+__device__ inline float row_results(const LogProbsFwd &a, int64_t row, const Sums &v, float x_label, bool labelled)
+{
+    const bool empty = v.s == 0.f;
+    const float log_s = __builtin_amdgcn_logf(v.s) * 0.693147181f;
+    if (a.max_log_sum) *reinterpret_cast<float2 *>(a.max_log_sum + 2 * row) = float2{v.m, empty ? 0.f : log_s};
+    if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - v.t / v.s;
+    if (a.log_prob) {
+        const float lp = empty ? -__builtin_inff() : (x_label - v.m) - log_s;
+        a.log_prob[row] = labelled ? lp : 0.f;
+    }
+    return log_s;
+}
+__device__ inline float top_value(const Sums &v, float x, float log_s) { return v.s == 0.f ? -__builtin_inff() : (x - v.m) - log_s; }
+
+// ---- rows in registers: LPR lanes a row, lane l holding the classes l + LPR e ------------------------------------------------
+template <typename T, int LPR>
+__global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
+{
+    constexpr int ROWS = THREADS / LPR, E = 8;
+    const int l = (int)threadIdx.x % LPR;
+    const int v = (int)a.v;
+    // (a row's lanes leave together)
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
+        const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+        float xs[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) xs[e] = l + LPR * e < v ? one_float<T>(x[l + LPR * e]) : -__builtin_inff();
+        const int label = a.labels ? a.labels[row] : -1;
+        const bool labelled = label >= 0 && label < v;
+        Sums u{-__builtin_inff(), 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < E; ++e) u.m = fmaxf(u.m, xs[e]);
+        u.m = row_max<LPR>(u.m);
+        const float m0 = u.m == -__builtin_inff() ? 0.f : u.m;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = xs[e] - m0, p = exp_of(d);
+            u.s += p;
+            u.t = __builtin_fmaf(p, bounded(d), u.t);
+        }
+        u.s = row_sum<LPR>(u.s);
+        u.t = row_sum<LPR>(u.t);
+        if (l == 0) row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
+        const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
+        // one class after the other: the largest of the lane's, then of the row's lanes; of equal ones the lowest index
+        uint32_t taken = 0u;
+        for (int k = 0; k < a.n_top; ++k) {
+            key_t64 best = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const key_t64 key = key_of(xs[e], (uint32_t)(l + LPR * e));
+                if (l + LPR * e < v && !(taken >> e & 1u) && key > best) best = key;
+            }
+#pragma unroll
+            for (int d = 1; d < LPR; d <<= 1) {
+                const key_t64 other = __shfl_xor(best, d);
+                if (other > best) best = other;
+            }
+            const uint32_t index = key_index(best);
+            if ((int)(index % LPR) == l) {
+                taken |= 1u << (index / LPR);
+                a.top_log_prob[row * a.n_top + k] = top_value(u, key_value(best), log_s);
+                a.top_index[row * a.n_top + k] = (int32_t)index;
+            }
+        }
+    }
+}
+
+// ---- long rows ------------------------------------------------------------------------------------------------------------
+// Classes [from, to) of a row by a thread block.
+template <typename T>
+__device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopList &list, bool want_top, int lane)
+{
+    u = Sums{-__builtin_inff(), 0.f, 0.f};
+    // eight classes a lane and step; the wave goes round together, so that the list sees all lanes
+    for (int64_t base = from + (int64_t)(threadIdx.x & ~63u) * 8; base < to; base += THREADS * 8) {
+        const int64_t at = base + lane * 8;
+        float v[8];
+        if (at + 8 <= to) {
+            Eight<T> raw;
+            load_eight(x + at, raw);
+            to_floats(raw, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = at + e < to ? one_float<T>(x[at + e]) : -__builtin_inff();
+        }
+        float m = v[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) m = fmaxf(m, v[e]);
+        if (m > u.m) {
+            if (u.m > -__builtin_inff()) {
+                const float g = bounded(u.m - m), a = exp_of(g);
+                u.t = a * (u.t + g * u.s);
+                u.s *= a;
+            }
+            u.m = m;
+        }
+        const float m0 = u.m == -__builtin_inff() ? 0.f : u.m;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = v[e] - m0, p = exp_of(d);
+            u.s += p;
+            u.t = __builtin_fmaf(p, bounded(d), u.t);
+        }
+        if (want_top && __ballot(!(m < key_value(list.last)) || list.last == 0)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) list.offer(at + e < to ? key_of(v[e], (uint32_t)(at + e)) : 0, lane);
+        }
+    }
+}
+
+struct Partial { float m, s, t, unused; };
+
+// The block's waves' sums and lists: the sums in all threads of wave 0, the list in wave 0.
+__device__ inline void join_waves(Sums &u, TopList &list, bool want_top, int lane, int wave)
+{
+    __shared__ Sums sums[WAVES];
+    __shared__ key_t64 keys[WAVES][64];
+    u = join_lanes(u, 64);
+    if (lane == 0) sums[wave] = u;
+    if (want_top) keys[wave][lane] = list.mine;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < WAVES; ++w) {
+        u.join(sums[w].m, sums[w].s, sums[w].t);
+        if (want_top) list.offer(lane < list.n_top ? keys[w][lane] : 0, lane);
+    }
+}
+
+__device__ inline void store_top(const LogProbsFwd &a, int64_t row, const Sums &u, const TopList &list, float log_s, int lane)
+{
+    if (lane >= a.n_top) return;
+    a.top_log_prob[row * a.n_top + lane] = top_value(u, key_value(list.mine), log_s);
+    a.top_index[row * a.n_top + lane] = (int32_t)key_index(list.mine);
+}
+
+template <typename T>
+__global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, int splits, int64_t per, Partial *parts, key_t64 *keys)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int64_t block = blockIdx.x; block < a.n * splits; block += gridDim.x) {
+        const int64_t row = block / splits;
+        const int split = (int)(block % splits);
+        const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+        const int64_t from = split * per, to = from + per < a.v ? from + per : a.v;
+        Sums u;
+        TopList list;
+        list.n_top = a.n_top;
+        const bool want_top = a.n_top > 0;
+        walk(x, from, to, u, list, want_top, lane);
+        join_waves(u, list, want_top, lane, wave);
+        if (wave == 0 && splits == 1) {
+            const int64_t label = a.labels ? a.labels[row] : -1;
+            const bool labelled = label >= 0 && label < a.v;
+            float log_s = 0.f;
+            if (lane == 0) log_s = row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
+            log_s = __shfl(log_s, 0);
+            if (want_top) store_top(a, row, u, list, log_s, lane);
+        } else if (wave == 0) {
+            if (lane == 0) parts[block] = Partial{u.m, u.s, u.t, 0.f};
+            if (lane < a.n_top) keys[block * a.n_top + lane] = list.mine;
+        }
+        __syncthreads();                                           // (the next row's sums go where these lay)
+    }
+}
+
+// one wave a row: the sums and lists of its splits
+template <typename T>
+__global__ __launch_bounds__(64) void join_fwd_kernel(const LogProbsFwd a, int splits, const Partial *parts, const key_t64 *keys)
+{
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x;                               // (few rows: they were split)
+    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+    Sums u{-__builtin_inff(), 0.f, 0.f};
+    for (int s = lane; s < splits; s += 64) {
+        const Partial p = parts[row * splits + s];
+        u.join(p.m, p.s, p.t);
+    }
+    u = join_lanes(u, 64);
+    TopList list;
+    list.n_top = a.n_top;
+    const int n = splits * a.n_top;
+    for (int i = 0; i < n; i += 64) list.offer(i + lane < n ? keys[row * n + i + lane] : 0, lane);
+    const int64_t label = a.labels ? a.labels[row] : -1;
+    const bool labelled = label >= 0 && label < a.v;
+    float log_s = 0.f;
+    if (lane == 0) log_s = row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
+    log_s = __shfl(log_s, 0);
+    if (a.n_top > 0) store_top(a, row, u, list, log_s, lane);
+}
+
+// ---- gradient --------------------------------------------------------------------------------------------------------------
+struct RowGrad { float m, log_s, h, dl, dh; int64_t label; };
+__device__ inline RowGrad row_grad(const LogProbsBwd &a, int64_t row)
+{
+    RowGrad g;
+    const int64_t label = a.labels ? a.labels[row] : -1;
+    g.label = label >= 0 && label < a.v ? label : -1;
+    g.m = a.max_log_sum[2 * row];
+    g.log_s = a.max_log_sum[2 * row + 1];
+    const bool empty = g.m == -__builtin_inff() && g.log_s == 0.f;
+    if (empty) g.m = 0.f;                                          // (every x is -inf: p = 0)
+    g.dl = a.d_log_prob && g.label >= 0 && !empty ? a.d_log_prob[row] : 0.f;
+    g.dh = a.d_entropy && !empty ? a.d_entropy[row] : 0.f;
+    g.h = a.d_entropy ? a.entropy[row] : 0.f;
+    return g;
+}
+__device__ inline float grad_of(const RowGrad &g, float x, bool hit)
+{
+    const float lp = (x - g.m) - g.log_s, p = exp_of(lp);
+    return (hit ? g.dl : 0.f) - p * g.dl - g.dh * (p * (bounded(lp) + g.h));
+}
+
+template <typename T, int LPR>
+__global__ __launch_bounds__(THREADS) void small_bwd_kernel(const LogProbsBwd a)
+{
+    constexpr int ROWS = THREADS / LPR, E = 8;
+    const int l = (int)threadIdx.x % LPR;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
+        const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+        T *d = static_cast<T *>(a.d_logits) + row * a.ld_d;
+        const RowGrad g = row_grad(a, row);
+        float xs[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) xs[e] = l + LPR * e < a.v ? one_float<T>(x[l + LPR * e]) : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (l + LPR * e < a.v) d[l + LPR * e] = one_of<T>(grad_of(g, xs[e], l + LPR * e == g.label));
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(THREADS) void long_bwd_kernel(const LogProbsBwd a, int chunks, int64_t per)
+{
+    for (int64_t block = blockIdx.x; block < a.n * chunks; block += gridDim.x) {
+        const int64_t row = block / chunks, from = block % chunks * per;
+        const int64_t to = from + per < a.v ? from + per : a.v;
+        const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+        T *d = static_cast<T *>(a.d_logits) + row * a.ld_d;
+        const RowGrad g = row_grad(a, row);
+        for (int64_t at = from + threadIdx.x * 8; at < to; at += THREADS * 8) {
+            if (at + 8 <= to) {
+                Eight<T> raw;
+                load_eight(x + at, raw);
+                float v[8];
+                to_floats(raw, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = grad_of(g, v[e], at + e == g.label);
+                store_eight(d + at, v);
+            } else {
+                for (int64_t j = at; j < to; ++j) d[j] = one_of<T>(grad_of(g, one_float<T>(x[j]), j == g.label));
+            }
+        }
+    }
+}
+
+// Blocks of a long row: one, unless there are too few rows to occupy the device; then pieces of at least 4096 classes.
+constexpr int64_t WANTED_BLOCKS = 1024;
+struct Split { int splits; int64_t per; };
+Split split_of(int64_t n, int64_t v)
+{
+    int64_t s = n > 0 ? WANTED_BLOCKS / n : 1;
+    const int64_t most = ceil_div(v, 4096);
+    if (s > most) s = most;
+    if (s < 1) s = 1;
+    const int64_t per = (ceil_div(v, s) + 7) / 8 * 8;
+    return Split{(int)ceil_div(v, per), per};
+}
+
+unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < MAX_BLOCKS ? blocks : MAX_BLOCKS); }
+
+template <typename F> void with_lanes(int64_t v, F f)
+{
+    if (v <= 32) return f(std::integral_constant<int, 4>{});
+    if (v <= 64) return f(std::integral_constant<int, 8>{});
+    if (v <= 128) return f(std::integral_constant<int, 16>{});
+    if (v <= 256) return f(std::integral_constant<int, 32>{});
+    return f(std::integral_constant<int, 64>{});
+}
+
+template <typename T>
+int launch_fwd(const LogProbsFwd &a, void *workspace, hipStream_t stream)
+{
+    if (a.v <= SMALL) {
+        with_lanes(a.v, [&](auto lanes) {
+            constexpr int LPR = decltype(lanes)::value;
+            small_fwd_kernel<T, LPR><<<grid_of(ceil_div(a.n, THREADS / LPR)), THREADS, 0, stream>>>(a);
+        });
+        PCPP_HIP_CHECK(hipGetLastError());
+        return PCPP_OK;
+    }
+    const Split s = split_of(a.n, a.v);
+    Partial *parts = static_cast<Partial *>(workspace);
+    key_t64 *keys = reinterpret_cast<key_t64 *>(static_cast<char *>(workspace) + align_up((size_t)a.n * s.splits * sizeof(Partial)));
+    long_fwd_kernel<T><<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per, parts, keys);
+    PCPP_HIP_CHECK(hipGetLastError());
+    if (s.splits == 1) return PCPP_OK;
+    join_fwd_kernel<T><<<(unsigned)a.n, 64, 0, stream>>>(a, s.splits, parts, keys);
+    PCPP_HIP_CHECK(hipGetLastError());
+    return PCPP_OK;
+}
+
+template <typename T>
+int launch_bwd(const LogProbsBwd &a, hipStream_t stream)
+{
+    if (a.v <= SMALL) {
+        with_lanes(a.v, [&](auto lanes) {
+            constexpr int LPR = decltype(lanes)::value;
+            small_bwd_kernel<T, LPR><<<grid_of(ceil_div(a.n, THREADS / LPR)), THREADS, 0, stream>>>(a);
+        });
+    } else {
+        const Split s = split_of(a.n, a.v);
+        long_bwd_kernel<T><<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per);
+    }
+    PCPP_HIP_CHECK(hipGetLastError());
+    return PCPP_OK;
+}
+
+}  // namespace
+
+size_t log_probs_workspace_bytes(int64_t n, int64_t v, int n_top)
+{
+    if (v <= SMALL) return 0;
+    const Split s = split_of(n, v);
+    if (s.splits == 1) return 0;
+    return align_up((size_t)n * s.splits * sizeof(Partial)) + align_up((size_t)n * s.splits * n_top * sizeof(key_t64));
+}
+
+int log_probs_fwd(const LogProbsFwd &a, int dtype, void *workspace, hipStream_t stream)
+{
+    return dtype == PCPP_F32 ? launch_fwd<float>(a, workspace, stream) : launch_fwd<bf16_t>(a, workspace, stream);
+}
+
+int log_probs_bwd(const LogProbsBwd &a, int dtype, hipStream_t stream)
+{
+    return dtype == PCPP_F32 ? launch_bwd<float>(a, stream) : launch_bwd<bf16_t>(a, stream);
+}
+
+}  // namespace pcpp

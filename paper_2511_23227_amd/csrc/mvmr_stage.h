@@ -48,6 +48,7 @@ __device__ static inline void split_pair(float x0, float x1, uint32_t &p1, uint3
 // of fewer channels than a lane reads.
 template <int RL, bool NARROW>
 struct Stage {
+    static constexpr bool CODED = false;
     static constexpr int ES = 2, NV = 8;                             // bytes of a channel, channels per lane
     static constexpr int CHK = RL * NV, NT = CHK / 16, PL = 1;
     static constexpr int NI = RL / 2, RPI = 64 / RL;                 // load instructions per window, rows per instruction
@@ -96,9 +97,8 @@ struct Stage {
         const int pos = place / NV, ch = lane_channel(pos, NV, c) + place % NV;
         return pos * NV < c && ch >= pos * NV ? ch : -1;
     }
-    // Requests of instruction I; offs: lane (m, g) holds the offset of triplet_of_lane's row.  A row's offset reaches its
-    // lanes by the DPP broadcast inside the add that forms the address.
-    template <int I> __device__ inline void load_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t offs, int c)
+    // What lane (m, g) holds of triplet_of_lane's row, in the lanes that read the row with instruction I
+    template <int I> __device__ static inline uint32_t of_row(uint32_t offs)
     {
         uint32_t at = 0u;
         constexpr int P = 16 / RL;                // rows per sixteen lanes
@@ -113,6 +113,13 @@ struct Stage {
             at = (uint32_t)__builtin_amdgcn_update_dpp((int)at, (int)offs, 0x150 + 4 * I + 2, 0xf, 0x4, false);
             at = (uint32_t)__builtin_amdgcn_update_dpp((int)at, (int)offs, 0x150 + 4 * I + 3, 0xf, 0x8, false);
         }
+        return at;
+    }
+    // Requests of instruction I; offs: lane (m, g) holds the offset of triplet_of_lane's row.  A row's offset reaches its
+    // lanes by the DPP broadcast inside the add that forms the address.
+    template <int I> __device__ inline void load_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t offs, int c)
+    {
+        uint32_t at = of_row<I>(offs);
         if constexpr (NARROW) {
             // fewer channels than a lane reads: one at a time (a whole piece could go past the tensor's end)
             at = col == 0u ? at : OOB_OFFSET;
@@ -167,10 +174,81 @@ struct Stage {
     }
 };
 
+// Rows in 8 bits (row_ops.h: q and one code for 32 channels), staged as the bf16 numbers that they are exactly: Stage's layout, half its bytes
+// from memory.  The codes of a row's chunk are one 32-bit word, looked up by the lane that knows the row and handed on like its offset.
+template <int RL, bool NARROW>
+struct Stage8 : Stage<RL, NARROW> {
+    using Base = Stage<RL, NARROW>;
+    static constexpr bool CODED = true;
+    static constexpr int ES = 1, NV = 8;
+    using Base::NI;
+
+    uint32_t q[NI][2];                            // rows in flight
+    uint32_t word;                                // ... and the codes of triplet_of_lane's row
+    uint32_t shift;                               // this lane's code in a word
+
+    __device__ inline void set_chunk(int chunk, int c, int lane)
+    {
+        const int pos = chunk * RL + lane % RL;
+        if constexpr (NARROW) this->col = pos == 0 ? 0u : OOB_OFFSET;
+        else this->col = pos * NV < c ? (uint32_t)lane_channel(pos, NV, c) : 0u;
+        shift = 8u * ((uint32_t)(pos * NV / 32) & 3u);   // (channels of another block that the lane reads too are not its own)
+    }
+    template <int I> __device__ inline void load_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t offs, int c)
+    {
+        uint32_t at = Base::template of_row<I>(offs);
+        if constexpr (NARROW) {
+            at = this->col == 0u ? at : OOB_OFFSET;
+            q[I][0] = q[I][1] = 0u;
+#pragma unroll
+            for (int e = 0; e < NV; ++e) {
+                const int off = (int)(e < c ? at + (uint32_t)e : OOB_OFFSET);
+                q[I][e >> 2] |= (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rs, off, 0, 0) << (8 * (e & 3));
+            }
+        } else {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(at + this->col), 0, 0);
+            q[I][0] = v[0];
+            q[I][1] = v[1];
+        }
+    }
+    __device__ inline void load_codes(const __amdgpu_buffer_rsrc_t &rs, uint32_t off) { word = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, (int)off, 0, 0); }
+    __device__ inline void load(const __amdgpu_buffer_rsrc_t &rs, uint32_t offs, int c)
+    {
+        load_one<0>(rs, offs, c);
+        load_one<1>(rs, offs, c);
+        if constexpr (NI > 2) { load_one<(NI > 2 ? 2 : 0)>(rs, offs, c); load_one<(NI > 2 ? 3 : 0)>(rs, offs, c); }
+        if constexpr (NI > 4) {
+            load_one<(NI > 4 ? 4 : 0)>(rs, offs, c); load_one<(NI > 4 ? 5 : 0)>(rs, offs, c);
+            load_one<(NI > 4 ? 6 : 0)>(rs, offs, c); load_one<(NI > 4 ? 7 : 0)>(rs, offs, c);
+        }
+    }
+    template <int I> __device__ inline void expand()
+    {
+        const float step = __uint_as_float((Base::template of_row<I>(word) >> shift & 255u) << 23);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t p = q[I][i >> 1] >> (16 * (i & 1));
+            this->x[I][i] = cvt_pk_bf16((float)(int8_t)p * step, (float)(int8_t)(p >> 8) * step);
+        }
+    }
+    __device__ inline void store()
+    {
+        expand<0>();
+        expand<1>();
+        if constexpr (NI > 2) { expand<(NI > 2 ? 2 : 0)>(); expand<(NI > 2 ? 3 : 0)>(); }
+        if constexpr (NI > 4) {
+            expand<(NI > 4 ? 4 : 0)>(); expand<(NI > 4 ? 5 : 0)>();
+            expand<(NI > 4 ? 6 : 0)>(); expand<(NI > 4 ? 7 : 0)>();
+        }
+        Base::store();
+    }
+};
+
 // fp32 rows.  Sixteen lanes read a row (or a chunk of it), NV = 2 or 4 channels each; lane (m, g) reads the rows of the
 // triplets 8 g .. 8 g + 7.  Operand tile t holds the channels NV m + t.
 template <int NV_, bool NARROW>
 struct Direct {
+    static constexpr bool CODED = false;
     static constexpr int ES = 4, NV = NV_, CHK = 16 * NV, NT = NV, PL = 3;
     static constexpr uint32_t BYTES = 0;
     __device__ static inline uint32_t triplet_of_lane(int m, int g) { return 8u * (uint32_t)g + ((uint32_t)m & 7u); }

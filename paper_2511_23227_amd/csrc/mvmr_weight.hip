@@ -13,6 +13,7 @@
 
 #include "mvmr_stage.h"
 #include "mvmr_walk.h"
+#include "row_ops.h"
 
 namespace pcpp {
 
@@ -303,6 +304,8 @@ __global__ __launch_bounds__(LDS_WAVES * 64, 2) void weight_lds_kernel(const uin
 // ---------------------------------------------------------------------------------------------
 struct WeightArgs {
     const void *x, *dy;
+    const uint8_t *codes;                                   // x in 8 bits: its rows' codes, code_row bytes each
+    uint32_t code_bytes, code_row;
     float *part;
     const int32_t *tri_o, *tri_i;
     const int64_t *seg;
@@ -333,8 +336,9 @@ constexpr int F32_CHUNK = 768;
 template <typename SO, typename SI>
 __global__ __launch_bounds__(WAVES * 64, (any_min_waves<SO, SI>())) void weight_any_kernel(const WeightArgs a)
 {
-    constexpr int ES = SO::ES, NTO = SO::NT, NTI = SI::NT, PL = SO::PL;
-    constexpr bool F32 = PL > 1;
+    constexpr int NTO = SO::NT, NTI = SI::NT, PL = SO::PL;
+    constexpr bool F32 = PL > 1, CODED = SI::CODED;
+    static_assert(CODED ? SI::PL == 1 : SI::PL == PL, "terms of x");
     static_assert(SEGMENT % (WINDOW * WAVES) == 0, "the waves' batches of a run continue across segments");
     extern __shared__ __attribute__((aligned(256))) char lds[];       // staged rows, [WAVES]; the sums of one row of tiles
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -349,7 +353,8 @@ __global__ __launch_bounds__(WAVES * 64, (any_min_waves<SO, SI>())) void weight_
     const uint32_t p_end = (uint32_t)((p0 + a.chunk < a.n_triplets ? p0 + a.chunk : a.n_triplets) - p0);
     const __amdgpu_buffer_rsrc_t xrs = make_rsrc(a.x, a.x_bytes), drs = make_rsrc(a.dy, a.dy_bytes);
     const __amdgpu_buffer_rsrc_t irs = make_rsrc(a.tri_i, a.tri_bytes), ors = make_rsrc(a.tri_o, a.tri_bytes);
-    const uint32_t xrow = (uint32_t)a.c_in * ES, drow = (uint32_t)a.c_out * ES;
+    const __amdgpu_buffer_rsrc_t crs = make_rsrc(CODED ? a.codes : nullptr, CODED ? a.code_bytes : 0u);
+    const uint32_t xrow = (uint32_t)a.c_in * SI::ES, drow = (uint32_t)a.c_out * SO::ES;
     SO so;
     SI si;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (uint32_t)wave * (SO::BYTES + SI::BYTES);
@@ -378,6 +383,7 @@ __global__ __launch_bounds__(WAVES * 64, (any_min_waves<SO, SI>())) void weight_
     };
     auto load_rows = [&](uint32_t n) {
         const uint32_t oi = ti < n ? ri * xrow : OOB_OFFSET, oo = to < n ? ro * drow : OOB_OFFSET;
+        if constexpr (CODED) si.load_codes(crs, ti < n ? ri * a.code_row + (uint32_t)(sub_i * SI::CHK / 128 * 4) : OOB_OFFSET);
         so.load(drs, oo, a.c_out);
         si.load(xrs, oi, a.c_in);
     };
@@ -430,9 +436,9 @@ __global__ __launch_bounds__(WAVES * 64, (any_min_waves<SO, SI>())) void weight_
                     }
                 }
             } else {
-                v4u bx[PL][NTI];
+                v4u bx[SI::PL][NTI];
 #pragma unroll
-                for (int pl = 0; pl < PL; ++pl) si.tiles(pl, 0, bx[pl]);
+                for (int pl = 0; pl < SI::PL; ++pl) si.tiles(pl, 0, bx[pl]);
                 auto mm = [&](const v4u &av, int q, int i, const v4f &c) {
                     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, av), __builtin_bit_cast(v8bf, bx[q][i]), c, 0, 0, 0);
                 };
@@ -449,9 +455,13 @@ __global__ __launch_bounds__(WAVES * 64, (any_min_waves<SO, SI>())) void weight_
 #pragma unroll
                     for (int i = 0; i < NTI; ++i) {
                         v4f lo = {0.f, 0.f, 0.f, 0.f};
-                        lo = mm(av[2][o], 0, i, mm(av[0][o], 2, i, lo));
-                        lo = mm(av[0][o], 1, i, mm(av[1][o], 1, i, lo));
-                        lo = mm(av[1][o], 0, i, lo);
+                        if constexpr (CODED) {             // x has one term: all three products
+                            lo = mm(av[1][o], 0, i, mm(av[2][o], 0, i, lo));
+                        } else {
+                            lo = mm(av[2][o], 0, i, mm(av[0][o], 2, i, lo));
+                            lo = mm(av[0][o], 1, i, mm(av[1][o], 1, i, lo));
+                            lo = mm(av[1][o], 0, i, lo);
+                        }
                         acc[o][i] = mm(av[0][o], 0, i, acc[o][i]) + lo;
                     }
             }
@@ -651,6 +661,13 @@ int launch_any(const WeightArgs &w, float *dw, hipStream_t stream)
 template <typename SO>
 int launch_any_in(const WeightArgs &w, float *dw, int ci, hipStream_t stream)
 {
+    if (w.codes) {
+        if (w.c_in < 8) return launch_any<SO, Stage8<4, true>>(w, dw, stream);
+        if (ci == 32) return launch_any<SO, Stage8<4, false>>(w, dw, stream);
+        if constexpr (SO::PL == 1 && SO::CHK < 128)
+            if (ci == 128) return launch_any<SO, Stage8<16, false>>(w, dw, stream);
+        return launch_any<SO, Stage8<8, false>>(w, dw, stream);
+    }
     if constexpr (SO::PL > 1) {
         if (w.c_in < 2) return launch_any<SO, Direct<2, true>>(w, dw, stream);
         return ci == 32 ? launch_any<SO, Direct<2, false>>(w, dw, stream) : launch_any<SO, Direct<4, false>>(w, dw, stream);
@@ -663,7 +680,8 @@ int launch_any_in(const WeightArgs &w, float *dw, int ci, hipStream_t stream)
     }
 }
 
-int launch_weight_any(const MvmrArgs &a, float *dw, const int32_t *tri_o, const int64_t *seg, float *part, hipStream_t stream)
+// codes: a.feat is in 8 bits, with these codes (a.in_dtype is dy's type)
+int launch_weight_any(const MvmrArgs &a, const uint8_t *codes, float *dw, const int32_t *tri_o, const int64_t *seg, float *part, hipStream_t stream)
 {
     const bool f32 = a.in_dtype == PCPP_F32;
     const AnyShape s = any_shape(f32, a.n_triplets, a.c_src, a.c_dst);
@@ -672,8 +690,9 @@ int launch_weight_any(const MvmrArgs &a, float *dw, const int32_t *tri_o, const 
     w.x = a.feat; w.dy = a.dense; w.part = part;
     w.tri_o = tri_o; w.tri_i = a.gather; w.seg = seg;
     w.n_triplets = a.n_triplets; w.n_chunks = s.n_chunks;
-    w.x_bytes = (uint32_t)((size_t)a.n_src * a.c_src * es); w.dy_bytes = (uint32_t)((size_t)a.n_centres * a.c_dst * es);
+    w.x_bytes = (uint32_t)((size_t)a.n_src * a.c_src * (codes ? 1 : es)); w.dy_bytes = (uint32_t)((size_t)a.n_centres * a.c_dst * es);
     w.tri_bytes = (uint32_t)((size_t)a.n_triplets * 4);
+    w.codes = codes; w.code_row = (uint32_t)act_code_bytes(a.c_src); w.code_bytes = (uint32_t)((size_t)a.n_src * w.code_row);
     w.K = a.K; w.c_in = a.c_src; w.c_out = a.c_dst; w.chunk = s.chunk; w.n_sub_in = s.n_sub_in; w.n_sub = s.n_sub;
     if (f32) {
         if (a.c_dst < 2) return launch_any_in<Direct<2, true>>(w, dw, s.ci, stream);
@@ -701,7 +720,26 @@ int mvmr_weight_mfma(const MvmrArgs &a, float *dw, const int32_t *tri_o, const i
     float *part = static_cast<float *>(workspace);
     // 256 -> 256: 31 + 22 us for 0.12 M triplets, 576 + 132 for 4.6 M, 4382 + 174 for 32 M (weight_any_kernel and its sums:
     // 54 + 21, 700 + 19, 8278 + 81, since each row is read by four sub-blocks)
-    return lds ? launch_weight_lds(a, dw, tri_o, seg, part, stream) : launch_weight_any(a, dw, tri_o, seg, part, stream);
+    return lds ? launch_weight_lds(a, dw, tri_o, seg, part, stream) : launch_weight_any(a, nullptr, dw, tri_o, seg, part, stream);
+}
+
+// The same from x in 8 bits (q and codes; a.in_dtype is dy's type).  Rows are gathered as they lie and become bf16 on their way through LDS.
+// Not for 256 -> 256 bf16, whose kernel moves rows to LDS without touching them (a bf16 copy of x costs it 0.15 ms of 4.7 for a million
+// points, where weight_any_kernel would take twice the time).
+bool mvmr_weight_packed_usable(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int dy_dtype)
+{
+    return !lds_shape(dy_dtype, c_in, c_out) && any_usable(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
+}
+
+int mvmr_weight_packed(const MvmrArgs &a, const uint8_t *codes, float *dw, const int32_t *tri_o, const int64_t *seg, void *workspace,
+                       hipStream_t stream)
+{
+    return launch_weight_any(a, codes, dw, tri_o, seg, static_cast<float *>(workspace), stream);
+}
+
+bool mvmr_weight_needs_plan(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int dy_dtype)
+{
+    return n_triplets > 0 && !lds_shape(dy_dtype, c_in, c_out) && !any_usable(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
 }
 
 size_t mvmr_weight_mfma_workspace_bytes(int64_t n_triplets, int c_in, int c_out, int K, int in_dtype)

@@ -44,10 +44,9 @@ int raise_lds_limit(const void *kernel, size_t bytes)
 
 namespace {
 
-int check_common(const char *fn, const void *a, const void *b, const void *c, int in_dtype, int out_dtype,
-                 int64_t n_in, int64_t n_out, int c_in, int c_out, int K, const int32_t *tri_o,
-                 const int32_t *tri_i, const int32_t *tri_k, const int64_t *seg_offsets, int64_t n_triplets,
-                 const void *plan, size_t plan_bytes, int plan_flags, int need_flags)
+int check_tensors(const char *fn, const void *a, const void *b, const void *c, int in_dtype, int out_dtype, int64_t n_in, int64_t n_out,
+                  int c_in, int c_out, int K, const int32_t *tri_o, const int32_t *tri_i, const int32_t *tri_k,
+                  const int64_t *seg_offsets, int64_t n_triplets)
 {
     if (n_in < 0 || n_out < 0 || n_triplets < 0 || K < 1) {
         set_error("%s: negative size or K < 1", fn);
@@ -61,16 +60,8 @@ int check_common(const char *fn, const void *a, const void *b, const void *c, in
         set_error("%s: null triplet arrays", fn);
         return PCPP_ERR_INVALID_ARG;
     }
-    if (!plan) {
-        set_error("%s: plan is NULL (build it with pcpp_build_triplets)", fn);
-        return PCPP_ERR_INVALID_ARG;
-    }
     if ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) & 15) {
         set_error("%s: tensors must be 16-byte aligned", fn);
-        return PCPP_ERR_INVALID_ARG;
-    }
-    if (reinterpret_cast<uintptr_t>(plan) & 255) {
-        set_error("%s: plan must be 256-byte aligned", fn);
         return PCPP_ERR_INVALID_ARG;
     }
     if (K > MAX_K || c_in < 1 || c_out < 1 || c_in > 1024 || c_out > 1024) {
@@ -86,15 +77,29 @@ int check_common(const char *fn, const void *a, const void *b, const void *c, in
         set_error("%s: sizes must be below 2^31", fn);
         return PCPP_ERR_UNSUPPORTED;
     }
-    if ((plan_flags & ~PLAN_FLAG_MASK) || (plan_flags & need_flags) != need_flags) {
-        set_error("%s: plan_flags 0x%x lack the part this call reads (0x%x) or hold unknown bits", fn, plan_flags,
-                  need_flags);
-        return PCPP_ERR_INVALID_ARG;
-    }
     int t = 1;
     while (t * t * t < K) ++t;
     if (t * t * t != K) {
         set_error("%s: K must be a cube", fn);
+        return PCPP_ERR_INVALID_ARG;
+    }
+    return PCPP_OK;
+}
+
+int check_plan(const char *fn, int64_t n_in, int64_t n_out, int K, int64_t n_triplets, const void *plan, size_t plan_bytes, int plan_flags,
+               int need_flags)
+{
+    if (!plan) {
+        set_error("%s: plan is NULL (build it with pcpp_build_triplets)", fn);
+        return PCPP_ERR_INVALID_ARG;
+    }
+    if (reinterpret_cast<uintptr_t>(plan) & 255) {
+        set_error("%s: plan must be 256-byte aligned", fn);
+        return PCPP_ERR_INVALID_ARG;
+    }
+    if ((plan_flags & ~PLAN_FLAG_MASK) || (plan_flags & need_flags) != need_flags) {
+        set_error("%s: plan_flags 0x%x lack the part this call reads (0x%x) or hold unknown bits", fn, plan_flags,
+                  need_flags);
         return PCPP_ERR_INVALID_ARG;
     }
     const size_t need = plan_layout(n_in, n_out, K, n_triplets, plan_flags).bytes;
@@ -103,6 +108,16 @@ int check_common(const char *fn, const void *a, const void *b, const void *c, in
         return PCPP_ERR_WORKSPACE;
     }
     return PCPP_OK;
+}
+
+int check_common(const char *fn, const void *a, const void *b, const void *c, int in_dtype, int out_dtype,
+                 int64_t n_in, int64_t n_out, int c_in, int c_out, int K, const int32_t *tri_o,
+                 const int32_t *tri_i, const int32_t *tri_k, const int64_t *seg_offsets, int64_t n_triplets,
+                 const void *plan, size_t plan_bytes, int plan_flags, int need_flags)
+{
+    if (int rc = check_tensors(fn, a, b, c, in_dtype, out_dtype, n_in, n_out, c_in, c_out, K, tri_o, tri_i, tri_k, seg_offsets, n_triplets))
+        return rc;
+    return check_plan(fn, n_in, n_out, K, n_triplets, plan, plan_bytes, plan_flags, need_flags);
 }
 
 PlanSideView side_view(const void *plan, const SideLayout &s, bool spatial)
@@ -155,6 +170,12 @@ bool workspace_expected(int in_dtype, int c_in, int c_out, int K)
     if (K > 64) return in_dtype == PCPP_BF16 && c_in == 256 && c_out == 256;
     if (in_dtype == PCPP_F32) return c_in == c_out && (c_in == 32 || c_in == 64);
     return (c_in == 64 && (c_out == 64 || c_out == 128)) || (c_in == 128 && c_out == 64) || (c_in == 256 && c_out == 256);
+}
+
+// The weight gradient from x in 8 bits goes by way of a copy of x where no kernel takes it as it is (256 -> 256 bf16, tensors of 4 GiB and more).
+bool packed_needs_copy(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int dy_dtype)
+{
+    return n_triplets > 0 && !mvmr_weight_packed_usable(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
 }
 
 constexpr int MAX_DEVICES = 64;
@@ -310,6 +331,62 @@ int pcpp_mvmr_bwd_weight(const void *x, const void *dy, float *dw, int in_dtype,
     rc = mvmr_weight_mfma(am, dw, tri_o, seg_offsets, workspace, workspace_bytes, stream, &handled);
     if (rc != PCPP_OK || handled) return rc;
     return mvmr_weight_generic(a, dw, workspace, workspace_bytes, stream);
+}
+
+size_t pcpp_mvmr_packed_workspace_bytes(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int K, int dy_dtype)
+{
+    const size_t w = pcpp_mvmr_workspace_bytes(2, n_in, n_out, n_triplets, c_in, c_out, K, dy_dtype);
+    if (w == 0) return 0;
+    // a copy of x in dy's type, for the kernels that read x in no other
+    const size_t es = dy_dtype == PCPP_F32 ? 4 : 2;
+    const bool copy = packed_needs_copy(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
+    return w + (copy ? align_up((size_t)n_in * c_in * es) : 0);
+}
+
+int pcpp_mvmr_bwd_weight_packed(const int8_t *xq, const uint8_t *xcodes, const void *dy, float *dw, int dy_dtype, int64_t n_in, int64_t n_out,
+                                int c_in, int c_out, int K, const int32_t *tri_o, const int32_t *tri_i, const int32_t *tri_k,
+                                const int64_t *seg_offsets, int64_t n_triplets, const void *plan, size_t plan_bytes, int plan_flags,
+                                void *workspace, size_t workspace_bytes, void *stream_)
+{
+    const char *fn = "pcpp_mvmr_bwd_weight_packed";
+    hipStream_t stream = static_cast<hipStream_t>(stream_);
+    int rc = check_tensors(fn, xq, dw, dy, dy_dtype, PCPP_F32, n_in, n_out, c_in, c_out, K, tri_o, tri_i, tri_k, seg_offsets, n_triplets);
+    if (rc != PCPP_OK) return rc;
+    if (n_in > 0 && n_out > 0 && !xcodes) {
+        set_error("%s: null tensor pointer", fn);
+        return PCPP_ERR_INVALID_ARG;
+    }
+    if (reinterpret_cast<uintptr_t>(xcodes) & 3) {
+        set_error("%s: codes must be 4-byte aligned", fn);
+        return PCPP_ERR_INVALID_ARG;
+    }
+    const bool copy = packed_needs_copy(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
+    const bool planless = !plan && !mvmr_weight_needs_plan(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
+    if (!planless && (rc = check_plan(fn, n_in, n_out, K, n_triplets, plan, plan_bytes, plan_flags, PCPP_PLAN_FWD)) != PCPP_OK) return rc;
+    const size_t need = pcpp_mvmr_packed_workspace_bytes(n_in, n_out, n_triplets, c_in, c_out, K, dy_dtype);
+    if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255)) {
+        set_error("%s: workspace missing, misaligned or smaller than %zu bytes", fn, need);
+        return PCPP_ERR_WORKSPACE;
+    }
+    if (n_triplets == 0) return fill_u32(reinterpret_cast<uint32_t *>(dw), 0u, (int64_t)K * c_out * c_in, stream);
+    MvmrArgs a{};
+    a.feat = xq; a.w = nullptr; a.dst = nullptr; a.dense = dy;
+    a.in_dtype = dy_dtype; a.out_dtype = PCPP_F32;
+    a.n_src = n_in; a.n_centres = n_out; a.c_src = c_in; a.c_dst = c_out; a.K = K;
+    a.gather = tri_i;
+    a.n_triplets = n_triplets;
+    if (!copy) return mvmr_weight_packed(a, xcodes, dw, tri_o, seg_offsets, workspace, stream);
+    const size_t sums = pcpp_mvmr_workspace_bytes(2, n_in, n_out, n_triplets, c_in, c_out, K, dy_dtype);
+    void *x = static_cast<char *>(workspace) + sums;
+    if ((rc = act_unpack(xq, xcodes, n_in, c_in, x, dy_dtype, stream)) != PCPP_OK) return rc;
+    a.feat = x;
+    bool handled = false;
+    rc = mvmr_weight_mfma(a, dw, tri_o, seg_offsets, workspace, sums, stream, &handled);
+    if (rc != PCPP_OK || handled) return rc;
+    const PlanLayout pl = plan_layout(n_in, n_out, K, n_triplets, plan_flags);
+    a.side = side_view(plan, pl.fwd, (plan_flags & PCPP_PLAN_SPATIAL) != 0);
+    if (a.side.gather) a.gather = a.side.gather;
+    return mvmr_weight_generic(a, dw, workspace, sums, stream);
 }
 
 size_t pcpp_static_scratch_bytes(void) { return STATIC_SCRATCH_BYTES; }

@@ -171,5 +171,14 @@ size_t mvmr_weight_workspace_bytes(int64_t n_centres, int c_in, int c_out, int K
 int mvmr_weight_mfma(const MvmrArgs &a, float *dw, const int32_t *tri_o, const int64_t *seg_offsets, void *workspace,
                      size_t workspace_bytes, hipStream_t stream, bool *handled);
 size_t mvmr_weight_mfma_workspace_bytes(int64_t n_triplets, int c_in, int c_out, int K, int in_dtype);
+// ... from x in 8 bits: a.feat = q, a.in_dtype = dy's type; a workspace for mvmr_weight_mfma is enough
+bool mvmr_weight_packed_usable(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int dy_dtype);
+int mvmr_weight_packed(const MvmrArgs &a, const uint8_t *codes, float *dw, const int32_t *tri_o, const int64_t *seg_offsets, void *workspace,
+                       hipStream_t stream);
+bool mvmr_weight_needs_plan(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int dy_dtype);   // the generic kernel's
+
+// ---- activations in 8 bits (act_pack.hip) -------------------------------------------------------------------------------
+int act_pack(const void *x, int dtype, int64_t n, int c, int8_t *q, uint8_t *codes, hipStream_t stream);
+int act_unpack(const int8_t *q, const uint8_t *codes, int64_t n, int c, void *x, int dtype, hipStream_t stream);
 
 }  // namespace pcpp
