@@ -141,8 +141,9 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else None
 
 
-def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+def _stream() -> int:
+    """The current device's current stream as the calls take it (0.2 us; by way of torch.cuda.current_stream() 3)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -368,6 +369,21 @@ def pcpp_mvmr_bwd_weight(x: torch.Tensor, dy: torch.Tensor, T: Triplets, dw: tor
 
 
 # ---- the operators around the convolution ------------------------------------------------------------------------
+# (Their smallest calls take the GPU 3 us, so what happens here counts: addresses go to the library as plain integers.)
+
+_CODES = {torch.float32: PCPP_F32, torch.bfloat16: PCPP_BF16}
+
+
+def _code(dtype: torch.dtype) -> int:
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return code
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
 
 @dataclass
 class Packed:
@@ -376,25 +392,30 @@ class Packed:
     codes: torch.Tensor      # uint8 [n, pcpp_act_code_bytes(c)]
 
 
+def _code_bytes(c: int) -> int:
+    return (c + 127) // 128 * 4
+
+
 def _empty_packed(n: int, c: int, device) -> Packed:
-    return Packed(torch.empty((n, c), dtype=torch.int8, device=device),
-                  torch.empty((n, library().pcpp_act_code_bytes(c)), dtype=torch.uint8, device=device))
+    return Packed(torch.empty((n, c), dtype=torch.int8, device=device), torch.empty((n, _code_bytes(c)), dtype=torch.uint8, device=device))
 
 
 def _check_packed(p: Packed):
-    assert p.q.is_cuda and p.codes.is_cuda and p.q.is_contiguous() and p.codes.is_contiguous()
-    assert p.q.dtype == torch.int8 and p.codes.dtype == torch.uint8
-    assert tuple(p.codes.shape) == (p.q.shape[0], library().pcpp_act_code_bytes(p.q.shape[1]))
+    q, codes = p.q, p.codes
+    assert q.is_cuda and codes.is_cuda and q.is_contiguous() and codes.is_contiguous()
+    assert q.dtype == torch.int8 and codes.dtype == torch.uint8
+    n, c = q.shape
+    assert codes.shape == (n, _code_bytes(c))
 
 
 def _pitch(t: torch.Tensor) -> int:
     """Row pitch of a [n, c] tensor whose rows are contiguous, in elements."""
-    n, c = t.shape
-    assert c <= 1 or t.stride(1) == 1, "the channels of a row must lie side by side"
+    (n, c), (pitch, step) = t.shape, t.stride()
+    assert c <= 1 or step == 1, "the channels of a row must lie side by side"
     if n <= 1:
         return c
-    assert t.stride(0) >= c, "rows must not overlap"
-    return t.stride(0)
+    assert pitch >= c, "rows must not overlap"
+    return pitch
 
 
 def pcpp_act_pack(x: torch.Tensor, out: Packed | None = None) -> Packed:
@@ -404,9 +425,12 @@ def pcpp_act_pack(x: torch.Tensor, out: Packed | None = None) -> Packed:
     n, c = x.shape
     if out is None:
         out = _empty_packed(n, c, x.device)
-    _check_packed(out)
-    assert out.q.shape == x.shape
-    _check(L.pcpp_act_pack(_ptr(x), _dtype_code(x), n, c, _ptr(out.q), _ptr(out.codes), _stream()))
+    else:
+        _check_packed(out)
+        assert out.q.shape == x.shape
+    rc = L.pcpp_act_pack(x.data_ptr(), _code(x.dtype), n, c, out.q.data_ptr(), out.codes.data_ptr(), _stream())
+    if rc:
+        _check(rc)
     return out
 
 
@@ -414,11 +438,15 @@ def pcpp_act_unpack(p: Packed, dtype: torch.dtype = torch.bfloat16, out: torch.T
     """The values of rows in 8 bits; bfloat16 holds them exactly."""
     L = library()
     _check_packed(p)
-    n, c = p.q.shape
+    q = p.q
     if out is None:
-        out = torch.empty((n, c), dtype=dtype, device=p.q.device)
-    assert out.is_cuda and out.is_contiguous() and out.shape == p.q.shape
-    _check(L.pcpp_act_unpack(_ptr(p.q), _ptr(p.codes), n, c, _ptr(out), _dtype_code(out), _stream()))
+        out = torch.empty_like(q, dtype=dtype)
+    else:
+        assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
+    n, c = q.shape
+    rc = L.pcpp_act_unpack(q.data_ptr(), p.codes.data_ptr(), n, c, out.data_ptr(), _code(out.dtype), _stream())
+    if rc:
+        _check(rc)
     return out
 
 
@@ -428,18 +456,23 @@ def pcpp_mvmr_bwd_weight_packed(x: Packed, dy: torch.Tensor, T: Triplets, dw: to
     L = library()
     _check_packed(x)
     assert dy.is_cuda and dy.is_contiguous()
-    c_in, c_out = x.q.shape[1], dy.shape[1]
-    assert x.q.shape[0] == T.n_in and dy.shape[0] == T.n_out
+    (n_in, c_in), (n_out, c_out), K = x.q.shape, dy.shape, T.K
+    assert n_in == T.n_in and n_out == T.n_out
+    dev = dy.device
     if dw is None:
-        dw = torch.empty((T.K, c_out, c_in), dtype=torch.float32, device=dy.device)
-    assert dw.is_cuda and dw.is_contiguous() and dw.dtype == torch.float32 and tuple(dw.shape) == (T.K, c_out, c_in)
-    code = _dtype_code(dy)
-    need = L.pcpp_mvmr_packed_workspace_bytes(T.n_in, T.n_out, T.n_triplets, c_in, c_out, T.K, code)
+        dw = torch.empty((K, c_out, c_in), dtype=torch.float32, device=dev)
+    else:
+        assert dw.is_cuda and dw.is_contiguous() and dw.dtype == torch.float32 and dw.shape == (K, c_out, c_in)
+    code, n = _code(dy.dtype), T.n_triplets
+    need = L.pcpp_mvmr_packed_workspace_bytes(n_in, n_out, n, c_in, c_out, K, code)
     if workspace is None or workspace.numel() < need:
-        workspace = _bytes(need, dy.device)
-    _check(L.pcpp_mvmr_bwd_weight_packed(_ptr(x.q), _ptr(x.codes), _ptr(dy), _ptr(dw), code, T.n_in, T.n_out, c_in, c_out,
-                                         T.K, _ptr(T.tri_o), _ptr(T.tri_i), _ptr(T.tri_k), _ptr(T.seg_offsets),
-                                         T.n_triplets, *_plan_args(T), _ptr(workspace), workspace.numel(), _stream()))
+        workspace = _bytes(need, dev)
+    rc = L.pcpp_mvmr_bwd_weight_packed(x.q.data_ptr(), x.codes.data_ptr(), dy.data_ptr(), dw.data_ptr(), code, n_in, n_out, c_in,
+                                       c_out, K, T.tri_o.data_ptr(), T.tri_i.data_ptr(), T.tri_k.data_ptr(),
+                                       T.seg_offsets.data_ptr(), n, *_plan_args(T), workspace.data_ptr(), workspace.numel(),
+                                       _stream())
+    if rc:
+        _check(rc)
     return dw
 
 
@@ -463,16 +496,18 @@ class BlockNormGrads:
 
 
 def _weights(w, c):
-    if w is not None:
-        assert w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and tuple(w.shape) == (c,)
-    return _ptr(w)
+    if w is None:
+        return None
+    assert w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and w.shape == (c,)
+    return w.data_ptr()
 
 
 def _gate_args(gate, n, c, dtype):
     if gate is None:
         return None, 0, 0
-    assert gate.is_cuda and gate.dtype == dtype and gate.dim() == 2 and gate.shape[0] == n and gate.shape[1] in (1, c)
-    return _ptr(gate), _pitch(gate), int(gate.shape[1])
+    rows, cols = gate.shape
+    assert gate.is_cuda and gate.dtype == dtype and rows == n and (cols == c or cols == 1)
+    return gate.data_ptr(), _pitch(gate), cols
 
 
 def pcpp_block_norm_fwd(x: torch.Tensor, f: torch.Tensor | None = None, gate: torch.Tensor | None = None,
@@ -487,27 +522,31 @@ def pcpp_block_norm_fwd(x: torch.Tensor, f: torch.Tensor | None = None, gate: to
     NORM_NONE: no h).  dtype: type of h where there is no f.  pack_f, pack_h: copies in 8 bits for the backward pass.
     """
     L = library()
-    assert x.is_cuda and x.is_contiguous() and x.dim() == 2
+    assert x.is_cuda and x.is_contiguous()
     n, c = x.shape
     if f is not None:
-        assert f.is_cuda and f.shape == x.shape
+        assert f.is_cuda and f.shape == (n, c)
         dtype = f.dtype
-    elif dtype is None:
-        dtype = x.dtype
-    code = {torch.float32: PCPP_F32, torch.bfloat16: PCPP_BF16}.get(dtype)
-    if code is None:
-        raise TypeError(f"unsupported dtype {dtype}")
-    r = torch.empty_like(x) if f is not None else None
-    h = torch.empty((n, c), dtype=dtype, device=x.device) if pre_norm != NORM_NONE else None
-    out = BlockNorm(x if f is None else r, h, _empty_packed(n, c, x.device) if pack_f else None,
-                    _empty_packed(n, c, x.device) if pack_h else None)
-    fp, hp = out.f_packed, out.h_packed
-    _check(L.pcpp_block_norm_fwd(_ptr(x), _ptr(f), _pitch(f) if f is not None else c, *_gate_args(gate, n, c, dtype),
-                                 _weights(w_post, c), _weights(w_pre, c), post_norm, pre_norm, float(residual_scale),
-                                 float(eps), n, c, _dtype_code(x), code, _ptr(r), _ptr(h),
-                                 _ptr(fp.q) if fp else None, _ptr(fp.codes) if fp else None,
-                                 _ptr(hp.q) if hp else None, _ptr(hp.codes) if hp else None, _stream()))
-    return out
+        r, f_at, ld_f = torch.empty_like(x), f.data_ptr(), _pitch(f)
+        r_at = r.data_ptr()
+    else:
+        if dtype is None:
+            dtype = x.dtype
+        r, r_at, f_at, ld_f = x, None, None, c
+    h = None if pre_norm == NORM_NONE else torch.empty_like(x, dtype=dtype)
+    fq = fe = hq = he = f_packed = h_packed = None
+    if pack_f:
+        f_packed = _empty_packed(n, c, x.device)
+        fq, fe = f_packed.q.data_ptr(), f_packed.codes.data_ptr()
+    if pack_h:
+        h_packed = _empty_packed(n, c, x.device)
+        hq, he = h_packed.q.data_ptr(), h_packed.codes.data_ptr()
+    rc = L.pcpp_block_norm_fwd(x.data_ptr(), f_at, ld_f, *_gate_args(gate, n, c, dtype), _weights(w_post, c), _weights(w_pre, c),
+                               post_norm, pre_norm, residual_scale, eps, n, c, _code(x.dtype), _code(dtype), r_at, _at(h), fq, fe,
+                               hq, he, _stream())
+    if rc:
+        _check(rc)
+    return BlockNorm(r, h, f_packed, h_packed)
 
 
 def pcpp_block_norm_bwd(dr: torch.Tensor | None, dh: torch.Tensor | None, r: torch.Tensor | None,
@@ -521,71 +560,78 @@ def pcpp_block_norm_bwd(dr: torch.Tensor | None, dh: torch.Tensor | None, r: tor
     default: f is not None).  dtype: type of the block's tensors where neither dh nor f says it."""
     L = library()
     packed = isinstance(f, Packed)
-    some = dr if dr is not None else dh
+    some = dh if dr is None else dr
     assert some is not None and some.is_cuda, "neither dr nor dh"
     n, c = some.shape
     for t in (dr, dh, r):
-        assert t is None or (t.is_cuda and t.is_contiguous() and tuple(t.shape) == (n, c))
+        assert t is None or (t.is_cuda and t.is_contiguous() and t.shape == (n, c))
     if dh is not None:
         dtype = dh.dtype
     elif f is not None and not packed:
         dtype = f.dtype
     elif gate is not None:
         dtype = gate.dtype
-    stream_dtype = r.dtype if r is not None else dr.dtype
+    stream_dtype = dr.dtype if r is None else r.dtype
     assert dr is None or dr.dtype == stream_dtype
     if dtype is None:
         dtype = stream_dtype
-    code = {torch.float32: PCPP_F32, torch.bfloat16: PCPP_BF16}.get(dtype)
-    if code is None:
-        raise TypeError(f"unsupported dtype {dtype}")
+    f_at = fq = fe = None
+    ld_f = c
     if packed:
         _check_packed(f)
-        assert tuple(f.q.shape) == (n, c)
-        f_args = (None, c, _ptr(f.q), _ptr(f.codes))
+        assert f.q.shape == (n, c)
+        fq, fe = f.q.data_ptr(), f.codes.data_ptr()
     elif f is not None:
-        assert f.is_cuda and tuple(f.shape) == (n, c) and f.dtype == dtype
-        f_args = (_ptr(f), _pitch(f), None, None)
-    else:
-        f_args = (None, c, None, None)
+        assert f.is_cuda and f.shape == (n, c) and f.dtype == dtype
+        f_at, ld_f = f.data_ptr(), _pitch(f)
     if block is None:
         block = f is not None
     dev = some.device
-    dx = torch.empty((n, c), dtype=stream_dtype, device=dev)
-    df = torch.empty((n, c), dtype=dtype, device=dev) if block else None
-    dgate = torch.empty(tuple(gate.shape), dtype=dtype, device=dev) if gate is not None else None
-    new = lambda wanted: torch.empty(c, dtype=torch.float32, device=dev) if wanted else None  # noqa: E731
-    dw_post, dw_pre = new(block and post_norm != NORM_NONE), new(pre_norm != NORM_NONE)
+    dx = torch.empty_like(some, dtype=stream_dtype)
+    df = torch.empty_like(some, dtype=dtype) if block else None
+    dgate = None if gate is None else torch.empty((n, gate.shape[1]), dtype=dtype, device=dev)
+    dw_post = torch.empty(c, dtype=torch.float32, device=dev) if block and post_norm != NORM_NONE else None
+    dw_pre = torch.empty(c, dtype=torch.float32, device=dev) if pre_norm != NORM_NONE else None
     need = L.pcpp_block_norm_workspace_bytes(n, c)
     if workspace is None or workspace.numel() < need:
         workspace = _bytes(need, dev)
-    _check(L.pcpp_block_norm_bwd(_ptr(dr), _ptr(dh), _ptr(r), *f_args, *_gate_args(gate, n, c, dtype),
-                                 _weights(w_post, c), _weights(w_pre, c), post_norm, pre_norm, float(residual_scale),
-                                 float(eps), n, c, PCPP_F32 if stream_dtype == torch.float32 else PCPP_BF16, code,
-                                 _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(workspace),
-                                 workspace.numel(), _stream()))
+    rc = L.pcpp_block_norm_bwd(_at(dr), _at(dh), _at(r), f_at, ld_f, fq, fe, *_gate_args(gate, n, c, dtype), _weights(w_post, c),
+                               _weights(w_pre, c), post_norm, pre_norm, residual_scale, eps, n, c, _code(stream_dtype), _code(dtype),
+                               dx.data_ptr(), _at(df), _at(dgate), _at(dw_post), _at(dw_pre), workspace.data_ptr(),
+                               workspace.numel(), _stream())
+    if rc:
+        _check(rc)
     return BlockNormGrads(dx, df, dgate, dw_post, dw_pre)
 
 
-@dataclass
 class LogProbs:
     """Result of pcpp_log_probs_fwd, fp32 [n]; max_log_sum [n, 2]: the row's maximum and the logarithm of its sum of exp(x - maximum);
     top_* [n, n_top], the most probable classes in descending order."""
-    log_prob: torch.Tensor | None
-    entropy: torch.Tensor
-    max_log_sum: torch.Tensor
-    top_log_prob: torch.Tensor
-    top_index: torch.Tensor
+    __slots__ = ("log_prob", "entropy", "max_log_sum", "_top_log_prob", "_top_index")
+
+    def __init__(self, log_prob, entropy, max_log_sum, top_log_prob=None, top_index=None):
+        self.log_prob, self.entropy, self.max_log_sum = log_prob, entropy, max_log_sum
+        self._top_log_prob, self._top_index = top_log_prob, top_index
 
     @property
     def lse(self) -> torch.Tensor:
         return self.max_log_sum.sum(1)
 
+    # (without alternatives the empty tensors are made when they are asked for: a training step never does)
+    @property
+    def top_log_prob(self) -> torch.Tensor:
+        return self.entropy.new_empty((self.entropy.shape[0], 0)) if self._top_log_prob is None else self._top_log_prob
+
+    @property
+    def top_index(self) -> torch.Tensor:
+        return self.entropy.new_empty((self.entropy.shape[0], 0), dtype=torch.int32) if self._top_index is None else self._top_index
+
 
 def _labels(labels, n):
-    if labels is not None:
-        assert labels.is_cuda and labels.is_contiguous() and labels.dtype == torch.int32 and tuple(labels.shape) == (n,)
-    return _ptr(labels)
+    if labels is None:
+        return None
+    assert labels.is_cuda and labels.is_contiguous() and labels.dtype == torch.int32 and labels.shape == (n,)
+    return labels.data_ptr()
 
 
 def pcpp_log_probs_fwd(logits: torch.Tensor, labels: torch.Tensor | None = None, n_top: int = 0,
@@ -593,19 +639,25 @@ def pcpp_log_probs_fwd(logits: torch.Tensor, labels: torch.Tensor | None = None,
     """Log probability of every row's label (a label outside 0 .. v - 1: none, 0), the entropy, and the n_top most probable
     classes.  logits [n, v], rows may be a slice of wider ones; labels int32 [n]."""
     L = library()
-    assert logits.is_cuda and logits.dim() == 2
+    assert logits.is_cuda
     n, v = logits.shape
     dev = logits.device
-    code, ld = _dtype_code(logits), _pitch(logits)
-    word = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)  # noqa: E731
-    out = LogProbs(word(n) if labels is not None else None, word(n), word(n, 2), word(n, n_top), word(n, n_top, dtype=torch.int32))
+    entropy = torch.empty(n, dtype=torch.float32, device=dev)
+    log_prob = None if labels is None else torch.empty_like(entropy)
+    max_log_sum = torch.empty((n, 2), dtype=torch.float32, device=dev)
+    top_log_prob = top_index = None
+    if n_top:
+        top_log_prob = torch.empty((n, n_top), dtype=torch.float32, device=dev)
+        top_index = torch.empty((n, n_top), dtype=torch.int32, device=dev)
     need = L.pcpp_log_probs_workspace_bytes(n, v, n_top)
     if need and (workspace is None or workspace.numel() < need):
         workspace = _bytes(need, dev)
-    _check(L.pcpp_log_probs_fwd(_ptr(logits), code, n, v, ld, _labels(labels, n), n_top, _ptr(out.log_prob),
-                                _ptr(out.entropy), _ptr(out.max_log_sum), _ptr(out.top_log_prob), _ptr(out.top_index),
-                                _ptr(workspace) if need else None, workspace.numel() if need else 0, _stream()))
-    return out
+    rc = L.pcpp_log_probs_fwd(logits.data_ptr(), _code(logits.dtype), n, v, _pitch(logits), _labels(labels, n), n_top, _at(log_prob),
+                              entropy.data_ptr(), max_log_sum.data_ptr(), _at(top_log_prob), _at(top_index),
+                              workspace.data_ptr() if need else None, workspace.numel() if need else 0, _stream())
+    if rc:
+        _check(rc)
+    return LogProbs(log_prob, entropy, max_log_sum, top_log_prob, top_index)
 
 
 def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forward: LogProbs,
@@ -614,15 +666,20 @@ def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forwar
     """Gradient of the logits from what flows to log_prob and to entropy (fp32 [n]).  out: where it goes, by default a new
     tensor; it may be the logits."""
     L = library()
-    assert logits.is_cuda and logits.dim() == 2
+    assert logits.is_cuda
     n, v = logits.shape
-    assert forward.max_log_sum.is_cuda and forward.max_log_sum.is_contiguous() and tuple(forward.max_log_sum.shape) == (n, 2)
-    for t in (d_log_prob, d_entropy, forward.entropy):
-        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and tuple(t.shape) == (n,))
+    stats, entropy = forward.max_log_sum, forward.entropy
+    assert stats.is_cuda and stats.is_contiguous() and stats.dtype == torch.float32 and stats.shape == (n, 2)
+    for t in (d_log_prob, d_entropy, entropy):
+        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and t.shape == (n,))
     if out is None:
         out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
-    assert out.is_cuda and out.dtype == logits.dtype and out.shape == logits.shape
-    _check(L.pcpp_log_probs_bwd(_ptr(logits), _dtype_code(logits), n, v, _pitch(logits), _labels(labels, n),
-                                _ptr(forward.max_log_sum), _ptr(forward.entropy), _ptr(d_log_prob), _ptr(d_entropy), _ptr(out),
-                                _pitch(out), _stream()))
+        pitch = v
+    else:
+        assert out.is_cuda and out.dtype == logits.dtype and out.shape == (n, v)
+        pitch = _pitch(out)
+    rc = L.pcpp_log_probs_bwd(logits.data_ptr(), _code(logits.dtype), n, v, _pitch(logits), _labels(labels, n), stats.data_ptr(),
+                              entropy.data_ptr(), _at(d_log_prob), _at(d_entropy), out.data_ptr(), pitch, _stream())
+    if rc:
+        _check(rc)
     return out

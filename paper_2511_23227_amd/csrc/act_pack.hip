@@ -27,12 +27,13 @@ __global__ __launch_bounds__(THREADS) void pack_kernel(const T *__restrict__ x, 
     const int lanes = row_lanes(c), rows = THREADS / lanes;
     const int r = (int)threadIdx.x / lanes, c0 = 8 * ((int)threadIdx.x % lanes);
     if (r >= rows) return;                                        // (whole quads, here and below)
+    const Span<WHOLE> span(c0, c);
     for (int64_t row = (int64_t)blockIdx.x * rows + r; row < n; row += (int64_t)gridDim.x * rows) {
         Eight<T> raw;
-        row_load<T, WHOLE>(x + row * c, c0, c, raw);
+        row_load<T>(x + row * c, span, raw);
         float v[8];
-        row_floats<T, WHOLE>(raw, c0, c, v);
-        act_store<WHOLE>(v, q + row * c, codes + row * act_code_bytes(c), c0, c);
+        to_floats(raw, v);
+        act_store(v, q + row * c, codes + row * act_code_bytes(c), span, c0, c);
     }
 }
 
@@ -43,12 +44,13 @@ __global__ __launch_bounds__(THREADS) void unpack_kernel(const int8_t *__restric
     const int lanes = row_lanes(c), rows = THREADS / lanes;
     const int r = (int)threadIdx.x / lanes, c0 = 8 * ((int)threadIdx.x % lanes);
     if (r >= rows) return;
+    const Span<WHOLE> span(c0, c);
     for (int64_t row = (int64_t)blockIdx.x * rows + r; row < n; row += (int64_t)gridDim.x * rows) {
         Eight8 raw;
-        act_load<WHOLE>(q + row * c, codes + row * act_code_bytes(c), c0, c, raw);
+        act_load(q + row * c, codes + row * act_code_bytes(c), span, c0, raw);
         float v[8];
-        act_floats<WHOLE>(raw, c0, c, v);
-        row_store<T, WHOLE>(x + row * c, c0, c, v);
+        act_floats(raw, span, v);
+        row_store(x + row * c, span, v);
     }
 }
 

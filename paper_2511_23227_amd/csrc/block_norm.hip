@@ -27,41 +27,41 @@ constexpr int MAX_BWD_BLOCKS = 1024;                              // backward: a
 
 __device__ inline float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * g)); }
 
-// The row's mean (LAYER; else 0) subtracted from v in place, channels past its end zero again, and 1 / sqrt(mean v^2 + eps).
-template <int LPR, int G>
-__device__ inline float centre_row(float (&v)[G][8], int kind, int c0, int c, float inv_c, float eps)
+// The row's mean (LAYER; else 0) subtracted from v in place, and 1 / sqrt(mean v^2 + eps).
+template <int LPR, int G, bool WHOLE>
+__device__ inline float centre_row(float (&v)[G][8], int kind, const Span<WHOLE> (&own)[G], float inv_c, float eps)
 {
     if (kind == PCPP_NORM_LAYER) {
         float s = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += v[g][e];
+            for (int e = 0; e < 8; ++e) s += WHOLE || own[g].own(e) ? v[g][e] : 0.f;
         const float mean = row_sum<LPR>(s) * inv_c;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[g][e] = c0 + 8 * LPR * g + e < c ? v[g][e] - mean : 0.f;
+            for (int e = 0; e < 8; ++e) v[g][e] = !WHOLE || own[g].any() ? v[g][e] - mean : 0.f;
     }
     float s = 0.f;
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = __builtin_fmaf(v[g][e], v[g][e], s);
+        for (int e = 0; e < 8; ++e) {
+            const float m = WHOLE || own[g].own(e) ? v[g][e] : 0.f;
+            s = __builtin_fmaf(m, m, s);
+        }
     return __builtin_amdgcn_rsqf(row_sum<LPR>(s) * inv_c + eps);
 }
 
-// w[c0 ..] of a weight vector, ones without one; zero past the row's end
-template <int LPR, int G>
-__device__ inline void load_weights(const float *w, int c0, int c, float (&v)[G][8])
+// the channels' weights, ones without; zero where there is no channel
+template <int G, bool WHOLE>
+__device__ inline void load_weights(const float *w, const Span<WHOLE> (&own)[G], float (&v)[G][8])
 {
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int ch = c0 + 8 * LPR * g + e;
-            v[g][e] = ch < c ? (w ? w[ch] : 1.f) : 0.f;
-        }
+        for (int e = 0; e < 8; ++e) v[g][e] = own[g].any() && (WHOLE || e < own[g].hi) ? (w ? w[own[g].at + e] : 1.f) : 0.f;
 }
 
 // S: type of the residual stream, T: of the block's tensors.  A row lies in LPR lanes, G times eight channels each.
@@ -70,43 +70,46 @@ __global__ __launch_bounds__(THREADS) void block_fwd_kernel(const BlockNormFwd a
 {
     constexpr int ROWS = THREADS / LPR, NEXT = 8 * LPR;
     const int c = a.c, c0 = 8 * ((int)threadIdx.x % LPR);
+    Span<WHOLE> own[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) own[g] = Span<WHOLE>(c0 + NEXT * g, c);
     float wp[G][8], wn[G][8];
-    load_weights<LPR, G>(a.w_post, c0, c, wp);
-    load_weights<LPR, G>(a.w_pre, c0, c, wn);
+    load_weights(a.w_post, own, wp);
+    load_weights(a.w_pre, own, wn);
     // (a row's lanes leave the loop together, and nothing in it reads another row's lanes)
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
         Eight<S> xr[G];
         Eight<T> fr[G], gr[G];
         float row_gate = 0.f;
 #pragma unroll
-        for (int g = 0; g < G; ++g) row_load<S, WHOLE>(static_cast<const S *>(a.x) + row * c, c0 + NEXT * g, c, xr[g]);
+        for (int g = 0; g < G; ++g) row_load<S>(static_cast<const S *>(a.x) + row * c, own[g], xr[g]);
         if (a.f) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) row_load<T, WHOLE>(static_cast<const T *>(a.f) + row * a.ld_f, c0 + NEXT * g, c, fr[g]);
+            for (int g = 0; g < G; ++g) row_load<T>(static_cast<const T *>(a.f) + row * a.ld_f, own[g], fr[g]);
             if (a.gate_cols > 1) {
 #pragma unroll
-                for (int g = 0; g < G; ++g) row_load<T, WHOLE>(static_cast<const T *>(a.gate) + row * a.ld_gate, c0 + NEXT * g, c, gr[g]);
+                for (int g = 0; g < G; ++g) row_load<T>(static_cast<const T *>(a.gate) + row * a.ld_gate, own[g], gr[g]);
             } else if (a.gate_cols == 1) {
                 row_gate = one_float<T>(static_cast<const T *>(a.gate)[row * a.ld_gate]);
             }
         }
         float r[G][8];
 #pragma unroll
-        for (int g = 0; g < G; ++g) row_floats<S, WHOLE>(xr[g], c0 + NEXT * g, c, r[g]);
+        for (int g = 0; g < G; ++g) to_floats(xr[g], r[g]);
         if (a.f) {
             float f[G][8];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                row_floats<T, WHOLE>(fr[g], c0 + NEXT * g, c, f[g]);
-                if (a.f_codes.q) act_store<WHOLE>(f[g], a.f_codes.q + row * c, a.f_codes.e + row * act_code_bytes(c), c0 + NEXT * g, c);
+                to_floats(fr[g], f[g]);
+                if (a.f_codes.q) act_store(f[g], a.f_codes.q + row * c, a.f_codes.e + row * act_code_bytes(c), own[g], c0 + NEXT * g, c);
             }
             float rstd = 1.f;
-            if (a.post != PCPP_NORM_NONE) rstd = centre_row<LPR, G>(f, a.post, c0, c, a.inv_c, a.eps);
+            if (a.post != PCPP_NORM_NONE) rstd = centre_row<LPR>(f, a.post, own, a.inv_c, a.eps);
             const float s1 = a.gate_cols == 1 ? sigmoid(row_gate) : 1.f;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float s[8];
-                if (a.gate_cols > 1) row_floats<T, WHOLE>(gr[g], c0 + NEXT * g, c, s);
+                if (a.gate_cols > 1) to_floats(gr[g], s);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float sg = a.gate_cols > 1 ? sigmoid(s[e]) : s1;
@@ -114,16 +117,16 @@ __global__ __launch_bounds__(THREADS) void block_fwd_kernel(const BlockNormFwd a
                 }
             }
 #pragma unroll
-            for (int g = 0; g < G; ++g) row_store<S, WHOLE>(static_cast<S *>(a.r) + row * c, c0 + NEXT * g, c, r[g]);
+            for (int g = 0; g < G; ++g) row_store(static_cast<S *>(a.r) + row * c, own[g], r[g]);
         }
         if (a.pre != PCPP_NORM_NONE) {
-            const float rstd = centre_row<LPR, G>(r, a.pre, c0, c, a.inv_c, a.eps);
+            const float rstd = centre_row<LPR>(r, a.pre, own, a.inv_c, a.eps);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) r[g][e] = wn[g][e] * (r[g][e] * rstd);
-                row_store<T, WHOLE>(static_cast<T *>(a.h) + row * c, c0 + NEXT * g, c, r[g]);
-                if (a.h_codes.q) act_store<WHOLE>(r[g], a.h_codes.q + row * c, a.h_codes.e + row * act_code_bytes(c), c0 + NEXT * g, c);
+                row_store(static_cast<T *>(a.h) + row * c, own[g], r[g]);
+                if (a.h_codes.q) act_store(r[g], a.h_codes.q + row * c, a.h_codes.e + row * act_code_bytes(c), own[g], c0 + NEXT * g, c);
             }
         }
     }
@@ -135,9 +138,12 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
     constexpr int ROWS = THREADS / LPR, NEXT = 8 * LPR;
     const int c = a.c, c0 = 8 * ((int)threadIdx.x % LPR);
     const bool pre = a.pre != PCPP_NORM_NONE, post = a.post != PCPP_NORM_NONE, branch = a.df != nullptr;
+    Span<WHOLE> own[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) own[g] = Span<WHOLE>(c0 + NEXT * g, c);
     float wp[G][8], wn[G][8], dwp[G][8], dwn[G][8];
-    load_weights<LPR, G>(a.w_post, c0, c, wp);
-    load_weights<LPR, G>(a.w_pre, c0, c, wn);
+    load_weights(a.w_post, own, wp);
+    load_weights(a.w_pre, own, wn);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -149,16 +155,15 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
         float row_gate = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const int ch = c0 + NEXT * g;
-            if (a.dr) row_load<S, WHOLE>(static_cast<const S *>(a.dr) + row * c, ch, c, drr[g]);
+            if (a.dr) row_load<S>(static_cast<const S *>(a.dr) + row * c, own[g], drr[g]);
             if (pre) {
-                row_load<T, WHOLE>(static_cast<const T *>(a.dh) + row * c, ch, c, dhr[g]);
-                row_load<S, WHOLE>(static_cast<const S *>(a.r) + row * c, ch, c, rr[g]);
+                row_load<T>(static_cast<const T *>(a.dh) + row * c, own[g], dhr[g]);
+                row_load<S>(static_cast<const S *>(a.r) + row * c, own[g], rr[g]);
             }
             if (branch) {
-                if (a.f_codes.q) act_load<WHOLE>(a.f_codes.q + row * c, a.f_codes.e + row * act_code_bytes(c), ch, c, qr[g]);
-                else if (a.f) row_load<T, WHOLE>(static_cast<const T *>(a.f) + row * a.ld_f, ch, c, fr[g]);
-                if (a.gate_cols > 1) row_load<T, WHOLE>(static_cast<const T *>(a.gate) + row * a.ld_gate, ch, c, gr[g]);
+                if (a.f_codes.q) act_load(a.f_codes.q + row * c, a.f_codes.e + row * act_code_bytes(c), own[g], c0 + NEXT * g, qr[g]);
+                else if (a.f) row_load<T>(static_cast<const T *>(a.f) + row * a.ld_f, own[g], fr[g]);
+                if (a.gate_cols > 1) row_load<T>(static_cast<const T *>(a.gate) + row * a.ld_gate, own[g], gr[g]);
             }
         }
         if (branch && a.gate_cols == 1) row_gate = one_float<T>(static_cast<const T *>(a.gate)[row * a.ld_gate]);
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
         float d[G][8];
         if (a.dr) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) row_floats<S, WHOLE>(drr[g], c0 + NEXT * g, c, d[g]);
+            for (int g = 0; g < G; ++g) to_floats(drr[g], d[g]);
         } else {
 #pragma unroll
             for (int g = 0; g < G; ++g)
@@ -177,10 +182,10 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
             float r[G][8], y[G][8];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                row_floats<S, WHOLE>(rr[g], c0 + NEXT * g, c, r[g]);
-                row_floats<T, WHOLE>(dhr[g], c0 + NEXT * g, c, y[g]);
+                to_floats(rr[g], r[g]);
+                to_floats(dhr[g], y[g]);
             }
-            const float rstd = centre_row<LPR, G>(r, a.pre, c0, c, a.inv_c, a.eps);
+            const float rstd = centre_row<LPR>(r, a.pre, own, a.inv_c, a.eps);
             float sy = 0.f, syn = 0.f;
 #pragma unroll
             for (int g = 0; g < G; ++g)
@@ -189,8 +194,9 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
                     r[g][e] *= rstd;                              // n(r)
                     dwn[g][e] = __builtin_fmaf(y[g][e], r[g][e], dwn[g][e]);
                     y[g][e] *= wn[g][e];
-                    sy += y[g][e];
-                    syn = __builtin_fmaf(y[g][e], r[g][e], syn);
+                    const float m = WHOLE || own[g].own(e) ? y[g][e] : 0.f;
+                    sy += m;
+                    syn = __builtin_fmaf(m, r[g][e], syn);
                 }
             const float my = a.pre == PCPP_NORM_LAYER ? row_sum<LPR>(sy) * a.inv_c : 0.f, myn = row_sum<LPR>(syn) * a.inv_c;
 #pragma unroll
@@ -204,7 +210,7 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
                 float o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = a.scale * d[g][e];
-                row_store<S, WHOLE>(static_cast<S *>(a.dx) + row * c, c0 + NEXT * g, c, o);
+                row_store(static_cast<S *>(a.dx) + row * c, own[g], o);
             }
         }
         if (!branch) continue;
@@ -213,37 +219,37 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             if (a.f_codes.q) {
-                act_floats<WHOLE>(qr[g], c0 + NEXT * g, c, f[g]);
+                act_floats(qr[g], own[g], f[g]);
             } else if (a.f) {
-                row_floats<T, WHOLE>(fr[g], c0 + NEXT * g, c, f[g]);
+                to_floats(fr[g], f[g]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[g][e] = 0.f;
             }
         }
         float rstd = 1.f;
-        if (post && has_f) rstd = centre_row<LPR, G>(f, a.post, c0, c, a.inv_c, a.eps);
+        if (post && has_f) rstd = centre_row<LPR>(f, a.post, own, a.inv_c, a.eps);
         const float s1 = a.gate_cols == 1 ? sigmoid(row_gate) : 1.f;
         float sz = 0.f, szn = 0.f, sg1 = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float s[8];
-            if (a.gate_cols > 1) row_floats<T, WHOLE>(gr[g], c0 + NEXT * g, c, s);
+            if (a.gate_cols > 1) to_floats(gr[g], s);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool inside = WHOLE ? c0 + NEXT * g < c : c0 + NEXT * g + e < c;
                 const float sg = a.gate_cols > 1 ? sigmoid(s[e]) : s1;
                 const float nf = f[g][e] * rstd;
-                const float du = inside ? d[g][e] * sg : 0.f;     // (past the row's end d holds what the mean left there)
+                const float du = d[g][e] * sg;
                 dwp[g][e] = __builtin_fmaf(du, nf, dwp[g][e]);
-                s[e] = du * (1.f - sg) * (wp[g][e] * nf);
-                sg1 += s[e];
-                d[g][e] = wp[g][e] * du;                          // z
-                sz += d[g][e];
-                szn = __builtin_fmaf(d[g][e], nf, szn);
+                d[g][e] = wp[g][e] * du;                          // z (zero where there is no channel, as the weights are)
+                s[e] = (1.f - sg) * (d[g][e] * nf);
+                const float m = WHOLE || own[g].own(e) ? d[g][e] : 0.f;
+                sg1 += WHOLE || own[g].own(e) ? s[e] : 0.f;
+                sz += m;
+                szn = __builtin_fmaf(m, nf, szn);
                 f[g][e] = nf;
             }
-            if (a.gate_cols > 1) row_store<T, WHOLE>(static_cast<T *>(a.dgate) + row * c, c0 + NEXT * g, c, s);
+            if (a.gate_cols > 1) row_store(static_cast<T *>(a.dgate) + row * c, own[g], s);
         }
         if (a.gate_cols == 1) {
             sg1 = row_sum<LPR>(sg1);
@@ -257,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
                 for (int e = 0; e < 8; ++e) d[g][e] = rstd * (d[g][e] - mz - f[g][e] * mzn);
         }
 #pragma unroll
-        for (int g = 0; g < G; ++g) row_store<T, WHOLE>(static_cast<T *>(a.df) + row * c, c0 + NEXT * g, c, d[g]);
+        for (int g = 0; g < G; ++g) row_store(static_cast<T *>(a.df) + row * c, own[g], d[g]);
     }
 
     // the weights' gradients: over the rows that the wave's lanes hold, then over the waves
@@ -273,9 +279,9 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
                 p += __shfl_xor(p, m);
                 n += __shfl_xor(n, m);
             }
-            if (lane < LPR) {
-                sums[wave][0][8 * lane + NEXT * g + e] = p;
-                sums[wave][1][8 * lane + NEXT * g + e] = n;
+            if (lane < LPR && own[g].own(e)) {
+                sums[wave][0][own[g].at + e] = p;
+                sums[wave][1][own[g].at + e] = n;
             }
         }
     __syncthreads();

@@ -48,16 +48,74 @@ __device__ inline key_t64 lane_of(key_t64 k, int lane)
     return (key_t64)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
 
+template <int D> __device__ inline uint32_t lane_xor(uint32_t v, int lane)   // the value of lane ^ D
+{
+    if constexpr (D == 1) return dpp<DPP_XOR1>(v);
+    if constexpr (D == 2) return dpp<DPP_XOR2>(v);
+    if constexpr (D == 4) return dpp<0x1b>(dpp<DPP_HALF_MIRROR>(v));              // xor 7, then xor 3
+    if constexpr (D == 8) return dpp<0x128>(v);                                   // rotation of sixteen lanes by eight
+    if constexpr (D == 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return (lane & 16) ? p[0] : p[1];
+    }
+    if constexpr (D == 32) {
+        const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return (lane & 32) ? p[0] : p[1];
+    }
+    return v;
+}
+template <int D> __device__ inline key_t64 lane_xor(key_t64 k, int lane)
+{
+    return (key_t64)lane_xor<D>((uint32_t)(k >> 32), lane) << 32 | lane_xor<D>((uint32_t)k, lane);
+}
+// The larger of the pair (lane, lane ^ D) to its lower lane, or to its upper one where `up`.
+template <int D> __device__ inline key_t64 exchange(key_t64 k, int lane, bool up)
+{
+    const key_t64 o = lane_xor<D>(k, lane);
+    return ((lane & D) != 0) == up ? (k > o ? k : o) : (k > o ? o : k);
+}
+// lanes' keys that rise and then fall (or the other way round), into descending order
+__device__ inline key_t64 bitonic_merge(key_t64 k, int lane)
+{
+    k = exchange<32>(k, lane, false);
+    k = exchange<16>(k, lane, false);
+    k = exchange<8>(k, lane, false);
+    k = exchange<4>(k, lane, false);
+    k = exchange<2>(k, lane, false);
+    return exchange<1>(k, lane, false);
+}
+__device__ inline key_t64 sort_lanes(key_t64 k, int lane)                         // any keys, into descending order
+{
+    bool up = lane & 2;
+    k = exchange<1>(k, lane, up);
+    up = lane & 4;
+    k = exchange<1>(exchange<2>(k, lane, up), lane, up);
+    up = lane & 8;
+    k = exchange<1>(exchange<2>(exchange<4>(k, lane, up), lane, up), lane, up);
+    up = lane & 16;
+    k = exchange<1>(exchange<2>(exchange<4>(exchange<8>(k, lane, up), lane, up), lane, up), lane, up);
+    up = lane & 32;
+    k = exchange<1>(exchange<2>(exchange<4>(exchange<8>(exchange<16>(k, lane, up), lane, up), lane, up), lane, up), lane, up);
+    return bitonic_merge(k, lane);
+}
+// the 64 largest of two lists in descending order
+__device__ inline key_t64 merge_lists(key_t64 a, key_t64 b, int lane)
+{
+    b = lane_xor<32>(lane_xor<16>((key_t64)dpp<DPP_MIRROR>((uint32_t)(b >> 32)) << 32 | dpp<DPP_MIRROR>((uint32_t)b), lane), lane);
+    return bitonic_merge(a > b ? a : b, lane);
+}
+
 // The largest keys seen by a wave: lane j holds the (j + 1)-th, 0 where there are fewer.
 struct TopList {
-    key_t64 mine = 0, last = 0;                                   // last: lane n_top - 1's, the one to pass
+    key_t64 mine = 0, last = 0;                                   // last: keys up to it do not belong to the n_top largest
     int n_top;
     __device__ inline void insert(key_t64 k, int lane)            // k: the same in all lanes, larger than `last`
     {
         const int at = __popcll(__ballot(mine > k));
-        const key_t64 before = __shfl_up(mine, 1);
+        const key_t64 before = (key_t64)dpp<0x138>((uint32_t)(mine >> 32)) << 32 | dpp<0x138>((uint32_t)mine);   // of the lane before
         mine = lane < at ? mine : (lane == at ? k : before);
-        last = lane_of(mine, n_top - 1);
+        const key_t64 l = lane_of(mine, n_top - 1);
+        if (l > last) last = l;
     }
     __device__ inline void offer(key_t64 k, int lane)             // every lane's own, 0: none
     {
@@ -68,6 +126,13 @@ struct TopList {
             const key_t64 c = lane_of(k, from);
             if (c > last) insert(c, lane);
         }
+    }
+    // In front of the first offers: every lane's largest key of those to come.  The n_top-th largest of these is a bound that n_top keys reach,
+    // so that hardly more than n_top of the first keys are put into the list.
+    __device__ inline void expect(key_t64 largest, int lane)
+    {
+        const key_t64 l = lane_of(sort_lanes(largest, lane), n_top - 1);
+        if (l) last = l - 1;
     }
 };
 
@@ -116,7 +181,7 @@ template <typename T, int LPR>
 __global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
 {
     constexpr int ROWS = THREADS / LPR, E = 8;
-    const int l = (int)threadIdx.x % LPR;
+    const int l = (int)threadIdx.x % LPR, lane = threadIdx.x & 63;
     const int v = (int)a.v;
     // (a row's lanes leave together)
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
@@ -142,22 +207,27 @@ __global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
         if (l == 0) row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
         const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
         // one class after the other: the largest of the lane's, then of the row's lanes; of equal ones the lowest index
-        uint32_t taken = 0u;
+        if (a.n_top == 0) continue;
+        key_t64 keys[E], mine = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            keys[e] = l + LPR * e < v ? key_of(xs[e], (uint32_t)(l + LPR * e)) : 0;
+            mine = keys[e] > mine ? keys[e] : mine;
+        }
         for (int k = 0; k < a.n_top; ++k) {
-            key_t64 best = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const key_t64 key = key_of(xs[e], (uint32_t)(l + LPR * e));
-                if (l + LPR * e < v && !(taken >> e & 1u) && key > best) best = key;
-            }
-#pragma unroll
-            for (int d = 1; d < LPR; d <<= 1) {
-                const key_t64 other = __shfl_xor(best, d);
-                if (other > best) best = other;
-            }
+            key_t64 best = mine;
+            auto with = [&](key_t64 o) { best = o > best ? o : best; };
+            if constexpr (LPR >= 2) with(lane_xor<1>(best, lane));
+            if constexpr (LPR >= 4) with(lane_xor<2>(best, lane));
+            if constexpr (LPR >= 8) with(lane_xor<4>(best, lane));
+            if constexpr (LPR >= 16) with(lane_xor<8>(best, lane));
+            if constexpr (LPR >= 32) with(lane_xor<16>(best, lane));
+            if constexpr (LPR >= 64) with(lane_xor<32>(best, lane));
             const uint32_t index = key_index(best);
-            if ((int)(index % LPR) == l) {
-                taken |= 1u << (index / LPR);
+            if (mine == best) {                                    // (one lane: keys are all different)
+                mine = 0;                                          // the largest of what is left
+#pragma unroll
+                for (int e = 0; e < E; ++e) mine = keys[e] < best && keys[e] > mine ? keys[e] : mine;
                 a.top_log_prob[row * a.n_top + k] = top_value(u, key_value(best), log_s);
                 a.top_index[row * a.n_top + k] = (int32_t)index;
             }
@@ -202,8 +272,15 @@ __device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopLi
             u.t = __builtin_fmaf(p, bounded(d), u.t);
         }
         if (want_top && __ballot(!(m < key_value(list.last)) || list.last == 0)) {
+            key_t64 keys[8], largest = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) list.offer(at + e < to ? key_of(v[e], (uint32_t)(at + e)) : 0, lane);
+            for (int e = 0; e < 8; ++e) {
+                keys[e] = at + e < to ? key_of(v[e], (uint32_t)(at + e)) : 0;
+                largest = keys[e] > largest ? keys[e] : largest;
+            }
+            if (list.last == 0) list.expect(largest, lane);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) list.offer(keys[e], lane);
         }
     }
 }
@@ -222,7 +299,7 @@ __device__ inline void join_waves(Sums &u, TopList &list, bool want_top, int lan
     if (wave != 0) return;
     for (int w = 1; w < WAVES; ++w) {
         u.join(sums[w].m, sums[w].s, sums[w].t);
-        if (want_top) list.offer(lane < list.n_top ? keys[w][lane] : 0, lane);
+        if (want_top) list.mine = merge_lists(list.mine, keys[w][lane], lane);
     }
 }
 
@@ -257,29 +334,30 @@ __global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, 
             if (want_top) store_top(a, row, u, list, log_s, lane);
         } else if (wave == 0) {
             if (lane == 0) parts[block] = Partial{u.m, u.s, u.t, 0.f};
-            if (lane < a.n_top) keys[block * a.n_top + lane] = list.mine;
+            if (lane < a.n_top) keys[block * a.n_top + lane] = list.mine;      // (0 past the end of a short list)
         }
         __syncthreads();                                           // (the next row's sums go where these lay)
     }
 }
 
-// one wave a row: the sums and lists of its splits
+// One block a row: the sums and lists of its splits, the lists by the waves in turn, then wave by wave.
 template <typename T>
-__global__ __launch_bounds__(64) void join_fwd_kernel(const LogProbsFwd a, int splits, const Partial *parts, const key_t64 *keys)
+__global__ __launch_bounds__(THREADS) void join_fwd_kernel(const LogProbsFwd a, int splits, const Partial *parts, const key_t64 *keys)
 {
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = blockIdx.x;                               // (few rows: they were split)
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     Sums u{-__builtin_inff(), 0.f, 0.f};
-    for (int s = lane; s < splits; s += 64) {
+    for (int s = threadIdx.x; s < splits; s += THREADS) {
         const Partial p = parts[row * splits + s];
         u.join(p.m, p.s, p.t);
     }
-    u = join_lanes(u, 64);
     TopList list;
     list.n_top = a.n_top;
-    const int n = splits * a.n_top;
-    for (int i = 0; i < n; i += 64) list.offer(i + lane < n ? keys[row * n + i + lane] : 0, lane);
+    if (a.n_top > 0)
+        for (int s = wave; s < splits; s += WAVES) list.mine = merge_lists(list.mine, lane < a.n_top ? keys[(row * splits + s) * a.n_top + lane] : 0, lane);
+    join_waves(u, list, a.n_top > 0, lane, wave);
+    if (wave != 0) return;
     const int64_t label = a.labels ? a.labels[row] : -1;
     const bool labelled = label >= 0 && label < a.v;
     float log_s = 0.f;
@@ -394,7 +472,7 @@ int launch_fwd(const LogProbsFwd &a, void *workspace, hipStream_t stream)
     long_fwd_kernel<T><<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per, parts, keys);
     PCPP_HIP_CHECK(hipGetLastError());
     if (s.splits == 1) return PCPP_OK;
-    join_fwd_kernel<T><<<(unsigned)a.n, 64, 0, stream>>>(a, s.splits, parts, keys);
+    join_fwd_kernel<T><<<(unsigned)a.n, THREADS, 0, stream>>>(a, s.splits, parts, keys);
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;
 }
