@@ -326,7 +326,7 @@ PCPP_API int pcpp_mvmr_bwd_weight_packed(const int8_t *xq, const uint8_t *xcodes
  *   dw_post, dw_pre  [c] fp32; NULL: not wanted
  *   workspace: pcpp_block_norm_workspace_bytes(n, c) bytes, 256-byte aligned (backward only)
  * The sums over rows are taken in a fixed order: the same result each time.
- * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (c outside 1..1024, n >= 2^31, dtype combination).
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (c outside 1..1024, n >= 2^31, pitch >= 2^24, dtype combination).
  * ------------------------------------------------------------------------------------------- */
 #define PCPP_NORM_NONE   0
 #define PCPP_NORM_RMS    1

@@ -27,248 +27,278 @@ constexpr int MAX_BWD_BLOCKS = 1024;                              // backward: a
 
 __device__ inline float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * g)); }
 
+// One element at a multiple of the descriptor's elements
+template <typename T> __device__ inline uint32_t load_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t at)     // as the bits of an fp32 number
+{
+    if constexpr (sizeof(T) == 4) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, (int)(at * 4u), 0, 0);
+    else return (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(at * 2u), 0, 0) << 16;
+}
+template <typename T> __device__ inline void store_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t at, float v)
+{
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rs, (int)(at * 4u), 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(one_of<bf16_t>(v), rs, (int)(at * 2u), 0, 0);
+}
+
 // The row's mean (LAYER; else 0) subtracted from v in place, and 1 / sqrt(mean v^2 + eps).
-template <int LPR, int G, bool WHOLE>
-__device__ inline float centre_row(float (&v)[G][8], int kind, const Span<WHOLE> (&own)[G], float inv_c, float eps)
+template <int LPR, int G, int MODE>
+__device__ inline float centre_row(float (&v)[G][8], int kind, const Span<MODE> (&own)[G], float inv_c, float eps)
 {
     if (kind == PCPP_NORM_LAYER) {
         float s = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += WHOLE || own[g].own(e) ? v[g][e] : 0.f;
+            for (int e = 0; e < 8; ++e) s += MODE == WHOLE || own[g].own(e) ? v[g][e] : 0.f;
         const float mean = row_sum<LPR>(s) * inv_c;
 #pragma unroll
-        for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g) {
+            const float m = own[g].any() ? mean : 0.f;            // (no channels: zeros stay)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[g][e] = !WHOLE || own[g].any() ? v[g][e] - mean : 0.f;
+            for (int e = 0; e < 8; ++e) v[g][e] -= m;
+        }
     }
     float s = 0.f;
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float m = WHOLE || own[g].own(e) ? v[g][e] : 0.f;
+            const float m = MODE == WHOLE || own[g].own(e) ? v[g][e] : 0.f;
             s = __builtin_fmaf(m, m, s);
         }
     return __builtin_amdgcn_rsqf(row_sum<LPR>(s) * inv_c + eps);
 }
 
 // the channels' weights, ones without; zero where there is no channel
-template <int G, bool WHOLE>
-__device__ inline void load_weights(const float *w, const Span<WHOLE> (&own)[G], float (&v)[G][8])
+template <int G, int MODE>
+__device__ inline void load_weights(const float *w, const Span<MODE> (&own)[G], int c, float (&v)[G][8])
 {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(w, w ? 4u * (uint32_t)c : 0u);
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int g = 0; g < G; ++g) {
+        Eight<float> r;
+        row_load<float>(rs, own[g].template offset<4>(0u), own[g], r);
+        to_floats(r, v[g]);
+        if (!w) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[g][e] = own[g].any() && (WHOLE || e < own[g].hi) ? (w ? w[own[g].at + e] : 1.f) : 0.f;
+            for (int e = 0; e < 8; ++e) v[g][e] = own[g].any() && (MODE != NARROW || e < c) ? 1.f : 0.f;
+        }
+    }
 }
 
-// S: type of the residual stream, T: of the block's tensors.  A row lies in LPR lanes, G times eight channels each.
-template <typename S, typename T, int LPR, int G, bool WHOLE>
+// S: type of the residual stream, T: of the block's tensors.  A row lies in LPR lanes, G times eight channels each.  FULL: a gate for
+// every channel.
+template <typename S, typename T, int LPR, int G, int MODE, bool FULL>
 __global__ __launch_bounds__(THREADS) void block_fwd_kernel(const BlockNormFwd a)
 {
-    constexpr int ROWS = THREADS / LPR, NEXT = 8 * LPR;
-    const int c = a.c, c0 = 8 * ((int)threadIdx.x % LPR);
-    Span<WHOLE> own[G];
+    constexpr int ROWS = 64 / LPR, SS = sizeof(S), TS = sizeof(T);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), c = a.c;
+    const uint32_t row = (uint32_t)(lane / LPR);
+    int c0[G];
+    Span<MODE> own[G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) own[g] = Span<WHOLE>(c0 + NEXT * g, c);
+    for (int g = 0; g < G; ++g) c0[g] = 8 * (lane % LPR) + 8 * LPR * g, own[g] = Span<MODE>(c0[g], c);
     float wp[G][8], wn[G][8];
-    load_weights(a.w_post, own, wp);
-    load_weights(a.w_pre, own, wn);
-    // (a row's lanes leave the loop together, and nothing in it reads another row's lanes)
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
+    load_weights(a.w_post, own, c, wp);
+    load_weights(a.w_pre, own, c, wn);
+    for (int64_t first = ((int64_t)blockIdx.x * WAVES + wave) * ROWS; first < a.n; first += (int64_t)gridDim.x * WAVES * ROWS) {
+        const __amdgpu_buffer_rsrc_t xs = rows_from<SS>(a.x, first, a.n, c, c, ROWS), fs = rows_from<TS>(a.f, first, a.n, a.ld_f, c, ROWS);
+        const __amdgpu_buffer_rsrc_t gs = rows_from<TS>(a.gate, first, a.n, a.ld_gate, a.gate_cols, ROWS);
         Eight<S> xr[G];
         Eight<T> fr[G], gr[G];
-        float row_gate = 0.f;
+        uint32_t row_gate = 0u;
 #pragma unroll
-        for (int g = 0; g < G; ++g) row_load<S>(static_cast<const S *>(a.x) + row * c, own[g], xr[g]);
-        if (a.f) {
-#pragma unroll
-            for (int g = 0; g < G; ++g) row_load<T>(static_cast<const T *>(a.f) + row * a.ld_f, own[g], fr[g]);
-            if (a.gate_cols > 1) {
-#pragma unroll
-                for (int g = 0; g < G; ++g) row_load<T>(static_cast<const T *>(a.gate) + row * a.ld_gate, own[g], gr[g]);
-            } else if (a.gate_cols == 1) {
-                row_gate = one_float<T>(static_cast<const T *>(a.gate)[row * a.ld_gate]);
-            }
+        for (int g = 0; g < G; ++g) {
+            row_load<S>(xs, own[g].template offset<SS>(row * (uint32_t)c), own[g], xr[g]);
+            row_load<T>(fs, own[g].template offset<TS>(row * (uint32_t)a.ld_f), own[g], fr[g]);
+            if constexpr (FULL) row_load<T>(gs, own[g].template offset<TS>(row * (uint32_t)a.ld_gate), own[g], gr[g]);
         }
+        if constexpr (!FULL) row_gate = load_one<T>(gs, row * (uint32_t)a.ld_gate);
         float r[G][8];
 #pragma unroll
         for (int g = 0; g < G; ++g) to_floats(xr[g], r[g]);
         if (a.f) {
             float f[G][8];
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                to_floats(fr[g], f[g]);
-                if (a.f_codes.q) act_store(f[g], a.f_codes.q + row * c, a.f_codes.e + row * act_code_bytes(c), own[g], c0 + NEXT * g, c);
+            for (int g = 0; g < G; ++g) to_floats(fr[g], f[g]);
+            if (a.f_codes.q) {
+                const ActRows to = act_rows(a.f_codes.q, a.f_codes.e, first, a.n, c, ROWS);
+#pragma unroll
+                for (int g = 0; g < G; ++g) act_store<LPR>(f[g], to, row, own[g], c0[g], c);
             }
             float rstd = 1.f;
             if (a.post != PCPP_NORM_NONE) rstd = centre_row<LPR>(f, a.post, own, a.inv_c, a.eps);
-            const float s1 = a.gate_cols == 1 ? sigmoid(row_gate) : 1.f;
+            const float s1 = a.gate_cols == 1 ? sigmoid(__uint_as_float(row_gate)) : 1.f;
+            const __amdgpu_buffer_rsrc_t rs = rows_from<SS>(a.r, first, a.n, c, c, ROWS);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float s[8];
-                if (a.gate_cols > 1) to_floats(gr[g], s);
+                if constexpr (FULL) to_floats(gr[g], s);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float sg = a.gate_cols > 1 ? sigmoid(s[e]) : s1;
+                    const float sg = FULL ? sigmoid(s[e]) : s1;
                     r[g][e] = __builtin_fmaf(sg, wp[g][e] * (f[g][e] * rstd), a.scale * r[g][e]);
                 }
+                row_store<S>(rs, own[g].template offset<SS>(row * (uint32_t)c), own[g], r[g]);
             }
-#pragma unroll
-            for (int g = 0; g < G; ++g) row_store(static_cast<S *>(a.r) + row * c, own[g], r[g]);
         }
         if (a.pre != PCPP_NORM_NONE) {
             const float rstd = centre_row<LPR>(r, a.pre, own, a.inv_c, a.eps);
+            const __amdgpu_buffer_rsrc_t hs = rows_from<TS>(a.h, first, a.n, c, c, ROWS);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) r[g][e] = wn[g][e] * (r[g][e] * rstd);
-                row_store(static_cast<T *>(a.h) + row * c, own[g], r[g]);
-                if (a.h_codes.q) act_store(r[g], a.h_codes.q + row * c, a.h_codes.e + row * act_code_bytes(c), own[g], c0 + NEXT * g, c);
+                row_store<T>(hs, own[g].template offset<TS>(row * (uint32_t)c), own[g], r[g]);
+            }
+            if (a.h_codes.q) {
+                const ActRows to = act_rows(a.h_codes.q, a.h_codes.e, first, a.n, c, ROWS);
+#pragma unroll
+                for (int g = 0; g < G; ++g) act_store<LPR>(r[g], to, row, own[g], c0[g], c);
             }
         }
     }
 }
 
-template <typename S, typename T, int LPR, int G, bool WHOLE>
+template <typename S, typename T, int LPR, int G, int MODE, bool FULL>
 __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a)
 {
-    constexpr int ROWS = THREADS / LPR, NEXT = 8 * LPR;
-    const int c = a.c, c0 = 8 * ((int)threadIdx.x % LPR);
-    const bool pre = a.pre != PCPP_NORM_NONE, post = a.post != PCPP_NORM_NONE, branch = a.df != nullptr;
-    Span<WHOLE> own[G];
+    constexpr int ROWS = 64 / LPR, SS = sizeof(S), TS = sizeof(T);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), c = a.c;
+    const uint32_t row = (uint32_t)(lane / LPR);
+    const bool pre = a.pre != PCPP_NORM_NONE, post = a.post != PCPP_NORM_NONE;
+    int c0[G];
+    Span<MODE> own[G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) own[g] = Span<WHOLE>(c0 + NEXT * g, c);
+    for (int g = 0; g < G; ++g) c0[g] = 8 * (lane % LPR) + 8 * LPR * g, own[g] = Span<MODE>(c0[g], c);
     float wp[G][8], wn[G][8], dwp[G][8], dwn[G][8];
-    load_weights(a.w_post, own, wp);
-    load_weights(a.w_pre, own, wn);
+    load_weights(a.w_post, own, c, wp);
+    load_weights(a.w_pre, own, c, wn);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) dwp[g][e] = dwn[g][e] = 0.f;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
+    for (int64_t first = ((int64_t)blockIdx.x * WAVES + wave) * ROWS; first < a.n; first += (int64_t)gridDim.x * WAVES * ROWS) {
+        const bool live = first + row < a.n;                      // (rows past the last are zeros; eps may be zero too)
         Eight<S> drr[G], rr[G];
         Eight<T> dhr[G], fr[G], gr[G];
         Eight8 qr[G];
-        float row_gate = 0.f;
+        uint32_t row_gate = 0u;
+        const __amdgpu_buffer_rsrc_t drs = rows_from<SS>(a.dr, first, a.n, c, c, ROWS), rs = rows_from<SS>(a.r, first, a.n, c, c, ROWS);
+        const __amdgpu_buffer_rsrc_t dhs = rows_from<TS>(a.dh, first, a.n, c, c, ROWS), gs = rows_from<TS>(a.gate, first, a.n, a.ld_gate, a.gate_cols, ROWS);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            if (a.dr) row_load<S>(static_cast<const S *>(a.dr) + row * c, own[g], drr[g]);
-            if (pre) {
-                row_load<T>(static_cast<const T *>(a.dh) + row * c, own[g], dhr[g]);
-                row_load<S>(static_cast<const S *>(a.r) + row * c, own[g], rr[g]);
-            }
-            if (branch) {
-                if (a.f_codes.q) act_load(a.f_codes.q + row * c, a.f_codes.e + row * act_code_bytes(c), own[g], c0 + NEXT * g, qr[g]);
-                else if (a.f) row_load<T>(static_cast<const T *>(a.f) + row * a.ld_f, own[g], fr[g]);
-                if (a.gate_cols > 1) row_load<T>(static_cast<const T *>(a.gate) + row * a.ld_gate, own[g], gr[g]);
-            }
+            row_load<S>(drs, own[g].template offset<SS>(row * (uint32_t)c), own[g], drr[g]);
+            row_load<S>(rs, own[g].template offset<SS>(row * (uint32_t)c), own[g], rr[g]);
+            row_load<T>(dhs, own[g].template offset<TS>(row * (uint32_t)c), own[g], dhr[g]);
+            if constexpr (FULL) row_load<T>(gs, own[g].template offset<TS>(row * (uint32_t)a.ld_gate), own[g], gr[g]);
         }
-        if (branch && a.gate_cols == 1) row_gate = one_float<T>(static_cast<const T *>(a.gate)[row * a.ld_gate]);
-
-        float d[G][8];
-        if (a.dr) {
+        if constexpr (!FULL) row_gate = load_one<T>(gs, row * (uint32_t)a.ld_gate);
+        if (a.f_codes.q) {
+            const ActRows from = act_rows(a.f_codes.q, a.f_codes.e, first, a.n, c, ROWS);
 #pragma unroll
-            for (int g = 0; g < G; ++g) to_floats(drr[g], d[g]);
+            for (int g = 0; g < G; ++g) act_load(from, row, own[g], c0[g], c, qr[g]);
         } else {
+            const __amdgpu_buffer_rsrc_t fs = rows_from<TS>(a.f, first, a.n, a.ld_f, c, ROWS);
 #pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[g][e] = 0.f;
+            for (int g = 0; g < G; ++g) row_load<T>(fs, own[g].template offset<TS>(row * (uint32_t)a.ld_f), own[g], fr[g]);
         }
-        if (pre) {
-            float r[G][8], y[G][8];
+
+        // through the norm in front of the next block (without one dh and r are zero, and rstd)
+        float d[G][8], r[G][8], y[G][8];
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                to_floats(rr[g], r[g]);
-                to_floats(dhr[g], y[g]);
+        for (int g = 0; g < G; ++g) {
+            to_floats(rr[g], r[g]);
+            to_floats(dhr[g], y[g]);
+        }
+        float rstd = centre_row<LPR>(r, a.pre, own, a.inv_c, a.eps);
+        rstd = pre && live ? rstd : 0.f;
+        float sy = 0.f, syn = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                r[g][e] *= rstd;                                  // n(r)
+                dwn[g][e] = __builtin_fmaf(y[g][e], r[g][e], dwn[g][e]);
+                y[g][e] *= wn[g][e];
+                const float m = MODE != RAGGED || own[g].own(e) ? y[g][e] : 0.f;    // (the weights are zero where there is no channel)
+                sy += m;
+                syn = __builtin_fmaf(m, r[g][e], syn);
             }
-            const float rstd = centre_row<LPR>(r, a.pre, own, a.inv_c, a.eps);
-            float sy = 0.f, syn = 0.f;
+        const float my = a.pre == PCPP_NORM_LAYER ? row_sum<LPR>(sy) * a.inv_c : 0.f, myn = row_sum<LPR>(syn) * a.inv_c;
 #pragma unroll
-            for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g) {
+            to_floats(drr[g], d[g]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    r[g][e] *= rstd;                              // n(r)
-                    dwn[g][e] = __builtin_fmaf(y[g][e], r[g][e], dwn[g][e]);
-                    y[g][e] *= wn[g][e];
-                    const float m = WHOLE || own[g].own(e) ? y[g][e] : 0.f;
-                    sy += m;
-                    syn = __builtin_fmaf(m, r[g][e], syn);
-                }
-            const float my = a.pre == PCPP_NORM_LAYER ? row_sum<LPR>(sy) * a.inv_c : 0.f, myn = row_sum<LPR>(syn) * a.inv_c;
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[g][e] = __builtin_fmaf(rstd, y[g][e] - my - r[g][e] * myn, d[g][e]);
+            for (int e = 0; e < 8; ++e) d[g][e] = __builtin_fmaf(rstd, y[g][e] - my - r[g][e] * myn, d[g][e]);
         }
         if (a.dx) {
+            const __amdgpu_buffer_rsrc_t xs = rows_from<SS>(a.dx, first, a.n, c, c, ROWS);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = a.scale * d[g][e];
-                row_store(static_cast<S *>(a.dx) + row * c, own[g], o);
+                row_store<S>(xs, own[g].template offset<SS>(row * (uint32_t)c), own[g], o);
             }
         }
-        if (!branch) continue;
+        if (!a.df) continue;
+
+        // through the gate and the norm behind the block
         float f[G][8];
-        const bool has_f = a.f_codes.q || a.f;
+        if (a.f_codes.q) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            if (a.f_codes.q) {
-                act_floats(qr[g], own[g], f[g]);
-            } else if (a.f) {
-                to_floats(fr[g], f[g]);
-            } else {
+            for (int g = 0; g < G; ++g) act_floats(qr[g], own[g], f[g]);
+        } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[g][e] = 0.f;
-            }
+            for (int g = 0; g < G; ++g) to_floats(fr[g], f[g]);
         }
-        float rstd = 1.f;
-        if (post && has_f) rstd = centre_row<LPR>(f, a.post, own, a.inv_c, a.eps);
-        const float s1 = a.gate_cols == 1 ? sigmoid(row_gate) : 1.f;
+        rstd = 1.f;
+        if (post) rstd = centre_row<LPR>(f, a.post, own, a.inv_c, a.eps);
+        rstd = live ? rstd : 0.f;
+        const float s1 = a.gate_cols == 1 ? sigmoid(__uint_as_float(row_gate)) : 1.f;
         float sz = 0.f, szn = 0.f, sg1 = 0.f;
+        const __amdgpu_buffer_rsrc_t dgs = rows_from<TS>(a.dgate, first, a.n, a.gate_cols, a.gate_cols, ROWS);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float s[8];
-            if (a.gate_cols > 1) to_floats(gr[g], s);
+            if constexpr (FULL) to_floats(gr[g], s);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float sg = a.gate_cols > 1 ? sigmoid(s[e]) : s1;
-                const float nf = f[g][e] * rstd;
+                const float sg = FULL ? sigmoid(s[e]) : s1;
                 const float du = d[g][e] * sg;
-                dwp[g][e] = __builtin_fmaf(du, nf, dwp[g][e]);
-                d[g][e] = wp[g][e] * du;                          // z (zero where there is no channel, as the weights are)
-                s[e] = (1.f - sg) * (d[g][e] * nf);
-                const float m = WHOLE || own[g].own(e) ? d[g][e] : 0.f;
-                sg1 += WHOLE || own[g].own(e) ? s[e] : 0.f;
+                f[g][e] *= rstd;                                  // n(f)
+                dwp[g][e] = __builtin_fmaf(du, f[g][e], dwp[g][e]);
+                d[g][e] = wp[g][e] * du;                          // z
+                const float m = MODE != RAGGED || own[g].own(e) ? d[g][e] : 0.f;
                 sz += m;
-                szn = __builtin_fmaf(m, nf, szn);
-                f[g][e] = nf;
+                if constexpr (FULL) {
+                    szn = __builtin_fmaf(m, f[g][e], szn);
+                    s[e] = (1.f - sg) * (d[g][e] * f[g][e]);
+                } else {
+                    sg1 = __builtin_fmaf(m, f[g][e], sg1);
+                }
             }
-            if (a.gate_cols > 1) row_store(static_cast<T *>(a.dgate) + row * c, own[g], s);
+            if constexpr (FULL) row_store<T>(dgs, own[g].template offset<TS>(row * (uint32_t)c), own[g], s);
         }
-        if (a.gate_cols == 1) {
-            sg1 = row_sum<LPR>(sg1);
-            if (c0 == 0) static_cast<T *>(a.dgate)[row] = one_of<T>(sg1);
+        if constexpr (!FULL) {
+            sg1 = row_sum<LPR>(sg1);                              // sum z n(f): the gate's gradient and the norm's
+            store_one<T>(dgs, lane % LPR == 0 && a.gate_cols ? row : OOB_OFFSET / TS, (1.f - s1) * sg1);
+            szn = sg1;
+        } else {
+            szn = row_sum<LPR>(szn);
         }
-        if (post) {
-            const float mz = a.post == PCPP_NORM_LAYER ? row_sum<LPR>(sz) * a.inv_c : 0.f, mzn = row_sum<LPR>(szn) * a.inv_c;
+        const float mz = a.post == PCPP_NORM_LAYER ? row_sum<LPR>(sz) * a.inv_c : 0.f, mzn = post ? szn * a.inv_c : 0.f;
+        const __amdgpu_buffer_rsrc_t dfs = rows_from<TS>(a.df, first, a.n, c, c, ROWS);
 #pragma unroll
-            for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[g][e] = rstd * (d[g][e] - mz - f[g][e] * mzn);
+            for (int e = 0; e < 8; ++e) d[g][e] = rstd * (d[g][e] - mz - f[g][e] * mzn);
+            row_store<T>(dfs, own[g].template offset<TS>(row * (uint32_t)c), own[g], d[g]);
         }
-#pragma unroll
-        for (int g = 0; g < G; ++g) row_store(static_cast<T *>(a.df) + row * c, own[g], d[g]);
     }
 
     // the weights' gradients: over the rows that the wave's lanes hold, then over the waves
     __shared__ float sums[WAVES][2][G * 8 * LPR];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -316,18 +346,10 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(const float *__restri
     if (to) to[i < c ? i : i - c] = v;
 }
 
-int bwd_blocks(int64_t n, int lpr)
+int blocks_for(int64_t n, int c, int most)
 {
-    const int64_t b = ceil_div(n, THREADS / lpr);
-    return (int)(b < MAX_BWD_BLOCKS ? b : MAX_BWD_BLOCKS);
-}
-
-// Lanes for a row of c channels: eight each, sixteen past 512.
-int row_lpr(int c)
-{
-    int lpr = 4;
-    while (lpr < 64 && 8 * lpr < c) lpr *= 2;
-    return lpr;
+    const int64_t b = ceil_div(n, WAVES * 64 / row_lanes(c));
+    return (int)(b < most ? b : most);
 }
 
 template <typename F> void with_types(int stream_dtype, int dtype, F f)
@@ -336,48 +358,33 @@ template <typename F> void with_types(int stream_dtype, int dtype, F f)
     else if (stream_dtype == PCPP_F32) f(float{}, bf16_t{});
     else f(bf16_t{}, bf16_t{});
 }
-template <int N> struct Int { static constexpr int value = N; };
-template <typename F> void with_shape(int c, F f)
-{
-    auto whole = [&](auto lpr, auto g) {
-        if (c % 8 == 0) f(lpr, g, std::true_type{});
-        else f(lpr, g, std::false_type{});
-    };
-    if (c > 512) return whole(Int<64>{}, Int<2>{});
-    switch (row_lpr(c)) {
-    case 4: return whole(Int<4>{}, Int<1>{});
-    case 8: return whole(Int<8>{}, Int<1>{});
-    case 16: return whole(Int<16>{}, Int<1>{});
-    case 32: return whole(Int<32>{}, Int<1>{});
-    default: return whole(Int<64>{}, Int<1>{});
-    }
-}
 
 }  // namespace
 
 int block_norm_fwd(const BlockNormFwd &a, int stream_dtype, int dtype, hipStream_t stream)
 {
-    const int64_t want = ceil_div(a.n, THREADS / row_lpr(a.c));
-    const unsigned blocks = (unsigned)(want < MAX_BLOCKS ? want : MAX_BLOCKS);
+    const unsigned blocks = (unsigned)blocks_for(a.n, a.c, MAX_BLOCKS);
     with_types(stream_dtype, dtype, [&](auto s, auto t) {
-        with_shape(a.c, [&](auto lpr, auto g, auto whole) {
-            block_fwd_kernel<decltype(s), decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(whole)::value>
-                <<<blocks, THREADS, 0, stream>>>(a);
+        with_rows(a.c, [&](auto lpr, auto g, auto mode) {
+            constexpr int LPR = decltype(lpr)::value, G = decltype(g)::value, MODE = decltype(mode)::value;
+            if (a.gate_cols > 1) block_fwd_kernel<decltype(s), decltype(t), LPR, G, MODE, true><<<blocks, THREADS, 0, stream>>>(a);
+            else block_fwd_kernel<decltype(s), decltype(t), LPR, G, MODE, false><<<blocks, THREADS, 0, stream>>>(a);
         });
     });
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;
 }
 
-size_t block_norm_bwd_workspace_bytes(int64_t n, int c) { return align_up((size_t)bwd_blocks(n, row_lpr(c)) * 2 * c * sizeof(float)); }
+size_t block_norm_bwd_workspace_bytes(int64_t n, int c) { return align_up((size_t)blocks_for(n, c, MAX_BWD_BLOCKS) * 2 * c * sizeof(float)); }
 
 int block_norm_bwd(const BlockNormBwd &a, int stream_dtype, int dtype, hipStream_t stream)
 {
-    const int blocks = bwd_blocks(a.n, row_lpr(a.c));
+    const int blocks = blocks_for(a.n, a.c, MAX_BWD_BLOCKS);
     with_types(stream_dtype, dtype, [&](auto s, auto t) {
-        with_shape(a.c, [&](auto lpr, auto g, auto whole) {
-            block_bwd_kernel<decltype(s), decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(whole)::value>
-                <<<(unsigned)blocks, THREADS, 0, stream>>>(a);
+        with_rows(a.c, [&](auto lpr, auto g, auto mode) {
+            constexpr int LPR = decltype(lpr)::value, G = decltype(g)::value, MODE = decltype(mode)::value;
+            if (a.gate_cols > 1) block_bwd_kernel<decltype(s), decltype(t), LPR, G, MODE, true><<<(unsigned)blocks, THREADS, 0, stream>>>(a);
+            else block_bwd_kernel<decltype(s), decltype(t), LPR, G, MODE, false><<<(unsigned)blocks, THREADS, 0, stream>>>(a);
         });
     });
     PCPP_HIP_CHECK(hipGetLastError());

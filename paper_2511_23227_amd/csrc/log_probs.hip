@@ -52,8 +52,8 @@ template <int D> __device__ inline uint32_t lane_xor(uint32_t v, int lane)   // 
 {
     if constexpr (D == 1) return dpp<DPP_XOR1>(v);
     if constexpr (D == 2) return dpp<DPP_XOR2>(v);
-    if constexpr (D == 4) return dpp<0x1b>(dpp<DPP_HALF_MIRROR>(v));              // xor 7, then xor 3
-    if constexpr (D == 8) return dpp<0x128>(v);                                   // rotation of sixteen lanes by eight
+    if constexpr (D == 4) return dpp<DPP_XOR3>(dpp<DPP_HALF_MIRROR>(v));              // xor 7, then xor 3
+    if constexpr (D == 8) return dpp<DPP_ROR + 8>(v);                                   // rotation of sixteen lanes by eight
     if constexpr (D == 16) {
         const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
         return (lane & 16) ? p[0] : p[1];

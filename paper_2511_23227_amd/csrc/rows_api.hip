@@ -12,6 +12,7 @@ namespace pcpp {
 namespace {
 
 constexpr int MAX_CHANNELS = 1024;
+constexpr int64_t MAX_PITCH = 1 << 24;                            // (a wave's sixteen rows within 32-bit offsets)
 
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 size_t dtype_bytes(int dtype) { return dtype == PCPP_F32 ? 4 : 2; }
@@ -58,6 +59,7 @@ int check_block(const char *fn, const void *f, int64_t ld_f, const void *gate, i
     if (n > 0 && (gate != nullptr) != (gate_cols != 0)) return invalid(fn, "gate and gate_cols do not agree");
     if (f && ld_f < c) return invalid(fn, "ld_f < c");
     if (gate && ld_gate < gate_cols) return invalid(fn, "ld_gate < gate_cols");
+    if ((f && ld_f >= MAX_PITCH) || (gate && ld_gate >= MAX_PITCH)) return unsupported(fn, "row pitches must be below 2^24");
     if (!aligned(f, dtype_bytes(dtype)) || !aligned(gate, dtype_bytes(dtype)) || !aligned(w_post, 4) || !aligned(w_pre, 4))
         return invalid(fn, "f, gate and the weights must be aligned to their elements");
     return PCPP_OK;
