@@ -128,11 +128,48 @@ struct TopList {
         }
     }
     // In front of the first offers: every lane's largest key of those to come.  The n_top-th largest of these is a bound that n_top keys reach,
-    // so that hardly more than n_top of the first keys are put into the list.
+    // so that hardly more than n_top of the first keys are candidates.
     __device__ inline void expect(key_t64 largest, int lane)
     {
         const key_t64 l = lane_of(sort_lanes(largest, lane), n_top - 1);
         if (l) last = l - 1;
+    }
+    // Several keys of every lane at once (`room`: 64 keys of LDS, the wave's own).  A few candidates are put into the list one by one; more
+    // are gathered 64 at a time, sorted and merged: 28 exchanges of lanes for 64, where one insertion takes as long as three.
+    template <int N> __device__ inline void offer_all(const key_t64 (&k)[N], key_t64 *room, int lane)
+    {
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) n += __popcll(__ballot(k[e] > last));
+        if (n <= 6) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) offer(k[e], lane);
+            return;
+        }
+        n = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            key_t64 m = __ballot(k[e] > last);
+            if (n + __popcll(m) > 64) {
+                merge(room, n, lane);
+                n = 0;
+                m = __ballot(k[e] > last);
+            }
+            if (k[e] > last) room[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u))] = k[e];
+            n += __popcll(m);
+        }
+        merge(room, n, lane);
+    }
+    __device__ inline void merge(const key_t64 *room, int n, int lane)
+    {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (the lanes' writes before the reads, and these before the next writes)
+        __builtin_amdgcn_wave_barrier();
+        const key_t64 k = lane < n ? room[lane] : 0;
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        mine = merge_lists(mine, sort_lanes(k, lane), lane);
+        const key_t64 l = lane_of(mine, n_top - 1);
+        if (l > last) last = l;
     }
 };
 
@@ -236,26 +273,49 @@ __global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
 }
 
 // ---- long rows ------------------------------------------------------------------------------------------------------------
-// Classes [from, to) of a row by a thread block.
-template <typename T>
-__device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopList &list, bool want_top, int lane)
+// Classes [from, to) of a row by a thread block.  A lane takes twice eight classes a step, and has the next step's on their way meanwhile.
+constexpr int DEEP = 2;
+
+// the lane's classes at + 512 j .. at + 512 j + 7 as they lie in memory, -inf behind the end
+template <typename T> __device__ inline void load_step(const T *x, int64_t at, int64_t to, Eight<T> (&r)[DEEP])
 {
-    u = Sums{-__builtin_inff(), 0.f, 0.f};
-    // eight classes a lane and step; the wave goes round together, so that the list sees all lanes
-    for (int64_t base = from + (int64_t)(threadIdx.x & ~63u) * 8; base < to; base += THREADS * 8) {
-        const int64_t at = base + lane * 8;
-        float v[8];
-        if (at + 8 <= to) {
-            Eight<T> raw;
-            load_eight(x + at, raw);
-            to_floats(raw, v);
+    constexpr uint32_t NOTHING = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+    for (int j = 0; j < DEEP; ++j) {
+        const int64_t p = at + 512 * j;
+        if (p + 8 <= to) {
+            load_eight(x + p, r[j]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = at + e < to ? one_float<T>(x[at + e]) : -__builtin_inff();
+            for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r[j].a[i] = v4u{NOTHING, NOTHING, NOTHING, NOTHING};
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+                if (p + e < to) {
+                    if constexpr (sizeof(T) == 4) r[j].a[e >> 2][e & 3] = __float_as_uint(x[p + e]);
+                    else r[j].a[0][e >> 1] = (e & 1) ? (r[j].a[0][e >> 1] & 0xffffu) | (uint32_t)x[p + e] << 16 : 0xff800000u | x[p + e];
+                }
         }
+    }
+}
+
+template <typename T, bool TOP>
+__device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopList &list, key_t64 *room, int lane, int wave)
+{
+    constexpr int N = 8 * DEEP, WAVE = 64 * N;
+    u = Sums{-__builtin_inff(), 0.f, 0.f};
+    // (the wave goes round together, so that the list sees all lanes)
+    int64_t base = from + wave * WAVE;
+    Eight<T> r[DEEP];
+    if (base < to) load_step(x, base + lane * 8, to, r);
+    for (; base < to; base += WAVES * WAVE) {
+        const int64_t at = base + lane * 8;
+        float v[N];
+#pragma unroll
+        for (int j = 0; j < DEEP; ++j) to_floats(r[j], *reinterpret_cast<float (*)[8]>(v + 8 * j));
+        if (base + WAVES * WAVE < to) load_step(x, at + WAVES * WAVE, to, r);
         float m = v[0];
 #pragma unroll
-        for (int e = 1; e < 8; ++e) m = fmaxf(m, v[e]);
+        for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
         if (m > u.m) {
             if (u.m > -__builtin_inff()) {
                 const float g = bounded(u.m - m), a = exp_of(g);
@@ -266,40 +326,47 @@ __device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopLi
         }
         const float m0 = u.m == -__builtin_inff() ? 0.f : u.m;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
             const float d = v[e] - m0, p = exp_of(d);
             u.s += p;
             u.t = __builtin_fmaf(p, bounded(d), u.t);
         }
-        if (want_top && __ballot(!(m < key_value(list.last)) || list.last == 0)) {
-            key_t64 keys[8], largest = 0;
+        if (TOP && __ballot(!(m < key_value(list.last)) || list.last == 0)) {
+            key_t64 keys[N], largest = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                keys[e] = at + e < to ? key_of(v[e], (uint32_t)(at + e)) : 0;
+            for (int e = 0; e < N; ++e) {
+                const int64_t index = at + 512 * (e / 8) + e % 8;
+                keys[e] = index < to ? key_of(v[e], (uint32_t)index) : 0;
                 largest = keys[e] > largest ? keys[e] : largest;
             }
             if (list.last == 0) list.expect(largest, lane);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) list.offer(keys[e], lane);
+            list.offer_all(keys, room, lane);
         }
     }
 }
 
 struct Partial { float m, s, t, unused; };
 
-// The block's waves' sums and lists: the sums in all threads of wave 0, the list in wave 0.
-__device__ inline void join_waves(Sums &u, TopList &list, bool want_top, int lane, int wave)
+// The sums and lists of a block's N waves (a power of two), pair by pair; both end in wave 0.
+template <int N, bool TOP>
+__device__ inline void join_waves(Sums &u, TopList &list, Sums *sums, key_t64 (*keys)[64], int lane, int wave)
 {
-    __shared__ Sums sums[WAVES];
-    __shared__ key_t64 keys[WAVES][64];
     u = join_lanes(u, 64);
     if (lane == 0) sums[wave] = u;
-    if (want_top) keys[wave][lane] = list.mine;
+    if (TOP) keys[wave][lane] = list.mine;
     __syncthreads();
-    if (wave != 0) return;
-    for (int w = 1; w < WAVES; ++w) {
-        u.join(sums[w].m, sums[w].s, sums[w].t);
-        if (want_top) list.mine = merge_lists(list.mine, keys[w][lane], lane);
+    if (wave == 0) {
+        u = join_lanes(sums[lane % N], N);                         // (in all lanes)
+    }
+    if (TOP) {
+#pragma unroll
+        for (int half = N / 2; half > 0; half >>= 1) {
+            if (wave < half) {
+                list.mine = merge_lists(list.mine, keys[wave + half][lane], lane);
+                keys[wave][lane] = list.mine;
+            }
+            if (half > 1) __syncthreads();
+        }
     }
 }
 
@@ -310,10 +377,12 @@ __device__ inline void store_top(const LogProbsFwd &a, int64_t row, const Sums &
     a.top_index[row * a.n_top + lane] = (int32_t)key_index(list.mine);
 }
 
-template <typename T>
+template <typename T, bool TOP>
 __global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, int splits, int64_t per, Partial *parts, key_t64 *keys)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ Sums wave_sums[WAVES];
+    __shared__ key_t64 wave_keys[TOP ? WAVES : 1][64], room[TOP ? WAVES : 1][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     for (int64_t block = blockIdx.x; block < a.n * splits; block += gridDim.x) {
         const int64_t row = block / splits;
         const int split = (int)(block % splits);
@@ -322,48 +391,49 @@ __global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, 
         Sums u;
         TopList list;
         list.n_top = a.n_top;
-        const bool want_top = a.n_top > 0;
-        walk(x, from, to, u, list, want_top, lane);
-        join_waves(u, list, want_top, lane, wave);
+        walk<T, TOP>(x, from, to, u, list, room[TOP ? wave : 0], lane, wave);
+        join_waves<WAVES, TOP>(u, list, wave_sums, wave_keys, lane, wave);
         if (wave == 0 && splits == 1) {
             const int64_t label = a.labels ? a.labels[row] : -1;
             const bool labelled = label >= 0 && label < a.v;
-            float log_s = 0.f;
-            if (lane == 0) log_s = row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
-            log_s = __shfl(log_s, 0);
-            if (want_top) store_top(a, row, u, list, log_s, lane);
+            const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
+            if (lane == 0) row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
+            if (TOP) store_top(a, row, u, list, log_s, lane);
         } else if (wave == 0) {
             if (lane == 0) parts[block] = Partial{u.m, u.s, u.t, 0.f};
-            if (lane < a.n_top) keys[block * a.n_top + lane] = list.mine;      // (0 past the end of a short list)
+            if (TOP && lane < a.n_top) keys[block * a.n_top + lane] = list.mine;      // (0 past the end of a short list)
         }
         __syncthreads();                                           // (the next row's sums go where these lay)
     }
 }
 
-// One block a row: the sums and lists of its splits, the lists by the waves in turn, then wave by wave.
-template <typename T>
-__global__ __launch_bounds__(THREADS) void join_fwd_kernel(const LogProbsFwd a, int splits, const Partial *parts, const key_t64 *keys)
+// One block a row: the sums and lists of its splits, the lists by the waves in turn, then pair by pair.
+constexpr int JOIN_WAVES = 16;
+template <typename T, bool TOP>
+__global__ __launch_bounds__(JOIN_WAVES * 64) void join_fwd_kernel(const LogProbsFwd a, int splits, const Partial *parts, const key_t64 *keys)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ Sums wave_sums[JOIN_WAVES];
+    __shared__ key_t64 wave_keys[TOP ? JOIN_WAVES : 1][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t row = blockIdx.x;                               // (few rows: they were split)
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     Sums u{-__builtin_inff(), 0.f, 0.f};
-    for (int s = threadIdx.x; s < splits; s += THREADS) {
+    for (int s = threadIdx.x; s < splits; s += JOIN_WAVES * 64) {
         const Partial p = parts[row * splits + s];
         u.join(p.m, p.s, p.t);
     }
     TopList list;
     list.n_top = a.n_top;
-    if (a.n_top > 0)
-        for (int s = wave; s < splits; s += WAVES) list.mine = merge_lists(list.mine, lane < a.n_top ? keys[(row * splits + s) * a.n_top + lane] : 0, lane);
-    join_waves(u, list, a.n_top > 0, lane, wave);
+    if (TOP)
+        for (int s = wave; s < splits; s += JOIN_WAVES)
+            list.mine = merge_lists(list.mine, lane < a.n_top ? keys[(row * splits + s) * a.n_top + lane] : 0, lane);
+    join_waves<JOIN_WAVES, TOP>(u, list, wave_sums, wave_keys, lane, wave);
     if (wave != 0) return;
     const int64_t label = a.labels ? a.labels[row] : -1;
     const bool labelled = label >= 0 && label < a.v;
-    float log_s = 0.f;
-    if (lane == 0) log_s = row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
-    log_s = __shfl(log_s, 0);
-    if (a.n_top > 0) store_top(a, row, u, list, log_s, lane);
+    const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
+    if (lane == 0) row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
+    if (TOP) store_top(a, row, u, list, log_s, lane);
 }
 
 // ---- gradient --------------------------------------------------------------------------------------------------------------
@@ -469,10 +539,12 @@ int launch_fwd(const LogProbsFwd &a, void *workspace, hipStream_t stream)
     const Split s = split_of(a.n, a.v);
     Partial *parts = static_cast<Partial *>(workspace);
     key_t64 *keys = reinterpret_cast<key_t64 *>(static_cast<char *>(workspace) + align_up((size_t)a.n * s.splits * sizeof(Partial)));
-    long_fwd_kernel<T><<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per, parts, keys);
+    auto kernel = a.n_top > 0 ? long_fwd_kernel<T, true> : long_fwd_kernel<T, false>;
+    kernel<<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per, parts, keys);
     PCPP_HIP_CHECK(hipGetLastError());
     if (s.splits == 1) return PCPP_OK;
-    join_fwd_kernel<T><<<(unsigned)a.n, THREADS, 0, stream>>>(a, s.splits, parts, keys);
+    auto join = a.n_top > 0 ? join_fwd_kernel<T, true> : join_fwd_kernel<T, false>;
+    join<<<(unsigned)a.n, JOIN_WAVES * 64, 0, stream>>>(a, s.splits, parts, keys);
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;
 }
