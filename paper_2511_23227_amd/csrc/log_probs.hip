@@ -68,14 +68,14 @@ template <int D> __device__ inline key_t64 lane_xor(key_t64 k, int lane)
 {
     return (key_t64)lane_xor<D>((uint32_t)(k >> 32), lane) << 32 | lane_xor<D>((uint32_t)k, lane);
 }
-// The larger of the pair (lane, lane ^ D) to its lower lane, or to its upper one where `up`.
-template <int D> __device__ inline key_t64 exchange(key_t64 k, int lane, bool up)
+// The larger of the pair (lane, lane ^ D) to its lower lane, or to its upper one where `up`.  (K: keys of 32 or 64 bits)
+template <int D, typename K> __device__ inline K exchange(K k, int lane, bool up)
 {
-    const key_t64 o = lane_xor<D>(k, lane);
+    const K o = lane_xor<D>(k, lane);
     return ((lane & D) != 0) == up ? (k > o ? k : o) : (k > o ? o : k);
 }
 // lanes' keys that rise and then fall (or the other way round), into descending order
-__device__ inline key_t64 bitonic_merge(key_t64 k, int lane)
+template <typename K> __device__ inline K bitonic_merge(K k, int lane)
 {
     k = exchange<32>(k, lane, false);
     k = exchange<16>(k, lane, false);
@@ -84,7 +84,7 @@ __device__ inline key_t64 bitonic_merge(key_t64 k, int lane)
     k = exchange<2>(k, lane, false);
     return exchange<1>(k, lane, false);
 }
-__device__ inline key_t64 sort_lanes(key_t64 k, int lane)                         // any keys, into descending order
+template <typename K> __device__ inline K sort_lanes(K k, int lane)               // any keys, into descending order
 {
     bool up = lane & 2;
     k = exchange<1>(k, lane, up);
@@ -117,45 +117,52 @@ struct TopList {
         const key_t64 l = lane_of(mine, n_top - 1);
         if (l > last) last = l;
     }
-    __device__ inline void offer(key_t64 k, int lane)             // every lane's own, 0: none
+    // A bound in front of the first offers, from every lane's largest value: the n_top-th largest of these is reached by n_top keys, so that
+    // hardly more than n_top of the first keys are candidates.
+    __device__ inline void expect(float largest, int lane)
     {
-        key_t64 left = __ballot(k > last);
-        while (left) {
-            const int from = __ffsll((long long)left) - 1;
-            left &= left - 1;
-            const key_t64 c = lane_of(k, from);
-            if (c > last) insert(c, lane);
-        }
+        const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)sort_lanes(ordered(largest), lane), n_top - 1);
+        if (o > ordered(-__builtin_inff())) raise((key_t64)o << 32);
     }
-    // In front of the first offers: every lane's largest key of those to come.  The n_top-th largest of these is a bound that n_top keys reach,
-    // so that hardly more than n_top of the first keys are candidates.
-    __device__ inline void expect(key_t64 largest, int lane)
+    __device__ inline void raise(key_t64 reached)                 // n_top keys of the row reach it
     {
-        const key_t64 l = lane_of(sort_lanes(largest, lane), n_top - 1);
-        if (l) last = l - 1;
+        if (reached > last) last = reached - 1;
     }
-    // Several keys of every lane at once (`room`: 64 keys of LDS, the wave's own).  A few candidates are put into the list one by one; more
-    // are gathered 64 at a time, sorted and merged: 28 exchanges of lanes for 64, where one insertion takes as long as three.
-    template <int N> __device__ inline void offer_all(const key_t64 (&k)[N], key_t64 *room, int lane)
+    // Several values of every lane at once; mask(e): the lanes whose value v[e] may belong, index(e): its class.  A few are put into the list
+    // one by one; more are gathered 64 at a time (`room`: 64 keys of LDS, the wave's own), sorted and merged, 28 exchanges of lanes for 64, where
+    // one insertion takes as long as three.
+    template <int N, typename Mask, typename Index>
+    __device__ inline void offer(const float (&v)[N], Mask mask, Index index, key_t64 *room, int lane)
     {
         int n = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e) n += __popcll(__ballot(k[e] > last));
+        for (int e = 0; e < N; ++e) n += __popcll(mask(e));
         if (n <= 6) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) offer(k[e], lane);
+            for (int e = 0; e < N; ++e)
+                for (key_t64 left = mask(e); left; left &= left - 1) {
+                    const int from = __ffsll((long long)left) - 1;
+                    const key_t64 k = key_of(__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[e]), from)),
+                                             (uint32_t)__builtin_amdgcn_readlane((int)index(e), from));
+                    if (k > last) insert(k, lane);
+                }
             return;
         }
         n = 0;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            key_t64 m = __ballot(k[e] > last);
+            const key_t64 all = mask(e);
+            if (!all) continue;
+            const key_t64 k = key_of(v[e], index(e));
+            bool in = (all >> lane & 1) && k > last;
+            key_t64 m = __ballot(in);
             if (n + __popcll(m) > 64) {
                 merge(room, n, lane);
                 n = 0;
-                m = __ballot(k[e] > last);
+                in = in && k > last;
+                m = __ballot(in);
             }
-            if (k[e] > last) room[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u))] = k[e];
+            if (in) room[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u))] = k;
             n += __popcll(m);
         }
         merge(room, n, lane);
@@ -213,12 +220,18 @@ __device__ inline float row_results(const LogProbsFwd &a, int64_t row, const Sum
 }
 __device__ inline float top_value(const Sums &v, float x, float log_s) { return v.s == 0.f ? -__builtin_inff() : (x - v.m) - log_s; }
 
+// op over the LPR lanes of a row, the same in all of them
+template <int LPR, typename Op> __device__ inline uint32_t row_best(uint32_t v, Op op)
+{
+    return __float_as_uint(row_reduce<LPR>(__uint_as_float(v), [&](float a, float b) { return __uint_as_float(op(__float_as_uint(a), __float_as_uint(b))); }));
+}
+
 // ---- rows in registers: LPR lanes a row, lane l holding the classes l + LPR e ------------------------------------------------
 template <typename T, int LPR>
 __global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
 {
     constexpr int ROWS = THREADS / LPR, E = 8;
-    const int l = (int)threadIdx.x % LPR, lane = threadIdx.x & 63;
+    const int l = (int)threadIdx.x % LPR;
     const int v = (int)a.v;
     // (a row's lanes leave together)
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
@@ -245,28 +258,24 @@ __global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
         const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
         // one class after the other: the largest of the lane's, then of the row's lanes; of equal ones the lowest index
         if (a.n_top == 0) continue;
-        key_t64 keys[E], mine = 0;
+        uint32_t value[E], mine = 0u, at = 0u;                     // 0: no class, or taken already; at: class of the lane's largest
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            keys[e] = l + LPR * e < v ? key_of(xs[e], (uint32_t)(l + LPR * e)) : 0;
-            mine = keys[e] > mine ? keys[e] : mine;
+            value[e] = l + LPR * e < v ? ordered(xs[e]) : 0u;
+            if (value[e] > mine) mine = value[e], at = (uint32_t)(l + LPR * e);
         }
         for (int k = 0; k < a.n_top; ++k) {
-            key_t64 best = mine;
-            auto with = [&](key_t64 o) { best = o > best ? o : best; };
-            if constexpr (LPR >= 2) with(lane_xor<1>(best, lane));
-            if constexpr (LPR >= 4) with(lane_xor<2>(best, lane));
-            if constexpr (LPR >= 8) with(lane_xor<4>(best, lane));
-            if constexpr (LPR >= 16) with(lane_xor<8>(best, lane));
-            if constexpr (LPR >= 32) with(lane_xor<16>(best, lane));
-            if constexpr (LPR >= 64) with(lane_xor<32>(best, lane));
-            const uint32_t index = key_index(best);
-            if (mine == best) {                                    // (one lane: keys are all different)
-                mine = 0;                                          // the largest of what is left
-#pragma unroll
-                for (int e = 0; e < E; ++e) mine = keys[e] < best && keys[e] > mine ? keys[e] : mine;
-                a.top_log_prob[row * a.n_top + k] = top_value(u, key_value(best), log_s);
+            const uint32_t best = row_best<LPR>(mine, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+            const uint32_t index = row_best<LPR>(mine == best ? at : ~0u, [](uint32_t p, uint32_t q) { return p < q ? p : q; });
+            if (at == index && mine == best) {                     // (one lane)
+                a.top_log_prob[row * a.n_top + k] = top_value(u, from_ordered(best), log_s);
                 a.top_index[row * a.n_top + k] = (int32_t)index;
+                mine = 0u;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if ((uint32_t)(l + LPR * e) == index) value[e] = 0u;
+                    if (value[e] > mine) mine = value[e], at = (uint32_t)(l + LPR * e);
+                }
             }
         }
     }
@@ -277,14 +286,15 @@ __global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
 constexpr int DEEP = 2;
 
 // the lane's classes at + 512 j .. at + 512 j + 7 as they lie in memory, -inf behind the end
-template <typename T> __device__ inline void load_step(const T *x, int64_t at, int64_t to, Eight<T> (&r)[DEEP])
+// ONCE: by way of no cache
+template <typename T, bool ONCE> __device__ inline void load_step(const T *x, int64_t at, int64_t to, Eight<T> (&r)[DEEP])
 {
     constexpr uint32_t NOTHING = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
 #pragma unroll
     for (int j = 0; j < DEEP; ++j) {
         const int64_t p = at + 512 * j;
         if (p + 8 <= to) {
-            load_eight(x + p, r[j]);
+            load_eight<ONCE>(x + p, r[j]);
         } else {
 #pragma unroll
             for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r[j].a[i] = v4u{NOTHING, NOTHING, NOTHING, NOTHING};
@@ -298,21 +308,23 @@ template <typename T> __device__ inline void load_step(const T *x, int64_t at, i
     }
 }
 
-template <typename T, bool TOP>
-__device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopList &list, key_t64 *room, int lane, int wave)
+// reached: LDS of the block, the largest key so far that n_top keys of one of its waves reach; zero at the start
+template <typename T, bool TOP, bool ONCE>
+__device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopList &list, key_t64 *room, key_t64 *reached, int lane, int wave)
 {
     constexpr int N = 8 * DEEP, WAVE = 64 * N;
     u = Sums{-__builtin_inff(), 0.f, 0.f};
     // (the wave goes round together, so that the list sees all lanes)
     int64_t base = from + wave * WAVE;
     Eight<T> r[DEEP];
-    if (base < to) load_step(x, base + lane * 8, to, r);
+    if (base < to) load_step<T, ONCE>(x, base + lane * 8, to, r);
     for (; base < to; base += WAVES * WAVE) {
         const int64_t at = base + lane * 8;
         float v[N];
 #pragma unroll
         for (int j = 0; j < DEEP; ++j) to_floats(r[j], *reinterpret_cast<float (*)[8]>(v + 8 * j));
-        if (base + WAVES * WAVE < to) load_step(x, at + WAVES * WAVE, to, r);
+        if (base + WAVES * WAVE < to) load_step<T, ONCE>(x, at + WAVES * WAVE, to, r);
+        const key_t64 others = TOP ? *reinterpret_cast<volatile key_t64 *>(reached) : 0;
         float m = v[0];
 #pragma unroll
         for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
@@ -331,17 +343,15 @@ __device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopLi
             u.s += p;
             u.t = __builtin_fmaf(p, bounded(d), u.t);
         }
-        if (TOP && __ballot(!(m < key_value(list.last)) || list.last == 0)) {
-            key_t64 keys[N], largest = 0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int64_t index = at + 512 * (e / 8) + e % 8;
-                keys[e] = index < to ? key_of(v[e], (uint32_t)index) : 0;
-                largest = keys[e] > largest ? keys[e] : largest;
-            }
-            if (list.last == 0) list.expect(largest, lane);
-            list.offer_all(keys, room, lane);
-        }
+        if (!TOP) continue;
+        list.raise((key_t64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(others >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)others));
+        if (list.last == 0) list.expect(m, lane);
+        const float bound = list.last ? key_value(list.last) : -__builtin_inff();
+        if (!__ballot(!(m < bound))) continue;
+        const key_t64 before = list.last;
+        list.offer(v, [&](int e) { return __ballot(!(v[e] < bound) && at + 512 * (e / 8) + e % 8 < to); },
+                   [&](int e) { return (uint32_t)(at + 512 * (e / 8) + e % 8); }, room, lane);
+        if (list.last > before && lane == 0) atomicMax(reached, list.last);
     }
 }
 
@@ -377,11 +387,11 @@ __device__ inline void store_top(const LogProbsFwd &a, int64_t row, const Sums &
     a.top_index[row * a.n_top + lane] = (int32_t)key_index(list.mine);
 }
 
-template <typename T, bool TOP>
+template <typename T, bool TOP, bool ONCE>
 __global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, int splits, int64_t per, Partial *parts, key_t64 *keys)
 {
     __shared__ Sums wave_sums[WAVES];
-    __shared__ key_t64 wave_keys[TOP ? WAVES : 1][64], room[TOP ? WAVES : 1][64];
+    __shared__ key_t64 wave_keys[TOP ? WAVES : 1][64], room[TOP ? WAVES : 1][64], reached;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     for (int64_t block = blockIdx.x; block < a.n * splits; block += gridDim.x) {
         const int64_t row = block / splits;
@@ -391,7 +401,11 @@ __global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, 
         Sums u;
         TopList list;
         list.n_top = a.n_top;
-        walk<T, TOP>(x, from, to, u, list, room[TOP ? wave : 0], lane, wave);
+        if (TOP) {
+            if (threadIdx.x == 0) reached = 0;
+            __syncthreads();
+        }
+        walk<T, TOP, ONCE>(x, from, to, u, list, room[TOP ? wave : 0], &reached, lane, wave);
         join_waves<WAVES, TOP>(u, list, wave_sums, wave_keys, lane, wave);
         if (wave == 0 && splits == 1) {
             const int64_t label = a.labels ? a.labels[row] : -1;
@@ -476,7 +490,7 @@ __global__ __launch_bounds__(THREADS) void small_bwd_kernel(const LogProbsBwd a)
     }
 }
 
-template <typename T>
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(THREADS) void long_bwd_kernel(const LogProbsBwd a, int chunks, int64_t per)
 {
     for (int64_t block = blockIdx.x; block < a.n * chunks; block += gridDim.x) {
@@ -488,7 +502,7 @@ __global__ __launch_bounds__(THREADS) void long_bwd_kernel(const LogProbsBwd a, 
         for (int64_t at = from + threadIdx.x * 8; at < to; at += THREADS * 8) {
             if (at + 8 <= to) {
                 Eight<T> raw;
-                load_eight(x + at, raw);
+                load_eight<ONCE>(x + at, raw);
                 float v[8];
                 to_floats(raw, v);
 #pragma unroll
@@ -513,6 +527,10 @@ Split split_of(int64_t n, int64_t v)
     const int64_t per = (ceil_div(v, s) + 7) / 8 * 8;
     return Split{(int)ceil_div(v, per), per};
 }
+
+// Logits that fill more than half of the memory's cache (256 MB) are read past the caches.  Forward and gradient with / without, us: 4096 x 32 768
+// bf16 (268 MB) 132 / 165, 2000 x 20 000 fp32 (160 MB) 99 / 105, bf16 (80 MB) 53 / 49.
+template <typename T> bool read_once(int64_t n, int64_t v) { return n * v * (int64_t)sizeof(T) > (int64_t)128 << 20; }
 
 unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < MAX_BLOCKS ? blocks : MAX_BLOCKS); }
 
@@ -539,7 +557,9 @@ int launch_fwd(const LogProbsFwd &a, void *workspace, hipStream_t stream)
     const Split s = split_of(a.n, a.v);
     Partial *parts = static_cast<Partial *>(workspace);
     key_t64 *keys = reinterpret_cast<key_t64 *>(static_cast<char *>(workspace) + align_up((size_t)a.n * s.splits * sizeof(Partial)));
-    auto kernel = a.n_top > 0 ? long_fwd_kernel<T, true> : long_fwd_kernel<T, false>;
+    const bool once = read_once<T>(a.n, a.v);
+    auto kernel = a.n_top > 0 ? (once ? long_fwd_kernel<T, true, true> : long_fwd_kernel<T, true, false>)
+                              : (once ? long_fwd_kernel<T, false, true> : long_fwd_kernel<T, false, false>);
     kernel<<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per, parts, keys);
     PCPP_HIP_CHECK(hipGetLastError());
     if (s.splits == 1) return PCPP_OK;
@@ -559,7 +579,8 @@ int launch_bwd(const LogProbsBwd &a, hipStream_t stream)
         });
     } else {
         const Split s = split_of(a.n, a.v);
-        long_bwd_kernel<T><<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per);
+        auto kernel = read_once<T>(a.n, a.v) ? long_bwd_kernel<T, true> : long_bwd_kernel<T, false>;
+        kernel<<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per);
     }
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;

@@ -44,11 +44,15 @@ template <typename T> __device__ inline void to_floats(const Eight<T> &r, float 
 }
 
 // ---- eight channels anywhere in memory, for rows that are walked (log_probs.hip) ----------------------------------------------
-struct __attribute__((packed, aligned(1))) Bytes16 { v4u v; };
-template <typename T> __device__ inline void load_eight(const T *p, Eight<T> &r)
+typedef v4u v4u_anywhere __attribute__((aligned(1)));
+template <bool ONCE, typename T> __device__ inline void load_eight(const T *p, Eight<T> &r)     // ONCE: past the caches
 {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.a[i] = reinterpret_cast<const Bytes16 *>(p)[i].v;
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) {
+        const v4u_anywhere *at = reinterpret_cast<const v4u_anywhere *>(p) + i;
+        if constexpr (ONCE) r.a[i] = __builtin_nontemporal_load(at);
+        else r.a[i] = *at;
+    }
 }
 template <typename T> __device__ inline void from_floats(const float (&v)[8], Eight<T> &r)
 {
@@ -65,7 +69,7 @@ template <typename T> __device__ inline void store_eight(T *p, const float (&v)[
     Eight<T> r;
     from_floats(v, r);
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<Bytes16 *>(p)[i].v = r.a[i];
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<v4u_anywhere *>(p)[i] = r.a[i];
 }
 
 // ---- rows in registers --------------------------------------------------------------------------------------------------------
