@@ -27,18 +27,6 @@ constexpr int MAX_BWD_BLOCKS = 1024;                              // backward: a
 
 __device__ inline float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * g)); }
 
-// One element at a multiple of the descriptor's elements
-template <typename T> __device__ inline uint32_t load_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t at)     // as the bits of an fp32 number
-{
-    if constexpr (sizeof(T) == 4) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, (int)(at * 4u), 0, 0);
-    else return (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(at * 2u), 0, 0) << 16;
-}
-template <typename T> __device__ inline void store_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t at, float v)
-{
-    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rs, (int)(at * 4u), 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b16(one_of<bf16_t>(v), rs, (int)(at * 2u), 0, 0);
-}
-
 // The row's mean (LAYER; else 0) subtracted from v in place, and 1 / sqrt(mean v^2 + eps).
 template <int LPR, int G, int MODE>
 __device__ inline float centre_row(float (&v)[G][8], int kind, const Span<MODE> (&own)[G], float inv_c, float eps)

@@ -9,10 +9,15 @@
 // entropy 0 and no gradient.  A row that holds a NaN or +inf has NaN everywhere but in its indices.
 //
 // Bound by memory, and in bf16 nearly as much by the exponentials.  Rows of up to 512 classes lie in the registers of a few lanes;
-// longer ones are walked by a thread block, or, where there are few rows, by several, whose sums a second kernel joins.
-// The most probable classes are kept as a list, sorted over the lanes of a wave, of 64-bit keys: the value in an order-preserving
-// form above the complement of the index, so that of equal values the lowest index is the largest key.  Hardly any element of a long
-// row passes the list's last entry, and only one that does costs more than the comparison.
+// longer ones are walked, by a wave or by a block of four, or, where there are few rows, by several blocks whose sums a second kernel
+// joins.
+//
+// The most probable classes.  A key is the value in an order-preserving form above the complement of the index, so that of equal
+// values the lowest index is the largest key, and no two are equal.  The n_top-th largest of the lanes' maxima so far is a bound that n_top
+// keys reach; it is close to the n_top-th largest key (of 64 maxima the 20th is about the 24th of all).  So only keys that pass it are
+// looked at: they go to a pool in LDS, and at the end every one that passes the last bound counts how many are larger, which is its place.
+// Rows whose order defeats the bound (their largest values in a few lanes) fill the pool; it is then sorted 64 keys at a time over the
+// lanes and merged into a list.
 
 #include "log_probs.h"
 #include "row_ops.h"
@@ -105,78 +110,94 @@ __device__ inline key_t64 merge_lists(key_t64 a, key_t64 b, int lane)
     return bitonic_merge(a > b ? a : b, lane);
 }
 
-// The largest keys seen by a wave: lane j holds the (j + 1)-th, 0 where there are fewer.
-struct TopList {
-    key_t64 mine = 0, last = 0;                                   // last: keys up to it do not belong to the n_top largest
-    int n_top;
-    __device__ inline void insert(key_t64 k, int lane)            // k: the same in all lanes, larger than `last`
-    {
-        const int at = __popcll(__ballot(mine > k));
-        const key_t64 before = (key_t64)dpp<0x138>((uint32_t)(mine >> 32)) << 32 | dpp<0x138>((uint32_t)mine);   // of the lane before
-        mine = lane < at ? mine : (lane == at ? k : before);
-        const key_t64 l = lane_of(mine, n_top - 1);
-        if (l > last) last = l;
-    }
-    // A bound in front of the first offers, from every lane's largest value: the n_top-th largest of these is reached by n_top keys, so that
-    // hardly more than n_top of the first keys are candidates.
-    __device__ inline void expect(float largest, int lane)
-    {
-        const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)sort_lanes(ordered(largest), lane), n_top - 1);
-        if (o > ordered(-__builtin_inff())) raise((key_t64)o << 32);
-    }
-    __device__ inline void raise(key_t64 reached)                 // n_top keys of the row reach it
-    {
-        if (reached > last) last = reached - 1;
-    }
-    // Several values of every lane at once; mask(e): the lanes whose value v[e] may belong, index(e): its class.  A few are put into the list
-    // one by one; more are gathered 64 at a time (`room`: 64 keys of LDS, the wave's own), sorted and merged, 28 exchanges of lanes for 64, where
-    // one insertion takes as long as three.
-    template <int N, typename Mask, typename Index>
-    __device__ inline void offer(const float (&v)[N], Mask mask, Index index, key_t64 *room, int lane)
-    {
+// The largest key that `n_top` of the wave's (N in each lane, as values in order) reach; not the largest such where some more reach it too, 0 where
+// fewer are not 0.
+template <int N> __device__ inline uint32_t bound_of(const uint32_t (&o)[N], int n_top)
+{
+    uint32_t bound = 0u;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t at = bound | 1u << bit;
         int n = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e) n += __popcll(mask(e));
-        if (n <= 6) {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                for (key_t64 left = mask(e); left; left &= left - 1) {
-                    const int from = __ffsll((long long)left) - 1;
-                    const key_t64 k = key_of(__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[e]), from)),
-                                             (uint32_t)__builtin_amdgcn_readlane((int)index(e), from));
-                    if (k > last) insert(k, lane);
-                }
-            return;
+        for (int e = 0; e < N; ++e) n += __popcll(__ballot(o[e] >= at));
+        if (n >= n_top) {
+            bound = at;
+            if (n <= n_top + 4) break;
         }
+    }
+    return bound;
+}
+
+// What a wave keeps of the keys that it has seen.
+constexpr int POOL = 256;
+struct TopKeys {
+    key_t64 list = 0, last = 0;                                   // list: lane j its (j + 1)-th largest; last: keys up to it do not belong
+    key_t64 *pool;                                                // LDS, the wave's own
+    int n = 0, n_top;
+    bool listed = false;
+
+    // (the lanes' writes before the reads, and these before the next writes)
+    __device__ static inline void settle()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    __device__ inline void raise(uint32_t bound) { if (bound && (key_t64)bound << 32 > last) last = ((key_t64)bound << 32) - 1; }
+    __device__ static inline uint32_t before(key_t64 m) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)); }
+    // the lanes' keys k where `in`
+    __device__ inline void push(key_t64 k, bool in, int lane)
+    {
+        in = in && k > last;
+        key_t64 m = __ballot(in);
+        if (n + __popcll(m) > POOL) {
+            flush(pool, lane);
+            in = in && k > last;
+            m = __ballot(in);
+        }
+        if (in) pool[n + before(m)] = k;
+        n += __popcll(m);
+    }
+    __device__ inline void merge(key_t64 k, int lane)             // the lanes' keys, in any order
+    {
+        k = sort_lanes(k, lane);
+        list = listed ? merge_lists(list, k, lane) : k;
+        listed = true;
+        const key_t64 l = lane_of(list, n_top - 1);
+        if (l > last) last = l;
+    }
+    __device__ inline void flush(const key_t64 *from, int lane)   // the n keys there into the list
+    {
+        settle();
+        for (int i = 0; i < n; i += 64) merge(i + lane < n ? from[i + lane] : 0, lane);
+        settle();
         n = 0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const key_t64 all = mask(e);
-            if (!all) continue;
-            const key_t64 k = key_of(v[e], index(e));
-            bool in = (all >> lane & 1) && k > last;
-            key_t64 m = __ballot(in);
-            if (n + __popcll(m) > 64) {
-                merge(room, n, lane);
-                n = 0;
-                in = in && k > last;
-                m = __ballot(in);
-            }
-            if (in) room[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u))] = k;
+    }
+    // Keys there that still belong, to the front of the pool behind those that it holds (at or in front of `from`).
+    __device__ inline void gather(const key_t64 *from, int count, int lane)
+    {
+        settle();
+        for (int i = 0; i < count; i += 64) {
+            const key_t64 k = i + lane < count ? from[i + lane] : 0;
+            const bool in = k > last;
+            const key_t64 m = __ballot(in);
+            settle();
+            if (in) pool[n + before(m)] = k;
             n += __popcll(m);
         }
-        merge(room, n, lane);
+        settle();
     }
-    __device__ inline void merge(const key_t64 *room, int n, int lane)
+    // put(place, key) for the n_top largest of the pool and the list, each in one lane
+    template <typename Put> __device__ inline void finish(int lane, Put put)
     {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (the lanes' writes before the reads, and these before the next writes)
-        __builtin_amdgcn_wave_barrier();
-        const key_t64 k = lane < n ? room[lane] : 0;
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        mine = merge_lists(mine, sort_lanes(k, lane), lane);
-        const key_t64 l = lane_of(mine, n_top - 1);
-        if (l > last) last = l;
+        if (!listed && n <= 64) {
+            const key_t64 k = lane < n ? pool[lane] : 0;
+            int place = 0;
+            for (int j = 0; j < n; ++j) place += pool[j] > k;
+            if (lane < n && place < n_top) put(place, k);
+        } else {
+            flush(pool, lane);
+            if (lane < n_top) put(lane, list);
+        }
     }
 };
 
@@ -196,27 +217,24 @@ struct Sums {
         m = nm;
     }
 };
-__device__ inline Sums join_lanes(Sums v, int lanes)
+// the sums of the LPR lanes of a row, in all of them
+template <int LPR> __device__ inline Sums join_lanes(Sums v)
 {
-    for (int d = 1; d < lanes; d <<= 1) {
-        const float om = __shfl_xor(v.m, d), os = __shfl_xor(v.s, d), ot = __shfl_xor(v.t, d);
-        v.join(om, os, ot);
-    }
-    return v;
+    const float m = row_max<LPR>(v.m), d = m == -__builtin_inff() ? 0.f : bounded(v.m - m), e = exp_of(d);
+    return Sums{m, row_sum<LPR>(e * v.s), row_sum<LPR>(e * (v.t + d * v.s))};
 }
 
 // what a row's sums say; NaN in S reaches everything
-__device__ inline float row_results(const LogProbsFwd &a, int64_t row, const Sums &v, float x_label, bool labelled)
+__device__ inline float log_of(float s) { return __builtin_amdgcn_logf(s) * 0.693147181f; }
+__device__ inline void row_results(const LogProbsFwd &a, int64_t row, const Sums &v, float log_s, float x_label, bool labelled)
 {
     const bool empty = v.s == 0.f;
-    const float log_s = __builtin_amdgcn_logf(v.s) * 0.693147181f;
     if (a.max_log_sum) *reinterpret_cast<float2 *>(a.max_log_sum + 2 * row) = float2{v.m, empty ? 0.f : log_s};
     if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - v.t / v.s;
     if (a.log_prob) {
         const float lp = empty ? -__builtin_inff() : (x_label - v.m) - log_s;
         a.log_prob[row] = labelled ? lp : 0.f;
     }
-    return log_s;
 }
 __device__ inline float top_value(const Sums &v, float x, float log_s) { return v.s == 0.f ? -__builtin_inff() : (x - v.m) - log_s; }
 
@@ -226,56 +244,90 @@ template <int LPR, typename Op> __device__ inline uint32_t row_best(uint32_t v, 
     return __float_as_uint(row_reduce<LPR>(__uint_as_float(v), [&](float a, float b) { return __uint_as_float(op(__float_as_uint(a), __float_as_uint(b))); }));
 }
 
-// ---- rows in registers: LPR lanes a row, lane l holding the classes l + LPR e ------------------------------------------------
-template <typename T, int LPR>
+// ---- rows in registers ---------------------------------------------------------------------------------------------------------
+// One class after the other: the largest of the lanes', of equal ones the lowest index.  (Rows in fewer than 64 lanes; n_top may be larger than their
+// number.)
+template <int LPR, typename Put> __device__ inline void take_in_turn(uint32_t (&value)[8], int at, int n_top, Put put)
+{
+    uint32_t mine = 0u, index = 0u;                                // 0: none left
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (value[e] > mine) mine = value[e], index = (uint32_t)(at + e);
+    for (int k = 0; k < n_top; ++k) {
+        const uint32_t best = row_best<LPR>(mine, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+        const uint32_t first = row_best<LPR>(mine == best ? index : ~0u, [](uint32_t p, uint32_t q) { return p < q ? p : q; });
+        if (index == first && mine == best) {                      // (one lane)
+            put(k, best, index);
+            mine = 0u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if ((uint32_t)(at + e) == first) value[e] = 0u;
+                if (value[e] > mine) mine = value[e], index = (uint32_t)(at + e);
+            }
+        }
+    }
+}
+
+template <typename T, int LPR, int MODE, bool TOP>
 __global__ __launch_bounds__(THREADS) void small_fwd_kernel(const LogProbsFwd a)
 {
-    constexpr int ROWS = THREADS / LPR, E = 8;
-    const int l = (int)threadIdx.x % LPR;
-    const int v = (int)a.v;
-    // (a row's lanes leave together)
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
-        const T *x = static_cast<const T *>(a.logits) + row * a.ld;
-        float xs[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) xs[e] = l + LPR * e < v ? one_float<T>(x[l + LPR * e]) : -__builtin_inff();
-        const int label = a.labels ? a.labels[row] : -1;
+    constexpr int ROWS = 64 / LPR, TS = sizeof(T);
+    __shared__ key_t64 pool[TOP && LPR == 64 ? WAVES : 1][POOL];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), v = (int)a.v;
+    const Span<MODE> own(8 * (lane % LPR), v);
+    const uint32_t in_wave = (uint32_t)(lane / LPR), off = own.template offset<TS>(in_wave * (uint32_t)a.ld);
+    for (int64_t first = ((int64_t)blockIdx.x * WAVES + wave) * ROWS; first < a.n; first += (int64_t)gridDim.x * WAVES * ROWS) {
+        const int64_t row = first + in_wave;
+        const bool live = row < a.n;
+        const __amdgpu_buffer_rsrc_t xs = rows_from<TS>(a.logits, first, a.n, a.ld, v, ROWS);
+        Eight<T> raw;
+        row_load<T>(xs, off, own, raw);
+        const int label = a.labels && live ? a.labels[row] : -1;
         const bool labelled = label >= 0 && label < v;
+        const float x_label = __uint_as_float(load_one<T>(xs, labelled ? in_wave * (uint32_t)a.ld + (uint32_t)label : OOB_OFFSET / TS));
+        float x[8];
+        to_floats(raw, x);
         Sums u{-__builtin_inff(), 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < E; ++e) u.m = fmaxf(u.m, xs[e]);
+        for (int e = 0; e < 8; ++e) {
+            x[e] = own.own(e) ? x[e] : -__builtin_inff();
+            u.m = fmaxf(u.m, x[e]);
+        }
+        const float lane_m = u.m;
         u.m = row_max<LPR>(u.m);
         const float m0 = u.m == -__builtin_inff() ? 0.f : u.m;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float d = xs[e] - m0, p = exp_of(d);
+        for (int e = 0; e < 8; ++e) {
+            const float d = x[e] - m0, p = exp_of(d);
             u.s += p;
             u.t = __builtin_fmaf(p, bounded(d), u.t);
         }
         u.s = row_sum<LPR>(u.s);
         u.t = row_sum<LPR>(u.t);
-        if (l == 0) row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
-        const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
-        // one class after the other: the largest of the lane's, then of the row's lanes; of equal ones the lowest index
-        if (a.n_top == 0) continue;
-        uint32_t value[E], mine = 0u, at = 0u;                     // 0: no class, or taken already; at: class of the lane's largest
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            value[e] = l + LPR * e < v ? ordered(xs[e]) : 0u;
-            if (value[e] > mine) mine = value[e], at = (uint32_t)(l + LPR * e);
-        }
-        for (int k = 0; k < a.n_top; ++k) {
-            const uint32_t best = row_best<LPR>(mine, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
-            const uint32_t index = row_best<LPR>(mine == best ? at : ~0u, [](uint32_t p, uint32_t q) { return p < q ? p : q; });
-            if (at == index && mine == best) {                     // (one lane)
-                a.top_log_prob[row * a.n_top + k] = top_value(u, from_ordered(best), log_s);
+        const float log_s = log_of(u.s);
+        if (live && lane % LPR == 0) row_results(a, row, u, log_s, x_label, labelled);
+        if constexpr (TOP) {
+            auto put = [&](int k, uint32_t value, uint32_t index) {
+                if (!live) return;
+                a.top_log_prob[row * a.n_top + k] = top_value(u, from_ordered(value), log_s);
                 a.top_index[row * a.n_top + k] = (int32_t)index;
-                mine = 0u;
+            };
+            if constexpr (LPR == 64) {
+                TopKeys keys;
+                keys.pool = pool[wave];
+                keys.n_top = a.n_top;
+                const uint32_t largest[1] = {lane_m > -__builtin_inff() ? ordered(lane_m) : 0u};
+                keys.raise(bound_of(largest, a.n_top));
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    if ((uint32_t)(l + LPR * e) == index) value[e] = 0u;
-                    if (value[e] > mine) mine = value[e], at = (uint32_t)(l + LPR * e);
-                }
+                for (int e = 0; e < 8; ++e) keys.push(key_of(x[e], (uint32_t)(own.at + e)), own.own(e), lane);
+                TopKeys::settle();
+                keys.finish(lane, [&](int k, key_t64 key) { put(k, (uint32_t)(key >> 32), key_index(key)); });
+                TopKeys::settle();
+            } else {
+                uint32_t value[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) value[e] = own.own(e) ? ordered(x[e]) : 0u;
+                take_in_turn<LPR>(value, own.at, a.n_top, put);
             }
         }
     }
@@ -308,23 +360,22 @@ template <typename T, bool ONCE> __device__ inline void load_step(const T *x, in
     }
 }
 
-// reached: LDS of the block, the largest key so far that n_top keys of one of its waves reach; zero at the start
-template <typename T, bool TOP, bool ONCE>
-__device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopList &list, key_t64 *room, key_t64 *reached, int lane, int wave)
+// W: waves that walk the row
+template <typename T, int W, bool TOP, bool ONCE>
+__device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopKeys &keys, int lane, int wave)
 {
     constexpr int N = 8 * DEEP, WAVE = 64 * N;
     u = Sums{-__builtin_inff(), 0.f, 0.f};
-    // (the wave goes round together, so that the list sees all lanes)
+    // (the wave goes round together, so that the pool sees all lanes)
     int64_t base = from + wave * WAVE;
     Eight<T> r[DEEP];
     if (base < to) load_step<T, ONCE>(x, base + lane * 8, to, r);
-    for (; base < to; base += WAVES * WAVE) {
+    for (; base < to; base += W * WAVE) {
         const int64_t at = base + lane * 8;
         float v[N];
 #pragma unroll
         for (int j = 0; j < DEEP; ++j) to_floats(r[j], *reinterpret_cast<float (*)[8]>(v + 8 * j));
-        if (base + WAVES * WAVE < to) load_step<T, ONCE>(x, at + WAVES * WAVE, to, r);
-        const key_t64 others = TOP ? *reinterpret_cast<volatile key_t64 *>(reached) : 0;
+        if (base + W * WAVE < to) load_step<T, ONCE>(x, at + W * WAVE, to, r);
         float m = v[0];
 #pragma unroll
         for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
@@ -344,80 +395,126 @@ __device__ inline void walk(const T *x, int64_t from, int64_t to, Sums &u, TopLi
             u.t = __builtin_fmaf(p, bounded(d), u.t);
         }
         if (!TOP) continue;
-        list.raise((key_t64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(others >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)others));
-        if (list.last == 0) list.expect(m, lane);
-        const float bound = list.last ? key_value(list.last) : -__builtin_inff();
-        if (!__ballot(!(m < bound))) continue;
-        const key_t64 before = list.last;
-        list.offer(v, [&](int e) { return __ballot(!(v[e] < bound) && at + 512 * (e / 8) + e % 8 < to); },
-                   [&](int e) { return (uint32_t)(at + 512 * (e / 8) + e % 8); }, room, lane);
-        if (list.last > before && lane == 0) atomicMax(reached, list.last);
+        auto bound = [&] { return keys.last ? key_value(keys.last) : -__builtin_inff(); };
+        if (!__ballot(!(m < bound()))) continue;
+        const uint32_t largest[1] = {u.m > -__builtin_inff() ? ordered(u.m) : 0u};
+        keys.raise(bound_of(largest, keys.n_top));
+        const float b = bound();
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int64_t index = at + 512 * (e / 8) + e % 8;
+            const bool in = !(v[e] < b) && index < to;
+            if (__ballot(in)) keys.push(key_of(v[e], (uint32_t)index), in, lane);
+        }
     }
 }
 
 struct Partial { float m, s, t, unused; };
 
-// The sums and lists of a block's N waves (a power of two), pair by pair; both end in wave 0.
-template <int N, bool TOP>
-__device__ inline void join_waves(Sums &u, TopList &list, Sums *sums, key_t64 (*keys)[64], int lane, int wave)
+// LDS of a block's N waves
+template <int N> struct Joint {
+    Sums sums[N];
+    uint32_t largest[N][64];
+    int count[N];
+    bool listed[N];
+    key_t64 last[N], list[N][64];
+};
+
+// The sums of a block's N waves, in wave 0.
+template <int N> __device__ inline void join_sums(Sums &u, Sums *sums, int lane, int wave)
 {
-    u = join_lanes(u, 64);
     if (lane == 0) sums[wave] = u;
-    if (TOP) keys[wave][lane] = list.mine;
     __syncthreads();
-    if (wave == 0) {
-        u = join_lanes(sums[lane % N], N);                         // (in all lanes)
+    if (wave == 0) u = join_lanes<N>(sums[lane % N]);               // (in all lanes)
+}
+
+// What N waves keep of a row, into wave 0's; pools: the waves' pools one behind the other.  largest: the lane's value, in order.
+template <int N>
+__device__ inline void join_keys(TopKeys &keys, Joint<N> &joint, key_t64 (*pools)[POOL], uint32_t largest, int lane, int wave)
+{
+    joint.largest[wave][lane] = largest;
+    if (keys.listed) joint.list[wave][lane] = keys.list;
+    if (lane == 0) {
+        joint.count[wave] = keys.n;
+        joint.listed[wave] = keys.listed;
+        joint.last[wave] = keys.last;
     }
-    if (TOP) {
+    __syncthreads();
+    if (wave != 0) return;
+    uint32_t o[N];
 #pragma unroll
-        for (int half = N / 2; half > 0; half >>= 1) {
-            if (wave < half) {
-                list.mine = merge_lists(list.mine, keys[wave + half][lane], lane);
-                keys[wave][lane] = list.mine;
-            }
-            if (half > 1) __syncthreads();
-        }
+    for (int w = 0; w < N; ++w) o[w] = joint.largest[w][lane];
+    keys.raise(bound_of(o, keys.n_top));
+#pragma unroll
+    for (int w = 1; w < N; ++w) {
+        const key_t64 l = joint.last[w];
+        if (l > keys.last) keys.last = l - 1;                     // (wave w may hold the key itself)
     }
+    keys.n = 0;
+#pragma unroll
+    for (int w = 0; w < N; ++w) keys.gather(pools[w], joint.count[w], lane);
+#pragma unroll
+    for (int w = 1; w < N; ++w)
+        if (joint.listed[w]) {
+            keys.list = keys.listed ? merge_lists(keys.list, joint.list[w][lane], lane) : joint.list[w][lane];
+            keys.listed = true;
+        }
 }
 
-__device__ inline void store_top(const LogProbsFwd &a, int64_t row, const Sums &u, const TopList &list, float log_s, int lane)
+// W waves a row, or a part of it
+template <typename T, int W, bool TOP, bool ONCE>
+__global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, int splits, int64_t per, Partial *parts, key_t64 *split_keys)
 {
-    if (lane >= a.n_top) return;
-    a.top_log_prob[row * a.n_top + lane] = top_value(u, key_value(list.mine), log_s);
-    a.top_index[row * a.n_top + lane] = (int32_t)key_index(list.mine);
-}
-
-template <typename T, bool TOP, bool ONCE>
-__global__ __launch_bounds__(THREADS) void long_fwd_kernel(const LogProbsFwd a, int splits, int64_t per, Partial *parts, key_t64 *keys)
-{
-    __shared__ Sums wave_sums[WAVES];
-    __shared__ key_t64 wave_keys[TOP ? WAVES : 1][64], room[TOP ? WAVES : 1][64], reached;
+    constexpr int ROWS = WAVES / W;
+    __shared__ Joint<W> joint;
+    __shared__ key_t64 pools[TOP ? WAVES : 1][POOL];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    for (int64_t block = blockIdx.x; block < a.n * splits; block += gridDim.x) {
+    // (W = 1: no barriers, so the waves need not go round together)
+    for (int64_t block = (int64_t)blockIdx.x * ROWS + wave / W; block < a.n * splits; block += (int64_t)gridDim.x * ROWS) {
         const int64_t row = block / splits;
         const int split = (int)(block % splits);
         const T *x = static_cast<const T *>(a.logits) + row * a.ld;
         const int64_t from = split * per, to = from + per < a.v ? from + per : a.v;
         Sums u;
-        TopList list;
-        list.n_top = a.n_top;
-        if (TOP) {
-            if (threadIdx.x == 0) reached = 0;
-            __syncthreads();
+        TopKeys keys;
+        keys.n_top = a.n_top;
+        keys.pool = pools[TOP ? wave : 0];
+        walk<T, W, TOP, ONCE>(x, from, to, u, keys, lane, wave % W);
+        const float lane_m = u.m;
+        u = join_lanes<64>(u);
+        if constexpr (W > 1) {
+            join_sums<W>(u, joint.sums, lane, wave);
+            if (TOP) join_keys<W>(keys, joint, pools, lane_m > -__builtin_inff() ? ordered(lane_m) : 0u, lane, wave);
+        } else if (TOP) {
+            const uint32_t largest[1] = {lane_m > -__builtin_inff() ? ordered(lane_m) : 0u};
+            keys.raise(bound_of(largest, a.n_top));
+            const int n = keys.n;
+            keys.n = 0;
+            keys.gather(keys.pool, n, lane);
         }
-        walk<T, TOP, ONCE>(x, from, to, u, list, room[TOP ? wave : 0], &reached, lane, wave);
-        join_waves<WAVES, TOP>(u, list, wave_sums, wave_keys, lane, wave);
-        if (wave == 0 && splits == 1) {
-            const int64_t label = a.labels ? a.labels[row] : -1;
-            const bool labelled = label >= 0 && label < a.v;
-            const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
-            if (lane == 0) row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
-            if (TOP) store_top(a, row, u, list, log_s, lane);
-        } else if (wave == 0) {
-            if (lane == 0) parts[block] = Partial{u.m, u.s, u.t, 0.f};
-            if (TOP && lane < a.n_top) keys[block * a.n_top + lane] = list.mine;      // (0 past the end of a short list)
+        if (wave % W == 0) {
+            if (splits == 1) {
+                const int64_t label = a.labels ? a.labels[row] : -1;
+                const bool labelled = label >= 0 && label < a.v;
+                const float log_s = log_of(u.s);
+                if (lane == 0) row_results(a, row, u, log_s, labelled ? one_float<T>(x[label]) : 0.f, labelled);
+                if (TOP)
+                    keys.finish(lane, [&](int k, key_t64 key) {
+                        a.top_log_prob[row * a.n_top + k] = top_value(u, key_value(key), log_s);
+                        a.top_index[row * a.n_top + k] = (int32_t)key_index(key);
+                    });
+            } else {
+                if (lane == 0) parts[block] = Partial{u.m, u.s, u.t, 0.f};
+                if (TOP) {
+                    key_t64 *to_keys = split_keys + block * a.n_top;
+                    const int held = keys.listed ? 64 : keys.n;
+                    if (lane >= held && lane < a.n_top) to_keys[lane] = 0;            // (a short part has fewer)
+                    keys.finish(lane, [&](int k, key_t64 key) { to_keys[k] = key; });
+                }
+            }
         }
-        __syncthreads();                                           // (the next row's sums go where these lay)
+        if constexpr (W > 1) __syncthreads();                      // (the next row's sums and keys go where these lay)
+        else if (TOP) TopKeys::settle();
     }
 }
 
@@ -426,8 +523,8 @@ constexpr int JOIN_WAVES = 16;
 template <typename T, bool TOP>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void join_fwd_kernel(const LogProbsFwd a, int splits, const Partial *parts, const key_t64 *keys)
 {
-    __shared__ Sums wave_sums[JOIN_WAVES];
-    __shared__ key_t64 wave_keys[TOP ? JOIN_WAVES : 1][64];
+    __shared__ Sums sums[JOIN_WAVES];
+    __shared__ key_t64 lists[TOP ? JOIN_WAVES : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t row = blockIdx.x;                               // (few rows: they were split)
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
@@ -436,18 +533,33 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_fwd_kernel(const LogProb
         const Partial p = parts[row * splits + s];
         u.join(p.m, p.s, p.t);
     }
-    TopList list;
-    list.n_top = a.n_top;
-    if (TOP)
-        for (int s = wave; s < splits; s += JOIN_WAVES)
-            list.mine = merge_lists(list.mine, lane < a.n_top ? keys[(row * splits + s) * a.n_top + lane] : 0, lane);
-    join_waves<JOIN_WAVES, TOP>(u, list, wave_sums, wave_keys, lane, wave);
+    u = join_lanes<64>(u);
+    key_t64 list = 0;
+    if (TOP) {
+        for (int s = wave; s < splits; s += JOIN_WAVES) {
+            const key_t64 k = lane < a.n_top ? keys[(row * splits + s) * a.n_top + lane] : 0;
+            list = s == wave ? k : merge_lists(list, k, lane);
+        }
+        lists[wave][lane] = list;
+    }
+    join_sums<JOIN_WAVES>(u, sums, lane, wave);
+    if (TOP) {
+        for (int half = JOIN_WAVES / 2; half > 0; half >>= 1) {
+            if (wave < half) {
+                if (wave + half < splits) lists[wave][lane] = list = merge_lists(list, lists[wave + half][lane], lane);
+            }
+            __syncthreads();
+        }
+    }
     if (wave != 0) return;
     const int64_t label = a.labels ? a.labels[row] : -1;
     const bool labelled = label >= 0 && label < a.v;
-    const float log_s = __builtin_amdgcn_logf(u.s) * 0.693147181f;
-    if (lane == 0) row_results(a, row, u, labelled ? one_float<T>(x[label]) : 0.f, labelled);
-    if (TOP) store_top(a, row, u, list, log_s, lane);
+    const float log_s = log_of(u.s);
+    if (lane == 0) row_results(a, row, u, log_s, labelled ? one_float<T>(x[label]) : 0.f, labelled);
+    if (TOP && lane < a.n_top) {
+        a.top_log_prob[row * a.n_top + lane] = top_value(u, key_value(list), log_s);
+        a.top_index[row * a.n_top + lane] = (int32_t)key_index(list);
+    }
 }
 
 // ---- gradient --------------------------------------------------------------------------------------------------------------
@@ -472,21 +584,25 @@ __device__ inline float grad_of(const RowGrad &g, float x, bool hit)
     return (hit ? g.dl : 0.f) - p * g.dl - g.dh * (p * (bounded(lp) + g.h));
 }
 
-template <typename T, int LPR>
+template <typename T, int LPR, int MODE>
 __global__ __launch_bounds__(THREADS) void small_bwd_kernel(const LogProbsBwd a)
 {
-    constexpr int ROWS = THREADS / LPR, E = 8;
-    const int l = (int)threadIdx.x % LPR;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; row < a.n; row += (int64_t)gridDim.x * ROWS) {
-        const T *x = static_cast<const T *>(a.logits) + row * a.ld;
-        T *d = static_cast<T *>(a.d_logits) + row * a.ld_d;
+    constexpr int ROWS = 64 / LPR, TS = sizeof(T);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), v = (int)a.v;
+    const Span<MODE> own(8 * (lane % LPR), v);
+    const uint32_t in_wave = (uint32_t)(lane / LPR), off = own.template offset<TS>(in_wave * (uint32_t)a.ld);
+    const uint32_t off_d = own.template offset<TS>(in_wave * (uint32_t)a.ld_d);
+    for (int64_t first = ((int64_t)blockIdx.x * WAVES + wave) * ROWS; first < a.n; first += (int64_t)gridDim.x * WAVES * ROWS) {
+        const int64_t row = first + in_wave < a.n ? first + in_wave : a.n - 1;      // (rows past the last are not written)
+        const __amdgpu_buffer_rsrc_t xs = rows_from<TS>(a.logits, first, a.n, a.ld, v, ROWS), ds = rows_from<TS>(a.d_logits, first, a.n, a.ld_d, v, ROWS);
+        Eight<T> raw;
+        row_load<T>(xs, off, own, raw);
         const RowGrad g = row_grad(a, row);
-        float xs[E];
+        float x[8];
+        to_floats(raw, x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) xs[e] = l + LPR * e < a.v ? one_float<T>(x[l + LPR * e]) : 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (l + LPR * e < a.v) d[l + LPR * e] = one_of<T>(grad_of(g, xs[e], l + LPR * e == g.label));
+        for (int e = 0; e < 8; ++e) x[e] = grad_of(g, x[e], own.at + e == g.label);
+        row_store<T>(ds, off_d, own, x);
     }
 }
 
@@ -528,28 +644,27 @@ Split split_of(int64_t n, int64_t v)
     return Split{(int)ceil_div(v, per), per};
 }
 
+// A row by a wave on its own: no barrier and no join, but a fourth of the waves.
+bool row_by_wave(int64_t n, int64_t v) { return v <= 4096 && n >= 2048; }
+
 // Logits that fill more than half of the memory's cache (256 MB) are read past the caches.  Forward and gradient with / without, us: 4096 x 32 768
 // bf16 (268 MB) 132 / 165, 2000 x 20 000 fp32 (160 MB) 99 / 105, bf16 (80 MB) 53 / 49.
 template <typename T> bool read_once(int64_t n, int64_t v) { return n * v * (int64_t)sizeof(T) > (int64_t)128 << 20; }
 
 unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < MAX_BLOCKS ? blocks : MAX_BLOCKS); }
 
-template <typename F> void with_lanes(int64_t v, F f)
-{
-    if (v <= 32) return f(std::integral_constant<int, 4>{});
-    if (v <= 64) return f(std::integral_constant<int, 8>{});
-    if (v <= 128) return f(std::integral_constant<int, 16>{});
-    if (v <= 256) return f(std::integral_constant<int, 32>{});
-    return f(std::integral_constant<int, 64>{});
-}
+// Rows in registers: up to 512 classes, and pitches with which a wave's sixteen rows lie within 32-bit offsets
+bool in_registers(int64_t v, int64_t ld) { return v <= SMALL && ld < 1 << 24; }
 
 template <typename T>
 int launch_fwd(const LogProbsFwd &a, void *workspace, hipStream_t stream)
 {
-    if (a.v <= SMALL) {
-        with_lanes(a.v, [&](auto lanes) {
-            constexpr int LPR = decltype(lanes)::value;
-            small_fwd_kernel<T, LPR><<<grid_of(ceil_div(a.n, THREADS / LPR)), THREADS, 0, stream>>>(a);
+    const bool top = a.n_top > 0;
+    if (in_registers(a.v, a.ld)) {
+        with_rows((int)a.v, [&](auto lanes, auto, auto mode) {
+            constexpr int LPR = decltype(lanes)::value, MODE = decltype(mode)::value;
+            auto kernel = top ? small_fwd_kernel<T, LPR, MODE, true> : small_fwd_kernel<T, LPR, MODE, false>;
+            kernel<<<grid_of(ceil_div(a.n, THREADS / LPR)), THREADS, 0, stream>>>(a);
         });
         PCPP_HIP_CHECK(hipGetLastError());
         return PCPP_OK;
@@ -557,13 +672,18 @@ int launch_fwd(const LogProbsFwd &a, void *workspace, hipStream_t stream)
     const Split s = split_of(a.n, a.v);
     Partial *parts = static_cast<Partial *>(workspace);
     key_t64 *keys = reinterpret_cast<key_t64 *>(static_cast<char *>(workspace) + align_up((size_t)a.n * s.splits * sizeof(Partial)));
-    const bool once = read_once<T>(a.n, a.v);
-    auto kernel = a.n_top > 0 ? (once ? long_fwd_kernel<T, true, true> : long_fwd_kernel<T, true, false>)
-                              : (once ? long_fwd_kernel<T, false, true> : long_fwd_kernel<T, false, false>);
-    kernel<<<grid_of(a.n * s.splits), THREADS, 0, stream>>>(a, s.splits, s.per, parts, keys);
+    const bool once = read_once<T>(a.n, a.v), wave = row_by_wave(a.n, a.v);
+    auto pick = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        auto kernel = top ? (once ? long_fwd_kernel<T, W, true, true> : long_fwd_kernel<T, W, true, false>)
+                          : (once ? long_fwd_kernel<T, W, false, true> : long_fwd_kernel<T, W, false, false>);
+        kernel<<<grid_of(ceil_div(a.n * s.splits, WAVES / W)), THREADS, 0, stream>>>(a, s.splits, s.per, parts, keys);
+    };
+    if (wave) pick(Int<1>{});
+    else pick(Int<WAVES>{});
     PCPP_HIP_CHECK(hipGetLastError());
     if (s.splits == 1) return PCPP_OK;
-    auto join = a.n_top > 0 ? join_fwd_kernel<T, true> : join_fwd_kernel<T, false>;
+    auto join = top ? join_fwd_kernel<T, true> : join_fwd_kernel<T, false>;
     join<<<(unsigned)a.n, JOIN_WAVES * 64, 0, stream>>>(a, s.splits, parts, keys);
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;
@@ -572,10 +692,10 @@ int launch_fwd(const LogProbsFwd &a, void *workspace, hipStream_t stream)
 template <typename T>
 int launch_bwd(const LogProbsBwd &a, hipStream_t stream)
 {
-    if (a.v <= SMALL) {
-        with_lanes(a.v, [&](auto lanes) {
+    if (in_registers(a.v, a.ld > a.ld_d ? a.ld : a.ld_d)) {
+        with_rows((int)a.v, [&](auto lanes, auto, auto mode) {
             constexpr int LPR = decltype(lanes)::value;
-            small_bwd_kernel<T, LPR><<<grid_of(ceil_div(a.n, THREADS / LPR)), THREADS, 0, stream>>>(a);
+            small_bwd_kernel<T, LPR, decltype(mode)::value><<<grid_of(ceil_div(a.n, THREADS / LPR)), THREADS, 0, stream>>>(a);
         });
     } else {
         const Split s = split_of(a.n, a.v);
@@ -590,7 +710,7 @@ int launch_bwd(const LogProbsBwd &a, hipStream_t stream)
 
 size_t log_probs_workspace_bytes(int64_t n, int64_t v, int n_top)
 {
-    if (v <= SMALL) return 0;
+    if (v <= SMALL) return 0;                                     // (of one block a row, whatever the pitch)
     const Split s = split_of(n, v);
     if (s.splits == 1) return 0;
     return align_up((size_t)n * s.splits * sizeof(Partial)) + align_up((size_t)n * s.splits * n_top * sizeof(key_t64));

@@ -139,6 +139,18 @@ template <typename T, int MODE> __device__ inline void row_store(const __amdgpu_
     }
 }
 
+// One element at a multiple of the descriptor's elements
+template <typename T> __device__ inline uint32_t load_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t at)     // as the bits of an fp32 number
+{
+    if constexpr (sizeof(T) == 4) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, (int)(at * 4u), 0, 0);
+    else return (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(at * 2u), 0, 0) << 16;
+}
+template <typename T> __device__ inline void store_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t at, float v)
+{
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rs, (int)(at * 4u), 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(one_of<bf16_t>(v), rs, (int)(at * 2u), 0, 0);
+}
+
 // Values of other lanes of a row of sixteen
 template <int CTRL> __device__ inline uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
 constexpr int DPP_XOR1 = 0xb1, DPP_XOR2 = 0x4e, DPP_XOR3 = 0x1b, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
