@@ -312,24 +312,27 @@ __global__ __launch_bounds__(THREADS) void block_bwd_kernel(const BlockNormBwd a
     }
 }
 
-// Sums of the blocks' partial sums [blocks][2][c]: wave w of sixteen adds the rows w, w + 16, ..., then the waves' sums in order of w.
+// Sums of the blocks' partial sums [blocks][2][c]: a block takes sixteen columns, a thread every 64th row of one; then the four threads of a
+// wave and the waves, in order.  (64 columns a block and every 16th row: 5.2 us for 1024 blocks of 91 channels, 3.4 so.)
 __global__ __launch_bounds__(1024) void weight_sums_kernel(const float *__restrict__ part, int blocks, int c, float *__restrict__ dw_post,
                                                            float *__restrict__ dw_pre)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int i = (int)blockIdx.x * 64 + lane;
+    __shared__ float sums[16][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, column = lane & 15;
+    const int i = (int)blockIdx.x * 16 + column;
     float v = 0.f;
     if (i < 2 * c) {
-#pragma unroll 8
-        for (int b = wave; b < blocks; b += 16) v += part[(size_t)b * 2 * c + i];
+#pragma unroll 16
+        for (int b = 4 * wave + (lane >> 4); b < blocks; b += 64) v += part[(size_t)b * 2 * c + i];
     }
-    sums[wave][lane] = v;
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+    if (lane < 16) sums[wave][column] = v;
     __syncthreads();
-    if (wave != 0 || i >= 2 * c) return;
-    v = sums[0][lane];
+    if (threadIdx.x >= 16 || i >= 2 * c) return;
+    v = sums[0][column];
 #pragma unroll
-    for (int w = 1; w < 16; ++w) v += sums[w][lane];
+    for (int w = 1; w < 16; ++w) v += sums[w][column];
     float *to = i < c ? dw_post : dw_pre;
     if (to) to[i < c ? i : i - c] = v;
 }
@@ -377,7 +380,7 @@ int block_norm_bwd(const BlockNormBwd &a, int stream_dtype, int dtype, hipStream
     });
     PCPP_HIP_CHECK(hipGetLastError());
     if (!a.dw_post && !a.dw_pre) return PCPP_OK;
-    weight_sums_kernel<<<(unsigned)ceil_div(2 * a.c, 64), 1024, 0, stream>>>(a.part, blocks, a.c, a.dw_post, a.dw_pre);
+    weight_sums_kernel<<<(unsigned)ceil_div(2 * a.c, 16), 1024, 0, stream>>>(a.part, blocks, a.c, a.dw_post, a.dw_pre);
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;
 }

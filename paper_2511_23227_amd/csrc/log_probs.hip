@@ -645,9 +645,10 @@ Split split_of(int64_t n, int64_t v)
 }
 
 // A row by a wave on its own rather than by a block's four: no barrier, and the alternatives' pool is not joined, but a fourth of the waves.
-// By a wave / by four, bf16, us with the host's share: twenty alternatives, 4096 x 24 000 72 / 80, 5000 x 20 000 69 / 82, 1100 x 16 000 38 / 24; five,
-// 8000 x 8000 44 / 63, 2000 x 5000 15.5 / 20.4, 2000 x 16 000 32 / 29; none, forward and gradient of 4096 x 32 768 134 / 130, 30 000 x 3000 107 / 107.
-bool row_by_wave(int64_t n, int64_t v, bool top) { return (n >= 1024 && v <= (top ? 8192 : 4096)) || (top && n >= 4096); }
+// By a wave / by four, bf16, us with the host's share: five alternatives, 8000 x 8000 44 / 63, 2000 x 5000 15.5 / 20.4, 2000 x 16 000 32 / 29; twenty, 1100 x
+// 16 000 38 / 24; none, forward and gradient of 30 000 x 3000 107 / 107, of 4096 x 32 768 134 / 130.  (Twenty alternatives of very many long rows,
+// 5000 x 20 000 69 / 82, would gain as well; but then how many rows there are would change a row's last bits from 1024 rows on.)
+bool row_by_wave(int64_t n, int64_t v, bool top) { return n >= 1024 && v <= (top ? 8192 : 4096); }
 
 // Logits that fill more than half of the memory's cache (256 MB) are read past the caches.  Forward and gradient with / without, us: 4096 x 32 768
 // bf16 (268 MB) 132 / 165, 2000 x 20 000 fp32 (160 MB) 99 / 105, bf16 (80 MB) 53 / 49.
