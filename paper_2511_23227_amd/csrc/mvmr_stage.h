@@ -176,12 +176,14 @@ struct Stage {
 
 // Rows in 8 bits (row_ops.h: q and one code for 32 channels), staged as the bf16 numbers that they are exactly: Stage's layout, half its bytes
 // from memory.  The codes of a row's chunk are one 32-bit word, looked up by the lane that knows the row and handed on like its offset.
-template <int RL, bool NARROW>
-struct Stage8 : Stage<RL, NARROW> {
+// Chunks of 32 channels: eight a lane.
+template <bool NARROW>
+struct Stage8 : Stage<4, NARROW> {
+    static constexpr int RL = 4;
     using Base = Stage<RL, NARROW>;
     static constexpr bool CODED = true;
-    static constexpr int ES = 1, NV = 8;
-    using Base::NI;
+    static constexpr int ES = 1, NV = 8, NI = Base::NI;
+    static_assert(NI == 2, "load and store");
 
     uint32_t q[NI][2];                            // rows in flight
     uint32_t word;                                // ... and the codes of triplet_of_lane's row
@@ -216,11 +218,6 @@ struct Stage8 : Stage<RL, NARROW> {
     {
         load_one<0>(rs, offs, c);
         load_one<1>(rs, offs, c);
-        if constexpr (NI > 2) { load_one<(NI > 2 ? 2 : 0)>(rs, offs, c); load_one<(NI > 2 ? 3 : 0)>(rs, offs, c); }
-        if constexpr (NI > 4) {
-            load_one<(NI > 4 ? 4 : 0)>(rs, offs, c); load_one<(NI > 4 ? 5 : 0)>(rs, offs, c);
-            load_one<(NI > 4 ? 6 : 0)>(rs, offs, c); load_one<(NI > 4 ? 7 : 0)>(rs, offs, c);
-        }
     }
     template <int I> __device__ inline void expand()
     {
@@ -235,12 +232,77 @@ struct Stage8 : Stage<RL, NARROW> {
     {
         expand<0>();
         expand<1>();
-        if constexpr (NI > 2) { expand<(NI > 2 ? 2 : 0)>(); expand<(NI > 2 ? 3 : 0)>(); }
-        if constexpr (NI > 4) {
-            expand<(NI > 4 ? 4 : 0)>(); expand<(NI > 4 ? 5 : 0)>();
-            expand<(NI > 4 ? 6 : 0)>(); expand<(NI > 4 ? 7 : 0)>();
-        }
         Base::store();
+    }
+};
+
+// Chunks of 64 and 128 channels: sixteen a lane, half the requests (128 -> 128 bf16, 2.4 M triplets: 145 us with eight a lane, 142 so; 64 -> 64, 2.8 M: 65, 62.5).
+// Rows of at least sixteen channels.
+template <int RL>
+struct Wide8 : Stage<RL, false> {
+    using Base = Stage<RL, false>;
+    using Lanes = Stage<RL / 2, false>;               // how rows are dealt to the lanes
+    static constexpr bool CODED = true;
+    static constexpr int ES = 1, NV = 16, LR = RL / 2, NI = LR / 2, RPI = 64 / LR;
+    static_assert(LR == 4 || LR == 8, "row width");
+
+    uint32_t q[NI][4];                            // rows in flight
+    uint32_t word;                                // ... and the codes of triplet_of_lane's row
+    uint32_t shift;                               // this lane's code in a word
+
+    __device__ static inline uint32_t triplet_of_lane(int m, int g) { return Lanes::triplet_of_lane(m, g); }
+    __device__ inline void init(uint32_t lds, int lane)
+    {
+        Base::init(lds, lane);
+        const uint32_t r = (uint32_t)lane / LR, byte = (uint32_t)lane % LR * 32u;
+        this->w_at[0] = lds + r * Base::ROWB + (byte ^ (32u * Base::unit(r)));
+        this->w_at[1] = lds + r * Base::ROWB + (byte ^ (32u * (Base::unit(r) ^ Base::unit(8u))));
+    }
+    __device__ inline void set_chunk(int chunk, int c, int lane)
+    {
+        const int pos = chunk * LR + lane % LR;
+        this->col = pos * NV < c ? (uint32_t)lane_channel(pos, NV, c) : 0u;
+        shift = 8u * ((uint32_t)(pos * NV / 32) & 3u);
+    }
+    __device__ static inline int channel(int chunk, int at, int c)
+    {
+        const int place = chunk * Base::CHK + at, pos = place / NV, ch = lane_channel(pos, NV, c) + place % NV;
+        return pos * NV < c && ch >= pos * NV ? ch : -1;
+    }
+    template <int I> __device__ inline void load_one(const __amdgpu_buffer_rsrc_t &rs, uint32_t offs)
+    {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(Lanes::template of_row<I>(offs) + this->col), 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[I][i] = v[i];
+    }
+    __device__ inline void load_codes(const __amdgpu_buffer_rsrc_t &rs, uint32_t off) { word = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, (int)off, 0, 0); }
+    __device__ inline void load(const __amdgpu_buffer_rsrc_t &rs, uint32_t offs, int)
+    {
+        load_one<0>(rs, offs);
+        load_one<1>(rs, offs);
+        if constexpr (NI > 2) { load_one<(NI > 2 ? 2 : 0)>(rs, offs); load_one<(NI > 2 ? 3 : 0)>(rs, offs); }
+    }
+    template <int I> __device__ inline void expand()
+    {
+        const float step = __uint_as_float((Lanes::template of_row<I>(word) >> shift & 255u) << 23);
+        uint32_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t p = q[I][i >> 1] >> (16 * (i & 1));
+            b[i] = cvt_pk_bf16((float)(int8_t)p * step, (float)(int8_t)(p >> 8) * step);
+        }
+        // row RPI I + r: bit 3 of the row comes from I where an instruction reads eight rows
+        const uint32_t at = (RPI == 8 ? this->w_at[I & 1] : this->w_at[0]) + (uint32_t)(RPI * I) * Base::ROWB;
+        *reinterpret_cast<__attribute__((address_space(3))) v4u *>(at) = v4u{b[0], b[1], b[2], b[3]};
+        *reinterpret_cast<__attribute__((address_space(3))) v4u *>(at + 16u) = v4u{b[4], b[5], b[6], b[7]};
+    }
+    __device__ inline void store()
+    {
+        expand<0>();
+        expand<1>();
+        if constexpr (NI > 2) { expand<(NI > 2 ? 2 : 0)>(); expand<(NI > 2 ? 3 : 0)>(); }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
     }
 };
 

@@ -666,11 +666,11 @@ template <typename SO>
 int launch_any_in(const WeightArgs &w, float *dw, int ci, hipStream_t stream)
 {
     if (w.codes) {
-        if (w.c_in < 8) return launch_any<SO, Stage8<4, true>>(w, dw, stream);
-        if (ci == 32) return launch_any<SO, Stage8<4, false>>(w, dw, stream);
+        if (w.c_in < 8) return launch_any<SO, Stage8<true>>(w, dw, stream);
+        if (ci == 32) return launch_any<SO, Stage8<false>>(w, dw, stream);
         if constexpr (SO::PL == 1 && SO::CHK < 128)
-            if (ci == 128) return launch_any<SO, Stage8<16, false>>(w, dw, stream);
-        return launch_any<SO, Stage8<8, false>>(w, dw, stream);
+            if (ci == 128) return launch_any<SO, Wide8<16>>(w, dw, stream);
+        return launch_any<SO, Wide8<8>>(w, dw, stream);
     }
     if constexpr (SO::PL > 1) {
         if (w.c_in < 2) return launch_any<SO, Direct<2, true>>(w, dw, stream);
