@@ -1,7 +1,9 @@
-"""ctypes binding of libpcpp.so: argument marshalling only (torch tensors -> device pointers)."""
+"""Binding of libpcpp.so: argument marshalling only (torch tensors -> device pointers), by ctypes, and by compiled code for the
+operators whose calls are short."""
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import threading
 from dataclasses import dataclass
@@ -369,20 +371,46 @@ def pcpp_mvmr_bwd_weight(x: torch.Tensor, dy: torch.Tensor, T: Triplets, dw: tor
 
 
 # ---- the operators around the convolution ------------------------------------------------------------------------
-# (Their smallest calls take the GPU 3 us, so what happens here counts: addresses go to the library as plain integers.)
+# Their smallest calls take the GPU 3 us, so tensors are checked, outputs made and the library called by compiled code
+# (csrc/torch_calls.cpp); what does not fit raises AssertionError or TypeError there, and a call's status PcppError here.
+
+_calls = None
+
+
+def _compiled():
+    """The compiled side of the calls, bound to the library (built first only if it is not there).  Raises if unavailable."""
+    global _calls
+    if _calls is None:
+        handle = library()._handle
+        path = os.path.join(HERE, "_torch_calls.so")
+        if not os.path.exists(path):
+            from .build import build_calls
+            build_calls()
+        spec = importlib.util.spec_from_file_location("_torch_calls", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(handle)
+        _calls = module
+    return _calls
+
+
+def _outputs(result):
+    """A call's outputs, or its error."""
+    if type(result) is int:
+        _check(result)
+    return result
+
 
 _CODES = {torch.float32: PCPP_F32, torch.bfloat16: PCPP_BF16}
 
 
-def _code(dtype: torch.dtype) -> int:
+def _code_or(dtype: torch.dtype | None) -> int:
+    if dtype is None:
+        return -1
     code = _CODES.get(dtype)
     if code is None:
         raise TypeError(f"unsupported dtype {dtype}")
     return code
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
 
 
 @dataclass
@@ -392,88 +420,22 @@ class Packed:
     codes: torch.Tensor      # uint8 [n, pcpp_act_code_bytes(c)]
 
 
-def _code_bytes(c: int) -> int:
-    return (c + 127) // 128 * 4
-
-
-def _empty_packed(n: int, c: int, device) -> Packed:
-    return Packed(torch.empty((n, c), dtype=torch.int8, device=device), torch.empty((n, _code_bytes(c)), dtype=torch.uint8, device=device))
-
-
-def _check_packed(p: Packed):
-    q, codes = p.q, p.codes
-    assert q.is_cuda and codes.is_cuda and q.is_contiguous() and codes.is_contiguous()
-    assert q.dtype == torch.int8 and codes.dtype == torch.uint8
-    n, c = q.shape
-    assert codes.shape == (n, _code_bytes(c))
-
-
-def _pitch(t: torch.Tensor) -> int:
-    """Row pitch of a [n, c] tensor whose rows are contiguous, in elements."""
-    (n, c), (pitch, step) = t.shape, t.stride()
-    assert c <= 1 or step == 1, "the channels of a row must lie side by side"
-    if n <= 1:
-        return c
-    assert pitch >= c, "rows must not overlap"
-    return pitch
-
-
 def pcpp_act_pack(x: torch.Tensor, out: Packed | None = None) -> Packed:
     """Activations in 8 bits for a later backward pass: blocks of 32 channels of a row share a power of two."""
-    L = library()
-    assert x.is_cuda and x.is_contiguous() and x.dim() == 2
-    n, c = x.shape
-    if out is None:
-        out = _empty_packed(n, c, x.device)
-    else:
-        _check_packed(out)
-        assert out.q.shape == x.shape
-    rc = L.pcpp_act_pack(x.data_ptr(), _code(x.dtype), n, c, out.q.data_ptr(), out.codes.data_ptr(), _stream())
-    if rc:
-        _check(rc)
-    return out
+    q, codes = (None, None) if out is None else (out.q, out.codes)
+    return Packed(*_outputs(_compiled().act_pack(x, q, codes, _stream())))
 
 
 def pcpp_act_unpack(p: Packed, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values of rows in 8 bits; bfloat16 holds them exactly."""
-    L = library()
-    _check_packed(p)
-    q = p.q
-    if out is None:
-        out = torch.empty_like(q, dtype=dtype)
-    else:
-        assert out.is_cuda and out.is_contiguous() and out.shape == q.shape
-    n, c = q.shape
-    rc = L.pcpp_act_unpack(q.data_ptr(), p.codes.data_ptr(), n, c, out.data_ptr(), _code(out.dtype), _stream())
-    if rc:
-        _check(rc)
-    return out
+    return _outputs(_compiled().act_unpack(p.q, p.codes, _code_or(dtype), out, _stream()))[0]
 
 
 def pcpp_mvmr_bwd_weight_packed(x: Packed, dy: torch.Tensor, T: Triplets, dw: torch.Tensor | None = None,
                                 workspace: torch.Tensor | None = None) -> torch.Tensor:
     """pcpp_mvmr_bwd_weight from an input that was kept in 8 bits: dW[k] = sum dy[o] (outer) x[i].  T.plan may be None."""
-    L = library()
-    _check_packed(x)
-    assert dy.is_cuda and dy.is_contiguous()
-    (n_in, c_in), (n_out, c_out), K = x.q.shape, dy.shape, T.K
-    assert n_in == T.n_in and n_out == T.n_out
-    dev = dy.device
-    if dw is None:
-        dw = torch.empty((K, c_out, c_in), dtype=torch.float32, device=dev)
-    else:
-        assert dw.is_cuda and dw.is_contiguous() and dw.dtype == torch.float32 and dw.shape == (K, c_out, c_in)
-    code, n = _code(dy.dtype), T.n_triplets
-    need = L.pcpp_mvmr_packed_workspace_bytes(n_in, n_out, n, c_in, c_out, K, code)
-    if workspace is None or workspace.numel() < need:
-        workspace = _bytes(need, dev)
-    rc = L.pcpp_mvmr_bwd_weight_packed(x.q.data_ptr(), x.codes.data_ptr(), dy.data_ptr(), dw.data_ptr(), code, n_in, n_out, c_in,
-                                       c_out, K, T.tri_o.data_ptr(), T.tri_i.data_ptr(), T.tri_k.data_ptr(),
-                                       T.seg_offsets.data_ptr(), n, *_plan_args(T), workspace.data_ptr(), workspace.numel(),
-                                       _stream())
-    if rc:
-        _check(rc)
-    return dw
+    return _outputs(_compiled().weight_packed(x.q, x.codes, dy, T.tri_o, T.tri_i, T.tri_k, T.seg_offsets, T.plan, T.plan_flags,
+                                              T.n_triplets, T.n_in, T.n_out, T.K, dw, workspace, _stream()))[0]
 
 
 @dataclass
@@ -495,21 +457,6 @@ class BlockNormGrads:
     dw_pre: torch.Tensor | None
 
 
-def _weights(w, c):
-    if w is None:
-        return None
-    assert w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and w.shape == (c,)
-    return w.data_ptr()
-
-
-def _gate_args(gate, n, c, dtype):
-    if gate is None:
-        return None, 0, 0
-    rows, cols = gate.shape
-    assert gate.is_cuda and gate.dtype == dtype and rows == n and (cols == c or cols == 1)
-    return gate.data_ptr(), _pitch(gate), cols
-
-
 def pcpp_block_norm_fwd(x: torch.Tensor, f: torch.Tensor | None = None, gate: torch.Tensor | None = None,
                         w_post: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, *,
                         post_norm: int = NORM_RMS, pre_norm: int = NORM_RMS, residual_scale: float = 1.0,
@@ -521,32 +468,9 @@ def pcpp_block_norm_fwd(x: torch.Tensor, f: torch.Tensor | None = None, gate: to
     logits; f and gate may be column slices.  post_norm / pre_norm: NORM_NONE, NORM_RMS or NORM_LAYER (pre_norm
     NORM_NONE: no h).  dtype: type of h where there is no f.  pack_f, pack_h: copies in 8 bits for the backward pass.
     """
-    L = library()
-    assert x.is_cuda and x.is_contiguous()
-    n, c = x.shape
-    if f is not None:
-        assert f.is_cuda and f.shape == (n, c)
-        dtype = f.dtype
-        r, f_at, ld_f = torch.empty_like(x), f.data_ptr(), _pitch(f)
-        r_at = r.data_ptr()
-    else:
-        if dtype is None:
-            dtype = x.dtype
-        r, r_at, f_at, ld_f = x, None, None, c
-    h = None if pre_norm == NORM_NONE else torch.empty_like(x, dtype=dtype)
-    fq = fe = hq = he = f_packed = h_packed = None
-    if pack_f:
-        f_packed = _empty_packed(n, c, x.device)
-        fq, fe = f_packed.q.data_ptr(), f_packed.codes.data_ptr()
-    if pack_h:
-        h_packed = _empty_packed(n, c, x.device)
-        hq, he = h_packed.q.data_ptr(), h_packed.codes.data_ptr()
-    rc = L.pcpp_block_norm_fwd(x.data_ptr(), f_at, ld_f, *_gate_args(gate, n, c, dtype), _weights(w_post, c), _weights(w_pre, c),
-                               post_norm, pre_norm, residual_scale, eps, n, c, _code(x.dtype), _code(dtype), r_at, _at(h), fq, fe,
-                               hq, he, _stream())
-    if rc:
-        _check(rc)
-    return BlockNorm(r, h, f_packed, h_packed)
+    r, h, fq, fe, hq, he = _outputs(_compiled().block_norm_fwd(x, f, gate, w_post, w_pre, post_norm, pre_norm, residual_scale, eps,
+                                                               _code_or(dtype), pack_f, pack_h, _stream()))
+    return BlockNorm(x if f is None else r, h, Packed(fq, fe) if pack_f else None, Packed(hq, he) if pack_h else None)
 
 
 def pcpp_block_norm_bwd(dr: torch.Tensor | None, dh: torch.Tensor | None, r: torch.Tensor | None,
@@ -558,50 +482,14 @@ def pcpp_block_norm_bwd(dr: torch.Tensor | None, dh: torch.Tensor | None, r: tor
     """Gradients of pcpp_block_norm_fwd.  dr (None: zero) and dh flow to its r and h; r is what it wrote, f what it was
     given or its copy in 8 bits.  `block`: there was a block, though nothing of f is needed (neither post norm nor gate;
     default: f is not None).  dtype: type of the block's tensors where neither dh nor f says it."""
-    L = library()
-    packed = isinstance(f, Packed)
-    some = dh if dr is None else dr
-    assert some is not None and some.is_cuda, "neither dr nor dh"
-    n, c = some.shape
-    for t in (dr, dh, r):
-        assert t is None or (t.is_cuda and t.is_contiguous() and t.shape == (n, c))
-    if dh is not None:
-        dtype = dh.dtype
-    elif f is not None and not packed:
-        dtype = f.dtype
-    elif gate is not None:
-        dtype = gate.dtype
-    stream_dtype = dr.dtype if r is None else r.dtype
-    assert dr is None or dr.dtype == stream_dtype
-    if dtype is None:
-        dtype = stream_dtype
-    f_at = fq = fe = None
-    ld_f = c
-    if packed:
-        _check_packed(f)
-        assert f.q.shape == (n, c)
-        fq, fe = f.q.data_ptr(), f.codes.data_ptr()
-    elif f is not None:
-        assert f.is_cuda and f.shape == (n, c) and f.dtype == dtype
-        f_at, ld_f = f.data_ptr(), _pitch(f)
+    fq = fe = None
     if block is None:
         block = f is not None
-    dev = some.device
-    dx = torch.empty_like(some, dtype=stream_dtype)
-    df = torch.empty_like(some, dtype=dtype) if block else None
-    dgate = None if gate is None else torch.empty((n, gate.shape[1]), dtype=dtype, device=dev)
-    dw_post = torch.empty(c, dtype=torch.float32, device=dev) if block and post_norm != NORM_NONE else None
-    dw_pre = torch.empty(c, dtype=torch.float32, device=dev) if pre_norm != NORM_NONE else None
-    need = L.pcpp_block_norm_workspace_bytes(n, c)
-    if workspace is None or workspace.numel() < need:
-        workspace = _bytes(need, dev)
-    rc = L.pcpp_block_norm_bwd(_at(dr), _at(dh), _at(r), f_at, ld_f, fq, fe, *_gate_args(gate, n, c, dtype), _weights(w_post, c),
-                               _weights(w_pre, c), post_norm, pre_norm, residual_scale, eps, n, c, _code(stream_dtype), _code(dtype),
-                               dx.data_ptr(), _at(df), _at(dgate), _at(dw_post), _at(dw_pre), workspace.data_ptr(),
-                               workspace.numel(), _stream())
-    if rc:
-        _check(rc)
-    return BlockNormGrads(dx, df, dgate, dw_post, dw_pre)
+    if isinstance(f, Packed):
+        f, fq, fe = None, f.q, f.codes
+    return BlockNormGrads(*_outputs(_compiled().block_norm_bwd(dr, dh, r, f, fq, fe, gate, w_post, w_pre, post_norm, pre_norm,
+                                                               residual_scale, eps, _code_or(dtype), block, workspace,
+                                                               _stream())))
 
 
 class LogProbs:
@@ -627,37 +515,11 @@ class LogProbs:
         return self.entropy.new_empty((self.entropy.shape[0], 0), dtype=torch.int32) if self._top_index is None else self._top_index
 
 
-def _labels(labels, n):
-    if labels is None:
-        return None
-    assert labels.is_cuda and labels.is_contiguous() and labels.dtype == torch.int32 and labels.shape == (n,)
-    return labels.data_ptr()
-
-
 def pcpp_log_probs_fwd(logits: torch.Tensor, labels: torch.Tensor | None = None, n_top: int = 0,
                        workspace: torch.Tensor | None = None) -> LogProbs:
     """Log probability of every row's label (a label outside 0 .. v - 1: none, 0), the entropy, and the n_top most probable
     classes.  logits [n, v], rows may be a slice of wider ones; labels int32 [n]."""
-    L = library()
-    assert logits.is_cuda
-    n, v = logits.shape
-    dev = logits.device
-    entropy = torch.empty(n, dtype=torch.float32, device=dev)
-    log_prob = None if labels is None else torch.empty_like(entropy)
-    max_log_sum = torch.empty((n, 2), dtype=torch.float32, device=dev)
-    top_log_prob = top_index = None
-    if n_top:
-        top_log_prob = torch.empty((n, n_top), dtype=torch.float32, device=dev)
-        top_index = torch.empty((n, n_top), dtype=torch.int32, device=dev)
-    need = L.pcpp_log_probs_workspace_bytes(n, v, n_top)
-    if need and (workspace is None or workspace.numel() < need):
-        workspace = _bytes(need, dev)
-    rc = L.pcpp_log_probs_fwd(logits.data_ptr(), _code(logits.dtype), n, v, _pitch(logits), _labels(labels, n), n_top, _at(log_prob),
-                              entropy.data_ptr(), max_log_sum.data_ptr(), _at(top_log_prob), _at(top_index),
-                              workspace.data_ptr() if need else None, workspace.numel() if need else 0, _stream())
-    if rc:
-        _check(rc)
-    return LogProbs(log_prob, entropy, max_log_sum, top_log_prob, top_index)
+    return LogProbs(*_outputs(_compiled().log_probs_fwd(logits, labels, n_top, workspace, _stream())))
 
 
 def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forward: LogProbs,
@@ -665,21 +527,5 @@ def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forwar
                        out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient of the logits from what flows to log_prob and to entropy (fp32 [n]).  out: where it goes, by default a new
     tensor; it may be the logits."""
-    L = library()
-    assert logits.is_cuda
-    n, v = logits.shape
-    stats, entropy = forward.max_log_sum, forward.entropy
-    assert stats.is_cuda and stats.is_contiguous() and stats.dtype == torch.float32 and stats.shape == (n, 2)
-    for t in (d_log_prob, d_entropy, entropy):
-        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and t.shape == (n,))
-    if out is None:
-        out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
-        pitch = v
-    else:
-        assert out.is_cuda and out.dtype == logits.dtype and out.shape == (n, v)
-        pitch = _pitch(out)
-    rc = L.pcpp_log_probs_bwd(logits.data_ptr(), _code(logits.dtype), n, v, _pitch(logits), _labels(labels, n), stats.data_ptr(),
-                              entropy.data_ptr(), _at(d_log_prob), _at(d_entropy), out.data_ptr(), pitch, _stream())
-    if rc:
-        _check(rc)
-    return out
+    return _outputs(_compiled().log_probs_bwd(logits, labels, forward.max_log_sum, forward.entropy, d_log_prob, d_entropy, out,
+                                              _stream()))[0]

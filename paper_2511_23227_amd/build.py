@@ -11,6 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpcpp.so")
+CALLS_LIB = os.path.join(HERE, "_torch_calls.so")      # host code: tensors' checks and outputs of the short calls
 PROBE_LIB = os.path.join(HERE, "libpcpp_probe.so")     # the benchmark's peak-rate probe, outside the library's interface
 
 # file -> extra flags.  The search kernels must not contract a*b+c into an FMA: the inclusion test
@@ -51,8 +52,27 @@ def _compile(name: str, extra) -> str:
     return obj
 
 
+def build_calls() -> str:
+    """The compiled side of the Python calls (host code against this torch's and Python's headers)."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(os.path.abspath(torch.__file__))
+    tmp = CALLS_LIB + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "torch_calls.cpp"), "-o", tmp,
+           "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-ldl"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for torch_calls.cpp:\n{r.stderr}")
+    os.replace(tmp, CALLS_LIB)
+    return CALLS_LIB
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
+    build_calls()
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         objs = list(ex.map(lambda kv: _compile(*kv), SOURCES.items()))
     tmp = LIB + ".tmp"
