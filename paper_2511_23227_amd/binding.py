@@ -394,6 +394,12 @@ def _compiled():
     return _calls
 
 
+def _where():
+    """The current device and its stream."""
+    device = torch._C._cuda_getDevice()
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
 def _outputs(result):
     """A call's outputs, or its error."""
     if type(result) is int:
@@ -423,19 +429,19 @@ class Packed:
 def pcpp_act_pack(x: torch.Tensor, out: Packed | None = None) -> Packed:
     """Activations in 8 bits for a later backward pass: blocks of 32 channels of a row share a power of two."""
     q, codes = (None, None) if out is None else (out.q, out.codes)
-    return Packed(*_outputs(_compiled().act_pack(x, q, codes, _stream())))
+    return Packed(*_outputs(_compiled().act_pack(x, q, codes, *_where())))
 
 
 def pcpp_act_unpack(p: Packed, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values of rows in 8 bits; bfloat16 holds them exactly."""
-    return _outputs(_compiled().act_unpack(p.q, p.codes, _code_or(dtype), out, _stream()))[0]
+    return _outputs(_compiled().act_unpack(p.q, p.codes, _code_or(dtype), out, *_where()))[0]
 
 
 def pcpp_mvmr_bwd_weight_packed(x: Packed, dy: torch.Tensor, T: Triplets, dw: torch.Tensor | None = None,
                                 workspace: torch.Tensor | None = None) -> torch.Tensor:
     """pcpp_mvmr_bwd_weight from an input that was kept in 8 bits: dW[k] = sum dy[o] (outer) x[i].  T.plan may be None."""
     return _outputs(_compiled().weight_packed(x.q, x.codes, dy, T.tri_o, T.tri_i, T.tri_k, T.seg_offsets, T.plan, T.plan_flags,
-                                              T.n_triplets, T.n_in, T.n_out, T.K, dw, workspace, _stream()))[0]
+                                              T.n_triplets, T.n_in, T.n_out, T.K, dw, workspace, *_where()))[0]
 
 
 @dataclass
@@ -469,7 +475,7 @@ def pcpp_block_norm_fwd(x: torch.Tensor, f: torch.Tensor | None = None, gate: to
     NORM_NONE: no h).  dtype: type of h where there is no f.  pack_f, pack_h: copies in 8 bits for the backward pass.
     """
     r, h, fq, fe, hq, he = _outputs(_compiled().block_norm_fwd(x, f, gate, w_post, w_pre, post_norm, pre_norm, residual_scale, eps,
-                                                               _code_or(dtype), pack_f, pack_h, _stream()))
+                                                               _code_or(dtype), pack_f, pack_h, *_where()))
     return BlockNorm(x if f is None else r, h, Packed(fq, fe) if pack_f else None, Packed(hq, he) if pack_h else None)
 
 
@@ -489,7 +495,7 @@ def pcpp_block_norm_bwd(dr: torch.Tensor | None, dh: torch.Tensor | None, r: tor
         f, fq, fe = None, f.q, f.codes
     return BlockNormGrads(*_outputs(_compiled().block_norm_bwd(dr, dh, r, f, fq, fe, gate, w_post, w_pre, post_norm, pre_norm,
                                                                residual_scale, eps, _code_or(dtype), block, workspace,
-                                                               _stream())))
+                                                               *_where())))
 
 
 class LogProbs:
@@ -519,7 +525,7 @@ def pcpp_log_probs_fwd(logits: torch.Tensor, labels: torch.Tensor | None = None,
                        workspace: torch.Tensor | None = None) -> LogProbs:
     """Log probability of every row's label (a label outside 0 .. v - 1: none, 0), the entropy, and the n_top most probable
     classes.  logits [n, v], rows may be a slice of wider ones; labels int32 [n]."""
-    return LogProbs(*_outputs(_compiled().log_probs_fwd(logits, labels, n_top, workspace, _stream())))
+    return LogProbs(*_outputs(_compiled().log_probs_fwd(logits, labels, n_top, workspace, *_where())))
 
 
 def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forward: LogProbs,
@@ -528,4 +534,4 @@ def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forwar
     """Gradient of the logits from what flows to log_prob and to entropy (fp32 [n]).  out: where it goes, by default a new
     tensor; it may be the logits."""
     return _outputs(_compiled().log_probs_bwd(logits, labels, forward.max_log_sum, forward.entropy, d_log_prob, d_entropy, out,
-                                              _stream()))[0]
+                                              *_where()))[0]

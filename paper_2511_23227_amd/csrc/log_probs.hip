@@ -192,7 +192,12 @@ struct TopKeys {
         if (!listed && n <= 64) {
             const key_t64 k = lane < n ? pool[lane] : 0;
             int place = 0;
-            for (int j = 0; j < n; ++j) place += pool[j] > k;
+            int j = 0;
+            for (; j + 4 <= n; j += 4) {                          // (four reads under way)
+                const key_t64 k0 = pool[j], k1 = pool[j + 1], k2 = pool[j + 2], k3 = pool[j + 3];
+                place += (k0 > k) + (k1 > k) + (k2 > k) + (k3 > k);
+            }
+            for (; j < n; ++j) place += pool[j] > k;
             if (lane < n && place < n_top) put(place, k);
         } else {
             flush(pool, lane);

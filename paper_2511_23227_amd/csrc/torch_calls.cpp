@@ -49,6 +49,7 @@ struct {
 struct Args {
     PyObject *const *a;
     Py_ssize_t n, at = 0;
+    int64_t device = -1;                                          // of the tensors so far
     PyObject *next()
     {
         if (at >= n) throw Fail{PyExc_TypeError, "too few arguments"};
@@ -61,6 +62,8 @@ struct Args {
         if (!THPVariable_Check(o)) throw Fail{PyExc_TypeError, "expected a tensor"};
         const Tensor &t = THPVariable_Unpack(o);
         need(t.is_cuda(), "tensors must be on the GPU");
+        need(device < 0 || device == t.get_device(), "tensors must be on one GPU");
+        device = t.get_device();
         return &t;
     }
     const Tensor &tensor()
@@ -87,8 +90,10 @@ struct Args {
         if (v == -1.0 && PyErr_Occurred()) throw Fail{nullptr, nullptr};
         return (float)v;
     }
+    // the last two arguments: the current device and its stream
     void *stream()
     {
+        need(integer() == device, "tensors must be on the current device");
         void *p = PyLong_AsVoidPtr(next());
         if (!p && PyErr_Occurred()) throw Fail{nullptr, nullptr};
         return p;
@@ -200,7 +205,7 @@ template <typename F> PyObject *guarded(PyObject *const *a, Py_ssize_t n, F f)
 }
 
 // ---- the calls ----------------------------------------------------------------------------------------------------------------
-// (x, q or None, codes or None, stream) -> (q, codes)
+// (x, q or None, codes or None, device, stream) -> (q, codes)
 PyObject *act_pack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {
@@ -218,7 +223,7 @@ PyObject *act_pack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
-// (q, codes, dtype code, out or None, stream) -> (x,)
+// (q, codes, dtype code, out or None, device, stream) -> (x,)
 PyObject *act_unpack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {
@@ -235,7 +240,8 @@ PyObject *act_unpack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
-// (q, codes, dy, tri_o, tri_i, tri_k, seg_offsets, plan or None, plan_flags, n_triplets, n_in, n_out, K, dw or None, workspace or None, stream) -> (dw,)
+// (q, codes, dy, tri_o, tri_i, tri_k, seg_offsets, plan or None, plan_flags, n_triplets, n_in, n_out, K, dw or None, workspace or None,
+//  device, stream) -> (dw,)
 PyObject *weight_packed(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {
@@ -281,7 +287,7 @@ struct Gate {
     }
 };
 
-// (x, f, gate, w_post, w_pre, post, pre, residual_scale, eps, dtype code (-1: x's), pack_f, pack_h, stream) -> (r, h, fq, fcodes, hq, hcodes)
+// (x, f, gate, w_post, w_pre, post, pre, residual_scale, eps, dtype code (-1: x's), pack_f, pack_h, device, stream) -> (r, h, fq, fcodes, hq, hcodes)
 PyObject *block_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {
@@ -313,7 +319,7 @@ PyObject *block_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 }
 
 // (dr, dh, r, f, fq, fcodes, gate, w_post, w_pre, post, pre, residual_scale, eps, dtype code (-1: of dh, f, gate, the stream), block, workspace,
-//  stream) -> (dx, df, dgate, dw_post, dw_pre)
+//  device, stream) -> (dx, df, dgate, dw_post, dw_pre)
 PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {
@@ -369,7 +375,7 @@ const float *floats_at(const Tensor *t, int64_t n)
     return static_cast<const float *>(t->data_ptr());
 }
 
-// (logits, labels, n_top, workspace, stream) -> (log_prob, entropy, max_log_sum, top_log_prob, top_index)
+// (logits, labels, n_top, workspace, device, stream) -> (log_prob, entropy, max_log_sum, top_log_prob, top_index)
 PyObject *log_probs_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {
@@ -397,7 +403,7 @@ PyObject *log_probs_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
-// (logits, labels, max_log_sum, entropy, d_log_prob, d_entropy, out, stream) -> (d_logits,)
+// (logits, labels, max_log_sum, entropy, d_log_prob, d_entropy, out, device, stream) -> (d_logits,)
 PyObject *log_probs_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {

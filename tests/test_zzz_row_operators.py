@@ -356,6 +356,17 @@ def test_block_norm_gradient_against_differences(pcpp, kind, gate):
         assert abs(slope - want) <= 2e-3 * scale, (name, slope, want, scale)
 
 
+def test_block_norm_without_eps(pcpp):
+    """eps = 0: rows that a wave holds past the last one have no norm, and must not reach the weights' gradients."""
+    for n, c in ((37, 32), (5, 91), (1, 7)):
+        r, f, ga, wp, wn, dr, dh = block_inputs(n, c, F32, F32, "full", 11)
+        got = pcpp.pcpp_block_norm_bwd(*cuda(dr, dh, r, f, ga, wp, wn), eps=0.0)
+        r, dh = wide(r, dh)
+        nr, _, mr = norm_reference(r, 1, 0.0, r.abs())
+        close(got.dw_pre, (dh * nr).sum(0), (dh.abs() * mr).sum(0), n + c, "dw_pre")
+        assert torch.isfinite(got.dw_post).all() and torch.isfinite(got.df).all()
+
+
 # ---- log probabilities -------------------------------------------------------------------------------------------
 
 def head_reference(x, labels, n_top):
@@ -568,3 +579,55 @@ def test_rows_past_32_bits(pcpp):
         assert torch.equal(y.log_prob[-2000:], z.log_prob) and torch.equal(y.top_index[-2000:], z.top_index)
         d = pcpp.pcpp_log_probs_bwd(logits, labels, y, ones, ones)[-2000:]
         assert torch.equal(d, pcpp.pcpp_log_probs_bwd(logits[-2000:], labels[-2000:].contiguous(), z, ones[-2000:].contiguous(), ones[-2000:].contiguous()))
+
+
+def test_packed_weight_gradient_past_32_bits(pcpp):
+    """A bf16 copy of x of more than 4 GiB: the kernel that needs the plan, and a refusal without one."""
+    if torch.cuda.get_device_properties(0).total_memory < 64 << 30:
+        pytest.skip("needs 64 GiB")
+    n_in, n_out, c_in, c_out = 2_200_000, 70, 1024, 8
+    g = torch.Generator(device="cuda").manual_seed(6)
+    xyz = torch.rand(n_in, 3, generator=g, device="cuda")
+    centres = xyz[-n_out:].contiguous()
+    T = pcpp.pcpp_build_triplets(xyz, centres, 0.01, 2)
+    p = pcpp.pcpp_act_pack(torch.randn(n_in, c_in, generator=g, device="cuda", dtype=BF16))
+    dy = torch.randn(n_out, c_out, generator=g, device="cuda").to(BF16)
+    got = pcpp.pcpp_mvmr_bwd_weight_packed(p, dy, T)
+    o, i, k = (t.long() for t in (T.tri_o, T.tri_i, T.tri_k))
+    x, d = pcpp.pcpp_act_unpack(pcpp.Packed(p.q[i].contiguous(), p.codes[i].contiguous()), F32).double().cpu(), dy[o].double().cpu()
+    for cell in range(T.K):
+        at = (k == cell).cpu()
+        close(got[cell], d[at].T @ x[at], d[at].abs().T @ x[at].abs(), int(at.sum()), ("dw", cell))
+    free = pcpp.Triplets(T.tri_o, T.tri_i, T.tri_k, T.seg_offsets, T.n_triplets, n_in, n_out, 2, None, 0)
+    with pytest.raises(pcpp.PcppError) as e:
+        pcpp.pcpp_mvmr_bwd_weight_packed(p, dy, free)
+    assert e.value.code == -1 and "plan" in str(e.value)
+
+
+def test_refusals_of_tensors(pcpp):
+    """What does not fit is refused before the library is called."""
+    x, f = torch.randn(6, 40, device="cuda"), torch.randn(6, 40, device="cuda")
+    p = pcpp.pcpp_act_pack(x)
+    i32 = torch.zeros(6, dtype=torch.int32, device="cuda")
+    y = pcpp.pcpp_log_probs_fwd(x, i32)
+    for call in (lambda: pcpp.pcpp_act_pack(x.cpu()), lambda: pcpp.pcpp_act_pack(x.t()), lambda: pcpp.pcpp_act_pack(x[0]),
+                 lambda: pcpp.pcpp_act_unpack(pcpp.Packed(p.q, p.codes[:5])), lambda: pcpp.pcpp_act_unpack(pcpp.Packed(p.codes, p.q)),
+                 lambda: pcpp.pcpp_act_unpack(p, out=torch.empty(6, 41, device="cuda")), lambda: pcpp.pcpp_block_norm_fwd(x, f[:5]),
+                 lambda: pcpp.pcpp_block_norm_fwd(x, f, f[:, :2]), lambda: pcpp.pcpp_block_norm_fwd(x, f, f.to(BF16)), lambda: pcpp.pcpp_block_norm_fwd(x, f.t()),
+                 lambda: pcpp.pcpp_block_norm_fwd(x, f, None, x[0, :39]), lambda: pcpp.pcpp_block_norm_fwd(x, f, None, x[0].to(BF16)),
+                 lambda: pcpp.pcpp_block_norm_bwd(None, None, x, f), lambda: pcpp.pcpp_block_norm_bwd(x, x, x.to(BF16), f),
+                 lambda: pcpp.pcpp_block_norm_bwd(x[:5], x, x, f), lambda: pcpp.pcpp_block_norm_bwd(x.t(), x, x, f),
+                 lambda: pcpp.pcpp_log_probs_fwd(x, i32.long()), lambda: pcpp.pcpp_log_probs_fwd(x, i32[:5]), lambda: pcpp.pcpp_log_probs_fwd(x.t()),
+                 lambda: pcpp.pcpp_log_probs_fwd(x[0]), lambda: pcpp.pcpp_log_probs_bwd(x[:5], None, y),
+                 lambda: pcpp.pcpp_log_probs_bwd(x, i32, y, x[:, 0]), lambda: pcpp.pcpp_log_probs_bwd(x, i32, y, out=x[:, :39])):
+        with pytest.raises((AssertionError, TypeError)):
+            call()
+    for call in (lambda: pcpp.pcpp_act_pack(x.half()), lambda: pcpp.pcpp_act_unpack(p, torch.float16), lambda: pcpp.pcpp_block_norm_fwd(x.half(), f.half()),
+                 lambda: pcpp.pcpp_log_probs_fwd(x.double()), lambda: pcpp.pcpp_block_norm_fwd(None, f), lambda: pcpp.pcpp_log_probs_fwd("x")):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: pcpp.pcpp_block_norm_fwd(x, f, pre_norm=7), lambda: pcpp.pcpp_block_norm_fwd(x, f, eps=-1.0),
+                 lambda: pcpp.pcpp_log_probs_fwd(x, None, 41), lambda: pcpp.pcpp_act_pack(torch.randn(2, 1025, device="cuda")),
+                 lambda: pcpp.pcpp_block_norm_bwd(x, x, x, None, f)):
+        with pytest.raises(pcpp.PcppError):
+            call()
