@@ -333,7 +333,7 @@ constexpr uint32_t SEGMENT = 8192;
 constexpr int F32_CHUNK = 768;
 
 // fp32 chunks with x in 8 bits, whose blocks multiply half as much and are bound by what they do at their ends: 100 000 points, 32 -> 32, 2.4 M
-// triplets 55.4 us with 768, 54 with 960 and 1280, 50.3 with 2560; 64 -> 64, 1.4 M 79, 76, 69.  (Relative errors 1.3e-7 and 1.4e-7.)
+// triplets 55.4 us with 768, 54 with 960 and 1280, 50.3 with 2560; 64 -> 64, 1.4 M 79, 76, 69.  (Relative errors 1.3e-7 and 1.5e-7.)
 constexpr int PACKED_F32_CHUNK = 2560;
 
 // SO, SI: how the rows of dy and x reach the matrix cores
