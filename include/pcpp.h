@@ -323,7 +323,7 @@ PCPP_API int pcpp_mvmr_bwd_weight_packed(const int8_t *xq, const uint8_t *xcodes
  *   f, or fq with fcodes (then f is NULL); both may be NULL if there was no block (df NULL) or neither a post norm
  *            nor a gate
  *   dx [n, c] stream_dtype; NULL: not wanted.  df [n, c] dtype, dgate [n, gate_cols] dtype: contiguous
- *   dw_post, dw_pre  [c] fp32; NULL: not wanted
+ *   dw_post (needs f; without a post norm the gradient of a scale for every channel of f), dw_pre  [c] fp32; NULL: not wanted
  *   workspace: pcpp_block_norm_workspace_bytes(n, c) bytes, 256-byte aligned (backward only)
  * The sums over rows are taken in a fixed order: the same result each time.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (c outside 1..1024, n >= 2^31, pitch >= 2^24, dtype combination).

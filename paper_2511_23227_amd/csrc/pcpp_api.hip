@@ -209,7 +209,7 @@ extern "C" {
 
 const char *pcpp_last_error(void) { return g_error; }
 
-int pcpp_version(void) { return 100; }
+int pcpp_version(void) { return 101; }
 
 size_t pcpp_mvmr_workspace_bytes(int op, int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int K,
                                  int in_dtype)

@@ -154,7 +154,7 @@ int pcpp_block_norm_bwd(const void *dr, const void *dh, const void *r, const voi
     if (df && !f && !fq && (post_norm != PCPP_NORM_NONE || gate_cols)) return invalid(fn, "f is NULL");
     if (!df && (f || fq || gate_cols || dw_post)) return invalid(fn, "df is NULL though there is a block");
     if ((dgate != nullptr) != (gate_cols != 0)) return invalid(fn, "dgate and gate_cols do not agree");
-    if (dw_post && post_norm == PCPP_NORM_NONE) return invalid(fn, "dw_post without a post norm");
+    if (dw_post && !f && !fq) return invalid(fn, "dw_post without f");
     if (dw_pre && pre_norm == PCPP_NORM_NONE) return invalid(fn, "dw_pre without a pre norm");
     if (!aligned(dr, 16) || !aligned(dh, 16) || !aligned(r, 16) || !aligned(fq, 16) || !aligned(fcodes, 4) || !aligned(dx, 16) || !aligned(df, 16) ||
         !aligned(dgate, 16))

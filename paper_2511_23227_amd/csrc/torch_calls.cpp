@@ -351,7 +351,7 @@ PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         Tensor dx = empty({n, c}, stream_type, *some), df, dgate, dw_post, dw_pre;
         if (block) df = empty({n, c}, type, *some);
         if (gate) dgate = empty({n, g.cols}, type, *some);
-        if (block && post != PCPP_NORM_NONE) dw_post = empty({c}, at::kFloat, *some);
+        if (block && (f || f8.q) && (post != PCPP_NORM_NONE || w_post)) dw_post = empty({c}, at::kFloat, *some);
         if (pre != PCPP_NORM_NONE) dw_pre = empty({c}, at::kFloat, *some);
         const Tensor ws = workspace_of(lib.block_norm_workspace_bytes(n, c), workspace, *some);
         auto to = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };

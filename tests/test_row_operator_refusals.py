@@ -108,7 +108,7 @@ def test_block_norm_backward(lib, p):
     assert call(dr=None, dh=None, r=None, pre=0, dwn=None) == INVALID               # nothing flows
     assert call(fq=a, fe=a) == INVALID and call(f=None, fq=a) == INVALID and call(f=None) == INVALID
     assert call(df=None) == INVALID and call(dgate=a) == INVALID and call(gate=a, cols=64) == INVALID
-    assert call(post=0) == INVALID and call(pre=0, dh=None, r=None) == INVALID      # a weight's gradient without its norm
+    assert call(f=None, post=0) == INVALID and call(pre=0, dh=None, r=None) == INVALID      # a weight's gradient without f, or without its norm
     assert call(dx=vp(p + 8)) == INVALID and call(dwp=vp(p + 2)) == INVALID
     assert call(ws=(None, need)) == WORKSPACE and call(ws=(a, need - 1)) == WORKSPACE and call(ws=(vp(p + 64), need)) == WORKSPACE
 

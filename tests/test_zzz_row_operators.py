@@ -262,12 +262,9 @@ def test_block_norm_backward(pcpp, case, packed):
     off = 1 + ga.abs() if ga is not None else 1.0
     du, dumag = d * sigma, dmag * sigma * off
     nf, rstd, mf = norm_reference(f, post, eps, f.abs())
-    df, mag = norm_bwd_reference(wp * du if post else wp * du, wp.abs() * dumag, nf, mf, rstd, post)
+    df, mag = norm_bwd_reference(wp * du, wp.abs() * dumag, nf, mf, rstd, post)
     close(got.df, df, mag, c, "df")
-    if post:
-        close(got.dw_post, (du * nf).sum(0), (dumag * mf).sum(0), n + c, "dw_post")
-    else:
-        assert got.dw_post is None
+    close(got.dw_post, (du * nf).sum(0), (dumag * mf).sum(0), n + c, "dw_post")      # (without a norm: of a scale for every channel)
     if ga is None:
         assert got.dgate is None
     else:
@@ -328,6 +325,15 @@ def test_block_norm_keeps_non_finite_rows_apart(pcpp):
     rows[7] = rows[20] = False
     assert torch.isnan(y.h[~rows]).all() and torch.equal(y.h[rows], ref.h[rows]) and torch.equal(y.r[rows], ref.r[rows])
     assert torch.equal(b.df[rows], back.df[rows]) and torch.equal(b.dx, back.dx)
+    # a gate's NaN, and gates so large that they are 0 and 1
+    ga2 = ga.clone()
+    ga2[3, 5], ga2[8, 1], ga2[9, 1], ga2[10, 1], ga2[11, 1] = math.nan, math.inf, -math.inf, 1e30, -1e30
+    y, b = pcpp.pcpp_block_norm_fwd(x, f, ga2, wp, wn), pcpp.pcpp_block_norm_bwd(dr, dh, x, f, ga2, wp, wn)
+    assert torch.isnan(y.r[3, 5]) and torch.isnan(y.h[3]).all() and torch.isnan(b.df[3]).all() and torch.isnan(b.dgate[3, 5])
+    assert torch.equal(y.r[9, 1], x[9, 1]) and torch.equal(y.r[11, 1], x[11, 1])
+    assert not b.dgate[8:12, 1].any() and torch.isfinite(b.df[4:20]).all()
+    one = pcpp.pcpp_block_norm_bwd(dr, dh, x, f, ga[:, :1].clone().fill_(math.nan), wp, wn)
+    assert torch.isnan(one.df).all() and torch.isnan(one.dgate).all() and torch.equal(one.dx, back.dx)
 
 
 @pytest.mark.parametrize("kind,gate", [(1, "full"), (2, "row"), (1, "none")])
