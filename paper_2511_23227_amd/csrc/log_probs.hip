@@ -629,7 +629,7 @@ __global__ __launch_bounds__(THREADS) void long_bwd_kernel(const LogProbsBwd a, 
                 to_floats(raw, v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = grad_of(g, v[e], at + e == g.label);
-                store_eight(d + at, v);
+                store_eight<ONCE>(d + at, v);
             } else {
                 for (int64_t j = at; j < to; ++j) d[j] = one_of<T>(grad_of(g, one_float<T>(x[j]), j == g.label));
             }
@@ -656,9 +656,9 @@ Split split_of(int64_t n, int64_t v)
 // 5000 x 20 000 69 / 82, would gain as well; but then how many rows there are would change a row's last bits from 1024 rows on.)
 bool row_by_wave(int64_t n, int64_t v, bool top) { return n >= 1024 && v <= (top ? 8192 : 4096); }
 
-// Logits that fill more than half of the memory's cache (256 MB) are read past the caches.  Forward and gradient with / without, us: 4096 x 32 768
-// bf16 (268 MB) 132 / 165, 2000 x 20 000 fp32 (160 MB) 99 / 105, bf16 (80 MB) 53 / 49.
-template <typename T> bool read_once(int64_t n, int64_t v) { return n * v * (int64_t)sizeof(T) > (int64_t)128 << 20; }
+// Logits of more than 64 MB, a quarter of the memory's cache, are read past the caches, and their gradient is written past them.  Forward and gradient so /
+// by way of the caches, us: 268 MB (4096 x 32 768 bf16) 143 / 164 (reads alone 152), 120 MB 73 / 76, 80 MB 52.7 / 54.5, 40 MB 27.9 / 24.6.
+template <typename T> bool read_once(int64_t n, int64_t v) { return n * v * (int64_t)sizeof(T) > (int64_t)64 << 20; }
 
 unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < MAX_BLOCKS ? blocks : MAX_BLOCKS); }
 

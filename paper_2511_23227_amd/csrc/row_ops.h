@@ -64,12 +64,16 @@ template <typename T> __device__ inline void from_floats(const float (&v)[8], Ei
         r.a[0] = v4u{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
     }
 }
-template <typename T> __device__ inline void store_eight(T *p, const float (&v)[8])
+template <bool ONCE, typename T> __device__ inline void store_eight(T *p, const float (&v)[8])
 {
     Eight<T> r;
     from_floats(v, r);
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<v4u_anywhere *>(p)[i] = r.a[i];
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) {
+        v4u_anywhere *at = reinterpret_cast<v4u_anywhere *>(p) + i;
+        if constexpr (ONCE) __builtin_nontemporal_store(r.a[i], at);
+        else *at = r.a[i];
+    }
 }
 
 // ---- rows in registers --------------------------------------------------------------------------------------------------------
