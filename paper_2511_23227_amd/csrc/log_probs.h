@@ -5,8 +5,6 @@
 
 namespace pcpp {
 
-constexpr int MAX_TOP = PCPP_MAX_ALTERNATIVES;
-
 struct LogProbsFwd {
     const void *logits;
     const int32_t *labels;

@@ -78,7 +78,6 @@ template <bool ONCE, typename T> __device__ inline void store_eight(T *p, const 
 
 // ---- rows in registers --------------------------------------------------------------------------------------------------------
 constexpr int RAGGED = 0, WHOLE = 1, NARROW = 2;                  // c >= 8, a multiple of eight, < 8
-constexpr int row_mode(int c) { return c < 8 ? NARROW : (c % 8 == 0 ? WHOLE : RAGGED); }
 // Lanes for a row of c <= 512 channels; rows of up to 1024 lie in 64 lanes, sixteen channels each.
 constexpr int row_lanes(int c) { return c <= 32 ? 4 : (c <= 64 ? 8 : (c <= 128 ? 16 : (c <= 256 ? 32 : 64))); }
 

@@ -2,7 +2,7 @@
 // binding.py's functions of the same names wrap the results.
 //
 // Their smallest calls take the GPU 3 us, so what the host does is what they cost: block_norm_fwd of three rows took 10.5 us through ctypes, of which
-// the launch is 3.3, and takes 6.5 so; block_norm_bwd 21.8 and 12.8, pack and unpack 14.5 and 9.7, log_probs_fwd of a split row 18.4 and 11.6.
+// the launch is 3.3, and takes 6.5 so; block_norm_bwd 21.8 and 12.3, pack and unpack 14.5 and 9.4, log_probs_fwd of a split row 18.4 and 9.1.
 //
 // Every function returns its outputs as a tuple, or the status of the call where it is not PCPP_OK.  Tensors that do not fit raise
 // AssertionError, types TypeError.
@@ -155,10 +155,26 @@ const float *weights(const Tensor *w, int64_t c)
 const void *at_of(const Tensor *t) { return t ? t->data_ptr() : nullptr; }
 
 Tensor empty(at::IntArrayRef size, at::ScalarType type, const Tensor &like) { return at::empty(size, like.options().dtype(type).requires_grad(false)); }
+// Outputs of one call that belong together share an allocation, which takes the host 0.7 us each time: a contiguous tensor from element `at` on.
+Tensor part_of(const Tensor &base, int64_t at, at::IntArrayRef size, at::ScalarType type)
+{
+    auto impl = c10::make_intrusive<at::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(type));
+    impl->set_storage_offset(at);
+    impl->set_sizes_contiguous(size);
+    return Tensor(std::move(impl));
+}
 Tensor workspace_of(size_t bytes, const Tensor *given, const Tensor &like)
 {
     if (given && (size_t)given->nbytes() >= bytes) return *given;
     return empty({(int64_t)(bytes > 256 ? bytes : 256)}, at::kByte, like);
+}
+
+// new rows in 8 bits: q, then the codes from the next 16 bytes on
+std::pair<Tensor, Tensor> new_rows8(int64_t n, int64_t c, const Tensor &like)
+{
+    const int64_t codes = (n * c + 15) / 16 * 16;
+    const Tensor all = empty({codes + n * code_bytes(c)}, at::kByte, like);
+    return {part_of(all, 0, {n, c}, at::kChar), part_of(all, codes, {n, code_bytes(c)}, at::kByte)};
 }
 
 // ---- results ------------------------------------------------------------------------------------------------------------------
@@ -217,7 +233,7 @@ PyObject *act_pack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const int c = channels(x), code = code_of(x.scalar_type());
         const Rows8 given = rows8(q, codes);
         if (given.q) need(shape(*given.q, n, c), "q has another shape than x");
-        const Tensor to = given.q ? *given.q : empty({n, c}, at::kChar, x), to_codes = given.q ? *given.codes : empty({n, code_bytes(c)}, at::kByte, x);
+        const auto [to, to_codes] = given.q ? std::pair<Tensor, Tensor>(*given.q, *given.codes) : new_rows8(n, c, x);
         const int rc = lib.act_pack(x.data_ptr(), code, n, c, static_cast<int8_t *>(to.data_ptr()), static_cast<uint8_t *>(to_codes.data_ptr()), stream);
         return result(rc, to, to_codes);
     });
@@ -308,8 +324,8 @@ PyObject *block_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         Tensor r, h, fq, fe, hq, he;
         if (f) r = empty({n, c}, x.scalar_type(), x);
         if (pre != PCPP_NORM_NONE) h = empty({n, c}, type, x);
-        if (pack_f) fq = empty({n, c}, at::kChar, x), fe = empty({n, code_bytes(c)}, at::kByte, x);
-        if (pack_h) hq = empty({n, c}, at::kChar, x), he = empty({n, code_bytes(c)}, at::kByte, x);
+        if (pack_f) std::tie(fq, fe) = new_rows8(n, c, x);
+        if (pack_h) std::tie(hq, he) = new_rows8(n, c, x);
         auto to = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
         const int rc = lib.block_norm_fwd(x.data_ptr(), at_of(f), f ? pitch(*f) : c, g.at, g.ld, g.cols, weights(w_post, c), weights(w_pre, c), post, pre, scale,
                                           eps, n, c, stream_code, code, to(r), to(h), static_cast<int8_t *>(to(fq)), static_cast<uint8_t *>(to(fe)),
@@ -351,8 +367,12 @@ PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         Tensor dx = empty({n, c}, stream_type, *some), df, dgate, dw_post, dw_pre;
         if (block) df = empty({n, c}, type, *some);
         if (gate) dgate = empty({n, g.cols}, type, *some);
-        if (block && (f || f8.q) && (post != PCPP_NORM_NONE || w_post)) dw_post = empty({c}, at::kFloat, *some);
-        if (pre != PCPP_NORM_NONE) dw_pre = empty({c}, at::kFloat, *some);
+        const bool of_post = block && (f || f8.q) && (post != PCPP_NORM_NONE || w_post), of_pre = pre != PCPP_NORM_NONE;
+        if (of_post || of_pre) {
+            const Tensor both = empty({2 * c}, at::kFloat, *some);
+            if (of_post) dw_post = part_of(both, 0, {c}, at::kFloat);
+            if (of_pre) dw_pre = part_of(both, c, {c}, at::kFloat);
+        }
         const Tensor ws = workspace_of(lib.block_norm_workspace_bytes(n, c), workspace, *some);
         auto to = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
         const int rc = lib.block_norm_bwd(at_of(dr), at_of(dh), at_of(r), at_of(f), f ? pitch(*f) : c, f8.at(), f8.codes_at(), g.at, g.ld, g.cols,
@@ -388,10 +408,12 @@ PyObject *log_probs_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const int64_t n = x.size(0), v = x.size(1), ld = pitch(x);
         const int32_t *label_at = labels_at(labels, n);
         const int code = code_of(x.scalar_type());
+        const int64_t k = n_top > 0 && n_top <= PCPP_MAX_ALTERNATIVES ? n_top : 0;       // (others are refused by the call)
+        const Tensor all = empty({n * (4 + 2 * k)}, at::kFloat, x);
         Tensor log_prob, top, index;
-        if (labels) log_prob = empty({n}, at::kFloat, x);
-        const Tensor entropy = empty({n}, at::kFloat, x), stats = empty({n, 2}, at::kFloat, x);
-        if (n_top > 0) top = empty({n, n_top}, at::kFloat, x), index = empty({n, n_top}, at::kInt, x);
+        const Tensor stats = part_of(all, 0, {n, 2}, at::kFloat), entropy = part_of(all, 2 * n, {n}, at::kFloat);
+        if (labels) log_prob = part_of(all, 3 * n, {n}, at::kFloat);
+        if (k) top = part_of(all, 4 * n, {n, k}, at::kFloat), index = part_of(all, (4 + k) * n, {n, k}, at::kInt);
         const size_t bytes = lib.log_probs_workspace_bytes(n, v, n_top);
         Tensor ws;
         if (bytes) ws = workspace_of(bytes, workspace, x);
