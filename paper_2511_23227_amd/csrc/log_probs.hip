@@ -8,8 +8,8 @@
 // A masked class has x = -inf (or the type's lowest value): its terms are zero.  A row without any class has log probabilities -inf,
 // entropy 0 and no gradient.  A row that holds a NaN or +inf has NaN everywhere but in its indices.
 //
-// Bound by memory, and in bf16 nearly as much by the exponentials: 4096 x 32 768 bf16 47 us = 5.8 TB/s, the gradient 82 us = 6.5; 115 200 x 17 fp32 with three
-// alternatives 8.3 us, one row of 131 072 bf16 with twenty 9.1 + 4.4.  Rows of up to 512 classes lie in the registers of a few lanes;
+// Bound by memory, and in bf16 nearly as much by the exponentials: 4096 x 32 768 bf16 46 us = 5.9 TB/s, the gradient 102 us = 5.3; 115 200 x 17 fp32 with three
+// alternatives 8.2 us, one row of 131 072 bf16 with twenty 8.9 + 4.3.  Rows of up to 512 classes lie in the registers of a few lanes;
 // longer ones are walked, by a wave or by a block of four, or, where there are few rows, by several blocks whose sums a second kernel
 // joins.
 //
