@@ -115,6 +115,14 @@ def test_weight_gradient_from_packed_input(pcpp, c_in, c_out, dtype, n, radius, 
         close(got[k], ref, dyd[o[a:b]].abs().T @ xd[i[a:b]].abs(), longest, ("dw", k))
 
 
+@pytest.mark.parametrize("c_in,c_out,dtype", [
+    (15, 4, F32), (16, 3, F32), (16, 9, F32), (17, 31, F32), (31, 32, F32), (32, 4, F32), (33, 17, F32), (5, 6, F32),
+    (15, 24, BF16), (16, 8, BF16), (17, 31, BF16), (31, 64, BF16), (32, 128, BF16), (32, 3, BF16),
+])
+def test_weight_gradient_from_packed_rows_of_few_channels(pcpp, c_in, c_out, dtype):
+    test_weight_gradient_from_packed_input(pcpp, c_in, c_out, dtype, 1500, 0.09, 3)
+
+
 def test_weight_gradient_from_packed_input_without_triplets(pcpp):
     p = pcpp.pcpp_act_pack(torch.randn(10, 24, device="cuda"))
     dy = torch.randn(5, 16, device="cuda")
