@@ -729,10 +729,12 @@ int mvmr_weight_mfma(const MvmrArgs &a, float *dw, const int32_t *tri_o, const i
 
 // The same from x in 8 bits (q and codes; a.in_dtype is dy's type).  Rows are gathered as they lie and become bf16 on their way through LDS.
 // Not for 256 -> 256 bf16, whose kernel moves rows to LDS without touching them (a bf16 copy of x costs it 0.15 ms of 4.7 for a million
-// points, where weight_any_kernel would take twice the time).
+// points, where weight_any_kernel would take twice the time), nor where the codes are beyond 32-bit offsets, which a row of one channel
+// reaches before x in bf16 does (four bytes of codes).
 bool mvmr_weight_packed_usable(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int dy_dtype)
 {
-    return !lds_shape(dy_dtype, c_in, c_out) && any_usable(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
+    return !lds_shape(dy_dtype, c_in, c_out) && any_usable(n_in, n_out, n_triplets, c_in, c_out, dy_dtype) &&
+           (size_t)n_in * act_code_bytes(c_in) <= MAX_BUFFER_BYTES;
 }
 
 int mvmr_weight_packed(const MvmrArgs &a, const uint8_t *codes, float *dw, const int32_t *tri_o, const int64_t *seg, void *workspace,
