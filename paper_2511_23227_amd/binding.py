@@ -160,6 +160,11 @@ def _bytes(n: int, device) -> torch.Tensor:
     return torch.empty(max(int(n), 256), dtype=torch.uint8, device=device)
 
 
+def _room(given: torch.Tensor | None, n: int) -> bool:
+    """Whether a caller's buffer has n bytes in one piece (an expanded tensor's numel() are not there)."""
+    return given is not None and given.is_contiguous() and given.numel() >= n
+
+
 @dataclass
 class Triplets:
     """Result of pcpp_build_triplets: T in (k, o, i) order plus the plan the compute calls read."""
@@ -184,7 +189,7 @@ def pcpp_count_triplets(in_xyz: torch.Tensor, out_xyz: torch.Tensor, radius: flo
     L = library()
     n_in, n_out = in_xyz.shape[0], out_xyz.shape[0]
     ws_bytes = L.pcpp_build_triplets_workspace_bytes(n_in, n_out, t)
-    ws = workspace if workspace is not None else _bytes(ws_bytes, in_xyz.device)
+    ws = workspace if _room(workspace, 0) else _bytes(ws_bytes, in_xyz.device)
     n = _landing_word()
     _check(L.pcpp_build_triplets(_ptr(in_xyz), n_in, _ptr(out_xyz), n_out, float(radius), int(t), None, None, None,
                                  0, None, n, None, 0, 0, _ptr(ws), ws.numel(), _stream()))
@@ -228,12 +233,12 @@ def pcpp_build_triplets(in_xyz: torch.Tensor, out_xyz: torch.Tensor, radius: flo
     ws_bytes = L.pcpp_build_triplets_workspace_bytes_for(n_in, n_out, t, cap)
     if ws_bytes == 0:
         raise PcppError(-1, "invalid sizes or t")
-    if ws is None or ws.numel() < ws_bytes:
+    if not _room(ws, ws_bytes):
         ws = _bytes(ws_bytes, dev)
 
     def buf(name, numel, dtype):
         b = buffers.get(name)
-        if b is None or b.numel() < numel or b.dtype != dtype:
+        if not _room(b, numel) or b.dtype != dtype:
             b = torch.empty(numel, dtype=dtype, device=dev)
         return b
 
@@ -242,7 +247,7 @@ def pcpp_build_triplets(in_xyz: torch.Tensor, out_xyz: torch.Tensor, radius: flo
     want_plan = bool(plan_flags & PLAN_MASK)
     plan_bytes = L.pcpp_plan_bytes(n_in, n_out, t, cap, plan_flags & PLAN_MASK) if want_plan else 0
     plan = buffers.get("plan")
-    if want_plan and (plan is None or plan.numel() < plan_bytes):
+    if want_plan and not _room(plan, plan_bytes):
         plan = _bytes(plan_bytes, dev)
     n = _landing_word()
     n_batches = 1
@@ -301,7 +306,7 @@ def _plan_args(T: Triplets):
 
 def _mvmr_ws(op, T: Triplets, c_in, c_out, code, dev, workspace):
     need = library().pcpp_mvmr_workspace_bytes(op, T.n_in, T.n_out, T.n_triplets, c_in, c_out, T.K, code)
-    if workspace is None or workspace.numel() < need:
+    if not _room(workspace, need):
         workspace = _bytes(need, dev)
     return workspace
 

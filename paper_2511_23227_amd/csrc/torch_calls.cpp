@@ -163,9 +163,10 @@ Tensor part_of(const Tensor &base, int64_t at, at::IntArrayRef size, at::ScalarT
     impl->set_sizes_contiguous(size);
     return Tensor(std::move(impl));
 }
+// The caller's workspace, or a new one where it is too small or does not lie in one piece (an expanded tensor's nbytes() are not there).
 Tensor workspace_of(size_t bytes, const Tensor *given, const Tensor &like)
 {
-    if (given && (size_t)given->nbytes() >= bytes) return *given;
+    if (given && given->is_contiguous() && (size_t)given->nbytes() >= bytes) return *given;
     return empty({(int64_t)(bytes > 256 ? bytes : 256)}, at::kByte, like);
 }
 

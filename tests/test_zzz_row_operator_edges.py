@@ -35,3 +35,55 @@ def test_packed_weight_gradient_whose_codes_pass_32_bit_offsets(pcpp):
     ref = torch.zeros(8, c_out, 1, dtype=torch.float64, device="cuda")
     ref.index_add_(0, cell.long(), (dy[o.long()].double() * value[:, None].double())[..., None])
     assert torch.equal(pcpp.pcpp_mvmr_bwd_weight_packed(p, dy, T).double(), ref)
+
+
+def expanded(n):
+    """One byte that says it is n: what is written past it belongs to others."""
+    return torch.full((1,), 7, dtype=torch.uint8, device="cuda").expand(max(int(n), 1))
+
+
+def test_workspaces_that_do_not_lie_in_one_piece(pcpp):
+    """A caller's workspace of enough bytes is used only if they are there: an expanded one is left alone, and the results are the same."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    lib = pcpp.library()
+    n, c = 900, 48
+    x, dy = (torch.randn(n, c, generator=g, device="cuda").to(BF16) for _ in range(2))
+    xyz = torch.rand(n, 3, generator=g, device="cuda")
+    T = pcpp.pcpp_build_triplets(xyz, xyz, 0.15, 3)
+    p = pcpp.pcpp_act_pack(x)
+    w = torch.randn(T.K, c, c, generator=g, device="cuda").to(BF16)
+    sizes = (n, n, T.n_triplets, c, c, T.K, 1)
+    logits = torch.randn(2, 20_000, generator=g, device="cuda")
+
+    def fields(y):
+        return [t for t in vars(y).values() if t is not None] if hasattr(y, "__dict__") else [y.log_prob, y.entropy, y.top_log_prob, y.top_index]
+
+    labels = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for need, call in (
+            (lib.pcpp_mvmr_packed_workspace_bytes(*sizes), lambda **k: [pcpp.pcpp_mvmr_bwd_weight_packed(p, dy, T, **k)]),
+            (lib.pcpp_block_norm_workspace_bytes(n, c), lambda **k: fields(pcpp.pcpp_block_norm_bwd(dy, dy, x, x, **k))),
+            (lib.pcpp_log_probs_workspace_bytes(2, 20_000, 5), lambda **k: fields(pcpp.pcpp_log_probs_fwd(logits, labels, 5, **k))),
+            (lib.pcpp_mvmr_workspace_bytes(0, *sizes), lambda **k: [pcpp.pcpp_mvmr_fwd(x, w, T, **k)]),
+            (lib.pcpp_mvmr_workspace_bytes(1, *sizes), lambda **k: [pcpp.pcpp_mvmr_bwd_input(dy, w, T, **k)]),
+            (lib.pcpp_mvmr_workspace_bytes(2, *sizes), lambda **k: [pcpp.pcpp_mvmr_bwd_weight(x, dy, T, **k)])):
+        assert need > 512
+        space = expanded(need)
+        for a, b in zip(call(), call(workspace=space)):
+            assert torch.equal(a, b)
+        assert int(space[0]) == 7
+        whole = torch.full((need,), 7, dtype=torch.uint8, device="cuda")
+        for a, b in zip(call(), call(workspace=whole)):
+            assert torch.equal(a, b)
+        assert (whole != 7).any()                      # (one piece: it is used)
+
+
+def test_triplets_into_buffers_that_do_not_lie_in_one_piece(pcpp):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    xyz = torch.rand(700, 3, generator=g, device="cuda")
+    ref = pcpp.pcpp_build_triplets(xyz, xyz, 0.15, 3)
+    one = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    space = expanded(1 << 28)
+    T = pcpp.pcpp_build_triplets(xyz, xyz, 0.15, 3, buffers={"workspace": space, "plan": space, "tri_o": one.expand(1 << 20)})
+    assert torch.equal(T.tri_o, ref.tri_o) and torch.equal(T.tri_i, ref.tri_i) and torch.equal(T.tri_k, ref.tri_k)
+    assert pcpp.pcpp_count_triplets(xyz, xyz, 0.15, 3, workspace=space) == ref.n_triplets
+    assert int(space[0]) == 7 and int(one[0]) == 7
