@@ -2,7 +2,7 @@
 // binding.py's functions of the same names wrap the results.
 //
 // Their smallest calls take the GPU 3 us, so what the host does is what they cost: block_norm_fwd of three rows took 10.5 us through ctypes, of which
-// the launch is 3.3, and takes 6.5 so; block_norm_bwd 21.8 and 12.3, pack and unpack 14.5 and 9.4, log_probs_fwd of a split row 18.4 and 9.1.
+// the launch is 3.3, and takes 5.8 so; block_norm_bwd 21.8 and 12, pack and unpack 14.5 and 10.4, log_probs_fwd of a split row 18.4 and 11.4.
 //
 // Every function returns its outputs as a tuple, or the status of the call where it is not PCPP_OK.  Tensors that do not fit raise
 // AssertionError, types TypeError.
@@ -154,15 +154,9 @@ const float *weights(const Tensor *w, int64_t c)
 }
 const void *at_of(const Tensor *t) { return t ? t->data_ptr() : nullptr; }
 
+// Every output has a storage of its own, at 0.6 us each: tensors of different types in one cannot be saved, and one that is kept or saved would
+// hold them all.
 Tensor empty(at::IntArrayRef size, at::ScalarType type, const Tensor &like) { return at::empty(size, like.options().dtype(type).requires_grad(false)); }
-// Outputs of one call that belong together share an allocation, which takes the host 0.7 us each time: a contiguous tensor from element `at` on.
-Tensor part_of(const Tensor &base, int64_t at, at::IntArrayRef size, at::ScalarType type)
-{
-    auto impl = c10::make_intrusive<at::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(type));
-    impl->set_storage_offset(at);
-    impl->set_sizes_contiguous(size);
-    return Tensor(std::move(impl));
-}
 // The caller's workspace, or a new one where it is too small or does not lie in one piece (an expanded tensor's nbytes() are not there).
 Tensor workspace_of(size_t bytes, const Tensor *given, const Tensor &like)
 {
@@ -170,12 +164,10 @@ Tensor workspace_of(size_t bytes, const Tensor *given, const Tensor &like)
     return empty({(int64_t)(bytes > 256 ? bytes : 256)}, at::kByte, like);
 }
 
-// new rows in 8 bits: q, then the codes from the next 16 bytes on
+// new rows in 8 bits: q and codes
 std::pair<Tensor, Tensor> new_rows8(int64_t n, int64_t c, const Tensor &like)
 {
-    const int64_t codes = (n * c + 15) / 16 * 16;
-    const Tensor all = empty({codes + n * code_bytes(c)}, at::kByte, like);
-    return {part_of(all, 0, {n, c}, at::kChar), part_of(all, codes, {n, code_bytes(c)}, at::kByte)};
+    return {empty({n, c}, at::kChar, like), empty({n, code_bytes(c)}, at::kByte, like)};
 }
 
 // ---- results ------------------------------------------------------------------------------------------------------------------
@@ -369,11 +361,8 @@ PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         if (block) df = empty({n, c}, type, *some);
         if (gate) dgate = empty({n, g.cols}, type, *some);
         const bool of_post = block && (f || f8.q) && (post != PCPP_NORM_NONE || w_post), of_pre = pre != PCPP_NORM_NONE;
-        if (of_post || of_pre) {
-            const Tensor both = empty({2 * c}, at::kFloat, *some);
-            if (of_post) dw_post = part_of(both, 0, {c}, at::kFloat);
-            if (of_pre) dw_pre = part_of(both, c, {c}, at::kFloat);
-        }
+        if (of_post) dw_post = empty({c}, at::kFloat, *some);
+        if (of_pre) dw_pre = empty({c}, at::kFloat, *some);
         const Tensor ws = workspace_of(lib.block_norm_workspace_bytes(n, c), workspace, *some);
         auto to = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
         const int rc = lib.block_norm_bwd(at_of(dr), at_of(dh), at_of(r), at_of(f), f ? pitch(*f) : c, f8.at(), f8.codes_at(), g.at, g.ld, g.cols,
@@ -410,11 +399,10 @@ PyObject *log_probs_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const int32_t *label_at = labels_at(labels, n);
         const int code = code_of(x.scalar_type());
         const int64_t k = n_top > 0 && n_top <= PCPP_MAX_ALTERNATIVES ? n_top : 0;       // (others are refused by the call)
-        const Tensor all = empty({n * (4 + 2 * k)}, at::kFloat, x);
         Tensor log_prob, top, index;
-        const Tensor stats = part_of(all, 0, {n, 2}, at::kFloat), entropy = part_of(all, 2 * n, {n}, at::kFloat);
-        if (labels) log_prob = part_of(all, 3 * n, {n}, at::kFloat);
-        if (k) top = part_of(all, 4 * n, {n, k}, at::kFloat), index = part_of(all, (4 + k) * n, {n, k}, at::kInt);
+        const Tensor stats = empty({n, 2}, at::kFloat, x), entropy = empty({n}, at::kFloat, x);
+        if (labels) log_prob = empty({n}, at::kFloat, x);
+        if (k) top = empty({n, k}, at::kFloat, x), index = empty({n, k}, at::kInt, x);
         const size_t bytes = lib.log_probs_workspace_bytes(n, v, n_top);
         Tensor ws;
         if (bytes) ws = workspace_of(bytes, workspace, x);

@@ -1,4 +1,6 @@
 """The operators around the convolution where sizes, storage and the caller's own tensors are out of the ordinary."""
+import io
+
 import pytest
 import torch
 
@@ -87,3 +89,29 @@ def test_triplets_into_buffers_that_do_not_lie_in_one_piece(pcpp):
     assert torch.equal(T.tri_o, ref.tri_o) and torch.equal(T.tri_i, ref.tri_i) and torch.equal(T.tri_k, ref.tri_k)
     assert pcpp.pcpp_count_triplets(xyz, xyz, 0.15, 3, workspace=space) == ref.n_triplets
     assert int(space[0]) == 7 and int(one[0]) == 7
+
+
+def test_outputs_have_storages_of_their_own(pcpp):
+    """What a call returns can be saved, alone and together, holds no more memory than its own, and can be resized without reaching another."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    n, c = 70, 40
+    x, f, gate, dr = (torch.randn(n, c, generator=g, device="cuda") for _ in range(4))
+    w = torch.ones(c, device="cuda")
+    y = pcpp.pcpp_block_norm_fwd(x, f, gate, w, w, pack_f=True, pack_h=True)
+    b = pcpp.pcpp_block_norm_bwd(dr, dr, y.r, f, gate, w, w)
+    p = pcpp.pcpp_act_pack(x)
+    lp = pcpp.pcpp_log_probs_fwd(x, torch.zeros(n, dtype=torch.int32, device="cuda"), 5)
+    split = pcpp.pcpp_log_probs_fwd(x.view(1, -1).repeat(1, 5), torch.zeros(1, dtype=torch.int32, device="cuda"), 5)
+    results = dict(r=y.r, h=y.h, fq=y.f_packed.q, fcodes=y.f_packed.codes, hq=y.h_packed.q, hcodes=y.h_packed.codes, dx=b.dx, df=b.df, dgate=b.dgate,
+                   dw_post=b.dw_post, dw_pre=b.dw_pre, q=p.q, codes=p.codes)
+    for name, l in (("lp", lp), ("split", split)):
+        results.update({name + k: getattr(l, k) for k in ("log_prob", "entropy", "max_log_sum", "top_log_prob", "top_index")})
+    at = [t.untyped_storage().data_ptr() for t in results.values()]
+    assert len(set(at)) == len(at)
+    for name, t in results.items():
+        assert t.storage_offset() == 0 and t.untyped_storage().nbytes() == t.numel() * t.element_size(), name
+    file = io.BytesIO()
+    torch.save(results, file)
+    file.seek(0)
+    for name, t in torch.load(file, weights_only=True).items():
+        assert torch.equal(t, results[name]), name
