@@ -2,8 +2,10 @@
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -52,10 +54,24 @@ def _compile(name: str, extra) -> str:
     return obj
 
 
+def _calls_need() -> str | None:
+    """What this machine lacks to compile the Python calls, or None.  The library itself needs none of it."""
+    try:
+        import torch
+    except ImportError as e:
+        return f"torch ({e})"
+    if shutil.which("g++") is None:
+        return "g++"
+    headers = (os.path.join(sysconfig.get_paths()["include"], "Python.h"),
+               os.path.join(os.path.dirname(os.path.abspath(torch.__file__)), "include", "torch", "csrc", "autograd", "python_variable.h"))
+    return next((h for h in headers if not os.path.exists(h)), None)
+
+
 def build_calls() -> str:
     """The compiled side of the Python calls (host code against this torch's and Python's headers)."""
-    import sysconfig
-
+    missing = _calls_need()
+    if missing:
+        raise RuntimeError(f"the compiled side of the Python calls cannot be built without {missing}")
     import torch
     root = os.path.dirname(os.path.abspath(torch.__file__))
     tmp = CALLS_LIB + ".tmp"
@@ -71,8 +87,8 @@ def build_calls() -> str:
 
 
 def build(verbose: bool = False) -> str:
+    """The library, then the compiled side of the Python calls, which is left out, with a note, where torch, g++ or the headers are missing."""
     os.makedirs(OBJ, exist_ok=True)
-    build_calls()
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         objs = list(ex.map(lambda kv: _compile(*kv), SOURCES.items()))
     tmp = LIB + ".tmp"
@@ -82,6 +98,11 @@ def build(verbose: bool = False) -> str:
     tmp = PROBE_LIB + ".tmp"
     subprocess.run(["hipcc", "-shared", "-fPIC", "--offload-arch=gfx950", "-o", tmp, probe], check=True)
     os.replace(tmp, PROBE_LIB)
+    missing = _calls_need()
+    if missing:
+        sys.stderr.write(f"the compiled side of the Python calls is not built: it needs {missing}\n")
+    else:
+        build_calls()
     if verbose:
         print("built", LIB)
     return LIB
