@@ -383,13 +383,14 @@ _calls = None
 
 
 def _compiled():
-    """The compiled side of the calls, bound to the library (built first only if it is not there).  Raises if unavailable."""
+    """The compiled side of the calls, bound to the library (built first only if there is none for this Python and torch).  Raises if
+    unavailable."""
     global _calls
     if _calls is None:
+        from .build import build_calls, calls_lib
         handle = library()._handle
-        path = os.path.join(HERE, "_torch_calls.so")
+        path = calls_lib()
         if not os.path.exists(path):
-            from .build import build_calls
             build_calls()
         spec = importlib.util.spec_from_file_location("_torch_calls", path)
         module = importlib.util.module_from_spec(spec)

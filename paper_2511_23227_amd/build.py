@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -13,7 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpcpp.so")
-CALLS_LIB = os.path.join(HERE, "_torch_calls.so")      # host code: tensors' checks and outputs of the short calls
+CALLS_DIR = HERE                                       # of the host code that checks tensors and makes outputs in the short calls
 PROBE_LIB = os.path.join(HERE, "libpcpp_probe.so")     # the benchmark's peak-rate probe, outside the library's interface
 
 # file -> extra flags.  The search kernels must not contract a*b+c into an FMA: the inclusion test
@@ -67,6 +68,12 @@ def _calls_need() -> str | None:
     return next((h for h in headers if not os.path.exists(h)), None)
 
 
+def calls_lib() -> str:
+    """The compiled side of the Python calls that fits this Python and this torch, whose binary interfaces it uses."""
+    import torch
+    return os.path.join(CALLS_DIR, re.sub(r"[^\w.-]", "_", f"_torch_calls.{sys.implementation.cache_tag}-torch{torch.__version__}") + ".so")
+
+
 def build_calls() -> str:
     """The compiled side of the Python calls (host code against this torch's and Python's headers)."""
     missing = _calls_need()
@@ -74,7 +81,8 @@ def build_calls() -> str:
         raise RuntimeError(f"the compiled side of the Python calls cannot be built without {missing}")
     import torch
     root = os.path.dirname(os.path.abspath(torch.__file__))
-    tmp = CALLS_LIB + ".tmp"
+    lib = calls_lib()
+    tmp = lib + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
            "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "torch_calls.cpp"), "-o", tmp,
@@ -82,8 +90,8 @@ def build_calls() -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed for torch_calls.cpp:\n{r.stderr}")
-    os.replace(tmp, CALLS_LIB)
-    return CALLS_LIB
+    os.replace(tmp, lib)
+    return lib
 
 
 def build(verbose: bool = False) -> str:

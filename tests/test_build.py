@@ -5,6 +5,8 @@ import sys
 
 import pytest
 
+import paper_2511_23227_amd
+from paper_2511_23227_amd import binding
 from paper_2511_23227_amd import build as b
 
 pytestmark = pytest.mark.timeout(300)
@@ -16,7 +18,7 @@ def small(tmp_path, monkeypatch):
     monkeypatch.setattr(b, "SOURCES", {"scan.hip": []})
     for name, file in (("OBJ", "_build"), ("LIB", "libpcpp.so"), ("PROBE_LIB", "libpcpp_probe.so")):
         monkeypatch.setattr(b, name, str(tmp_path / file))
-    monkeypatch.setattr(b, "CALLS_LIB", str(tmp_path / "_torch_calls.so"))
+    monkeypatch.setattr(b, "CALLS_DIR", str(tmp_path))
     return tmp_path
 
 
@@ -38,3 +40,24 @@ def test_library_is_built_where_the_calls_do_not_compile(small, monkeypatch):
     with pytest.raises(RuntimeError, match="no compiler here"):
         b.build()
     assert (small / "libpcpp.so").exists() and (small / "libpcpp_probe.so").exists()
+
+
+def test_compiled_calls_belong_to_one_python_and_torch(monkeypatch):
+    import torch
+    here = b.calls_lib()
+    assert sys.implementation.cache_tag in os.path.basename(here)
+    monkeypatch.setattr(torch, "__version__", "99.0+other")
+    other = b.calls_lib()
+    assert other != here and not os.path.exists(other)
+    # a module of another version is not loaded: the calls ask for their own
+    asked = []
+    monkeypatch.setattr(b, "build_calls", lambda: asked.append(b.calls_lib()))
+    monkeypatch.setattr(binding, "_calls", None)
+    with pytest.raises((ImportError, OSError)):
+        binding._compiled()
+    assert asked == [other]
+
+
+def test_the_package_has_its_compiled_calls():
+    assert os.path.dirname(b.calls_lib()) == os.path.dirname(os.path.abspath(paper_2511_23227_amd.__file__))
+    binding._compiled()
