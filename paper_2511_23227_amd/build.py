@@ -1,6 +1,8 @@
 """Compile the HIP sources into paper_2511_23227_amd/libpcpp.so for gfx950 (hipcc cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import contextlib
+import fcntl
 import os
 import re
 import shutil
@@ -74,8 +76,22 @@ def calls_lib() -> str:
     return os.path.join(CALLS_DIR, re.sub(r"[^\w.-]", "_", f"_torch_calls.{sys.implementation.cache_tag}-torch{torch.__version__}") + ".so")
 
 
+@contextlib.contextmanager
+def _alone():
+    """One build of this folder at a time, among processes and threads: they write the same intermediate files."""
+    os.makedirs(OBJ, exist_ok=True)
+    with open(os.path.join(OBJ, "lock"), "w") as lock:
+        fcntl.flock(lock, fcntl.LOCK_EX)                # (given back when the file is closed)
+        yield
+
+
 def build_calls() -> str:
     """The compiled side of the Python calls (host code against this torch's and Python's headers)."""
+    with _alone():
+        return _build_calls()
+
+
+def _build_calls() -> str:
     missing = _calls_need()
     if missing:
         raise RuntimeError(f"the compiled side of the Python calls cannot be built without {missing}")
@@ -96,7 +112,11 @@ def build_calls() -> str:
 
 def build(verbose: bool = False) -> str:
     """The library, then the compiled side of the Python calls, which is left out, with a note, where torch, g++ or the headers are missing."""
-    os.makedirs(OBJ, exist_ok=True)
+    with _alone():
+        return _build(verbose)
+
+
+def _build(verbose: bool) -> str:
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         objs = list(ex.map(lambda kv: _compile(*kv), SOURCES.items()))
     tmp = LIB + ".tmp"
@@ -110,7 +130,7 @@ def build(verbose: bool = False) -> str:
     if missing:
         sys.stderr.write(f"the compiled side of the Python calls is not built: it needs {missing}\n")
     else:
-        build_calls()
+        _build_calls()
     if verbose:
         print("built", LIB)
     return LIB

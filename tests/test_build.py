@@ -2,6 +2,8 @@
 import os
 import stat
 import sys
+import threading
+import time
 
 import pytest
 
@@ -56,6 +58,35 @@ def test_compiled_calls_belong_to_one_python_and_torch(monkeypatch):
     with pytest.raises((ImportError, OSError)):
         binding._compiled()
     assert asked == [other]
+
+
+def test_builds_at_the_same_time_take_turns(small, monkeypatch):
+    inside, most = [0], [0]
+
+    def run(cmd, **_):
+        inside[0] += 1
+        most[0] = max(most[0], inside[0])
+        time.sleep(0.2)
+        with open(cmd[cmd.index("-o") + 1], "w") as f:
+            f.write("built")
+        inside[0] -= 1
+        return type("Done", (), {"returncode": 0, "stderr": ""})
+
+    monkeypatch.setattr(b.subprocess, "run", run)
+    failed = []
+
+    def build():
+        try:
+            b.build_calls()
+        except Exception as e:                         # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=build) for _ in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed and most[0] == 1 and [p.name for p in small.glob("_torch_calls*")] and not list(small.glob("*.tmp"))
 
 
 def test_the_package_has_its_compiled_calls():
