@@ -165,6 +165,13 @@ def _room(given: torch.Tensor | None, n: int) -> bool:
     return given is not None and given.is_contiguous() and given.numel() >= n
 
 
+def _written(*given: torch.Tensor | None):
+    """Tensors of the caller's that a call has written: autograd is to refuse to go on with what it saved of them."""
+    for t in given:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 @dataclass
 class Triplets:
     """Result of pcpp_build_triplets: T in (k, o, i) order plus the plan the compute calls read."""
@@ -236,10 +243,14 @@ def pcpp_build_triplets(in_xyz: torch.Tensor, out_xyz: torch.Tensor, radius: flo
     if not _room(ws, ws_bytes):
         ws = _bytes(ws_bytes, dev)
 
+    given = []
+
     def buf(name, numel, dtype):
         b = buffers.get(name)
         if not _room(b, numel) or b.dtype != dtype:
             b = torch.empty(numel, dtype=dtype, device=dev)
+        else:
+            given.append(b)
         return b
 
     tri_o, tri_i, tri_k = (buf(nm, cap, torch.int32) for nm in ("tri_o", "tri_i", "tri_k"))
@@ -262,6 +273,7 @@ def pcpp_build_triplets(in_xyz: torch.Tensor, out_xyz: torch.Tensor, radius: flo
                                        _ptr(plan) if want_plan else None, plan.numel() if want_plan else 0, plan_flags,
                                        _ptr(ws), ws.numel(), _stream())
     nt = int(n[0])
+    _written(*given)
     if rc == ERR_CAPACITY:
         raise _capacity_error(cap, nt)
     _check(rc)
@@ -318,12 +330,14 @@ def pcpp_mvmr_fwd(x: torch.Tensor, w: torch.Tensor, T: Triplets, out: torch.Tens
     assert x.is_cuda and x.is_contiguous() and w.is_contiguous() and x.dtype == w.dtype
     K, c_out, c_in = w.shape
     assert K == T.K and x.shape == (T.n_in, c_in)
+    given = out
     if out is None:
         out = torch.empty((T.n_out, c_out), dtype=out_dtype, device=x.device)
     ws = _mvmr_ws(0, T, c_in, c_out, _dtype_code(x), x.device, workspace)
     _check(L.pcpp_mvmr_fwd(_ptr(x), _ptr(w), _ptr(out), _dtype_code(x), _dtype_code(out), T.n_in, T.n_out, c_in, c_out,
                            K, _ptr(T.tri_o), _ptr(T.tri_i), _ptr(T.tri_k), _ptr(T.seg_offsets), T.n_triplets,
                            *_plan_args(T), _ptr(ws), ws.numel(), _stream()))
+    _written(given)
     return out
 
 
@@ -338,6 +352,7 @@ def pcpp_mvmr_fwd_static(x: torch.Tensor, w: torch.Tensor, T: Triplets, out: tor
     _check(L.pcpp_mvmr_fwd_static(_ptr(x), _ptr(w), _ptr(out), _dtype_code(x), _dtype_code(out), T.n_in, T.n_out, c_in,
                                   c_out, K, _ptr(T.tri_o), _ptr(T.tri_i), _ptr(T.tri_k), _ptr(T.seg_offsets),
                                   T.n_triplets, *_plan_args(T), _stream()))
+    _written(out)
     return out
 
 
@@ -350,12 +365,14 @@ def pcpp_mvmr_bwd_input(dy: torch.Tensor, w: torch.Tensor, T: Triplets, dx: torc
     assert K == T.K and dy.shape == (T.n_out, c_out)
     if not (T.plan_flags & PLAN_BWD_INPUT):
         raise PcppError(-1, "triplets were built without PLAN_BWD_INPUT")
+    given = dx
     if dx is None:
         dx = torch.empty((T.n_in, c_in), dtype=out_dtype, device=dy.device)
     ws = _mvmr_ws(1, T, c_in, c_out, _dtype_code(dy), dy.device, workspace)
     _check(L.pcpp_mvmr_bwd_input(_ptr(dy), _ptr(w), _ptr(dx), _dtype_code(dy), _dtype_code(dx), T.n_in, T.n_out, c_in,
                                  c_out, K, _ptr(T.tri_o), _ptr(T.tri_i), _ptr(T.tri_k), _ptr(T.seg_offsets),
                                  T.n_triplets, *_plan_args(T), _ptr(ws), ws.numel(), _stream()))
+    _written(given)
     return dx
 
 
@@ -366,12 +383,14 @@ def pcpp_mvmr_bwd_weight(x: torch.Tensor, dy: torch.Tensor, T: Triplets, dw: tor
     assert x.is_cuda and x.is_contiguous() and dy.is_contiguous() and x.dtype == dy.dtype
     c_in, c_out = x.shape[1], dy.shape[1]
     assert x.shape[0] == T.n_in and dy.shape[0] == T.n_out
+    given = dw
     if dw is None:
         dw = torch.empty((T.K, c_out, c_in), dtype=torch.float32, device=x.device)
     ws = _mvmr_ws(2, T, c_in, c_out, _dtype_code(x), x.device, workspace)
     _check(L.pcpp_mvmr_bwd_weight(_ptr(x), _ptr(dy), _ptr(dw), _dtype_code(x), T.n_in, T.n_out, c_in, c_out, T.K,
                                   _ptr(T.tri_o), _ptr(T.tri_i), _ptr(T.tri_k), _ptr(T.seg_offsets), T.n_triplets,
                                   *_plan_args(T), _ptr(ws), ws.numel(), _stream()))
+    _written(given)
     return dw
 
 

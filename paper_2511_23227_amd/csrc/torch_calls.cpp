@@ -170,6 +170,12 @@ std::pair<Tensor, Tensor> new_rows8(int64_t n, int64_t c, const Tensor &like)
     return {empty({n, c}, at::kChar, like), empty({n, code_bytes(c)}, at::kByte, like)};
 }
 
+// A tensor of the caller's that a call has written: autograd is to refuse to go on with what it saved of it.
+void written(const Tensor *t)
+{
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 // ---- results ------------------------------------------------------------------------------------------------------------------
 PyObject *wrapped(const Tensor &t)
 {
@@ -228,6 +234,8 @@ PyObject *act_pack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         if (given.q) need(shape(*given.q, n, c), "q has another shape than x");
         const auto [to, to_codes] = given.q ? std::pair<Tensor, Tensor>(*given.q, *given.codes) : new_rows8(n, c, x);
         const int rc = lib.act_pack(x.data_ptr(), code, n, c, static_cast<int8_t *>(to.data_ptr()), static_cast<uint8_t *>(to_codes.data_ptr()), stream);
+        written(given.q);
+        written(given.codes);
         return result(rc, to, to_codes);
     });
 }
@@ -245,7 +253,9 @@ PyObject *act_unpack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const int c = channels(q);
         if (given) need_rows(*given, n, c, "out has another shape than q, or is not contiguous");
         const Tensor out = given ? *given : empty({n, c}, type_of(code), q);
-        return result(lib.act_unpack(rows.at(), rows.codes_at(), n, c, out.data_ptr(), code_of(out.scalar_type()), stream), out);
+        const int rc = lib.act_unpack(rows.at(), rows.codes_at(), n, c, out.data_ptr(), code_of(out.scalar_type()), stream);
+        written(given);
+        return result(rc, out);
     });
 }
 
@@ -278,6 +288,7 @@ PyObject *weight_packed(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const int rc = lib.mvmr_bwd_weight_packed(x.at(), x.codes_at(), dy.data_ptr(), static_cast<float *>(dw.data_ptr()), code, n_in, n_out, c_in, c_out, K,
                                                   words(tri_o), words(tri_i), words(tri_k), static_cast<const int64_t *>(seg.data_ptr()), n, at_of(plan),
                                                   plan ? plan->nbytes() : 0, flags, ws.data_ptr(), ws.nbytes(), stream);
+        written(given);
         return result(rc, dw);
     });
 }
@@ -431,6 +442,7 @@ PyObject *log_probs_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const Tensor out = given ? *given : empty({n, v}, x.scalar_type(), x);
         const int rc = lib.log_probs_bwd(x.data_ptr(), code, n, v, ld, labels_at(labels, n), static_cast<const float *>(stats.data_ptr()), floats_at(entropy, n),
                                          floats_at(d_log_prob, n), floats_at(d_entropy, n), out.data_ptr(), given ? pitch(*given) : v, stream);
+        written(given);
         return result(rc, out);
     });
 }

@@ -115,3 +115,41 @@ def test_outputs_have_storages_of_their_own(pcpp):
     file.seek(0)
     for name, t in torch.load(file, weights_only=True).items():
         assert torch.equal(t, results[name]), name
+
+
+def test_outputs_that_the_caller_gives_are_seen_by_autograd(pcpp):
+    """A call that writes a caller's tensor raises its version, so that a graph that saved the tensor refuses to use what now stands there."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    n, c = 60, 32
+    labels = torch.arange(n, dtype=torch.int32, device="cuda") % c
+    head = torch.randn(c, c, generator=g, device="cuda", requires_grad=True)
+    logits = torch.randn(n, c, generator=g, device="cuda") @ head
+    penalty = (logits * logits).sum()                  # (saves the logits)
+    y = pcpp.pcpp_log_probs_fwd(logits, labels)
+    pcpp.pcpp_log_probs_bwd(logits, labels, y, torch.ones(n, device="cuda"), out=logits)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        penalty.backward()
+
+    x = torch.randn(n, c, generator=g, device="cuda")
+    xyz = torch.rand(n, 3, generator=g, device="cuda")
+    T = pcpp.pcpp_build_triplets(xyz, xyz, 0.4, 2)
+    w = torch.randn(T.K, c, c, generator=g, device="cuda")
+    p, rows = pcpp.pcpp_act_pack(x), torch.empty(n, c, device="cuda")
+    dw = torch.empty(T.K, c, c, device="cuda")
+    kept = pcpp.Packed(torch.empty_like(p.q), torch.empty_like(p.codes))
+    buffers = {k: torch.empty(48 * 1024, dtype=torch.int32, device="cuda") for k in ("tri_o", "tri_i", "tri_k")}
+    for call, given in ((lambda: pcpp.pcpp_act_pack(x, out=kept), (kept.q, kept.codes)),
+                        (lambda: pcpp.pcpp_act_unpack(p, out=rows), (rows,)),
+                        (lambda: pcpp.pcpp_mvmr_bwd_weight_packed(p, x, T, dw=dw), (dw,)),
+                        (lambda: pcpp.pcpp_mvmr_fwd(x, w, T, out=rows), (rows,)),
+                        (lambda: pcpp.pcpp_mvmr_fwd_static(x, w, T, rows), (rows,)),
+                        (lambda: pcpp.pcpp_mvmr_bwd_input(x, w, T, dx=rows), (rows,)),
+                        (lambda: pcpp.pcpp_mvmr_bwd_weight(x, x, T, dw=dw), (dw,)),
+                        (lambda: pcpp.pcpp_build_triplets(xyz, xyz, 0.4, 2, buffers=buffers), tuple(buffers.values()))):
+        before = [t._version for t in given]
+        call()
+        assert all(t._version > v for t, v in zip(given, before))
+    with torch.inference_mode():                       # (such tensors have no version)
+        inference = torch.empty(n, c, device="cuda")
+    assert torch.equal(pcpp.pcpp_act_unpack(p, out=inference), pcpp.pcpp_act_unpack(p, F32))
+    assert torch.equal(pcpp.pcpp_mvmr_fwd(x, w, T, out=inference), pcpp.pcpp_mvmr_fwd(x, w, T))
