@@ -280,8 +280,10 @@ PCPP_API int pcpp_act_unpack(const int8_t *q, const uint8_t *codes, int64_t n, i
  * pcpp_mvmr_bwd_weight with the layer's input kept in 8 bits (pcpp_act_pack):
  *   dw[k] = sum_{(o,i,k) in T} dy[o, :] (outer) values(xq, xcodes)[i, :],   dw [K, c_out, c_in] always fp32.
  *   dy [n_out, c_out] dy_dtype.  The 8-bit values enter the products as they are, dy as in pcpp_mvmr_bwd_weight.
- * tri_* / seg_offsets as there.  plan may be NULL (with plan_bytes = 0 and plan_flags = 0) unless xq, dy or the
- * triplet list takes 4 GiB or more.  A code of 255 is a non-finite feature (see the conventions above).
+ * tri_* / seg_offsets as there.  plan may be NULL (with plan_bytes = 0 and plan_flags = 0) unless x in dy's type
+ * (n_in * c_in elements: xq from 1 GiB with PCPP_F32, 2 GiB with PCPP_BF16), dy or tri_i takes more than 4 GiB less 4 KiB;
+ * 256 -> 256 channels in PCPP_BF16 never need one.  Such x, those 256 -> 256 channels, and rows of one channel whose codes are
+ * as large go by way of a copy of x in dy's type, which is part of the workspace.  A code of 255 is a non-finite feature (see the conventions above).
  * workspace: pcpp_mvmr_packed_workspace_bytes(...) bytes, 256-byte aligned.
  * Errors: as pcpp_mvmr_bwd_weight.
  * ------------------------------------------------------------------------------------------- */

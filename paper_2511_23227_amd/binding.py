@@ -464,7 +464,8 @@ def pcpp_act_unpack(p: Packed, dtype: torch.dtype = torch.bfloat16, out: torch.T
 
 def pcpp_mvmr_bwd_weight_packed(x: Packed, dy: torch.Tensor, T: Triplets, dw: torch.Tensor | None = None,
                                 workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """pcpp_mvmr_bwd_weight from an input that was kept in 8 bits: dW[k] = sum dy[o] (outer) x[i].  T.plan may be None."""
+    """pcpp_mvmr_bwd_weight from an input that was kept in 8 bits: dW[k] = sum dy[o] (outer) x[i].  T.plan may be None unless x in dy's
+    type, dy or the triplets' indices take 4 GiB."""
     return _outputs(_compiled().weight_packed(x.q, x.codes, dy, T.tri_o, T.tri_i, T.tri_k, T.seg_offsets, T.plan, T.plan_flags,
                                               T.n_triplets, T.n_in, T.n_out, T.K, dw, workspace, *_where()))[0]
 

@@ -172,7 +172,8 @@ bool workspace_expected(int in_dtype, int c_in, int c_out, int K)
     return (c_in == 64 && (c_out == 64 || c_out == 128)) || (c_in == 128 && c_out == 64) || (c_in == 256 && c_out == 256);
 }
 
-// The weight gradient from x in 8 bits goes by way of a copy of x where no kernel takes it as it is (256 -> 256 bf16, tensors of 4 GiB and more).
+// The weight gradient from x in 8 bits goes by way of a copy of x in dy's type where no kernel takes it as it is: 256 -> 256 bf16, and where that
+// copy, dy, the list or the codes are beyond 32-bit offsets.
 bool packed_needs_copy(int64_t n_in, int64_t n_out, int64_t n_triplets, int c_in, int c_out, int dy_dtype)
 {
     return n_triplets > 0 && !mvmr_weight_packed_usable(n_in, n_out, n_triplets, c_in, c_out, dy_dtype);
