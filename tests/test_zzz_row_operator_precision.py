@@ -74,3 +74,82 @@ def test_packed_weight_gradient_in_fp32_keeps_24_bits(pcpp, c_in, c_out):
     assert float((short - ref).norm() / ref.norm()) > 1e-6
     got = pcpp.pcpp_mvmr_bwd_weight_packed(p, dy.cuda(), T).double().cpu()
     assert float((got - ref).norm() / ref.norm()) <= 1e-6
+
+
+# ---- log probabilities: every class of a row counts ---------------------------------------------------------------------------------
+
+def head_reference(x, labels):
+    """log S, T / S and what the bounds need, in binary64."""
+    x = x.double().cpu()
+    m = x.amax(1, keepdim=True)
+    d = x - m
+    z = torch.exp(d)
+    s = z.sum(1, keepdim=True)
+    p, log_s = z / s, torch.log(s)
+    at = labels.long().cpu()[:, None]
+    lp = d - log_s
+    return m[:, 0], log_s[:, 0], lp, p, lp.gather(1, at)[:, 0], -(p * lp).sum(1), (p * d * d).sum(1)
+
+
+# lengths about a step of a lane's eight classes, of a wave's and a block's, and a split's 4096, with rests of one class to one short
+LENGTHS = [513, 519, 1023, 1025, 1031, 2047, 2056, 4095, 4097, 4103, 8191, 8193, 8200, 9999, 12_295, 16_385, 65_537, 70_001, 131_071, 131_072]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [9, 17, 63, 65, 255, 257, 511] + LENGTHS)
+def test_log_probs_of_equal_classes(pcpp, v, dtype):
+    """v equal logits: S is v exactly (sums of ones under 2^24), so log S is off by the logarithm alone, two roundings of a number under 17 and one of its product
+    with log 2: under 4 u log v.  A class lost or counted twice changes it by 1 / v, which is more."""
+    bound = 4 * U * math.log(v)
+    assert 1 / (v + 1) > 1.3 * bound
+    for n in (1, 3, 300, 1100) if v < 20_000 else (1, 3, 70):
+        x = torch.full((n, v), 1.5, dtype=dtype, device="cuda")
+        labels = torch.arange(n, dtype=torch.int32, device="cuda") % v
+        for n_top in (0, 3):
+            y = pcpp.pcpp_log_probs_fwd(x, labels, n_top)
+            m, log_s = y.max_log_sum.double().unbind(1)
+            assert (m == 1.5).all() and float((log_s - math.log(v)).abs().max()) <= bound, (n, n_top)
+            assert float((y.log_prob.double() + math.log(v)).abs().max()) <= bound
+            assert float((y.entropy.double() - math.log(v)).abs().max()) <= bound
+            if n_top:
+                assert torch.equal(y.top_index, torch.arange(3, dtype=torch.int32, device="cuda").repeat(n, 1))
+        d = pcpp.pcpp_log_probs_bwd(x, labels, y, torch.ones(n, device="cuda")).double()
+        hit = torch.arange(v, device="cuda") == labels[:, None]
+        size = 2.0 ** -8 if dtype == BF16 else 0.0
+        # p is off by its logarithm's error, the exponent's rounding (log v times 2 u) and its own
+        off = (d - (hit.double() - 1 / v)).abs() - (hit.double() + 1 / v) * size
+        assert float((off - (1 / v) * (bound + (2 * math.log(v) + 4) * U) - hit.double() * 2 * U).max()) <= 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", LENGTHS)
+def test_log_probs_to_32_bits(pcpp, v, dtype):
+    """Random rows.  exp(d) is off by (1.5 |d| + 2) u of itself; S by that over all classes, at most 1.5 E|d| + 2 <= 1.5 sqrt(E d^2) + 2, and by
+    a tree of additions, under 8 u as independent roundings; log S by three more.  T / S by the same times |d|: (1.5 E d^2 + 10 E|d|) u.  With
+    E d^2 <= 60 here that is under 2e-6 (1 + |log S|) and 2e-6 (1 + log S + E d^2); a log probability has its two subtractions, of x and m, beside."""
+    for n in (1, 3, 1100 if v < 5000 else 40 if v < 20_000 else 9):
+        g = torch.Generator().manual_seed(v + n)
+        x = (2 * torch.randn(n, v, generator=g) + torch.randn(n, 1, generator=g)).to(dtype)
+        labels = torch.randint(v, (n,), generator=g, dtype=torch.int32)
+        labels[0] = v - 1                              # the last class of a rest
+        m, log_s, lp, p, picked, entropy, spread = head_reference(x, labels)
+        assert float(spread.max()) <= 60
+        y = pcpp.pcpp_log_probs_fwd(x.cuda(), labels.cuda(), 4)
+        gm, glog = y.max_log_sum.double().cpu().unbind(1)
+        assert torch.equal(gm, m) and ((glog - log_s).abs() <= 2e-6 * (1 + log_s)).all()
+        assert ((y.log_prob.double().cpu() - picked).abs() <= 2e-6 * (1 + picked.abs() + log_s)).all()
+        top, index = torch.sort(-x.double(), dim=1, stable=True)
+        assert torch.equal(y.top_index.cpu().long(), index[:, :4])
+        assert ((y.top_log_prob.double().cpu() - lp.gather(1, index[:, :4])).abs() <= 2e-6 * (1 + log_s[:, None] + m[:, None].abs())).all()
+        assert ((y.entropy.double().cpu() - entropy).abs() <= 2e-6 * (1 + log_s + spread)).all()
+        dl, dh = torch.randn(n, generator=g), torch.randn(n, generator=g)
+        got = pcpp.pcpp_log_probs_bwd(x.cuda(), labels.cuda(), y, dl.cuda(), dh.cuda()).double().cpu()
+        hit = torch.nn.functional.one_hot(labels.long(), v).double()
+        dl, dh = dl.double()[:, None], dh.double()[:, None]
+        ref = dl * (hit - p) - dh * p * (lp + entropy[:, None])
+        parts = dl.abs() * (hit + p) + dh.abs() * p * (lp.abs() + entropy[:, None] + 1)
+        # p is off by what its logarithm is: the row's log S, and the roundings of a number of its size
+        tol = parts * (2e-6 * (1 + log_s + spread)[:, None] + 4 * U * lp.abs())
+        if dtype == BF16:
+            tol = tol + 2.0 ** -8 * (ref.abs() + tol)
+        assert ((got - ref).abs() <= tol + 1e-40).all()
