@@ -153,3 +153,42 @@ def test_log_probs_to_32_bits(pcpp, v, dtype):
         if dtype == BF16:
             tol = tol + 2.0 ** -8 * (ref.abs() + tol)
         assert ((got - ref).abs() <= tol + 1e-40).all()
+
+
+# ---- gradients of the norms' weights: every row of a large cloud counts ----------------------------------------------------------------
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("n,c,stream,dtype,kind,gate", [
+    (70_001, 64, F32, BF16, 1, "full"), (70_001, 64, F32, F32, 2, "row"), (9001, 520, F32, F32, 1, "full"), (9001, 520, BF16, BF16, 2, "none"),
+    (200_003, 32, F32, F32, 1, "row"), (70_003, 91, F32, BF16, 2, "full"), (140_001, 7, F32, F32, 1, "full"),
+])
+def test_weights_gradients_over_many_rounds(pcpp, n, c, stream, dtype, kind, gate, packed):
+    """More rows than the largest launch holds at a time, so that every block goes round and all its sums join.  A column's sum goes through the rounds of
+    a lane (under 8), log2 of the lanes (4), the waves (4) and the blocks' sums (1024 / 64 + 2 + 16), 50 additions at most, and a term, formed from
+    statistics of a row in registers (8 to 16 elements and 6 steps over the lanes, each norm twice), is off by under 80 u of its magnitude: 130 u of the
+    magnitudes' sum.  A few rows weigh 64 times the others, the first and the last among them: without one of these some column is off by more."""
+    from test_zzz_row_operators import block_inputs, cuda, norm_bwd_reference, norm_reference, wide
+    eps, scale = 1e-6, 0.75
+    r, f, ga, wp, wn, dr, dh = block_inputs(n, c, stream, dtype, gate, 21)
+    for t in (dr, dh):                                 # rows that are the first and last of their rounds weigh more
+        t[[0, 1, n // 2, n - 2, n - 1]] *= 64
+    dev = cuda(dr, dh, r, f, ga, wp, wn)
+    if packed:
+        dev[3] = pcpp.pcpp_act_pack(dev[3])
+        f = pcpp.pcpp_act_unpack(dev[3], F32)
+    got = pcpp.pcpp_block_norm_bwd(*dev, post_norm=kind, pre_norm=kind, residual_scale=scale, eps=eps, dtype=dtype)
+    r, f, ga, wp, wn, dr, dh = wide(r, f, ga, wp, wn, dr, dh)
+    nr, rstd, mr = norm_reference(r, kind, eps, r.abs())
+    y = wn * dh
+    through, tmag = norm_bwd_reference(y, y.abs(), nr, mr, rstd, kind)
+    d, dmag = dr + through, dr.abs() + tmag
+    sigma, off = (torch.sigmoid(ga), 1 + ga.abs()) if ga is not None else (1.0, 1.0)
+    nf, _, mf = norm_reference(f, kind, eps, f.abs())
+    for what, terms, mags in (("dw_pre", dh * nr, dh.abs() * mr), ("dw_post", d * sigma * nf, dmag * sigma * off * mf)):
+        off_by = (getattr(got, what).double().cpu() - terms.sum(0)).abs()
+        bound = 130 * U * mags.sum(0)
+        assert (off_by <= bound).all(), (what, float((off_by / bound).max()))
+        for row in (0, n - 1):                         # a lost first or last row would be seen
+            assert (terms[row].abs() > 2 * bound).any(), what
+    again = pcpp.pcpp_block_norm_bwd(*dev, post_norm=kind, pre_norm=kind, residual_scale=scale, eps=eps, dtype=dtype)
+    assert torch.equal(got.dw_pre, again.dw_pre) and torch.equal(got.dw_post, again.dw_post)
