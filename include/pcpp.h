@@ -267,8 +267,8 @@ PCPP_API int pcpp_tune_plan_order(const float *in_xyz, int64_t n_in, const float
  *   codes  [n, pcpp_act_code_bytes(c)] uint8: one code for 32 channels of the row, in order; the rest of the row's
  *          whole 32-bit words is zero
  * and stands for the values q * 2^(code - 127).  code is the smallest with which no channel of the 32 rounds past
- * +-127, at least 1; q is the channel over that power of two, rounded to nearest even.  The values are bf16 numbers
- * exactly.  Code 255 (q = 0) marks channels of which one is Inf or NaN: they are read as NaN.
+ * +-127, at least 1 and at most 248; q is the channel over that power of two, rounded to nearest even, and +-127 where it
+ * would pass that (finite magnitudes from 127.5 * 2^121 = 3.39e38 on).  The values are bf16 numbers exactly.  Code 255 (q = 0) marks channels of which one is Inf or NaN: they are read as NaN.
  *   x  [n, c] dtype (PCPP_F32 or PCPP_BF16), row-major, 16-byte aligned, as is q; codes 4-byte aligned.
  * Errors: INVALID_ARG, UNSUPPORTED (c outside 1..1024, n >= 2^31, dtype).
  * ------------------------------------------------------------------------------------------- */

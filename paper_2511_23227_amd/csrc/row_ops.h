@@ -186,12 +186,14 @@ constexpr int ACT_BLOCK = 32;
 constexpr int act_code_bytes(int c) { return (int)ceil_div(c, 4 * ACT_BLOCK) * 4; }     // per row, whole 32-bit words
 
 // Code of a block from the bits of its largest magnitude: the smallest power of two with which nothing rounds past 127 (a magnitude of
-// 127.5 steps or more takes the next), not below 2^-126; 255 where a value is Inf or NaN.
+// 127.5 steps or more takes the next), not below 2^-126 nor above 2^121, whose next would round such a magnitude to 2^128, an Inf; 255 where a
+// value is Inf or NaN.
+constexpr uint32_t ACT_TOP_CODE = 248u;
 __device__ inline uint32_t act_code(uint32_t amax)
 {
     if (amax >= 0x7f800000u) return 255u;
     const int e = (int)((amax + 0x10000u) >> 23) - 6;
-    return (uint32_t)(e < 1 ? 1 : e);
+    return e < 1 ? 1u : (e < (int)ACT_TOP_CODE ? (uint32_t)e : ACT_TOP_CODE);
 }
 __device__ inline float act_step(uint32_t code) { return __uint_as_float(code << 23); }  // 255: Inf, with q = 0 a NaN
 
@@ -215,6 +217,10 @@ template <int MODE> __device__ inline uint32_t act_quantise(const float (&v)[8],
     uint32_t b[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(__builtin_fmaf(v[e], scale, 12582912.0f));
+    if (code == ACT_TOP_CODE) {                                   // (127.5 steps and more, which have no next power of two, stay at 127)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(b[e]), 12582785.0f, 12583039.0f));
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t lo = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u);

@@ -153,3 +153,29 @@ def test_outputs_that_the_caller_gives_are_seen_by_autograd(pcpp):
         inference = torch.empty(n, c, device="cuda")
     assert torch.equal(pcpp.pcpp_act_unpack(p, out=inference), pcpp.pcpp_act_unpack(p, F32))
     assert torch.equal(pcpp.pcpp_mvmr_fwd(x, w, T, out=inference), pcpp.pcpp_mvmr_fwd(x, w, T))
+
+
+@pytest.mark.parametrize("c", [1, 7, 20, 32, 91, 128, 640])
+def test_pack_of_the_largest_numbers(pcpp, c):
+    """Finite magnitudes from 127.5 steps of 2^121 on, the type's largest and lowest among them, stay at 127 steps: the next power of two would round them to
+    2^128.  Others of their block are rounded in the same steps, and Inf is still Inf's code."""
+    step = 2.0 ** 121
+    for dtype in (F32, BF16):
+        top = torch.finfo(dtype)
+        x = torch.zeros(8, c, dtype=torch.float64)
+        x[0], x[1], x[2], x[3] = top.max, top.min, 127.25 * step, -127.5 * step
+        x[4, ::2], x[4, 1::2] = top.max, 3.5 * step
+        x[5], x[6] = 63.75 * step, 100 * step
+        x[6, -1] = top.min
+        x = x.to(dtype).cuda()
+        p = pcpp.pcpp_act_pack(x)
+        blocks = -(-c // 32)
+        assert (p.codes[:7, :blocks] == 248).all() and (p.codes[7, :blocks] == 1).all()
+        steps = (x.double() / step).round().clamp(-127, 127)
+        assert torch.equal(p.q.double(), steps)
+        for out in (F32, BF16):
+            assert torch.equal(pcpp.pcpp_act_unpack(p, out).double(), steps * step)
+        x[0, 0] = float("inf")
+        assert int(pcpp.pcpp_act_pack(x).codes[0, 0]) == 255
+        y = pcpp.pcpp_block_norm_fwd(torch.zeros(1, c, device="cuda"), x[1:2], None, post_norm=0, pack_f=True)
+        assert torch.equal(y.f_packed.q, p.q[1:2]) and torch.equal(y.f_packed.codes, p.codes[1:2])
