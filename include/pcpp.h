@@ -314,7 +314,8 @@ PCPP_API int pcpp_mvmr_bwd_weight_packed(const int8_t *xq, const uint8_t *xcodes
  *   fq, fcodes / hq, hcodes   optional 8-bit copies of f and h (pcpp_act_pack) for the backward pass
  * stream_dtype is dtype, or PCPP_F32 with dtype PCPP_BF16.  All arithmetic is fp32, each output is rounded once (h
  * and its 8-bit copy from the unrounded r).  x, r, h and hq, fq are contiguous and 16-byte aligned; f and gate need
- * only the alignment of an element.  Outputs may not overlap inputs.  A row with an Inf or NaN gives NaN in that row only.
+ * only the alignment of an element.  Outputs may not overlap inputs.  A row with an Inf or NaN gives NaN in that row only; one
+ * whose sum of squares passes fp32's range has n(v) = 0.
  *
  * Gradients.  dr is what flows to r from behind (NULL: nothing), dh what flows to h:
  *   y = w_pre * dh,  d = dr + rstd * (y - [mean(y)] - n(r) * mean(y * n(r)))          ([..]: PCPP_NORM_LAYER)

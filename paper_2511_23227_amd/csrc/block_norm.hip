@@ -8,9 +8,9 @@
 //              z = w_post du,  df = rstd (z - [mean z] - n(f) mean(z n(f)))
 //              dw_pre = sum over rows dh n(r),  dw_post = sum over rows du n(f)
 //
-// Bound by memory: every tensor is read or written once.  Backward, 1 000 000 x 256 bf16 with a gate for every channel 812 us = 5.0 TB/s (a 2 GiB
-// copy reaches 4.9), 99 991 x 91 35.5 us = 4.4; forward, 115 200 x 64 bf16 beside an fp32 stream with 8-bit copies 22.7 us = 5.2, 100 000 x 32 fp32 10.7 us =
-// 4.8, three rows 2.3 us, which is an empty launch's.  A row stays in the registers of 4 .. 64 lanes (row_ops.h), all sums over it
+// Bound by memory: every tensor is read or written once.  Backward, 1 000 000 x 256 bf16 with a gate for every channel 815 us = 5.0 TB/s (a 2 GiB
+// copy reaches 4.9), 99 991 x 91 35.7 us = 4.4; forward, 115 200 x 64 bf16 beside an fp32 stream with 8-bit copies 23.3 us = 5.1, 100 000 x 32 fp32 11.1 us =
+// 4.6, three rows 2.4 us, which is an empty launch's.  A row stays in the registers of 4 .. 64 lanes (row_ops.h), all sums over it
 // are taken there in 32 bits, and what the backward pass needs of the row's statistics it takes from the row again, which costs no
 // memory.  h is formed from r before r is rounded, and the 8-bit copy of h before h is rounded: one rounding each.  The blocks
 // walk the rows with the weights in registers; the weights' gradients are summed there too, then over the lanes and waves of a block,

@@ -8,8 +8,8 @@
 // A masked class has x = -inf (or the type's lowest value): its terms are zero.  A row without any class has log probabilities -inf,
 // entropy 0 and no gradient.  A row that holds a NaN or +inf has NaN everywhere but in its indices.
 //
-// Bound by memory, and in bf16 nearly as much by the exponentials: 4096 x 32 768 bf16 46 us = 5.9 TB/s, the gradient 102 us = 5.3; 115 200 x 17 fp32 with three
-// alternatives 8.2 us, one row of 131 072 bf16 with twenty 8.9 + 4.3.  Rows of up to 512 classes lie in the registers of a few lanes;
+// Bound by memory, and in bf16 nearly as much by the exponentials: 4096 x 32 768 bf16 46 us = 5.8 TB/s, the gradient 102 us = 5.3; 115 200 x 17 fp32 with three
+// alternatives 8.5 us, one row of 131 072 bf16 with twenty 9.1 + 4.3.  Rows of up to 512 classes lie in the registers of a few lanes;
 // longer ones are walked, by a wave or by a block of four, or, where there are few rows, by several blocks whose sums a second kernel
 // joins.
 //
@@ -33,6 +33,9 @@ constexpr int SMALL = 512;                                        // classes of 
 constexpr float LOG2E = 1.44269504f;
 typedef unsigned long long key_t64;
 
+// The rounding of x log2(e) puts the power off by about |x| 2^-24 of itself, 5e-7 at -10, 3e-6 at -60, where a class has no weight in a sum; in a
+// gradient it shows in such classes' own elements.  The product's second term would take two more instructions an element, in passes that these bound
+// nearly as much as memory.  Powers below 2^-126 are zero.
 __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
 // A logarithm of a probability beside the probability, in products of the two: below -104 the probability is zero, and so has the product to
@@ -251,8 +254,11 @@ template <int LPR, typename Op> __device__ inline uint32_t row_best(uint32_t v, 
 }
 
 // ---- rows in registers ---------------------------------------------------------------------------------------------------------
-// One class after the other: the largest of the lanes', of equal ones the lowest index.  (Rows in fewer than 64 lanes; n_top may be larger than their
-// number.)
+// One class after the other: the largest of the lanes', of equal ones the lowest index.  For rows in fewer than 64 lanes, that is up to 256 classes; n_top
+// may be larger than the lanes' number.  So / by the pool with a row in a whole wave, 200 000 rows in bf16, us a call: three alternatives of 32 classes
+// 10 / 107, of 64 17 / 111, 128 30 / 116, 129 67 / 131, 256 66 / 128; five of 256 84 / 131; twenty of 32 44 / 190, 64 55 / 208, 128 106 / 258, 129
+// 234 / 372, but of 200 230 / 171 and of 256 231 / 151, which a line by n_top as well would give to the pool.  On the other side, twenty of 400: 519 /
+// 158.
 template <int LPR, typename Put> __device__ inline void take_in_turn(uint32_t (&value)[8], int at, int n_top, Put put)
 {
     uint32_t mine = 0u, index = 0u;                                // 0: none left
@@ -651,7 +657,7 @@ Split split_of(int64_t n, int64_t v)
 }
 
 // A row by a wave on its own rather than by a block's four: no barrier, and the alternatives' pool is not joined, but a fourth of the waves.
-// By a wave / by four, bf16, us with the host's share: five alternatives, 8000 x 8000 44 / 63, 2000 x 5000 15.5 / 20.4, 2000 x 16 000 32 / 29; twenty, 1100 x
+// By a wave / by four, bf16, us a call, one behind the other: five alternatives, 8000 x 8000 44 / 63, 2000 x 5000 15.5 / 20.4, 2000 x 16 000 32 / 29; twenty, 1100 x
 // 16 000 38 / 24; none, forward and gradient of 30 000 x 3000 107 / 107, of 4096 x 32 768 134 / 130.  (Twenty alternatives of very many long rows,
 // 5000 x 20 000 69 / 82, would gain as well; but then how many rows there are would change a row's last bits from 1024 rows on.)
 bool row_by_wave(int64_t n, int64_t v, bool top) { return n >= 1024 && v <= (top ? 8192 : 4096); }

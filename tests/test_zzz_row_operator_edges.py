@@ -179,3 +179,19 @@ def test_pack_of_the_largest_numbers(pcpp, c):
         assert int(pcpp.pcpp_act_pack(x).codes[0, 0]) == 255
         y = pcpp.pcpp_block_norm_fwd(torch.zeros(1, c, device="cuda"), x[1:2], None, post_norm=0, pack_f=True)
         assert torch.equal(y.f_packed.q, p.q[1:2]) and torch.equal(y.f_packed.codes, p.codes[1:2])
+
+
+@pytest.mark.parametrize("kind", [1, 2])
+def test_block_norm_of_rows_past_the_range_of_squares(pcpp, kind):
+    """Finite rows whose sum of squares is past fp32 come out as zero, not as NaN, and reach no other row; just under the line they are normal."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(5, 64, generator=g, device="cuda")
+    ref = pcpp.pcpp_block_norm_fwd(x, None, pre_norm=kind).h
+    big = x.clone()
+    big[1] *= 2.0 ** 70
+    big[3] *= 2.0 ** 55                                # (eps is nothing beside either)
+    h = pcpp.pcpp_block_norm_fwd(big, None, pre_norm=kind).h
+    assert not h[1].any() and torch.equal(h[[0, 2, 4]], ref[[0, 2, 4]]) and torch.allclose(h[3], ref[3], rtol=0, atol=1e-5)
+    ones = torch.ones_like(x)
+    d = pcpp.pcpp_block_norm_bwd(None, ones, big, pre_norm=kind)
+    assert not d.dx[1].any() and torch.isfinite(d.dx).all() and torch.isfinite(d.dw_pre).all()
