@@ -376,6 +376,116 @@ PCPP_API int pcpp_log_probs_bwd(const void *logits, int dtype, int64_t n, int64_
                                 const float *max_log_sum, const float *entropy, const float *d_log_prob,
                                 const float *d_entropy, void *d_logits, int64_t ld_d, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Random numbers of the calls below.  `random` is a DEVICE array int64 [2], (seed, step), read when the kernel runs: a captured graph
+ * whose caller adds to the step between replays draws other numbers each time.  `site` tells a program's operators apart.  The sixteen
+ * bits of the element in row i, channel j of c come from ten rounds of Philox 4x32 (Salmon et al., "Parallel random
+ * numbers: as easy as 1, 2, 3", 2011) with the seed's low and high words as key and the counter
+ *   (i * ceil(c / 8) + j / 8, site, low word of step, high word of step):
+ * of its four words, channel j has the low (j even) or high (j odd) half of word (j % 8) / 2.  So equal arguments give equal
+ * numbers, whatever the type or pitch, and a backward pass draws the forward pass's.  n * ceil(c / 8) must be below 2^32 - 65536.
+ *
+ * Clouds of the calls below: rows [offsets[b], offsets[b + 1]) are cloud b's, offsets DEVICE int32 [n_clouds + 1], ascending, within 0 .. n;
+ * NULL (with n_clouds = 1): all rows are one cloud's.  1 <= n_clouds <= 65536.  Clouds may be empty; what a call would write
+ * for a row that belongs to none is not written.  (Entries outside 0 .. n count as the nearer end; no order of them makes a call leave its
+ * tensors.)
+ * ------------------------------------------------------------------------------------------- */
+
+/* ---------------------------------------------------------------------------------------------
+ * Dropout of a branch, with the residual behind it:  y = residual + k * x * 65536 / (65536 - t),  t = round(65536 p), where k is 1 if the
+ * sixteen bits of the element are t or more, else 0 (also where x is Inf or NaN).  p = 1 leaves the residual.
+ *   x         [n, c] dtype, row pitch ld_x elements, aligned to an element
+ *   residual  [n, c] stream_dtype, contiguous; NULL: none
+ *   y         [n, c] stream_dtype, contiguous
+ *   scope     what stays or goes as one: PCPP_DROP_ELEMENTS, PCPP_DROP_ROWS (row i draws as element (i, 0) of one channel) or
+ *             PCPP_DROP_CLOUDS (cloud b draws as row b); offsets and n_clouds belong to the last one and are NULL and 1 otherwise
+ * stream_dtype is dtype, or PCPP_F32 with dtype PCPP_BF16.  Gradient: dx = k * dy * 65536 / (65536 - t) with dy [n, c] stream_dtype,
+ * dx [n, c] dtype, both contiguous; dy itself flows on to the residual.  Tensors are aligned to an element; outputs may not overlap inputs.
+ * Errors: INVALID_ARG (also: p outside 0 .. 1, y in place of x or the residual), UNSUPPORTED (c outside 1..65536, n >= 2^31, pitch >= 2^24,
+ * dtype combination, too many random numbers).
+ * ------------------------------------------------------------------------------------------- */
+#define PCPP_DROP_ELEMENTS  0
+#define PCPP_DROP_ROWS      1
+#define PCPP_DROP_CLOUDS    2
+
+PCPP_API int pcpp_dropout_fwd(const void *x, int64_t ld_x, const void *residual, const int64_t *random, uint32_t site, float p,
+                              int scope, const int32_t *offsets, int n_clouds, int64_t n, int c, int dtype, int stream_dtype,
+                              void *y, void *stream);
+PCPP_API int pcpp_dropout_bwd(const void *dy, const int64_t *random, uint32_t site, float p, int scope, const int32_t *offsets,
+                              int n_clouds, int64_t n, int c, int dtype, int stream_dtype, void *dx, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Group norm with an activation and dropout behind it, channels last.  Over the rows of each cloud and the c / groups neighbouring
+ * channels of each group:
+ *   v = (x - mean) * rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps),  z = w * v + b,  y = drop(act(z))
+ *   act: PCPP_ACT_NONE, PCPP_ACT_RELU, PCPP_ACT_SILU (z / (1 + exp(-z))), PCPP_ACT_GELU (z (1 + erf(z / sqrt 2)) / 2)
+ *   x          [n, c] dtype, row pitch ld_x elements, aligned to an element
+ *   w, b       [c] fp32; NULL: ones, zeros
+ *   random, site, p   dropout of the elements as in pcpp_dropout_fwd; p = 0: none (random may be NULL)
+ *   y          [n, c] dtype, contiguous
+ *   mean_rstd  [n_clouds, groups, 2] fp32, for the gradient (NULL: not wanted); (0, 0) for an empty cloud
+ *   workspace  pcpp_group_norm_workspace_bytes(n, c, n_clouds, groups, 0) bytes, 256-byte aligned (may be NULL if that is 0)
+ * An Inf or NaN makes its cloud's group NaN, and no other.
+ *
+ * Gradients, from dy [n, c] dtype, contiguous, and the forward pass's mean_rstd:
+ *   dz = drop(dy) * act'(z),  dx = rstd * (w * dz - m1 - v * m2),  m1, m2 = means of w * dz and of w * dz * v over the cloud and group,
+ *   dw = sum over rows of dz * v,  db = sum over rows of dz               (act'(0) = 0 for PCPP_ACT_RELU)
+ *   dx  [n, c] dtype, contiguous; dw, db  [c] fp32; each NULL if not wanted
+ *   workspace  pcpp_group_norm_workspace_bytes(n, c, n_clouds, groups, 1) bytes
+ * Arithmetic is fp32, each output is rounded once; sums have one order: the same result each time.  Outputs may not overlap inputs.
+ * Errors: INVALID_ARG (also: groups do not divide c, eps not finite or below 2^-126, p outside 0 .. 1), WORKSPACE, UNSUPPORTED (c
+ * outside 1..1024, n >= 2^31, pitch >= 2^24, dtype, too many random numbers).
+ * ------------------------------------------------------------------------------------------- */
+#define PCPP_ACT_NONE  0
+#define PCPP_ACT_RELU  1
+#define PCPP_ACT_SILU  2
+#define PCPP_ACT_GELU  3
+
+PCPP_API size_t pcpp_group_norm_workspace_bytes(int64_t n, int c, int n_clouds, int groups, int backward);
+PCPP_API int pcpp_group_norm_fwd(const void *x, int64_t ld_x, const float *w, const float *b, const int32_t *offsets, int n_clouds,
+                                 int groups, int act, float eps, const int64_t *random, uint32_t site, float p,
+                                 int64_t n, int c, int dtype, void *y, float *mean_rstd,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+PCPP_API int pcpp_group_norm_bwd(const void *dy, const void *x, int64_t ld_x, const float *mean_rstd, const float *w, const float *b,
+                                 const int32_t *offsets, int n_clouds, int groups, int act,
+                                 const int64_t *random, uint32_t site, float p, int64_t n, int c, int dtype,
+                                 void *dx, float *dw, float *db, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rows in microscaled 4-bit floating point (sign, two bits of exponent, one of fraction; 32 elements share a power of two), for
+ * linear layers.  A row of c channels becomes
+ *   q       pcpp_mx_row_bytes(c) = 16 * ceil(c / 32) bytes: two elements a byte, the even channel's in the low half; codes 0 .. 7 are
+ *           0, 0.5, 1, 1.5, 2, 3, 4, 6, with 8 added their negatives; past the last channel 0
+ *   scales  pcpp_mx_scale_bytes(c) = 4 * ceil(c / 128) bytes: one code s for 32 channels, in order, for 2^(s - 127); the rest is zero
+ * s is the smallest with which no channel of the 32 rounds past 6, at least 1 and at most 252; larger numbers than fit then become 6.  Code 255
+ * (q = 0) marks channels of which one is Inf or NaN: they are read as NaN.  To nearest (random NULL): ties go to the even fraction.
+ * At random (random, site; row i and channel j of x): with m the magnitude in steps of where it lies (0.5 below 2, 1 below 4, then 2, times 2^(s - 127)), up
+ * if floor(65536 (m - floor(m))) + its sixteen bits reach 65536; s is then such that nothing passes 6.
+ *   x            [n, c] dtype, row pitch ld_x elements, aligned to an element
+ *   q, scales    the rows; both NULL: not wanted
+ *   qt, scales_t the columns: the same form of x transposed, [c] rows of n elements; both NULL: not wanted
+ * q and qt are 16-byte aligned, scales 4-byte.  pcpp_mx_unpack writes the values, [n, c] dtype, contiguous; they are bf16 numbers exactly.
+ * Errors: INVALID_ARG, UNSUPPORTED (c >= 2^24, n >= 2^31, with columns n >= 2^24, pitch >= 2^31, dtype, too many random numbers).
+ *
+ * Products of such rows, out[i, j] = act(sum_l a[i, l] * b[j, l] + bias[j]) with a [n, k], b [m, k], bias [m] fp32 (NULL: none), out [n, m] out_dtype,
+ * contiguous, aligned to an element.  Products and sums are fp32, rounded once.  A linear layer y = x W^T and its gradients dx = dy W, dW = dy^T x are
+ * this call on rows of x and W; rows of dy and columns of W; columns of dy and of x.
+ * pcpp_mx_linear takes a as x [n, k] x_dtype, row pitch ld_x, and rounds it to 4 bits to nearest on the way.
+ *   workspace  pcpp_mx_product_workspace_bytes / pcpp_mx_linear_workspace_bytes(n, m, k) bytes, 256-byte aligned (may be NULL if that is 0)
+ * Errors: INVALID_ARG (also: m or k < 1), WORKSPACE, UNSUPPORTED (k or m >= 2^24, n >= 2^31, pitch >= 2^31, dtype).
+ * ------------------------------------------------------------------------------------------- */
+PCPP_API size_t pcpp_mx_row_bytes(int64_t c);    /* 0 if c is outside 1 .. 2^24 - 1 */
+PCPP_API size_t pcpp_mx_scale_bytes(int64_t c);
+PCPP_API int pcpp_mx_pack(const void *x, int64_t ld_x, int dtype, int64_t n, int64_t c, const int64_t *random, uint32_t site,
+                          uint8_t *q, uint8_t *scales, uint8_t *qt, uint8_t *scales_t, void *stream);
+PCPP_API int pcpp_mx_unpack(const uint8_t *q, const uint8_t *scales, int64_t n, int64_t c, void *x, int dtype, void *stream);
+PCPP_API size_t pcpp_mx_product_workspace_bytes(int64_t n, int64_t m, int64_t k);
+PCPP_API int pcpp_mx_product(const uint8_t *a, const uint8_t *a_scales, const uint8_t *b, const uint8_t *b_scales, const float *bias, int act,
+                             int64_t n, int64_t m, int64_t k, void *out, int out_dtype, void *workspace, size_t workspace_bytes, void *stream);
+PCPP_API size_t pcpp_mx_linear_workspace_bytes(int64_t n, int64_t m, int64_t k);
+PCPP_API int pcpp_mx_linear(const void *x, int64_t ld_x, int x_dtype, const uint8_t *w, const uint8_t *w_scales, const float *bias, int act,
+                            int64_t n, int64_t m, int64_t k, void *out, int out_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

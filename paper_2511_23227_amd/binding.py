@@ -18,6 +18,8 @@ PLAN_FWD, PLAN_BWD_INPUT, PLAN_SPATIAL = 1, 2, 4
 BUILD_TEST_SHORT_LISTS, BUILD_TEST_WIDE_KEYS, BUILD_VOXEL = 0x100, 0x200, 0x400
 PLAN_MASK = PLAN_FWD | PLAN_BWD_INPUT | PLAN_SPATIAL
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+DROP_ELEMENTS, DROP_ROWS, DROP_CLOUDS = 0, 1, 2
 ERR_CAPACITY = -2
 
 EXPORTS = ("pcpp_last_error", "pcpp_version", "pcpp_build_triplets_workspace_bytes",
@@ -27,7 +29,10 @@ EXPORTS = ("pcpp_last_error", "pcpp_version", "pcpp_build_triplets_workspace_byt
            "pcpp_build_triplets_batched", "pcpp_voxel_subsample_workspace_bytes", "pcpp_voxel_subsample",
            "pcpp_act_code_bytes", "pcpp_act_pack", "pcpp_act_unpack", "pcpp_mvmr_packed_workspace_bytes",
            "pcpp_mvmr_bwd_weight_packed", "pcpp_block_norm_fwd", "pcpp_block_norm_workspace_bytes", "pcpp_block_norm_bwd",
-           "pcpp_log_probs_workspace_bytes", "pcpp_log_probs_fwd", "pcpp_log_probs_bwd")
+           "pcpp_log_probs_workspace_bytes", "pcpp_log_probs_fwd", "pcpp_log_probs_bwd",
+           "pcpp_dropout_fwd", "pcpp_dropout_bwd", "pcpp_group_norm_workspace_bytes", "pcpp_group_norm_fwd", "pcpp_group_norm_bwd",
+           "pcpp_mx_row_bytes", "pcpp_mx_scale_bytes", "pcpp_mx_pack", "pcpp_mx_unpack", "pcpp_mx_product_workspace_bytes",
+           "pcpp_mx_product", "pcpp_mx_linear_workspace_bytes", "pcpp_mx_linear")
 
 
 class PcppError(RuntimeError):
@@ -110,6 +115,34 @@ def library() -> ctypes.CDLL:
     L.pcpp_log_probs_fwd.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     L.pcpp_log_probs_bwd.restype = i32
     L.pcpp_log_probs_bwd.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    u32 = ctypes.c_uint32
+    drop = [vp, u32, f32]                                                  # random state, site, p
+    L.pcpp_dropout_fwd.restype = i32
+    L.pcpp_dropout_fwd.argtypes = [vp, i64, vp] + drop + [i32, vp, i32, i64, i32, i32, i32, vp, vp]
+    L.pcpp_dropout_bwd.restype = i32
+    L.pcpp_dropout_bwd.argtypes = [vp] + drop + [i32, vp, i32, i64, i32, i32, i32, vp, vp]
+    L.pcpp_group_norm_workspace_bytes.restype = sz
+    L.pcpp_group_norm_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    L.pcpp_group_norm_fwd.restype = i32
+    L.pcpp_group_norm_fwd.argtypes = [vp, i64, vp, vp, vp, i32, i32, i32, f32] + drop + [i64, i32, i32, vp, vp, vp, sz, vp]
+    L.pcpp_group_norm_bwd.restype = i32
+    L.pcpp_group_norm_bwd.argtypes = [vp, vp, i64, vp, vp, vp, vp, i32, i32, i32] + drop + [i64, i32, i32, vp, vp, vp, vp, sz, vp]
+    L.pcpp_mx_row_bytes.restype = sz
+    L.pcpp_mx_row_bytes.argtypes = [i64]
+    L.pcpp_mx_scale_bytes.restype = sz
+    L.pcpp_mx_scale_bytes.argtypes = [i64]
+    L.pcpp_mx_pack.restype = i32
+    L.pcpp_mx_pack.argtypes = [vp, i64, i32, i64, i64, vp, u32, vp, vp, vp, vp, vp]
+    L.pcpp_mx_unpack.restype = i32
+    L.pcpp_mx_unpack.argtypes = [vp, vp, i64, i64, vp, i32, vp]
+    L.pcpp_mx_product_workspace_bytes.restype = sz
+    L.pcpp_mx_product_workspace_bytes.argtypes = [i64, i64, i64]
+    L.pcpp_mx_product.restype = i32
+    L.pcpp_mx_product.argtypes = [vp, vp, vp, vp, vp, i32, i64, i64, i64, vp, i32, vp, sz, vp]
+    L.pcpp_mx_linear_workspace_bytes.restype = sz
+    L.pcpp_mx_linear_workspace_bytes.argtypes = [i64, i64, i64]
+    L.pcpp_mx_linear.restype = i32
+    L.pcpp_mx_linear.argtypes = [vp, i64, i32, vp, vp, vp, i32, i64, i64, i64, vp, i32, vp, sz, vp]
     _lib = L
     return L
 
@@ -561,3 +594,105 @@ def pcpp_log_probs_bwd(logits: torch.Tensor, labels: torch.Tensor | None, forwar
     tensor; it may be the logits."""
     return _outputs(_compiled().log_probs_bwd(logits, labels, forward.max_log_sum, forward.entropy, d_log_prob, d_entropy, out,
                                               *_where()))[0]
+
+
+# ---- the pointwise layers ----------------------------------------------------------------------------------------
+
+@dataclass
+class Random:
+    """Where an operator's random numbers come from: a program's state, int64 [2] on the GPU (seed, step), read when the kernel runs, and
+    the operator's own number among those that draw from it.  The same state, site and shape draw the same numbers."""
+    state: torch.Tensor
+    site: int = 0
+
+
+def _draws(random: Random | None):
+    return (None, 0) if random is None else (random.state, random.site)
+
+
+def pcpp_dropout_fwd(x: torch.Tensor, p: float, random: Random, residual: torch.Tensor | None = None, *, scope: int = DROP_ELEMENTS,
+                     offsets: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """residual + dropout(x): elements (DROP_ELEMENTS), whole rows (DROP_ROWS) or whole clouds (DROP_CLOUDS, with the batch's
+    offsets, int32 [clouds + 1]) go with probability p, in steps of 2^-16, and what stays is scaled up.  x [n, c] may be a
+    slice of wider rows; the residual (x's type or float32) and out are contiguous.  No mask is kept: the backward pass draws it again."""
+    return _outputs(_compiled().dropout_fwd(x, residual, *_draws(random), p, scope, offsets, out, *_where()))[0]
+
+
+def pcpp_dropout_bwd(dy: torch.Tensor, p: float, random: Random, *, scope: int = DROP_ELEMENTS, offsets: torch.Tensor | None = None,
+                     dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of x (of type `dtype`, default dy's); the residual's is dy itself."""
+    return _outputs(_compiled().dropout_bwd(dy, *_draws(random), p, scope, offsets, _code_or(dtype), out, *_where()))[0]
+
+
+@dataclass
+class GroupNorm:
+    """Result of pcpp_group_norm_fwd; mean_rstd float32 [clouds, groups, 2] is what the backward pass needs of it."""
+    y: torch.Tensor
+    mean_rstd: torch.Tensor | None
+
+
+@dataclass
+class GroupNormGrads:
+    """Result of pcpp_group_norm_bwd; what is not wanted is None."""
+    dx: torch.Tensor | None
+    dw: torch.Tensor | None
+    db: torch.Tensor | None
+
+
+def pcpp_group_norm_fwd(x: torch.Tensor, groups: int, w: torch.Tensor | None = None, b: torch.Tensor | None = None,
+                        offsets: torch.Tensor | None = None, *, act: int = ACT_NONE, eps: float = 1e-5, p: float = 0.0,
+                        random: Random | None = None, statistics: bool = True, out: torch.Tensor | None = None,
+                        workspace: torch.Tensor | None = None) -> GroupNorm:
+    """y = dropout(act(w v + b)), v: x [n, c] normalised over the rows of each cloud (offsets int32 [clouds + 1]; None: one cloud) and
+    the neighbouring channels of each group.  x may be a slice of wider rows.  statistics = False: an answer only.  Rows that belong to
+    no cloud are not written."""
+    return GroupNorm(*_outputs(_compiled().group_norm_fwd(x, groups, w, b, offsets, act, eps, *_draws(random), p, statistics, out,
+                                                          workspace, *_where())))
+
+
+def pcpp_group_norm_bwd(dy: torch.Tensor, x: torch.Tensor, mean_rstd: torch.Tensor, w: torch.Tensor | None = None,
+                        b: torch.Tensor | None = None, offsets: torch.Tensor | None = None, *, act: int = ACT_NONE, p: float = 0.0,
+                        random: Random | None = None, of_x: bool = True, of_weights: bool = True,
+                        workspace: torch.Tensor | None = None) -> GroupNormGrads:
+    """Gradients of pcpp_group_norm_fwd from what flows to y; the arguments are the forward pass's, mean_rstd what it returned."""
+    return GroupNormGrads(*_outputs(_compiled().group_norm_bwd(dy, x, mean_rstd, w, b, offsets, act, *_draws(random), p, of_x, of_weights,
+                                                               workspace, *_where())))
+
+
+@dataclass
+class MxRows:
+    """Rows in microscaled 4-bit floating point: two elements a byte, a power of two for 32 channels."""
+    q: torch.Tensor          # uint8 [n, pcpp_mx_row_bytes(c)]
+    scales: torch.Tensor     # uint8 [n, pcpp_mx_scale_bytes(c)]
+    c: int
+
+
+@dataclass
+class Mx:
+    """Result of pcpp_mx_pack: the rows of x [n, c], and its columns as c rows of n elements; what is not wanted is None."""
+    rows: MxRows | None
+    columns: MxRows | None
+
+
+def pcpp_mx_pack(x: torch.Tensor, *, rows: bool = True, columns: bool = False, random: Random | None = None) -> Mx:
+    """x [n, c] in 4 bits, to nearest, or at random (unbiased) with `random`.  A product sums over what shares a power of two: rows
+    for y = x W^T and dx = dy W, columns for dW = dy^T x.  Both at once read x once."""
+    q, s, qt, st = _outputs(_compiled().mx_pack(x, rows, columns, *_draws(random), *_where()))
+    return Mx(MxRows(q, s, x.shape[1]) if rows else None, MxRows(qt, st, x.shape[0]) if columns else None)
+
+
+def pcpp_mx_unpack(m: MxRows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values of rows in 4 bits; bfloat16 holds them exactly."""
+    return _outputs(_compiled().mx_unpack(m.q, m.scales, m.c, _code_or(dtype), out, *_where()))[0]
+
+
+def pcpp_mx_product(a: MxRows, b: MxRows, bias: torch.Tensor | None = None, *, act: int = ACT_NONE, dtype: torch.dtype = torch.bfloat16,
+                    out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """act(a b^T + bias): every row of a with every row of b, summed in fp32, bias float32 [rows of b]."""
+    return _outputs(_compiled().mx_product(a.q, a.scales, a.c, b.q, b.scales, b.c, bias, act, _code_or(dtype), out, workspace, *_where()))[0]
+
+
+def pcpp_mx_linear(x: torch.Tensor, w: MxRows, bias: torch.Tensor | None = None, *, act: int = ACT_NONE, dtype: torch.dtype | None = None,
+                   out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """act(x w^T + bias) with x [n, k] rounded to 4 bits on the way, as pcpp_mx_pack does to nearest.  dtype: the result's, default x's."""
+    return _outputs(_compiled().mx_linear(x, w.q, w.scales, w.c, bias, act, _code_or(dtype), out, workspace, *_where()))[0]

@@ -36,6 +36,11 @@ SOURCES = {
     "block_norm.hip": [],
     "log_probs.hip": [],
     "rows_api.hip": [],
+    "dropout.hip": [],
+    "group_norm.hip": [],
+    "mx_pack.hip": [],
+    "mx_product.hip": [],
+    "pointwise_api.hip": [],
 }
 
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", "-Wno-unused-function",

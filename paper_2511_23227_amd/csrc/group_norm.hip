@@ -1,0 +1,669 @@
+// Group norm with an activation and dropout behind it, channels last, over the clouds of a batch; and its gradients.
+//
+//   over the rows of a cloud and the channels of a group:  v = (x - mean) rstd,  rstd = 1 / sqrt(mean (x - mean)^2 + eps)
+//   forward    z = w v + b,  y = drop(act(z))
+//   backward   dz = drop(dy) act'(z),  dw = sum dz v,  db = sum dz,  dx = rstd (w dz - m1 - v m2),
+//              m1, m2 = means over the cloud's rows and the group's channels of w dz and of w dz v
+//
+// Rows are cut into chunks, whatever clouds they belong to; a block takes a chunk and in it one cloud after the other.  What it finds for
+// (chunk i, cloud b) goes to slot i + b: along the rows either the chunk or the cloud goes on, so no two have the same slot.  So the host needs to know
+// nothing of the clouds but their number, and every sum has one order.
+//
+// Statistics: a lane sums x - k and (x - k)^2, k the range's first row, which cannot lose what the variance is made of unless that row lies
+// thousands of deviations off; channels, chunks and clouds are joined by their means and sums of squares about them.
+#include "pointwise.h"
+
+namespace pcpp {
+
+namespace {
+
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int64_t SMALL = 16384;                                  // elements that one block goes through alone
+
+// A lane's channels and weights
+template <int LPR, int G, int MODE> struct Lane {
+    int c0[G];
+    Span<MODE> own[G];
+    uint32_t row;                                                 // of the wave's rows
+    __device__ inline explicit Lane(int c)
+    {
+        const int lane = threadIdx.x & 63;
+        row = (uint32_t)(lane / LPR);
+#pragma unroll
+        for (int g = 0; g < G; ++g) c0[g] = 8 * (lane % LPR) + 8 * LPR * g, own[g] = Span<MODE>(c0[g], c);
+    }
+};
+__device__ inline int wave_of() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+template <int G, int MODE>
+__device__ inline void load_affine(const float *w, float without, const Span<MODE> (&own)[G], int c, float (&v)[G][8])
+{
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(w, w ? 4u * (uint32_t)c : 0u);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        Eight<float> r;
+        row_load<float>(rs, own[g].template offset<4>(0u), own[g], r);
+        to_floats(r, v[g]);
+        if (!w) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[g][e] = without;
+        }
+    }
+}
+
+// Which of the lane's elements stay; `at` is the lane's row in the tensor.  All lanes of a row call it.
+template <int LPR, int G, int MODE>
+__device__ inline void keep_bits(const Philox &philox, uint32_t at, int c, uint32_t threshold, const Lane<LPR, G, MODE> &lane, uint32_t (&bits)[G])
+{
+    const uint32_t first = at * (uint32_t)((c + 7) / 8);
+#pragma unroll
+    for (int g = 0; g < G; ++g) bits[g] = kept(philox, first + (uint32_t)lane.c0[g] / 8u, threshold);
+    if constexpr (MODE == RAGGED) {
+        // (some of the last eight channels are the lane before's)
+        uint32_t before[G];
+        const int l = threadIdx.x & 63;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            before[g] = __shfl_up(bits[g], 1);
+            if (g > 0) {
+                const uint32_t last = __shfl(bits[g > 0 ? g - 1 : 0], l + LPR - 1);
+                before[g] = l % LPR == 0 ? last : before[g];
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int lo = lane.own[g].lo;
+            if (lo > 0 && lo < 8) bits[g] = before[g] >> (8 - lo) | bits[g] << lo;
+        }
+    }
+}
+
+template <int ACT> struct Act { static constexpr int value = ACT; };
+// f(activation): a branch that all lanes take alike
+template <typename F> __device__ inline void as_act(int act, F f)
+{
+    if (act == PCPP_ACT_SILU) f(Act<PCPP_ACT_SILU>{});
+    else if (act == PCPP_ACT_GELU) f(Act<PCPP_ACT_GELU>{});
+    else if (act == PCPP_ACT_RELU) f(Act<PCPP_ACT_RELU>{});
+    else f(Act<PCPP_ACT_NONE>{});
+}
+
+// Two sums for every channel over the rows of a wave's lanes, then over the waves: [2][CP] in `total`.  (CP: channels in whole lanes)
+template <int LPR, int G, int MODE, int CP>
+__device__ inline void channel_sums(const float (&p)[G][8], const float (&q)[G][8], const Lane<LPR, G, MODE> &lane, int c, float (*sums)[2][CP], float (*total)[CP])
+{
+    const int l = threadIdx.x & 63, wave = wave_of();
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a = p[g][e], b = q[g][e];
+#pragma unroll
+            for (int m = LPR; m < 64; m <<= 1) {
+                a += __shfl_xor(a, m);
+                b += __shfl_xor(b, m);
+            }
+            if (l < LPR && lane.own[g].own(e)) {
+                sums[wave][0][lane.own[g].at + e] = a;
+                sums[wave][1][lane.own[g].at + e] = b;
+            }
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * c; i += THREADS) {
+        const int which = i >= c, ch = which ? i - c : i;
+        float v = sums[0][which][ch];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += sums[w][which][ch];
+        total[which][ch] = v;
+    }
+    __syncthreads();
+}
+
+// For every group f(first channel, lane among `per`, per, sum over those lanes) by neighbouring lanes of a wave
+template <typename F> __device__ inline void for_groups(int groups, F f)
+{
+    int per = 64;
+    while (per > 1 && per * groups > THREADS) per >>= 1;
+    const int lane = (int)threadIdx.x % per;
+    auto sum = [&](float v) {
+        for (int m = 1; m < per; m <<= 1) v += __shfl_xor(v, m);
+        return v;
+    };
+    for (int g0 = 0; g0 < groups; g0 += THREADS / per) {
+        const int g = g0 + (int)threadIdx.x / per;                // (past the last: as the last, without an effect)
+        f(g < groups ? g : groups - 1, lane, per, sum, g < groups);
+    }
+}
+
+// Mean and sum of squares about it of every group over rows [lo, hi), not empty: f(group, mean, squares), by one thread each.
+template <typename T, int LPR, int G, int MODE, int CP, typename F>
+__device__ inline void range_statistics(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, float (*sums)[2][CP], float (*total)[CP],
+                                        float *shift, F f)
+{
+    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
+    const int c = a.c;
+    float k[G][8], s[G][8], q[G][8];
+    const __amdgpu_buffer_rsrc_t ks = rows_from<ES>(a.x, lo, hi, a.ld_x, c, 1);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        Eight<T> raw;
+        row_load<T>(ks, lane.own[g].template offset<ES>(0u), lane.own[g], raw);
+        to_floats(raw, k[g]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[g][e] = q[g][e] = 0.f;
+            if ((int)threadIdx.x < LPR && lane.own[g].own(e)) shift[lane.own[g].at + e] = k[g][e];
+        }
+    }
+    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += WAVES * ROWS) {
+        const __amdgpu_buffer_rsrc_t xs = rows_from<ES>(a.x, first, hi, a.ld_x, c, ROWS);
+        const bool live = first + lane.row < hi;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            Eight<T> raw;
+            float v[8];
+            row_load<T>(xs, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.ld_x), lane.own[g], raw);
+            to_floats(raw, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = live ? v[e] - k[g][e] : 0.f;
+                s[g][e] += d;
+                q[g][e] = __builtin_fmaf(d, d, q[g][e]);
+            }
+        }
+    }
+    channel_sums<LPR, G, MODE, CP>(s, q, lane, c, sums, total);
+    const float rows = (float)(hi - lo), inv = 1.f / rows;
+    for (int ch = threadIdx.x; ch < c; ch += THREADS) {
+        const float sum = total[0][ch], off = sum * inv, m2 = total[1][ch] - sum * off;
+        total[0][ch] = shift[ch] + off;
+        total[1][ch] = m2 < 0.f ? 0.f : m2;                       // (a NaN stays)
+    }
+    __syncthreads();
+    const int width = c / a.groups;
+    for_groups(a.groups, [&](int group, int l, int per, auto sum, bool write) {
+        float mean = 0.f, m2 = 0.f, about = 0.f;
+        const float pivot = total[0][group * width];
+        for (int i = l; i < width; i += per) {
+            const float d = total[0][group * width + i] - pivot;
+            mean += d;
+            m2 += total[1][group * width + i];
+        }
+        mean = sum(mean) / (float)width;
+        for (int i = l; i < width; i += per) {
+            const float d = total[0][group * width + i] - pivot - mean;
+            about = __builtin_fmaf(d, d, about);
+        }
+        m2 = sum(m2) + rows * sum(about);
+        if (write && l == 0) f(group, pivot + mean, m2);
+    });
+    __syncthreads();                                              // (the sums are free again)
+}
+
+// The lane's channels' mean and rstd; stats: [groups][2] of the cloud
+template <int LPR, int G, int MODE>
+__device__ inline void lane_statistics(const float *stats, const Divisor &width, const Lane<LPR, G, MODE> &lane, float (&mean)[G][8], float (&rstd)[G][8])
+{
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool there = lane.own[g].any() && (MODE != NARROW || e < lane.own[g].n);
+            const uint32_t group = there ? width.quotient((uint32_t)(lane.own[g].at + e)) : 0u;
+            mean[g][e] = stats[2u * group];
+            rstd[g][e] = stats[2u * group + 1u];
+        }
+}
+
+// y of rows [lo, hi)
+template <typename T, int LPR, int G, int MODE>
+__device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8], const float (&b)[G][8],
+                                   const float *stats, const Divisor &width, const Philox &philox)
+{
+    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
+    const int c = a.c;
+    float mean[G][8], rstd[G][8];
+    lane_statistics(stats, width, lane, mean, rstd);
+    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += WAVES * ROWS) {
+        const __amdgpu_buffer_rsrc_t xs = rows_from<ES>(a.x, first, hi, a.ld_x, c, ROWS), ys = rows_from<ES>(a.y, first, hi, c, c, ROWS);
+        Eight<T> raw[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) row_load<T>(xs, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.ld_x), lane.own[g], raw[g]);
+        uint32_t bits[G];
+        if (a.drop.threshold) keep_bits(philox, (uint32_t)first + lane.row, c, a.drop.threshold, lane, bits);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float v[8];
+            to_floats(raw[g], v);
+            as_act(a.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = activate<decltype(act)::value>(__builtin_fmaf(w[g][e], (v[e] - mean[g][e]) * rstd[g][e], b[g][e]));
+            });
+            if (a.drop.threshold) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = bits[g] >> e & 1u ? v[e] * a.drop.scale : 0.f;
+            }
+            row_store<T>(ys, lane.own[g].template offset<ES>(lane.row * (uint32_t)c), lane.own[g], v);
+        }
+    }
+}
+
+// What flows to z, and v, of a wave's rows from `first` on: f(element, dz, v) for all of the lane's, zeros in rows past the last
+template <typename T, int LPR, int G, int MODE, typename F>
+__device__ inline void gradient_rows(const GroupNormArgs &a, int64_t first, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8],
+                                     const float (&b)[G][8], const float (&mean)[G][8], const float (&rstd)[G][8], const Philox &philox, F f)
+{
+    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
+    const int c = a.c;
+    const __amdgpu_buffer_rsrc_t xs = rows_from<ES>(a.x, first, hi, a.ld_x, c, ROWS), ds = rows_from<ES>(a.dy, first, hi, c, c, ROWS);
+    const bool live = first + lane.row < hi;
+    Eight<T> xr[G], dr[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        row_load<T>(xs, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.ld_x), lane.own[g], xr[g]);
+        row_load<T>(ds, lane.own[g].template offset<ES>(lane.row * (uint32_t)c), lane.own[g], dr[g]);
+    }
+    uint32_t bits[G];
+    if (a.drop.threshold) keep_bits(philox, (uint32_t)first + lane.row, c, a.drop.threshold, lane, bits);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        float v[8], d[8];
+        to_floats(xr[g], v);
+        to_floats(dr[g], d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = live ? (v[e] - mean[g][e]) * rstd[g][e] : 0.f;
+        if (a.drop.threshold) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = bits[g] >> e & 1u ? d[e] * a.drop.scale : 0.f;
+        }
+        as_act(a.act, [&](auto act) {
+            if constexpr (decltype(act)::value != PCPP_ACT_NONE) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] *= slope<decltype(act)::value>(__builtin_fmaf(w[g][e], v[e], b[g][e]));
+            }
+        });
+        f(g, d, v);
+    }
+}
+
+// Sums of dz and dz v of every channel over rows [lo, hi), not empty: [2][CP] in `total`
+template <typename T, int LPR, int G, int MODE, int CP>
+__device__ inline void range_gradients(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8], const float (&b)[G][8],
+                                       const float *stats, const Divisor &width, const Philox &philox, float (*sums)[2][CP], float (*total)[CP])
+{
+    float mean[G][8], rstd[G][8], s[G][8], q[G][8];
+    lane_statistics(stats, width, lane, mean, rstd);
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[g][e] = q[g][e] = 0.f;
+    for (int64_t first = lo + (int64_t)wave_of() * (64 / LPR); first < hi; first += WAVES * (64 / LPR))
+        gradient_rows<T>(a, first, hi, lane, w, b, mean, rstd, philox, [&](int g, const float (&d)[8], const float (&v)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s[g][e] += d[e];
+                q[g][e] = __builtin_fmaf(d[e], v[e], q[g][e]);
+            }
+        });
+    channel_sums<LPR, G, MODE, CP>(s, q, lane, a.c, sums, total);
+}
+
+// m1 and m2 of every group of a cloud of `rows` rows from its channels' sums: [groups][2] in `coef`
+template <int CP> __device__ inline void group_means(const GroupNormArgs &a, const float (*total)[CP], double rows, float *coef)
+{
+    const int width = a.c / a.groups;
+    const float inv = (float)(1.0 / (rows * (double)width));
+    for_groups(a.groups, [&](int group, int l, int per, auto sum, bool write) {
+        float m1 = 0.f, m2 = 0.f;
+        for (int i = group * width + l; i < (group + 1) * width; i += per) {
+            const float w = a.w ? a.w[i] : 1.f;
+            m1 = __builtin_fmaf(w, total[0][i], m1);
+            m2 = __builtin_fmaf(w, total[1][i], m2);
+        }
+        m1 = sum(m1);
+        m2 = sum(m2);
+        if (write && l == 0) coef[2 * group] = m1 * inv, coef[2 * group + 1] = m2 * inv;
+    });
+    __syncthreads();
+}
+
+// dx of rows [lo, hi)
+template <typename T, int LPR, int G, int MODE>
+__device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8],
+                                      const float (&b)[G][8], const float *stats, const float *coef, const Divisor &width, const Philox &philox)
+{
+    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
+    float mean[G][8], rstd[G][8], m1[G][8], m2[G][8];
+    lane_statistics(stats, width, lane, mean, rstd);
+    lane_statistics(coef, width, lane, m1, m2);
+    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += WAVES * ROWS) {
+        const __amdgpu_buffer_rsrc_t os = rows_from<ES>(a.dx, first, hi, a.c, a.c, ROWS);
+        gradient_rows<T>(a, first, hi, lane, w, b, mean, rstd, philox, [&](int g, const float (&d)[8], const float (&v)[8]) {
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = rstd[g][e] * (__builtin_fmaf(w[g][e], d[e], -m1[g][e]) - v[e] * m2[g][e]);
+            row_store<T>(os, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.c), lane.own[g], o);
+        });
+    }
+}
+
+// A chunk's rows and the clouds in it
+struct Chunk {
+    int64_t lo, hi;
+    int first, last;
+    __device__ inline Chunk(const Clouds &clouds, int64_t rows, int i)
+    {
+        lo = (int64_t)i * rows;
+        hi = lo + rows < clouds.n ? lo + rows : clouds.n;
+        first = clouds.at(lo);
+        last = hi < clouds.n ? clouds.at(hi) : clouds.count - 1;
+        if (first >= clouds.count) first = clouds.count - 1;      // (rows behind the last cloud: it has none of them)
+        if (last >= clouds.count) last = clouds.count - 1;
+    }
+    __device__ inline bool range(const Clouds &clouds, int b, int64_t &from, int64_t &to) const
+    {
+        const int64_t f = clouds.first(b), e = clouds.end(b);
+        from = f > lo ? f : lo;
+        to = e < hi ? e : hi;
+        return from < to;
+    }
+};
+
+template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THREADS) void chunk_statistics_kernel(const GroupNormArgs a, int64_t rows)
+{
+    constexpr int CP = 8 * LPR * G;
+    __shared__ float sums[WAVES][2][CP], total[2][CP], shift[CP];
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const Chunk chunk(clouds, rows, (int)blockIdx.x);
+    const Lane<LPR, G, MODE> lane(a.c);
+    for (int b = chunk.first; b <= chunk.last; ++b) {
+        float *to = a.part + ((size_t)blockIdx.x + (size_t)b) * 2 * a.groups;
+        int64_t lo, hi;
+        if (!chunk.range(clouds, b, lo, hi)) continue;            // (nothing reads the slot)
+        range_statistics<T, LPR, G, MODE, CP>(a, lo, hi, lane, sums, total, shift, [&](int g, float mean, float m2) { to[2 * g] = mean, to[2 * g + 1] = m2; });
+    }
+}
+
+// The chunks of a cloud joined: a block takes sixteen groups, a thread every 64th chunk of one.
+__global__ __launch_bounds__(1024) void cloud_statistics_kernel(const GroupNormArgs a, int64_t rows)
+{
+    __shared__ float sums[64][16][3];
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const int b = (int)blockIdx.x, gl = threadIdx.x & 15, sl = threadIdx.x >> 4, group = (int)blockIdx.y * 16 + gl;
+    const int64_t lo = clouds.first(b), hi = clouds.end(b);
+    float *to = a.stats + ((size_t)b * a.groups + group) * 2;
+    if (lo >= hi) {
+        if (sl == 0 && group < a.groups) to[0] = to[1] = 0.f;
+        return;
+    }
+    const int i0 = (int)(lo / rows), i1 = (int)((hi - 1) / rows);
+    const float *part = a.part + ((size_t)b * a.groups + group) * 2;
+    const size_t pitch = (size_t)a.groups * 2;
+    float s = 0.f, q = 0.f, m = 0.f, pivot = 0.f;
+    if (group < a.groups) {
+        pivot = part[(size_t)i0 * pitch];
+#pragma unroll 4
+        for (int i = i0 + sl; i <= i1; i += 64) {
+            const int64_t from = (int64_t)i * rows > lo ? (int64_t)i * rows : lo, to_ = (int64_t)(i + 1) * rows < hi ? (int64_t)(i + 1) * rows : hi;
+            const float cnt = (float)(to_ - from), d = part[(size_t)i * pitch] - pivot;
+            s = __builtin_fmaf(cnt, d, s);
+            q = __builtin_fmaf(cnt * d, d, q);
+            m += part[(size_t)i * pitch + 1];
+        }
+    }
+    sums[sl][gl][0] = s;
+    sums[sl][gl][1] = q;
+    sums[sl][gl][2] = m;
+    for (int step = 32; step > 0; step >>= 1) {
+        __syncthreads();
+        if (sl < step) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) sums[sl][gl][k] += sums[sl + step][gl][k];
+        }
+    }
+    if (sl != 0 || group >= a.groups) return;
+    const float n = (float)(hi - lo), width = (float)(a.c / a.groups);
+    s = sums[0][gl][0], q = sums[0][gl][1], m = sums[0][gl][2];
+    const float off = s / n, between = q - s * off, m2 = m + width * (between < 0.f ? 0.f : between);
+    to[0] = pivot + off;
+    to[1] = 1.f / sqrtf(m2 / (n * width) + a.eps);
+}
+
+template <typename T, int LPR, int G, int MODE>
+__global__ __launch_bounds__(THREADS) void apply_kernel(const GroupNormArgs a, int64_t rows, const Divisor width)
+{
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const Chunk chunk(clouds, rows, (int)(gridDim.x - 1 - blockIdx.x));         // (from the end on: what was read last is still in the caches)
+    const Lane<LPR, G, MODE> lane(a.c);
+    const Philox philox(a.drop.random);
+    float w[G][8], b[G][8];
+    load_affine(a.w, 1.f, lane.own, a.c, w);
+    load_affine(a.b, 0.f, lane.own, a.c, b);
+    for (int i = chunk.first; i <= chunk.last; ++i) {
+        int64_t lo, hi;
+        if (chunk.range(clouds, i, lo, hi)) apply_range<T>(a, lo, hi, lane, w, b, a.stats + (size_t)i * a.groups * 2, width, philox);
+    }
+}
+
+// Few rows: a block takes a cloud from its statistics to y.
+template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THREADS) void small_forward_kernel(const GroupNormArgs a, const Divisor width)
+{
+    constexpr int CP = 8 * LPR * G;
+    __shared__ float sums[WAVES][2][CP], total[2][CP], shift[CP], stats[2 * CP];
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const Lane<LPR, G, MODE> lane(a.c);
+    const Philox philox(a.drop.random);
+    const int64_t lo = clouds.first((int)blockIdx.x), hi = clouds.end((int)blockIdx.x);
+    float *to = a.stats ? a.stats + (size_t)blockIdx.x * a.groups * 2 : nullptr;
+    if (lo >= hi) {
+        if (to)
+            for (int i = threadIdx.x; i < 2 * a.groups; i += THREADS) to[i] = 0.f;
+        return;
+    }
+    const float count = (float)(hi - lo) * (float)(a.c / a.groups);
+    range_statistics<T, LPR, G, MODE, CP>(a, lo, hi, lane, sums, total, shift, [&](int g, float mean, float m2) {
+        const float rstd = 1.f / sqrtf(m2 / count + a.eps);
+        stats[2 * g] = mean, stats[2 * g + 1] = rstd;
+        if (to) to[2 * g] = mean, to[2 * g + 1] = rstd;
+    });
+    float w[G][8], b[G][8];
+    load_affine(a.w, 1.f, lane.own, a.c, w);
+    load_affine(a.b, 0.f, lane.own, a.c, b);
+    apply_range<T>(a, lo, hi, lane, w, b, stats, width, philox);
+}
+
+template <typename T, int LPR, int G, int MODE>
+__global__ __launch_bounds__(THREADS) void chunk_gradients_kernel(const GroupNormArgs a, int64_t rows, const Divisor width)
+{
+    constexpr int CP = 8 * LPR * G;
+    __shared__ float sums[WAVES][2][CP], total[2][CP];
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const Chunk chunk(clouds, rows, (int)blockIdx.x);
+    const Lane<LPR, G, MODE> lane(a.c);
+    const Philox philox(a.drop.random);
+    float w[G][8], b[G][8];
+    load_affine(a.w, 1.f, lane.own, a.c, w);
+    load_affine(a.b, 0.f, lane.own, a.c, b);
+    for (int i = chunk.first; i <= chunk.last; ++i) {
+        int64_t lo, hi;
+        if (!chunk.range(clouds, i, lo, hi)) continue;            // (nothing reads the slot)
+        range_gradients<T, LPR, G, MODE, CP>(a, lo, hi, lane, w, b, a.stats + (size_t)i * a.groups * 2, width, philox, sums, total);
+        float *to = a.part + ((size_t)blockIdx.x + (size_t)i) * 2 * a.c;
+        for (int k = threadIdx.x; k < 2 * a.c; k += THREADS) to[k] = total[k >= a.c][k >= a.c ? k - a.c : k];
+        __syncthreads();
+    }
+}
+
+// The chunks of a cloud summed, channel by channel, to a.coef [clouds][2][c]: a block takes sixteen columns, a thread every 64th chunk.
+__global__ __launch_bounds__(1024) void cloud_gradients_kernel(const GroupNormArgs a, int64_t rows)
+{
+    __shared__ float sums[64][16];
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const int b = (int)blockIdx.x, cl = threadIdx.x & 15, sl = threadIdx.x >> 4, column = (int)blockIdx.y * 16 + cl;
+    const int64_t lo = clouds.first(b), hi = clouds.end(b);
+    float v = 0.f;
+    if (lo < hi && column < 2 * a.c) {
+        const int i0 = (int)(lo / rows), i1 = (int)((hi - 1) / rows);
+        const float *part = a.part + (size_t)b * 2 * a.c + column;
+#pragma unroll 8
+        for (int i = i0 + sl; i <= i1; i += 64) v += part[(size_t)i * 2 * a.c];
+    }
+    sums[sl][cl] = v;
+    for (int step = 32; step > 0; step >>= 1) {
+        __syncthreads();
+        if (sl < step) sums[sl][cl] += sums[sl + step][cl];
+    }
+    if (sl == 0 && column < 2 * a.c) a.coef[(size_t)b * 2 * a.c + column] = sums[0][cl];
+}
+
+// dx, and in blocks behind the chunks' the weights' gradients: the clouds' sums joined, sixteen columns a block
+template <typename T, int LPR, int G, int MODE>
+__global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a, int64_t rows, int chunks, const Divisor width)
+{
+    constexpr int CP = 8 * LPR * G;
+    __shared__ float total[2][CP], coef[2 * CP];
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    if ((int)blockIdx.x >= chunks) {
+        const int column = ((int)blockIdx.x - chunks) * 16 + (threadIdx.x & 15), sl = threadIdx.x >> 4;
+        float v = 0.f;
+        if (column < 2 * a.c) {
+#pragma unroll 4
+            for (int b = sl; b < a.n_clouds; b += 16) v += a.coef[(size_t)b * 2 * a.c + column];
+        }
+        __shared__ float parts[16][16];
+        parts[sl][threadIdx.x & 15] = v;
+        __syncthreads();
+        if (sl != 0 || column >= 2 * a.c) return;
+        for (int i = 1; i < 16; ++i) v += parts[i][threadIdx.x & 15];
+        float *to = column < a.c ? a.db : a.dw;                   // (sums of dz, sums of dz v)
+        if (to) to[column < a.c ? column : column - a.c] = v;
+        return;
+    }
+    const Chunk chunk(clouds, rows, chunks - 1 - (int)blockIdx.x);
+    const Lane<LPR, G, MODE> lane(a.c);
+    const Philox philox(a.drop.random);
+    float w[G][8], b[G][8];
+    load_affine(a.w, 1.f, lane.own, a.c, w);
+    load_affine(a.b, 0.f, lane.own, a.c, b);
+    for (int i = chunk.first; i <= chunk.last; ++i) {
+        int64_t lo, hi;
+        if (!chunk.range(clouds, i, lo, hi)) continue;
+        const float *from = a.coef + (size_t)i * 2 * a.c;
+        for (int k = threadIdx.x; k < 2 * a.c; k += THREADS) total[k >= a.c][k >= a.c ? k - a.c : k] = from[k];
+        __syncthreads();
+        group_means<CP>(a, total, (double)(clouds.end(i) - clouds.first(i)), coef);
+        gradient_range<T>(a, lo, hi, lane, w, b, a.stats + (size_t)i * a.groups * 2, coef, width, philox);
+        __syncthreads();
+    }
+}
+
+// Few rows: one block, cloud by cloud
+template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THREADS) void small_backward_kernel(const GroupNormArgs a, const Divisor width)
+{
+    constexpr int CP = 8 * LPR * G;
+    __shared__ float sums[WAVES][2][CP], total[2][CP], coef[2 * CP], all[2][CP];
+    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const Lane<LPR, G, MODE> lane(a.c);
+    const Philox philox(a.drop.random);
+    float w[G][8], b[G][8];
+    load_affine(a.w, 1.f, lane.own, a.c, w);
+    load_affine(a.b, 0.f, lane.own, a.c, b);
+    for (int k = threadIdx.x; k < CP; k += THREADS) all[0][k] = all[1][k] = 0.f;
+    for (int i = 0; i < a.n_clouds; ++i) {
+        const int64_t lo = clouds.first(i), hi = clouds.end(i);
+        if (lo >= hi) continue;
+        const float *stats = a.stats + (size_t)i * a.groups * 2;
+        range_gradients<T, LPR, G, MODE, CP>(a, lo, hi, lane, w, b, stats, width, philox, sums, total);
+        for (int k = threadIdx.x; k < a.c; k += THREADS) all[0][k] += total[0][k], all[1][k] += total[1][k];
+        if (a.dx) {
+            group_means<CP>(a, total, (double)(hi - lo), coef);
+            gradient_range<T>(a, lo, hi, lane, w, b, stats, coef, width, philox);
+        }
+        __syncthreads();
+    }
+    for (int k = threadIdx.x; k < a.c; k += THREADS) {
+        if (a.db) a.db[k] = all[0][k];
+        if (a.dw) a.dw[k] = all[1][k];
+    }
+}
+
+template <typename F> void with_kernel(int dtype, int c, F f)
+{
+    with_rows(c, [&](auto lpr, auto g, auto mode) { dtype == PCPP_F32 ? f(float{}, lpr, g, mode) : f(bf16_t{}, lpr, g, mode); });
+}
+
+bool one_block(int64_t n, int c, int n_clouds) { return n * c <= SMALL && n_clouds <= 64; }
+
+}  // namespace
+
+// part: what the blocks find, for every slot; extra: forward the statistics where the caller does not want them, backward the clouds' sums
+GroupNormSizes group_norm_sizes(int64_t n, int c, int n_clouds, int groups, bool backward)
+{
+    GroupNormSizes s{};
+    const int64_t step = WAVES * 64 / row_lanes(c);               // rows that a block takes at a time
+    int64_t rows = ceil_div(ceil_div(n, 1024), step) * step;
+    if (rows < 2 * step) rows = 2 * step;
+    s.rows = rows;
+    s.chunks = (int)ceil_div(n > 0 ? n : 1, rows);
+    s.slots = (size_t)s.chunks + (size_t)n_clouds - 1;
+    s.part = one_block(n, c, n_clouds) ? 0 : align_up(s.slots * 2 * (size_t)(backward ? c : groups) * sizeof(float));
+    s.extra = backward ? (s.part ? align_up((size_t)n_clouds * 2 * c * sizeof(float)) : 0) : (s.part ? align_up((size_t)n_clouds * groups * 2 * sizeof(float)) : 0);
+    s.bytes = s.part + s.extra;
+    return s;
+}
+
+int group_norm_fwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
+{
+    const Divisor width = make_divisor((uint32_t)(a.c / a.groups));
+    if (one_block(a.n, a.c, a.n_clouds)) {
+        with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
+            small_forward_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value><<<(unsigned)a.n_clouds, THREADS, 0, stream>>>(a, width);
+        });
+        PCPP_HIP_CHECK(hipGetLastError());
+        return PCPP_OK;
+    }
+    const GroupNormSizes s = group_norm_sizes(a.n, a.c, a.n_clouds, a.groups, false);
+    with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
+        chunk_statistics_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
+            <<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows);
+    });
+    PCPP_HIP_CHECK(hipGetLastError());
+    cloud_statistics_kernel<<<dim3((unsigned)a.n_clouds, (unsigned)ceil_div(a.groups, 16)), 1024, 0, stream>>>(a, s.rows);
+    PCPP_HIP_CHECK(hipGetLastError());
+    with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
+        apply_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
+            <<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
+    });
+    PCPP_HIP_CHECK(hipGetLastError());
+    return PCPP_OK;
+}
+
+int group_norm_bwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
+{
+    const Divisor width = make_divisor((uint32_t)(a.c / a.groups));
+    if (one_block(a.n, a.c, a.n_clouds)) {
+        with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
+            small_backward_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value><<<1, THREADS, 0, stream>>>(a, width);
+        });
+        PCPP_HIP_CHECK(hipGetLastError());
+        return PCPP_OK;
+    }
+    const GroupNormSizes s = group_norm_sizes(a.n, a.c, a.n_clouds, a.groups, true);
+    with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
+        chunk_gradients_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
+            <<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
+    });
+    PCPP_HIP_CHECK(hipGetLastError());
+    cloud_gradients_kernel<<<dim3((unsigned)a.n_clouds, (unsigned)ceil_div(2 * a.c, 16)), 1024, 0, stream>>>(a, s.rows);
+    PCPP_HIP_CHECK(hipGetLastError());
+    const int sums = a.dw || a.db ? (int)ceil_div(2 * a.c, 16) : 0, chunks = a.dx ? s.chunks : 0;
+    if (sums + chunks == 0) return PCPP_OK;
+    with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
+        gradient_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
+            <<<(unsigned)(chunks + sums), THREADS, 0, stream>>>(a, s.rows, chunks, width);
+    });
+    PCPP_HIP_CHECK(hipGetLastError());
+    return PCPP_OK;
+}
+
+}  // namespace pcpp

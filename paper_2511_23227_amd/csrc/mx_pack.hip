@@ -1,0 +1,245 @@
+// Rows to microscaled 4-bit floating point and back.
+//
+// Rows: a thread takes eight neighbouring channels, a quad of threads the 32 that share a power of two.  Columns (32 rows of a channel share it; the result is
+// the transposed matrix, for products that sum over the rows): a wave takes 32 rows of 64 channels, a lane four rows of eight channels, so that the maximum goes
+// over eight lanes; a block's 128 rows go through LDS and leave in pieces of 64 bytes of a channel.  Both forms come of one pass where both are wanted.
+// Scaling by a power of two is exact, so the codes are the same in any implementation.
+#include "mx.h"
+
+namespace pcpp {
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int TILE_ROWS = 128, TILE_CHANNELS = 64;
+
+// channels c0 .. of a row of c; zeros past the last
+template <typename T> __device__ inline void load_up_to_eight(const T *row, int64_t c0, int64_t c, float (&v)[8])
+{
+    if (c0 + 8 <= c) {
+        Eight<T> r;
+        load_eight<false>(row + c0, r);
+        to_floats(r, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c0 + e < c ? one_float(row[c0 + e]) : 0.f;
+}
+template <typename T> __device__ inline void store_up_to_eight(T *row, int64_t c0, int64_t c, const float (&v)[8])
+{
+    if (c0 + 8 <= c) return store_eight<false>(row + c0, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c0 + e < c) row[c0 + e] = one_of<T>(v[e]);
+}
+__device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }     // (as integers: a NaN is larger than any number)
+__device__ inline uint32_t largest(const float (&v)[8])
+{
+    uint32_t m = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = m > magnitude(v[e]) ? m : magnitude(v[e]);
+    return m;
+}
+__device__ inline uint32_t quad_largest(uint32_t m)
+{
+    uint32_t o = dpp<DPP_XOR1>(m);
+    m = m > o ? m : o;
+    o = dpp<DPP_XOR2>(m);
+    return m > o ? m : o;
+}
+// Eight numbers of one block as codes
+template <bool RANDOM> __device__ inline uint32_t quantise(const float (&v)[8], uint32_t code, const uint32_t (&u)[4])
+{
+    const float by = mx_inverse(code);
+    uint32_t r = 0u;
+    if constexpr (RANDOM) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r |= mx_random(v[e] * by, half_of(u, e)) << (4 * e);
+    } else {
+        float s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = v[e] * by;
+        r = mx_nearest(s);
+    }
+    return code == MX_NAN_CODE ? 0u : r;
+}
+
+// Rows `first` .. of the tensor; `threads` is a multiple of four, `per_row` of a row
+template <typename T, bool RANDOM>
+__global__ __launch_bounds__(THREADS) void pack_rows_kernel(const MxPackArgs a, int64_t first, uint32_t threads, const Divisor per_row)
+{
+    const uint32_t id = blockIdx.x * (uint32_t)THREADS + threadIdx.x;
+    if (id >= threads) return;                                    // (quads stay whole)
+    const uint32_t r = per_row.quotient(id), j = id - r * per_row.by;
+    const int64_t row = first + r, c0 = 8 * (int64_t)j;
+    float v[8];
+    load_up_to_eight(static_cast<const T *>(a.x) + row * a.ld_x, c0, a.c, v);
+    uint32_t u[4] = {0u, 0u, 0u, 0u};
+    if constexpr (RANDOM) Philox(a.random).draw((uint32_t)row * (uint32_t)ceil_div(a.c, 8) + j, u);
+    const uint32_t code = mx_code(quad_largest(largest(v)), RANDOM);
+    reinterpret_cast<uint32_t *>(a.q + row * mx_row_bytes(a.c))[j] = quantise<RANDOM>(v, code, u);
+    if (j % 4 == 0) {
+        uint8_t *to = a.scales + row * mx_scale_bytes(a.c);
+        to[j / 4] = (uint8_t)code;
+        if (j / 4 + 1 == mx_blocks(a.c))
+            for (int64_t i = j / 4 + 1; i < mx_scale_bytes(a.c); ++i) to[i] = 0;
+    }
+}
+
+template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREADS) void pack_columns_kernel(const MxPackArgs a, const Divisor row_tiles)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t tile[TILE_CHANNELS][80];    // 64 bytes a channel, and a pitch that spreads the banks
+    __shared__ uint32_t words[TILE_CHANNELS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rl = lane / 8, cl = lane % 8;
+    const uint32_t tile_y = row_tiles.quotient(blockIdx.x), tile_x = blockIdx.x - tile_y * row_tiles.by;
+    const int64_t row0 = (int64_t)tile_x * TILE_ROWS + 32 * wave + 4 * rl, c0 = (int64_t)tile_y * TILE_CHANNELS + 8 * cl;
+    float v[4][8];
+    uint32_t u[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + i;
+        load_up_to_eight(static_cast<const T *>(a.x) + (row < a.n ? row : 0) * a.ld_x, c0, row < a.n ? a.c : 0, v[i]);
+    }
+    if constexpr (RANDOM) {
+        const Philox philox(a.random);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) philox.draw((uint32_t)(row0 + i) * (uint32_t)ceil_div(a.c, 8) + (uint32_t)(c0 / 8), u[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[i][k] = 0u;
+    }
+    if constexpr (ROWS) {
+        const int64_t block = c0 / MX_BLOCK;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = row0 + i;
+            const uint32_t code = mx_code(quad_largest(largest(v[i])), RANDOM), bits = quantise<RANDOM>(v[i], code, u[i]);
+            if (row < a.n && block < mx_blocks(a.c)) {
+                reinterpret_cast<uint32_t *>(a.q + row * mx_row_bytes(a.c))[c0 / 8] = bits;
+                if (cl % 4 == 0) {
+                    uint8_t *to = a.scales + row * mx_scale_bytes(a.c);
+                    to[block] = (uint8_t)code;
+                    if (block + 1 == mx_blocks(a.c))
+                        for (int64_t k = block + 1; k < mx_scale_bytes(a.c); ++k) to[k] = 0;
+                }
+            }
+        }
+    }
+    // channel by channel: the largest of the wave's 32 rows, four codes of the lane's rows
+    if (threadIdx.x < TILE_CHANNELS) words[threadIdx.x] = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        uint32_t m = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = m > magnitude(v[i][e]) ? m : magnitude(v[i][e]);
+#pragma unroll
+        for (int k = 8; k < 64; k <<= 1) {
+            const uint32_t o = __shfl_xor(m, k);
+            m = m > o ? m : o;
+        }
+        const uint32_t code = mx_code(m, RANDOM);
+        const float by = mx_inverse(code);
+        uint32_t bits = 0u;
+        if constexpr (RANDOM) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits |= mx_random(v[i][e] * by, half_of(u[i], e)) << (4 * i);
+        } else {
+            bits = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(bits, v[0][e] * by, v[1][e] * by, 1.f, 0);
+            bits = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(bits, v[2][e] * by, v[3][e] * by, 1.f, 1);
+        }
+        if (code == MX_NAN_CODE) bits = 0u;
+        *reinterpret_cast<uint16_t *>(&tile[8 * cl + e][16 * wave + 2 * rl]) = (uint16_t)bits;
+        if (rl == 0 && (int64_t)tile_x * TILE_ROWS + 32 * wave < a.n) reinterpret_cast<uint8_t *>(&words[8 * cl + e])[wave] = (uint8_t)code;
+    }
+    __syncthreads();
+    const int ch = threadIdx.x / 4, part = threadIdx.x % 4;
+    const int64_t channel = (int64_t)tile_y * TILE_CHANNELS + ch, block = 4 * (int64_t)tile_x + part;
+    if (channel >= a.c) return;
+    if (block < mx_blocks(a.n)) *reinterpret_cast<v4u *>(a.qt + channel * mx_row_bytes(a.n) + 16 * block) = *reinterpret_cast<const v4u *>(&tile[ch][16 * part]);
+    if (part == 0) reinterpret_cast<uint32_t *>(a.scales_t + channel * mx_scale_bytes(a.n))[tile_x] = words[ch];
+}
+
+template <typename T>
+__global__ __launch_bounds__(THREADS) void unpack_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ scales, int64_t first, uint32_t threads, int64_t c,
+                                                         T *__restrict__ x, const Divisor per_row)
+{
+    const uint32_t id = blockIdx.x * (uint32_t)THREADS + threadIdx.x;
+    if (id >= threads) return;
+    const uint32_t r = per_row.quotient(id), j = id - r * per_row.by;
+    const int64_t row = first + r;
+    const uint32_t bits = reinterpret_cast<const uint32_t *>(q + row * mx_row_bytes(c))[j], code = scales[row * mx_scale_bytes(c) + j / 4];
+    const float step = __uint_as_float(code << 23), half_step = code ? 0.5f * step : 0x1p-128f;           // (code 0: 2^-127, subnormal)
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t k = bits >> (4 * e) & 7u;
+        const float twice = (float)(k < 4u ? k : (k & 1u ? (k == 5u ? 6u : 12u) : (k == 4u ? 4u : 8u)));
+        v[e] = code == MX_NAN_CODE ? __builtin_nanf("") : twice * half_step;
+        v[e] = bits >> (4 * e) & 8u ? -v[e] : v[e];
+    }
+    store_up_to_eight(x + row * c, 8 * (int64_t)j, c, v);
+}
+
+template <typename F> void with_type(int dtype, F f)
+{
+    if (dtype == PCPP_F32) f(float{});
+    else f(bf16_t{});
+}
+// f(first row, rows) for pieces of whole rows of less than 2^31 threads
+template <typename F> void in_pieces(int64_t n, int64_t per_row, F f)
+{
+    const int64_t most = ((int64_t)1 << 30) / per_row;            // (at least 256)
+    for (int64_t first = 0; first < n; first += most) f(first, n - first < most ? n - first : most);
+}
+
+}  // namespace
+
+int mx_pack(const MxPackArgs &a, int dtype, hipStream_t stream)
+{
+    if (!a.qt) {
+        const int64_t per_row = 4 * mx_blocks(a.c);
+        in_pieces(a.n, per_row, [&](int64_t first, int64_t rows) {
+            const uint32_t threads = (uint32_t)(rows * per_row);
+            with_type(dtype, [&](auto t) {
+                const unsigned blocks = (unsigned)ceil_div(threads, THREADS);
+                if (a.random.state) pack_rows_kernel<decltype(t), true><<<blocks, THREADS, 0, stream>>>(a, first, threads, make_divisor((uint32_t)per_row));
+                else pack_rows_kernel<decltype(t), false><<<blocks, THREADS, 0, stream>>>(a, first, threads, make_divisor((uint32_t)per_row));
+            });
+        });
+        PCPP_HIP_CHECK(hipGetLastError());
+        return PCPP_OK;
+    }
+    const Divisor row_tiles = make_divisor((uint32_t)ceil_div(a.n, TILE_ROWS));
+    const unsigned grid = (unsigned)(row_tiles.by * ceil_div(a.c, TILE_CHANNELS));
+    with_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        if (a.random.state) {
+            if (a.q) pack_columns_kernel<T, true, true><<<grid, THREADS, 0, stream>>>(a, row_tiles);
+            else pack_columns_kernel<T, true, false><<<grid, THREADS, 0, stream>>>(a, row_tiles);
+        } else {
+            if (a.q) pack_columns_kernel<T, false, true><<<grid, THREADS, 0, stream>>>(a, row_tiles);
+            else pack_columns_kernel<T, false, false><<<grid, THREADS, 0, stream>>>(a, row_tiles);
+        }
+    });
+    PCPP_HIP_CHECK(hipGetLastError());
+    return PCPP_OK;
+}
+
+int mx_unpack(const uint8_t *q, const uint8_t *scales, int64_t n, int64_t c, void *x, int dtype, hipStream_t stream)
+{
+    const int64_t per_row = 4 * mx_blocks(c);
+    in_pieces(n, per_row, [&](int64_t first, int64_t rows) {
+        const uint32_t threads = (uint32_t)(rows * per_row);
+        with_type(dtype, [&](auto t) {
+            unpack_kernel<<<(unsigned)ceil_div(threads, THREADS), THREADS, 0, stream>>>(q, scales, first, threads, c, static_cast<decltype(t) *>(x),
+                                                                                        make_divisor((uint32_t)per_row));
+        });
+    });
+    PCPP_HIP_CHECK(hipGetLastError());
+    return PCPP_OK;
+}
+
+}  // namespace pcpp

@@ -42,6 +42,17 @@ struct {
     CALL(log_probs_workspace_bytes);
     CALL(log_probs_fwd);
     CALL(log_probs_bwd);
+    CALL(dropout_fwd);
+    CALL(dropout_bwd);
+    CALL(group_norm_workspace_bytes);
+    CALL(group_norm_fwd);
+    CALL(group_norm_bwd);
+    CALL(mx_pack);
+    CALL(mx_unpack);
+    CALL(mx_product_workspace_bytes);
+    CALL(mx_product);
+    CALL(mx_linear_workspace_bytes);
+    CALL(mx_linear);
 #undef CALL
 } lib;
 
@@ -447,6 +458,269 @@ PyObject *log_probs_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
+// ---- the pointwise layers ---------------------------------------------------------------------------------------------------------
+// a program's random state and the operator's site: (state or None, site)
+struct Draws {
+    const int64_t *state = nullptr;
+    uint32_t site = 0;
+    explicit Draws(Args &args)
+    {
+        const Tensor *t = args.optional();
+        const int64_t at = args.integer();
+        need(at >= 0 && at <= (int64_t)UINT32_MAX, "the site is a 32-bit number");
+        site = (uint32_t)at;
+        if (!t) return;
+        need(t->scalar_type() == at::kLong && t->is_contiguous() && t->numel() == 2, "the random state is int64 [2]: seed, step");
+        state = static_cast<const int64_t *>(t->data_ptr());
+    }
+};
+// a batch's offsets or None
+struct CloudsOf {
+    const int32_t *offsets = nullptr;
+    int count = 1;
+    explicit CloudsOf(const Tensor *t)
+    {
+        if (!t) return;
+        need(t->scalar_type() == at::kInt && t->dim() == 1 && t->is_contiguous() && t->numel() >= 2 && t->numel() <= INT32_MAX, "offsets are int32 [clouds + 1]");
+        offsets = static_cast<const int32_t *>(t->data_ptr());
+        count = (int)t->numel() - 1;
+    }
+};
+
+// (x, residual or None, state, site, p, scope, offsets or None, out or None, device, stream) -> (y,)
+PyObject *dropout_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Tensor &x = args.tensor();
+        const Tensor *residual = args.optional();
+        const Draws draws(args);
+        const float p = args.number();
+        const int scope = args.small();
+        const CloudsOf clouds(args.optional());
+        const Tensor *given = args.optional();
+        void *stream = args.stream();
+        need(x.dim() == 2, "x is [n, c]");
+        const int64_t n = x.size(0);
+        const int c = channels(x), code = code_of(x.scalar_type());
+        if (residual) need_rows(*residual, n, c, "the residual is [n, c], contiguous");
+        if (given) need_rows(*given, n, c, "out is [n, c], contiguous");
+        const at::ScalarType type = residual ? residual->scalar_type() : (given ? given->scalar_type() : x.scalar_type());
+        if (given) need(given->scalar_type() == type, "out is of the residual's type");
+        const Tensor y = given ? *given : empty({n, c}, type, x);
+        const int rc = lib.dropout_fwd(x.data_ptr(), pitch(x), at_of(residual), draws.state, draws.site, p, scope, clouds.offsets, clouds.count, n, c, code,
+                                       code_of(type), y.data_ptr(), stream);
+        written(given);
+        return result(rc, y);
+    });
+}
+
+// (dy, state, site, p, scope, offsets or None, dtype code (-1: dy's), out or None, device, stream) -> (dx,)
+PyObject *dropout_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Tensor &dy = args.tensor();
+        const Draws draws(args);
+        const float p = args.number();
+        const int scope = args.small();
+        const CloudsOf clouds(args.optional());
+        const int64_t wanted = args.integer();
+        const Tensor *given = args.optional();
+        void *stream = args.stream();
+        need(dy.dim() == 2 && dy.is_contiguous(), "dy is [n, c], contiguous");
+        const int64_t n = dy.size(0);
+        const int c = channels(dy);
+        if (given) need_rows(*given, n, c, "out is [n, c], contiguous");
+        const at::ScalarType type = given ? given->scalar_type() : (wanted < 0 ? dy.scalar_type() : type_of(wanted));
+        const Tensor dx = given ? *given : empty({n, c}, type, dy);
+        const int rc = lib.dropout_bwd(dy.data_ptr(), draws.state, draws.site, p, scope, clouds.offsets, clouds.count, n, c, code_of(type),
+                                       code_of(dy.scalar_type()), dx.data_ptr(), stream);
+        written(given);
+        return result(rc, dx);
+    });
+}
+
+// (x, groups, w, b, offsets, act, eps, state, site, p, statistics wanted, out, workspace, device, stream) -> (y, mean_rstd)
+PyObject *group_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Tensor &x = args.tensor();
+        const int groups = args.small();
+        const Tensor *w = args.optional(), *b = args.optional();
+        const CloudsOf clouds(args.optional());
+        const int act = args.small();
+        const float eps = args.number();
+        const Draws draws(args);
+        const float p = args.number();
+        const bool keep = args.integer();
+        const Tensor *given = args.optional(), *workspace = args.optional();
+        void *stream = args.stream();
+        need(x.dim() == 2, "x is [n, c]");
+        const int64_t n = x.size(0);
+        const int c = channels(x), code = code_of(x.scalar_type());
+        if (given) {
+            need_rows(*given, n, c, "out is [n, c], contiguous");
+            need(given->scalar_type() == x.scalar_type(), "out is of x's type");
+        }
+        const Tensor y = given ? *given : empty({n, c}, x.scalar_type(), x);
+        Tensor stats, ws;
+        if (keep) stats = empty({clouds.count, groups > 0 ? groups : 1, 2}, at::kFloat, x);
+        const size_t bytes = lib.group_norm_workspace_bytes(n, c, clouds.count, groups, 0);
+        if (bytes) ws = workspace_of(bytes, workspace, x);
+        const int rc = lib.group_norm_fwd(x.data_ptr(), pitch(x), weights(w, c), weights(b, c), clouds.offsets, clouds.count, groups, act, eps, draws.state, draws.site,
+                                          p, n, c, code, y.data_ptr(), keep ? static_cast<float *>(stats.data_ptr()) : nullptr, bytes ? ws.data_ptr() : nullptr,
+                                          bytes ? ws.nbytes() : 0, stream);
+        written(given);
+        return result(rc, y, stats);
+    });
+}
+
+// (dy, x, mean_rstd, w, b, offsets, act, state, site, p, dx wanted, weights' gradients wanted, workspace, device, stream) -> (dx, dw, db)
+PyObject *group_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Tensor &dy = args.tensor(), &x = args.tensor(), &stats = args.tensor();
+        const Tensor *w = args.optional(), *b = args.optional();
+        const CloudsOf clouds(args.optional());
+        const int act = args.small();
+        const Draws draws(args);
+        const float p = args.number();
+        const bool of_x = args.integer(), of_weights = args.integer();
+        const Tensor *workspace = args.optional();
+        void *stream = args.stream();
+        need(x.dim() == 2, "x is [n, c]");
+        const int64_t n = x.size(0);
+        const int c = channels(x), code = code_of(x.scalar_type());
+        need_rows(dy, n, c, "dy is [n, c], contiguous");
+        need(dy.scalar_type() == x.scalar_type(), "dy is of x's type");
+        need(stats.scalar_type() == at::kFloat && stats.is_contiguous() && stats.dim() == 3 && stats.size(0) == clouds.count && stats.size(1) >= 1 &&
+                 stats.size(1) <= c && stats.size(2) == 2, "mean_rstd is float32 [clouds, groups, 2]");
+        const int groups = (int)stats.size(1);
+        Tensor dx, dw, db, ws;
+        if (of_x) dx = empty({n, c}, x.scalar_type(), x);
+        if (of_weights) dw = empty({c}, at::kFloat, x), db = empty({c}, at::kFloat, x);
+        const size_t bytes = lib.group_norm_workspace_bytes(n, c, clouds.count, groups, 1);
+        if (bytes) ws = workspace_of(bytes, workspace, x);
+        auto to = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+        const int rc = lib.group_norm_bwd(dy.data_ptr(), x.data_ptr(), pitch(x), static_cast<const float *>(stats.data_ptr()), weights(w, c), weights(b, c),
+                                          clouds.offsets, clouds.count, groups, act, draws.state, draws.site, p, n, c, code, to(dx), static_cast<float *>(to(dw)),
+                                          static_cast<float *>(to(db)), to(ws), bytes ? ws.nbytes() : 0, stream);
+        return result(rc, dx, dw, db);
+    });
+}
+
+int64_t mx_row_bytes(int64_t c) { return (c + 31) / 32 * 16; }
+int64_t mx_scale_bytes(int64_t c) { return (c + 127) / 128 * 4; }
+struct Rows4 {
+    const uint8_t *q, *scales;
+    int64_t n, c;
+    explicit Rows4(Args &args)                                    // (q, scales, c)
+    {
+        const Tensor &codes = args.tensor(), &exponents = args.tensor();
+        c = args.integer();
+        need(c >= 1 && c < (1 << 24), "channels outside 1 .. 2^24 - 1");
+        n = codes.dim() == 2 ? codes.size(0) : -1;
+        need(codes.scalar_type() == at::kByte && exponents.scalar_type() == at::kByte && codes.is_contiguous() && exponents.is_contiguous() &&
+                 shape(codes, n, mx_row_bytes(c)) && shape(exponents, n, mx_scale_bytes(c)),
+             "q is uint8 [n, pcpp_mx_row_bytes(c)] and scales uint8 [n, pcpp_mx_scale_bytes(c)], both contiguous");
+        q = static_cast<const uint8_t *>(codes.data_ptr());
+        scales = static_cast<const uint8_t *>(exponents.data_ptr());
+    }
+};
+
+// (x, rows wanted, columns wanted, state, site, device, stream) -> (q, scales, qt, scales_t)
+PyObject *mx_pack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Tensor &x = args.tensor();
+        const bool rows = args.integer(), columns = args.integer();
+        const Draws draws(args);
+        void *stream = args.stream();
+        need(x.dim() == 2, "x is [n, c]");
+        need(rows || columns, "neither rows nor columns are wanted");
+        const int64_t n = x.size(0), c = x.size(1);
+        const int code = code_of(x.scalar_type());
+        need(c >= 1 && c < (1 << 24) && (!columns || n < (1 << 24)), "a form's rows have 1 .. 2^24 - 1 elements");
+        Tensor q, s, qt, st;
+        if (rows) q = empty({n, mx_row_bytes(c)}, at::kByte, x), s = empty({n, mx_scale_bytes(c)}, at::kByte, x);
+        if (columns) qt = empty({c, mx_row_bytes(n)}, at::kByte, x), st = empty({c, mx_scale_bytes(n)}, at::kByte, x);
+        auto to = [](const Tensor &t) { return t.defined() ? static_cast<uint8_t *>(t.data_ptr()) : nullptr; };
+        const int rc = lib.mx_pack(x.data_ptr(), pitch(x), code, n, c, draws.state, draws.site, to(q), to(s), to(qt), to(st), stream);
+        return result(rc, q, s, qt, st);
+    });
+}
+
+// (q, scales, c, dtype code, out or None, device, stream) -> (x,)
+PyObject *mx_unpack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Rows4 rows(args);
+        const Tensor &like = THPVariable_Unpack(args.a[0]);
+        const int64_t code = args.integer();
+        const Tensor *given = args.optional();
+        void *stream = args.stream();
+        if (given) need_rows(*given, rows.n, rows.c, "out has another shape than the rows, or is not contiguous");
+        const Tensor out = given ? *given : empty({rows.n, rows.c}, type_of(code), like);
+        const int rc = lib.mx_unpack(rows.q, rows.scales, rows.n, rows.c, out.data_ptr(), code_of(out.scalar_type()), stream);
+        written(given);
+        return result(rc, out);
+    });
+}
+
+const float *bias_at(const Tensor *t, int64_t m)
+{
+    if (!t) return nullptr;
+    need(t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == m && t->is_contiguous(), "the bias is float32 [m]");
+    return static_cast<const float *>(t->data_ptr());
+}
+
+// (a's q, scales, c, b's q, scales, c, bias, act, dtype code, out, workspace, device, stream) -> (out,)
+PyObject *mx_product(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Rows4 x(args);
+        const Tensor &like = THPVariable_Unpack(args.a[0]);
+        const Rows4 w(args);
+        const Tensor *bias = args.optional();
+        const int act = args.small();
+        const int64_t wanted = args.integer();
+        const Tensor *given = args.optional(), *workspace = args.optional();
+        void *stream = args.stream();
+        need(x.c == w.c, "both sides have the same number of channels");
+        if (given) need_rows(*given, x.n, w.n, "out is [n, m], contiguous");
+        const Tensor out = given ? *given : empty({x.n, w.n}, type_of(wanted), like);
+        const size_t bytes = lib.mx_product_workspace_bytes(x.n, w.n, x.c);
+        Tensor ws;
+        if (bytes) ws = workspace_of(bytes, workspace, like);
+        const int rc = lib.mx_product(x.q, x.scales, w.q, w.scales, bias_at(bias, w.n), act, x.n, w.n, x.c, out.data_ptr(), code_of(out.scalar_type()),
+                                      bytes ? ws.data_ptr() : nullptr, bytes ? ws.nbytes() : 0, stream);
+        written(given);
+        return result(rc, out);
+    });
+}
+
+// (x, w's q, scales, c, bias, act, dtype code (-1: x's), out, workspace, device, stream) -> (out,)
+PyObject *mx_linear(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    return guarded(a, n_args, [](Args &args) {
+        const Tensor &x = args.tensor();
+        const Rows4 w(args);
+        const Tensor *bias = args.optional();
+        const int act = args.small();
+        const int64_t wanted = args.integer();
+        const Tensor *given = args.optional(), *workspace = args.optional();
+        void *stream = args.stream();
+        need(x.dim() == 2 && x.size(1) == w.c, "x is [n, k] with the weights' channels");
+        const int64_t n = x.size(0);
+        if (given) need_rows(*given, n, w.n, "out is [n, m], contiguous");
+        const Tensor out = given ? *given : empty({n, w.n}, wanted < 0 ? x.scalar_type() : type_of(wanted), x);
+        const Tensor ws = workspace_of(lib.mx_linear_workspace_bytes(n, w.n, w.c), workspace, x);
+        const int rc = lib.mx_linear(x.data_ptr(), pitch(x), code_of(x.scalar_type()), w.q, w.scales, bias_at(bias, w.n), act, n, w.n, w.c, out.data_ptr(),
+                                     code_of(out.scalar_type()), ws.data_ptr(), ws.nbytes(), stream);
+        written(given);
+        return result(rc, out);
+    });
+}
+
 // bind(handle): the library's functions
 PyObject *bind(PyObject *, PyObject *arg)
 {
@@ -467,6 +741,17 @@ PyObject *bind(PyObject *, PyObject *arg)
     find(lib.log_probs_workspace_bytes, "pcpp_log_probs_workspace_bytes");
     find(lib.log_probs_fwd, "pcpp_log_probs_fwd");
     find(lib.log_probs_bwd, "pcpp_log_probs_bwd");
+    find(lib.dropout_fwd, "pcpp_dropout_fwd");
+    find(lib.dropout_bwd, "pcpp_dropout_bwd");
+    find(lib.group_norm_workspace_bytes, "pcpp_group_norm_workspace_bytes");
+    find(lib.group_norm_fwd, "pcpp_group_norm_fwd");
+    find(lib.group_norm_bwd, "pcpp_group_norm_bwd");
+    find(lib.mx_pack, "pcpp_mx_pack");
+    find(lib.mx_unpack, "pcpp_mx_unpack");
+    find(lib.mx_product_workspace_bytes, "pcpp_mx_product_workspace_bytes");
+    find(lib.mx_product, "pcpp_mx_product");
+    find(lib.mx_linear_workspace_bytes, "pcpp_mx_linear_workspace_bytes");
+    find(lib.mx_linear, "pcpp_mx_linear");
     if (!ok) {
         PyErr_SetString(PyExc_OSError, "libpcpp.so lacks a function");
         return nullptr;
@@ -476,7 +761,8 @@ PyObject *bind(PyObject *, PyObject *arg)
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(act_pack), METHOD(act_unpack), METHOD(weight_packed), METHOD(block_norm_fwd), METHOD(block_norm_bwd), METHOD(log_probs_fwd),
-                         METHOD(log_probs_bwd), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         METHOD(log_probs_bwd), METHOD(dropout_fwd), METHOD(dropout_bwd), METHOD(group_norm_fwd), METHOD(group_norm_bwd), METHOD(mx_pack), METHOD(mx_unpack),
+                         METHOD(mx_product), METHOD(mx_linear), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,134 @@
+"""What the entry points of the pointwise layers' operators refuse, and the sizes they name, before any GPU call."""
+import ctypes
+
+import pytest
+
+F32, BF16 = 0, 1
+INVALID, WORKSPACE, UNSUPPORTED = -1, -3, -4
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2511_23227_amd import binding
+    return binding.library()
+
+
+@pytest.fixture(scope="module")
+def p():
+    """A 256-byte aligned address; nothing is read from it."""
+    buf = ctypes.create_string_buffer(8192)
+    at = (ctypes.addressof(buf) + 255) // 256 * 256
+    p.keep = buf
+    return at
+
+
+def vp(at):
+    return ctypes.c_void_p(at)
+
+
+def test_dropout(lib, p):
+    a, y = vp(p), vp(p + 1024)
+
+    def fwd(x=a, ld=64, res=None, rng=a, prob=0.5, scope=0, off=None, clouds=1, n=4, c=64, dtype=F32, stream=F32, out=y):
+        return lib.pcpp_dropout_fwd(x, ld, res, rng, 1, prob, scope, off, clouds, n, c, dtype, stream, out, None)
+
+    def bwd(dy=a, rng=a, prob=0.5, scope=0, off=None, clouds=1, n=4, c=64, dtype=F32, stream=F32, out=y, **_):
+        return lib.pcpp_dropout_bwd(dy, rng, 1, prob, scope, off, clouds, n, c, dtype, stream, out, None)
+
+    for call in (fwd, bwd):
+        assert call(n=-1) == INVALID and call(c=0, ld=0) == UNSUPPORTED and call(c=65537, ld=65537) == UNSUPPORTED and call(n=2 ** 31 - 1) == UNSUPPORTED
+        assert call(dtype=7, stream=7) == UNSUPPORTED and call(dtype=F32, stream=BF16) == UNSUPPORTED
+        for bad in (-0.1, 1.5, float("nan")):
+            assert call(prob=bad) == INVALID
+        assert call(scope=-1) == INVALID and call(scope=3) == INVALID
+        assert call(scope=2, off=a, clouds=0) == INVALID and call(scope=2, off=a, clouds=65537) == INVALID and call(scope=2, clouds=2) == INVALID
+        assert call(off=a, clouds=2) == INVALID and call(scope=1, off=a) == INVALID and call(scope=2, off=vp(p + 2)) == INVALID
+        assert call(rng=None) == INVALID and call(rng=vp(p + 4)) == INVALID and call(out=None) == INVALID and call(out=a) == INVALID
+        assert call(n=2 ** 30, c=32, ld=32) == UNSUPPORTED and b"random" in lib.pcpp_last_error()
+        assert call(out=vp(p + 1026)) == INVALID
+        assert call(n=0, x=None, dy=None, out=None) == 0 if call is bwd else call(n=0, x=None, out=None) == 0
+    assert fwd(x=None) == INVALID and fwd(ld=63) == INVALID and fwd(ld=2 ** 24) == UNSUPPORTED and fwd(res=y) == INVALID and fwd(x=vp(p + 2)) == INVALID
+    assert bwd(dy=None) == INVALID
+
+
+def test_group_norm(lib, p):
+    a, y = vp(p), vp(p + 1024)
+    size = lib.pcpp_group_norm_workspace_bytes
+    assert [size(*s) for s in ((-1, 64, 1, 8, 0), (100, 0, 1, 1, 0), (100, 1025, 1, 1, 0), (100, 64, 0, 8, 0), (100, 64, 65537, 8, 0), (100, 64, 1, 7, 0),
+                               (100, 64, 1, 0, 0), (2 ** 31, 64, 1, 8, 0))] == [0] * 8
+    assert size(100_000, 64, 4, 8, 0) > 0 and size(100_000, 64, 4, 8, 1) >= size(100_000, 64, 4, 8, 0)
+    need = {b: size(100_000, 64, 4, 8, b) for b in (0, 1)}
+
+    def fwd(x=a, ld=64, w=None, b=None, off=a, clouds=4, groups=8, act=0, eps=1e-5, rng=a, prob=0.0, n=100_000, c=64, dtype=F32, out=y, stats=a,
+            ws=(a, need[0])):
+        return lib.pcpp_group_norm_fwd(x, ld, w, b, off, clouds, groups, act, eps, rng, 1, prob, n, c, dtype, out, stats, *ws, None)
+
+    def bwd(dy=a, x=a, ld=64, stats=a, w=None, b=None, off=a, clouds=4, groups=8, act=0, rng=a, prob=0.0, n=100_000, c=64, dtype=F32, out=y, dw=a, db=a,
+            ws=(a, need[1])):
+        return lib.pcpp_group_norm_bwd(dy, x, ld, stats, w, b, off, clouds, groups, act, rng, 1, prob, n, c, dtype, out, dw, db, *ws, None)
+
+    for call, i in ((fwd, 0), (bwd, 1)):
+        assert call(n=-1) == INVALID and call(c=0) == UNSUPPORTED and call(c=1025, ld=1025, groups=1) == UNSUPPORTED and call(n=2 ** 31 - 1) == UNSUPPORTED
+        assert call(dtype=2) == UNSUPPORTED and call(groups=0) == INVALID and call(groups=7) == INVALID and call(act=4) == INVALID and call(act=-1) == INVALID
+        assert call(prob=1.1) == INVALID and call(prob=float("nan")) == INVALID and call(prob=0.1, rng=None) == INVALID and call(prob=0.1, rng=vp(p + 4)) == INVALID
+        assert call(prob=0.1, n=2 ** 30) == UNSUPPORTED
+        assert call(clouds=0) == INVALID and call(clouds=65537) == INVALID and call(off=None) == INVALID and call(off=vp(p + 2)) == INVALID
+        assert call(ld=63) == INVALID and call(ld=2 ** 24) == UNSUPPORTED and call(w=vp(p + 2)) == INVALID and call(b=vp(p + 1)) == INVALID
+        assert call(x=None) == INVALID and call(x=vp(p + 2)) == INVALID and call(out=a) == INVALID and call(out=vp(p + 8)) == INVALID
+        assert call(stats=vp(p + 4)) == INVALID
+        assert call(ws=(None, need[i])) == WORKSPACE and call(ws=(a, need[i] - 1)) == WORKSPACE and call(ws=(vp(p + 16), need[i])) == WORKSPACE
+    for bad in (0.0, -1.0, 1e-39, float("inf"), float("nan")):
+        assert fwd(eps=bad) == INVALID
+    assert fwd(out=None) == INVALID
+    assert bwd(dy=None) == INVALID and bwd(stats=None) == INVALID and bwd(dy=vp(p + 8)) == INVALID and bwd(dw=vp(p + 2)) == INVALID
+    assert bwd(out=None, dw=None, db=None) == INVALID
+    assert fwd(n=0, x=None, out=None, stats=None, ws=(None, 0)) == 0 and bwd(n=0, x=None, dy=None, out=None, dw=None, db=None, ws=(None, 0)) == 0
+
+
+def test_rows_in_four_bits(lib, p):
+    a = vp(p)
+    assert [lib.pcpp_mx_row_bytes(c) for c in (0, 1, 32, 33, 128, 2 ** 24 - 1, 2 ** 24)] == [0, 16, 16, 32, 64, 2 ** 23, 0]
+    assert [lib.pcpp_mx_scale_bytes(c) for c in (-1, 1, 128, 129, 4096, 2 ** 24)] == [0, 4, 4, 8, 128, 0]
+
+    def pack(x=a, ld=64, dtype=F32, n=4, c=64, rng=None, q=a, s=a, qt=None, st=None):
+        return lib.pcpp_mx_pack(x, ld, dtype, n, c, rng, 1, q, s, qt, st, None)
+
+    assert pack(n=-1) == INVALID and pack(c=0) == INVALID and pack(c=2 ** 24, ld=2 ** 24) == UNSUPPORTED and pack(n=2 ** 31) == UNSUPPORTED
+    assert pack(dtype=5) == UNSUPPORTED and pack(ld=63) == INVALID and pack(ld=2 ** 31) == UNSUPPORTED
+    assert pack(x=None) == INVALID and pack(q=None) == INVALID and pack(s=None) == INVALID and pack(q=None, s=None) == INVALID and pack(qt=a) == INVALID
+    assert pack(q=vp(p + 8)) == INVALID and pack(s=vp(p + 2)) == INVALID and pack(x=vp(p + 2)) == INVALID and pack(qt=vp(p + 4), st=a) == INVALID
+    assert pack(qt=a, st=a, n=2 ** 24) == UNSUPPORTED and pack(rng=vp(p + 4)) == INVALID and pack(rng=a, n=2 ** 30) == UNSUPPORTED
+    assert pack(n=0, x=None, q=None, s=None) == 0
+
+    def unpack(q=a, s=a, n=4, c=64, x=a, dtype=F32):
+        return lib.pcpp_mx_unpack(q, s, n, c, x, dtype, None)
+
+    assert unpack(q=None) == INVALID and unpack(s=None) == INVALID and unpack(x=None) == INVALID and unpack(n=-1) == INVALID and unpack(c=0) == INVALID
+    assert unpack(dtype=3) == UNSUPPORTED and unpack(q=vp(p + 8)) == INVALID and unpack(s=vp(p + 1)) == INVALID and unpack(x=vp(p + 2)) == INVALID
+    assert unpack(n=0, q=None) == 0
+
+
+def test_products(lib, p):
+    a = vp(p)
+    size, linear_size = lib.pcpp_mx_product_workspace_bytes, lib.pcpp_mx_linear_workspace_bytes
+    for f in (size, linear_size):
+        assert [f(*s) for s in ((-1, 8, 8), (8, 0, 8), (8, 8, 0), (8, 2 ** 24, 8), (8, 8, 2 ** 24), (2 ** 31, 8, 8))] == [0] * 6
+    parts = (64, 64, 100_000)                              # few results, long sums: cut into parts
+    need, linear_need = size(*parts), linear_size(*parts)
+    assert need >= 2 * 64 * 64 * 4 and linear_need >= need + 64 * 50_000 and size(4096, 4096, 64) == 0
+
+    def product(q=a, s=a, wq=a, ws_=a, bias=None, act=0, n=64, m=64, k=100_000, out=a, dtype=F32, ws=(a, need)):
+        return lib.pcpp_mx_product(q, s, wq, ws_, bias, act, n, m, k, out, dtype, *ws, None)
+
+    def linear(x=a, ld=100_000, xdtype=F32, wq=a, ws_=a, bias=None, act=0, n=64, m=64, k=100_000, out=a, dtype=F32, ws=(a, linear_need)):
+        return lib.pcpp_mx_linear(x, ld, xdtype, wq, ws_, bias, act, n, m, k, out, dtype, *ws, None)
+
+    for call, room in ((product, need), (linear, linear_need)):
+        assert call(n=-1) == INVALID and call(m=0) == INVALID and call(k=0) == INVALID and call(n=2 ** 31) == UNSUPPORTED
+        assert call(m=2 ** 24) == UNSUPPORTED and call(k=2 ** 24) == UNSUPPORTED and call(dtype=9) == UNSUPPORTED and call(act=4) == INVALID
+        assert call(wq=None) == INVALID and call(ws_=None) == INVALID and call(out=None) == INVALID
+        assert call(wq=vp(p + 8)) == INVALID and call(ws_=vp(p + 2)) == INVALID and call(bias=vp(p + 2)) == INVALID and call(out=vp(p + 2)) == INVALID
+        assert call(ws=(None, room)) == WORKSPACE and call(ws=(a, room - 1)) == WORKSPACE and call(ws=(vp(p + 8), room)) == WORKSPACE
+        assert call(n=0, ws=(None, 0)) == 0
+    assert product(q=None) == INVALID and product(s=None) == INVALID and product(q=vp(p + 4)) == INVALID
+    assert linear(x=None) == INVALID and linear(ld=99_999) == INVALID and linear(xdtype=4) == UNSUPPORTED and linear(x=vp(p + 2)) == INVALID
