@@ -41,12 +41,33 @@ struct Clouds {
 
 // ---- activations --------------------------------------------------------------------------------------------------------------
 __device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
+// The normal distribution below z, (1 + erf(z / sqrt 2)) / 2, and its density without 1 / sqrt(2 pi).  erfc(x) = exp(-x^2) t P(t) with t = 1 / (1 + 0.49 x): P
+// of degree 8 by least squares for the relative error over 0 <= x <= 14, reweighted until its largest, 5.5e-8, was level.  In fp32 off by 1.8e-7 at most, and by
+// 3e-6 of itself where it is small.  The library's erff took twice the time of the whole epilogue.
+__device__ inline float normal(float z, float &density)
+{
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.34648232f, __builtin_fabsf(z), 1.f));
+    density = __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+    float p = -0.0269294106f;
+    p = __builtin_fmaf(p, t, 0.137322286f);
+    p = __builtin_fmaf(p, t, -0.252138865f);
+    p = __builtin_fmaf(p, t, 0.16366231f);
+    p = __builtin_fmaf(p, t, -0.0237202372f);
+    p = __builtin_fmaf(p, t, 0.106285078f);
+    p = __builtin_fmaf(p, t, 0.118834596f);
+    p = __builtin_fmaf(p, t, 0.13846641f);
+    p = __builtin_fmaf(p, t, 0.138217861f);
+    const float below = p * t * density;
+    return z < 0.f ? below : 1.f - below;
+}
 template <int ACT> __device__ inline float activate(float z)
 {
     if constexpr (ACT == PCPP_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
     else if constexpr (ACT == PCPP_ACT_SILU) return z * logistic(z);
-    else if constexpr (ACT == PCPP_ACT_GELU) return 0.5f * z * (1.f + erff(0.70710678f * z));
-    else return z;
+    else if constexpr (ACT == PCPP_ACT_GELU) {
+        float density;
+        return z * normal(z, density);
+    } else return z;
 }
 template <int ACT> __device__ inline float slope(float z)         // the derivative
 {
@@ -54,9 +75,11 @@ template <int ACT> __device__ inline float slope(float z)         // the derivat
     else if constexpr (ACT == PCPP_ACT_SILU) {
         const float s = logistic(z);
         return s * (1.f + z * (1.f - s));
-    } else if constexpr (ACT == PCPP_ACT_GELU)
-        return 0.5f * (1.f + erff(0.70710678f * z)) + z * 0.39894228f * __builtin_amdgcn_exp2f(-0.72134752f * z * z);
-    else return 1.f;
+    } else if constexpr (ACT == PCPP_ACT_GELU) {
+        float density;
+        const float below = normal(z, density);
+        return __builtin_fmaf(0.39894228f * z, density, below);
+    } else return 1.f;
 }
 template <typename F> void with_act(int act, F f)
 {
