@@ -13,57 +13,6 @@ namespace {
 constexpr int THREADS = 256;
 constexpr int TILE_ROWS = 128, TILE_CHANNELS = 64;
 
-// channels c0 .. of a row of c; zeros past the last
-template <typename T> __device__ inline void load_up_to_eight(const T *row, int64_t c0, int64_t c, float (&v)[8])
-{
-    if (c0 + 8 <= c) {
-        Eight<T> r;
-        load_eight<false>(row + c0, r);
-        to_floats(r, v);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c0 + e < c ? one_float(row[c0 + e]) : 0.f;
-}
-template <typename T> __device__ inline void store_up_to_eight(T *row, int64_t c0, int64_t c, const float (&v)[8])
-{
-    if (c0 + 8 <= c) return store_eight<false>(row + c0, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (c0 + e < c) row[c0 + e] = one_of<T>(v[e]);
-}
-__device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }     // (as integers: a NaN is larger than any number)
-__device__ inline uint32_t largest(const float (&v)[8])
-{
-    uint32_t m = 0u;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = m > magnitude(v[e]) ? m : magnitude(v[e]);
-    return m;
-}
-__device__ inline uint32_t quad_largest(uint32_t m)
-{
-    uint32_t o = dpp<DPP_XOR1>(m);
-    m = m > o ? m : o;
-    o = dpp<DPP_XOR2>(m);
-    return m > o ? m : o;
-}
-// Eight numbers of one block as codes
-template <bool RANDOM> __device__ inline uint32_t quantise(const float (&v)[8], uint32_t code, const uint32_t (&u)[4])
-{
-    const float by = mx_inverse(code);
-    uint32_t r = 0u;
-    if constexpr (RANDOM) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r |= mx_random(v[e] * by, half_of(u, e)) << (4 * e);
-    } else {
-        float s[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = v[e] * by;
-        r = mx_nearest(s);
-    }
-    return code == MX_NAN_CODE ? 0u : r;
-}
-
 // Rows `first` .. of the tensor; `threads` is a multiple of four, `per_row` of a row
 template <typename T, bool RANDOM>
 __global__ __launch_bounds__(THREADS) void pack_rows_kernel(const MxPackArgs a, int64_t first, uint32_t threads, const Divisor per_row)
@@ -72,12 +21,12 @@ __global__ __launch_bounds__(THREADS) void pack_rows_kernel(const MxPackArgs a, 
     if (id >= threads) return;                                    // (quads stay whole)
     const uint32_t r = per_row.quotient(id), j = id - r * per_row.by;
     const int64_t row = first + r, c0 = 8 * (int64_t)j;
-    float v[8];
-    load_up_to_eight(static_cast<const T *>(a.x) + row * a.ld_x, c0, a.c, v);
+    Eight<T> v;
+    load_channels(static_cast<const T *>(a.x) + row * a.ld_x, c0, a.c, v);
     uint32_t u[4] = {0u, 0u, 0u, 0u};
     if constexpr (RANDOM) Philox(a.random).draw((uint32_t)row * (uint32_t)ceil_div(a.c, 8) + j, u);
     const uint32_t code = mx_code(quad_largest(largest(v)), RANDOM);
-    reinterpret_cast<uint32_t *>(a.q + row * mx_row_bytes(a.c))[j] = quantise<RANDOM>(v, code, u);
+    reinterpret_cast<uint32_t *>(a.q + row * mx_row_bytes(a.c))[j] = mx_quantise<RANDOM>(v, code, u);
     if (j % 4 == 0) {
         uint8_t *to = a.scales + row * mx_scale_bytes(a.c);
         to[j / 4] = (uint8_t)code;
@@ -86,6 +35,54 @@ __global__ __launch_bounds__(THREADS) void pack_rows_kernel(const MxPackArgs a, 
     }
 }
 
+// over the lanes that hold other rows of the same channels: lanes 8, 16 and 32 apart
+template <typename Op> __device__ inline uint32_t over_rows(uint32_t m, Op op)
+{
+    m = op(m, dpp<DPP_ROR + 8>(m));
+    const auto a = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    m = op(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return op(b[0], b[1]);
+}
+// The largest magnitudes of the lane's eight channels over its four rows and the wave's, and the four rows' pairs (0, 1), (2, 3) of a channel
+template <typename T> struct Columns;
+template <> struct Columns<float> {
+    uint32_t most[8];
+    __device__ inline explicit Columns(const Eight<float> (&v)[4])
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint32_t m = 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = larger(m, v[i].a[e >> 2][e & 3] & 0x7fffffffu);
+            most[e] = over_rows(m, larger);
+        }
+    }
+    __device__ inline uint32_t largest_of(int e) const { return most[e]; }
+    __device__ static inline Pair<float> pair(const Eight<float> &a, const Eight<float> &b, int e)
+    {
+        return Pair<float>{__uint_as_float(a.a[e >> 2][e & 3]), __uint_as_float(b.a[e >> 2][e & 3])};
+    }
+};
+template <> struct Columns<bf16_t> {
+    uint32_t most[4];
+    __device__ inline explicit Columns(const Eight<bf16_t> (&v)[4])
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t m = v[0].a[0][k] & 0x7fff7fffu;
+#pragma unroll
+            for (int i = 1; i < 4; ++i) m = larger_pair(m, v[i].a[0][k] & 0x7fff7fffu);
+            most[k] = over_rows(m, larger_pair);
+        }
+    }
+    __device__ inline uint32_t largest_of(int e) const { return (e & 1) ? most[e >> 1] & 0xffff0000u : most[e >> 1] << 16; }
+    __device__ static inline Pair<bf16_t> pair(const Eight<bf16_t> &a, const Eight<bf16_t> &b, int e)
+    {
+        return Pair<bf16_t>{__builtin_amdgcn_perm(b.a[0][e >> 1], a.a[0][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u)};
+    }
+};
+
 template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREADS) void pack_columns_kernel(const MxPackArgs a, const Divisor row_tiles)
 {
     __shared__ __attribute__((aligned(16))) uint8_t tile[TILE_CHANNELS][80];    // 64 bytes a channel, and a pitch that spreads the banks
@@ -93,12 +90,17 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rl = lane / 8, cl = lane % 8;
     const uint32_t tile_y = row_tiles.quotient(blockIdx.x), tile_x = blockIdx.x - tile_y * row_tiles.by;
     const int64_t row0 = (int64_t)tile_x * TILE_ROWS + 32 * wave + 4 * rl, c0 = (int64_t)tile_y * TILE_CHANNELS + 8 * cl;
-    float v[4][8];
+    if (threadIdx.x < TILE_CHANNELS) words[threadIdx.x] = 0u;
+    Eight<T> v[4];
     uint32_t u[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t row = row0 + i;
-        load_up_to_eight(static_cast<const T *>(a.x) + (row < a.n ? row : 0) * a.ld_x, c0, row < a.n ? a.c : 0, v[i]);
+        load_channels(static_cast<const T *>(a.x) + (row < a.n ? row : a.n - 1) * a.ld_x, c0, a.c, v[i]);
+        if (row >= a.n) {
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(T) / 2); ++k) v[i].a[k] = v4u{0u, 0u, 0u, 0u};
+        }
     }
     if constexpr (RANDOM) {
         const Philox philox(a.random);
@@ -115,7 +117,7 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t row = row0 + i;
-            const uint32_t code = mx_code(quad_largest(largest(v[i])), RANDOM), bits = quantise<RANDOM>(v[i], code, u[i]);
+            const uint32_t code = mx_code(quad_largest(largest(v[i])), RANDOM), bits = mx_quantise<RANDOM>(v[i], code, u[i]);
             if (row < a.n && block < mx_blocks(a.c)) {
                 reinterpret_cast<uint32_t *>(a.q + row * mx_row_bytes(a.c))[c0 / 8] = bits;
                 if (cl % 4 == 0) {
@@ -128,27 +130,19 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
         }
     }
     // channel by channel: the largest of the wave's 32 rows, four codes of the lane's rows
-    if (threadIdx.x < TILE_CHANNELS) words[threadIdx.x] = 0u;
+    const Columns<T> columns(v);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        uint32_t m = 0u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m = m > magnitude(v[i][e]) ? m : magnitude(v[i][e]);
-#pragma unroll
-        for (int k = 8; k < 64; k <<= 1) {
-            const uint32_t o = __shfl_xor(m, k);
-            m = m > o ? m : o;
-        }
-        const uint32_t code = mx_code(m, RANDOM);
-        const float by = mx_inverse(code);
+        const uint32_t code = mx_code(columns.largest_of(e), RANDOM);
+        const float step = mx_step(code);
+        const Pair<T> first = Columns<T>::pair(v[0], v[1], e), second = Columns<T>::pair(v[2], v[3], e);
         uint32_t bits = 0u;
         if constexpr (RANDOM) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bits |= mx_random(v[i][e] * by, half_of(u[i], e)) << (4 * i);
+            bits = __builtin_amdgcn_perm(second.random(first_seed(u[2], e), second_seed(u[3], e), step), first.random(first_seed(u[0], e), second_seed(u[1], e), step), 0x0c0c0400u);
         } else {
-            bits = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(bits, v[0][e] * by, v[1][e] * by, 1.f, 0);
-            bits = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(bits, v[2][e] * by, v[3][e] * by, 1.f, 1);
+            bits = first.template nearest<0>(bits, step);
+            bits = second.template nearest<1>(bits, step);
         }
         if (code == MX_NAN_CODE) bits = 0u;
         *reinterpret_cast<uint16_t *>(&tile[8 * cl + e][16 * wave + 2 * rl]) = (uint16_t)bits;
@@ -160,6 +154,14 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
     if (channel >= a.c) return;
     if (block < mx_blocks(a.n)) *reinterpret_cast<v4u *>(a.qt + channel * mx_row_bytes(a.n) + 16 * block) = *reinterpret_cast<const v4u *>(&tile[ch][16 * part]);
     if (part == 0) reinterpret_cast<uint32_t *>(a.scales_t + channel * mx_scale_bytes(a.n))[tile_x] = words[ch];
+}
+
+template <typename T> __device__ inline void store_up_to_eight(T *row, int64_t c0, int64_t c, const float (&v)[8])
+{
+    if (c0 + 8 <= c) return store_eight<false>(row + c0, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c0 + e < c) row[c0 + e] = one_of<T>(v[e]);
 }
 
 template <typename T>

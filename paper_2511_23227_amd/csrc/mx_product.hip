@@ -14,7 +14,6 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_anywhere __attribute__((ext_vector_type(4), aligned(4)));
 typedef v2u32 v2u32_anywhere __attribute__((aligned(2)));
 
-constexpr int THREADS = 256;
 
 // BYTE: which byte of the scales
 template <int BYTE> __device__ inline v4f multiply(const v4u &b, const v4u &a, v4f sum, uint32_t b_scale, uint32_t a_scale)
@@ -23,38 +22,44 @@ template <int BYTE> __device__ inline v4f multiply(const v4u &b, const v4u &a, v
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, sum, 4, 4, BYTE, (int)b_scale, BYTE, (int)a_scale);
 }
 
-// four neighbouring columns of a row of out, of which `left` are there
-template <typename T> __device__ inline void store_four(T *to, const float (&v)[4], int64_t left)
+// N neighbouring columns of a row of out, of which `left` are there
+template <int N, typename T> __device__ inline void store_columns(T *to, const float (&v)[N], int64_t left)
 {
-    if (left >= 4) {
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f_anywhere *>(to) = v4f{v[0], v[1], v[2], v[3]};
-        else *reinterpret_cast<v2u32_anywhere *>(to) = v2u32{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+    if (left >= N) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; i += 4) reinterpret_cast<v4u_anywhere *>(to)[i / 4] = v4u{__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])};
+        } else if constexpr (N == 8) {
+            *reinterpret_cast<v4u_anywhere *>(to) = v4u{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+        } else {
+            *reinterpret_cast<v2u32_anywhere *>(to) = v2u32{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+        }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < N - 1; ++i)
         if (i < left) to[i] = one_of<T>(v[i]);
 }
-template <typename T> __device__ inline void finish_four(const MxProductArgs &p, int64_t i, int64_t j, const float (&v)[4])
+template <int N> __device__ inline void load_bias(const float *bias, int64_t j, int64_t m, float (&v)[N])
 {
-    float o[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = v[e] + (p.bias && j + e < p.m ? p.bias[j + e] : 0.f);
-    auto each = [&](auto act) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = activate<decltype(act)::value>(o[e]);
-    };
-    if (p.act == PCPP_ACT_RELU) each(Int<PCPP_ACT_RELU>{});
-    else if (p.act == PCPP_ACT_SILU) each(Int<PCPP_ACT_SILU>{});
-    else if (p.act == PCPP_ACT_GELU) each(Int<PCPP_ACT_GELU>{});
-    store_four(static_cast<T *>(p.out) + i * p.m + j, o, p.m - j);
+    for (int e = 0; e < N; ++e) v[e] = bias && j + e < m ? bias[j + e] : 0.f;
+}
+// f(activation): a branch that all lanes take alike
+template <typename F> __device__ inline void as_act(int act, F f)
+{
+    if (act == PCPP_ACT_NONE) f(Int<PCPP_ACT_NONE>{});
+    else if (act == PCPP_ACT_SILU) f(Int<PCPP_ACT_SILU>{});
+    else if (act == PCPP_ACT_GELU) f(Int<PCPP_ACT_GELU>{});
+    else f(Int<PCPP_ACT_RELU>{});
 }
 
 // ---- tiles through LDS --------------------------------------------------------------------------------------------------------------
 // A block of WA x WB waves takes 16 WA FA rows of a and 16 WB FB of b, a wave 16 FA and 16 FB of them.  A stage is 256 elements: of every row 128 bytes of
 // codes and two words of scales, moved straight into LDS, the next stage while the matrix cores work on this one.
 //
-// A row's eight 16-byte pieces (blocks) lie in LDS at piece ^ (row / 2 mod 8), so that sixteen lanes reading one piece of sixteen rows meet all banks.
+// A row's eight 16-byte pieces (blocks) lie in LDS at piece ^ s, s a function of the row that makes sixteen lanes reading one piece of an instruction's sixteen rows
+// meet all banks.  b's rows go to two instructions in turn, four by four, so that a lane ends with eight neighbouring columns of a row of out.
 // Lane (r, l) of an instruction has row r; over the stage's two instructions it takes the blocks 2 l and 2 l + 1, whose scales are one 16-bit read (the order in
 // which blocks are summed is free).
 constexpr int STAGE = 256, STAGE_BYTES = 128, STAGE_BLOCKS = 8;
@@ -111,16 +116,18 @@ __global__ __launch_bounds__(64 * WA * WB, WA *WB == 8 ? 2 : 1) void tile_kernel
     const v4u bq = scalar_rows(p.b, j0, p.m, pitch, S::B), bs = scalar_rows(p.b_scales, j0, p.m, scale_pitch, S::B);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     // what the lane moves: piece `piece` of rows 8 (wave + i WAVES) + lane / 8, word lane % 2 of rows 32 (wave + i WAVES) + lane / 2
-    const uint32_t piece = (uint32_t)(lane & 7) ^ ((4u * (uint32_t)wave + (uint32_t)(lane >> 4)) & 7u);
-    const uint32_t code_at = (8u * (uint32_t)wave + (uint32_t)(lane >> 3)) * pitch + 16u * piece, word_at = (32u * (uint32_t)wave + (uint32_t)(lane >> 1)) * scale_pitch + 4u * (uint32_t)(lane & 1);
+    const uint32_t a_piece = (uint32_t)(lane & 7) ^ ((4u * (uint32_t)wave + (uint32_t)(lane >> 4)) & 7u);          // s = row / 2 mod 8
+    const uint32_t b_piece = (uint32_t)(lane & 7) ^ (2u * ((uint32_t)wave & 3u) + ((uint32_t)(lane >> 4) & 1u));     // s = 2 (row / 8 mod 4) + row / 2 mod 2
+    const uint32_t code_at = (8u * (uint32_t)wave + (uint32_t)(lane >> 3)) * pitch, word_at = (32u * (uint32_t)wave + (uint32_t)(lane >> 1)) * scale_pitch + 4u * (uint32_t)(lane & 1);
     auto request = [&](int64_t stage, uint32_t buffer) {
         const uint32_t to = lds0 + buffer * S::BYTES, block0 = STAGE_BLOCKS * (uint32_t)stage, word = 2u * (uint32_t)stage + (uint32_t)(lane & 1);
-        const bool some = block0 + piece < blocks;
+        const uint32_t a_at = block0 + a_piece < blocks ? code_at + 16u * (block0 + a_piece) : OOB_OFFSET, b_at = block0 + b_piece < blocks ? code_at + 16u * (block0 + b_piece) : OOB_OFFSET;
 #pragma unroll
         for (int i = 0; i < S::CODE_LOADS; ++i) {
             const bool of_a = 8 * i * S::WAVES < S::A;
             const uint32_t row = 8u * (uint32_t)i * S::WAVES - (of_a ? 0u : (uint32_t)S::A);
-            rows_to_lds_b128(of_a ? aq : bq, some ? code_at + row * pitch + 16u * block0 : OOB_OFFSET, to + (uint32_t)(8 * (wave + i * S::WAVES)) * STAGE_BYTES);
+            const uint32_t at = of_a ? a_at : b_at;
+            rows_to_lds_b128(of_a ? aq : bq, at == OOB_OFFSET ? at : at + row * pitch, to + (uint32_t)(8 * (wave + i * S::WAVES)) * STAGE_BYTES);
         }
 #pragma unroll
         for (int i = 0; i < S::SCALE_LOADS; ++i) {
@@ -131,7 +138,9 @@ __global__ __launch_bounds__(64 * WA * WB, WA *WB == 8 ? 2 : 1) void tile_kernel
         }
     };
     const int wa = wave / WB, wb = wave % WB;
-    const uint32_t read_at = (uint32_t)r * STAGE_BYTES + 16u * ((2u * (uint32_t)l) ^ ((uint32_t)r >> 1 & 7u));
+    const int b_row = 8 * (r >> 2) + (r & 3);                     // of the even one of two instructions; the odd one's are four further on, with the same s
+    const uint32_t read_a = (uint32_t)r * STAGE_BYTES + 16u * ((2u * (uint32_t)l) ^ ((uint32_t)r >> 1 & 7u));
+    const uint32_t read_b = (uint32_t)b_row * STAGE_BYTES + 16u * ((2u * (uint32_t)l) ^ (2u * ((uint32_t)r >> 2) + ((uint32_t)r >> 1 & 1u)));
     v4f sum[FA][FB];
 #pragma unroll
     for (int y = 0; y < FA; ++y)
@@ -151,62 +160,176 @@ __global__ __launch_bounds__(64 * WA * WB, WA *WB == 8 ? 2 : 1) void tile_kernel
 #pragma unroll
         for (int y = 0; y < FA; ++y) sa[y] = *reinterpret_cast<const uint16_t *>(scales + (16 * (wa * FA + y) + r) * STAGE_BLOCKS + 2 * l) & mask;
 #pragma unroll
-        for (int x = 0; x < FB; ++x) sb[x] = *reinterpret_cast<const uint16_t *>(scales + (S::A + 16 * (wb * FB + x) + r) * STAGE_BLOCKS + 2 * l) & mask;
+        for (int x = 0; x < FB; ++x) sb[x] = *reinterpret_cast<const uint16_t *>(scales + (S::A + 16 * (wb * FB + (x & ~1)) + 4 * (x & 1) + b_row) * STAGE_BLOCKS + 2 * l) & mask;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const uint8_t *at = codes + (read_at ^ (16u * t));
+            const uint8_t *at_a = codes + (read_a ^ (16u * t)), *at_b = codes + S::A * STAGE_BYTES + (read_b ^ (16u * t));
             v4u va[FA], vb[FB];
 #pragma unroll
-            for (int x = 0; x < FB; ++x) vb[x] = *reinterpret_cast<const v4u *>(at + (S::A + 16 * (wb * FB + x)) * STAGE_BYTES);
+            for (int x = 0; x < FB; ++x) vb[x] = *reinterpret_cast<const v4u *>(at_b + (16 * (wb * FB + (x & ~1)) + 4 * (x & 1)) * STAGE_BYTES);
 #pragma unroll
-            for (int y = 0; y < FA; ++y) va[y] = *reinterpret_cast<const v4u *>(at + 16 * (wa * FA + y) * STAGE_BYTES);
+            for (int y = 0; y < FA; ++y) va[y] = *reinterpret_cast<const v4u *>(at_a + 16 * (wa * FA + y) * STAGE_BYTES);
 #pragma unroll
             for (int y = 0; y < FA; ++y)
 #pragma unroll
                 for (int x = 0; x < FB; ++x) sum[y][x] = t == 0 ? multiply<0>(vb[x], va[y], sum[y][x], sb[x], sa[y]) : multiply<1>(vb[x], va[y], sum[y][x], sb[x], sa[y]);
         }
     }
+    as_act(PARTS ? PCPP_ACT_NONE : p.act, [&](auto act) {
 #pragma unroll
-    for (int y = 0; y < FA; ++y)
+        for (int x = 0; x < FB; x += 2) {
+            const int64_t j = j0 + 16 * (wb * FB + x) + 8 * l;
+            float bias[8];
+            load_bias<8>(PARTS ? nullptr : p.bias, j, p.m, bias);
 #pragma unroll
-        for (int x = 0; x < FB; ++x) {
-            const int64_t i = i0 + 16 * (wa * FA + y) + r, j = j0 + 16 * (wb * FB + x) + 4 * l;
-            if (i >= p.n || j >= p.m) continue;
-            const float v[4] = {sum[y][x][0], sum[y][x][1], sum[y][x][2], sum[y][x][3]};
-            if constexpr (PARTS) store_four(p.part + ((int64_t)blockIdx.y * p.n + i) * p.m + j, v, p.m - j);
-            else finish_four<T>(p, i, j, v);
+            for (int y = 0; y < FA; ++y) {
+                const int64_t i = i0 + 16 * (wa * FA + y) + r;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = activate<decltype(act)::value>(sum[y][x + e / 4][e % 4] + bias[e]);
+                if (i >= p.n || j >= p.m) continue;
+                if constexpr (PARTS) store_columns<8>(p.part + ((int64_t)blockIdx.y * p.n + i) * p.m + j, v, p.m - j);
+                else store_columns<8>(static_cast<T *>(p.out) + i * p.m + j, v, p.m - j);
+            }
         }
+    });
 }
 
-template <typename T> __global__ __launch_bounds__(THREADS) void join_kernel(const MxProductArgs p, int parts)
+// Parts of a sum joined: a block takes 256 neighbouring elements of out, a wave every sixteenth part of them, then the waves' sums in order.
+template <typename T> __global__ __launch_bounds__(1024) void join_kernel(const MxProductArgs p, int parts, const Divisor columns)
 {
-    const int64_t fours = ceil_div(p.m, 4);
-    const int64_t id = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-    if (id >= p.n * fours) return;
-    const int64_t i = id / fours, j = 4 * (id - i * fours);
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < parts; ++s) {
-        const float *from = p.part + ((int64_t)s * p.n + i) * p.m + j;
+    __shared__ v4f sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t total = (uint32_t)(p.n * p.m), at = 256u * blockIdx.x + 4u * (uint32_t)lane;
+    v4f v = {0.f, 0.f, 0.f, 0.f};
+    if (at + 4u <= total) {
+#pragma unroll 8
+        for (int s = wave; s < parts; s += 16) v += *reinterpret_cast<const v4f_anywhere *>(p.part + (size_t)s * total + at);
+    } else {
+        for (int s = wave; s < parts; s += 16)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += j + e < p.m ? from[e] : 0.f;
+            for (int e = 0; e < 3; ++e) v[e] += at + e < total ? p.part[(size_t)s * total + at + e] : 0.f;
     }
-    finish_four<T>(p, i, j, v);
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) v += sums[w][lane];
+    as_act(p.act, [&](auto act) {
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t i = at + e, j = i - columns.quotient(i) * columns.by;
+            o[e] = activate<decltype(act)::value>(v[e] + (p.bias ? p.bias[j] : 0.f));
+        }
+        if (at < total) store_columns<4>(static_cast<T *>(p.out) + at, o, (int64_t)(total - at));
+    });
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------------------------------
+// Up to sixteen rows of a: what counts is reading b once.  A block takes sixteen rows of b, its waves every WAVES-th stage of the sum; codes go from memory to the
+// registers of the lanes that multiply them.  a comes in 4 bits or, of few elements, as it is: the block rounds it into LDS while its first rows of b are on
+// their way.
+constexpr int FEW_ROWS = 16;
+constexpr int64_t FEW_ELEMENTS = 32768;                           // of a that every block rounds for itself (17 KB of LDS)
+
+template <typename T, typename X, int WAVES> __global__ __launch_bounds__(64 * WAVES) void few_kernel(const MxProductArgs p, const X *__restrict__ x, int64_t ld_x)
+{
+    constexpr bool ROUND = sizeof(X) > 1;
+    __shared__ v4f sums[WAVES][64];
+    extern __shared__ __attribute__((aligned(16))) uint8_t own[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r = lane & 15, l = lane >> 4;
+    const int64_t j0 = 16 * (int64_t)blockIdx.x;
+    const uint32_t pitch = (uint32_t)mx_row_bytes(p.k), scale_pitch = (uint32_t)mx_scale_bytes(p.k), blocks = (uint32_t)mx_blocks(p.k), n = (uint32_t)p.n;
+    const uint32_t stages = (uint32_t)ceil_div(p.k, STAGE);
+    const __amdgpu_buffer_rsrc_t bq = rows_from<1>(p.b, j0, p.m, pitch, (int)pitch, 16), bs = rows_from<1>(p.b_scales, j0, p.m, scale_pitch, (int)scale_pitch, 16);
+    struct Some {
+        v4u q[2];
+        uint32_t scales;
+    };
+    // two blocks of the lane's row in stage s; zeros past the last
+    auto load = [&](const __amdgpu_buffer_rsrc_t &q, const __amdgpu_buffer_rsrc_t &scales, uint32_t row, uint32_t s, Some &v) {
+        const uint32_t block = STAGE_BLOCKS * s + 2u * (uint32_t)l;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const auto c = __builtin_amdgcn_raw_buffer_load_b128(q, (int)(block + t < blocks ? row * pitch + 16u * (block + t) : OOB_OFFSET), 0, 0);
+            v.q[t] = v4u{c[0], c[1], c[2], c[3]};
+        }
+        v.scales = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(scales, (int)(block < blocks ? row * scale_pitch + block : OOB_OFFSET), 0, 0);
+        if (block + 1u >= blocks) v.scales &= 0xffu;              // (scales behind a row's last block may be anything)
+    };
+    constexpr int AHEAD = 4;
+    Some b[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load(bq, bs, (uint32_t)r, (uint32_t)(wave + i * WAVES), b[i]);
+    if constexpr (ROUND) {
+        const uint32_t per_row = 4u * blocks;
+        for (uint32_t id = threadIdx.x; id < n * per_row; id += 64 * WAVES) {
+            const uint32_t row = id / per_row, j = id - row * per_row;
+            Eight<X> v;
+            load_channels(x + row * ld_x, 8 * (int64_t)j, p.k, v);
+            const uint32_t none[4] = {0u, 0u, 0u, 0u}, code = mx_code(quad_largest(largest(v)), false);
+            reinterpret_cast<uint32_t *>(own + row * pitch)[j] = mx_quantise<false>(v, code, none);
+            if (j % 4u == 0u) own[n * pitch + row * scale_pitch + j / 4u] = (uint8_t)code;
+        }
+        __syncthreads();
+    }
+    const __amdgpu_buffer_rsrc_t aq = rows_from<1>(p.a, 0, p.n, pitch, (int)pitch, 16), as = rows_from<1>(p.a_scales, 0, p.n, scale_pitch, (int)scale_pitch, 16);
+    v4f sum = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t s0 = (uint32_t)wave; s0 < stages; s0 += AHEAD * WAVES) {
+        Some a[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const uint32_t s = s0 + i * WAVES;
+            if constexpr (ROUND) {
+                const uint32_t block = STAGE_BLOCKS * s + 2u * (uint32_t)l, at = (uint32_t)r < n ? (uint32_t)r : 0u;
+                const bool here = (uint32_t)r < n && block < blocks, both = here && block + 1u < blocks;
+                a[i].q[0] = here ? *reinterpret_cast<const v4u *>(own + at * pitch + 16u * block) : v4u{0u, 0u, 0u, 0u};
+                a[i].q[1] = both ? *reinterpret_cast<const v4u *>(own + at * pitch + 16u * (block + 1u)) : v4u{0u, 0u, 0u, 0u};
+                a[i].scales = here ? *reinterpret_cast<const uint16_t *>(own + n * pitch + at * scale_pitch + block) & (both ? 0xffffu : 0xffu) : 0u;
+            } else {
+                load(aq, as, (uint32_t)r, s, a[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            sum = multiply<0>(b[i].q[0], a[i].q[0], sum, b[i].scales, a[i].scales);
+            sum = multiply<1>(b[i].q[1], a[i].q[1], sum, b[i].scales, a[i].scales);
+            if (s0 + AHEAD * WAVES < stages) load(bq, bs, (uint32_t)r, s0 + (AHEAD + i) * WAVES, b[i]);
+        }
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += sums[w][lane];
+    const int64_t j = j0 + 4 * l;
+    if ((uint32_t)r >= n || j >= p.m) return;
+    as_act(p.act, [&](auto act) {
+        float bias[4], v[4];
+        load_bias<4>(p.bias, j, p.m, bias);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = activate<decltype(act)::value>(sum[e] + bias[e]);
+        store_columns<4>(static_cast<T *>(p.out) + (int64_t)r * p.m + j, v, p.m - j);
+    });
 }
 
 // How a product is cut: tiles, and parts of the sum where the tiles do not fill the card.
 struct Shape {
-    bool large;
+    bool few, large;
     int64_t rows, columns, stages, parts, of_part;
 };
 Shape shape_of(int64_t n, int64_t m, int64_t k)
 {
     Shape s{};
     s.stages = ceil_div(k, STAGE);
+    s.parts = 1;
+    s.few = n <= FEW_ROWS;
+    if (s.few) return s;
     s.large = ceil_div(n, 256) * ceil_div(m, 256) >= 192 && s.stages >= 4;
     const int tile = s.large ? 256 : 128;
     s.rows = ceil_div(n, tile);
     s.columns = ceil_div(m, tile);
-    s.parts = 1;
     const int64_t tiles = s.rows * s.columns;
     if (tiles < 256 && s.stages >= 8) {
         s.parts = ceil_div(512, tiles);
@@ -237,7 +360,26 @@ template <typename T, bool PARTS, int WA, int WB, int FA, int FB> int launch_til
     return PCPP_OK;
 }
 
+// (more waves a block where the blocks are few)
+template <typename T, typename X> void launch_few(const MxProductArgs &p, const X *x, int64_t ld_x, hipStream_t stream)
+{
+    const unsigned blocks = (unsigned)ceil_div(p.m, 16);
+    const size_t bytes = sizeof(X) > 1 ? (size_t)(p.n * (mx_row_bytes(p.k) + mx_scale_bytes(p.k))) : 0;
+    if (blocks < 256) few_kernel<T, X, 16><<<blocks, 1024, bytes, stream>>>(p, x, ld_x);
+    else few_kernel<T, X, 4><<<blocks, 256, bytes, stream>>>(p, x, ld_x);
+}
+
 }  // namespace
+
+bool mx_linear_few(int64_t n, int64_t k) { return n <= FEW_ROWS && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
+int mx_linear_few(const MxProductArgs &p, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream)
+{
+    auto with = [&](auto t, auto s) { launch_few<decltype(t)>(p, static_cast<const decltype(s) *>(x), ld_x, stream); };
+    if (x_dtype == PCPP_F32) out_dtype == PCPP_F32 ? with(float{}, float{}) : with(bf16_t{}, float{});
+    else out_dtype == PCPP_F32 ? with(float{}, bf16_t{}) : with(bf16_t{}, bf16_t{});
+    PCPP_HIP_CHECK(hipGetLastError());
+    return PCPP_OK;
+}
 
 size_t mx_product_workspace_bytes(int64_t n, int64_t m, int64_t k)
 {
@@ -250,9 +392,13 @@ int mx_product(const MxProductArgs &p, int out_dtype, hipStream_t stream)
     const Shape s = shape_of(p.n, p.m, p.k);
     auto with = [&](auto t) -> int {
         typedef decltype(t) T;
+        if (s.few) {
+            launch_few<T, uint8_t>(p, nullptr, 0, stream);
+            return PCPP_OK;
+        }
         if (s.parts > 1) {
             if (int rc = launch_tiles<float, true, 2, 2, 4, 4>(p, s, stream)) return rc;
-            join_kernel<T><<<(unsigned)ceil_div(p.n * ceil_div(p.m, 4), THREADS), THREADS, 0, stream>>>(p, (int)s.parts);
+            join_kernel<T><<<(unsigned)ceil_div(p.n * p.m, 256), 1024, 0, stream>>>(p, (int)s.parts, make_divisor((uint32_t)p.m));
             return PCPP_OK;
         }
         return s.large ? launch_tiles<T, false, 4, 2, 4, 8>(p, s, stream) : launch_tiles<T, false, 2, 2, 4, 4>(p, s, stream);

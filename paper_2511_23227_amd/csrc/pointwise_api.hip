@@ -259,7 +259,8 @@ int pcpp_mx_product(const uint8_t *a, const uint8_t *a_scales, const uint8_t *b,
 
 size_t pcpp_mx_linear_workspace_bytes(int64_t n, int64_t m, int64_t k)
 {
-    return sizes(n, m, k) ? linear_codes(n, k) + linear_scales(n, k) + mx_product_workspace_bytes(n, m, k) : 0;
+    if (!sizes(n, m, k) || mx_linear_few(n, k)) return 0;
+    return linear_codes(n, k) + linear_scales(n, k) + mx_product_workspace_bytes(n, m, k);
 }
 
 int pcpp_mx_linear(const void *x, int64_t ld_x, int x_dtype, const uint8_t *w, const uint8_t *w_scales, const float *bias, int act, int64_t n, int64_t m, int64_t k,
@@ -275,15 +276,17 @@ int pcpp_mx_linear(const void *x, int64_t ld_x, int x_dtype, const uint8_t *w, c
     if (!aligned(x, dtype_bytes(x_dtype))) return invalid(fn, "x must be aligned to its elements");
     if (n == 0) return PCPP_OK;
     if (int rc = check_workspace(fn, workspace, workspace_bytes, pcpp_mx_linear_workspace_bytes(n, m, k))) return rc;
+    MxProductArgs p{};
+    p.b = w; p.b_scales = w_scales; p.bias = bias; p.out = out;
+    p.n = n; p.m = m; p.k = k; p.act = act;
+    if (mx_linear_few(n, k)) return mx_linear_few(p, x, x_dtype, ld_x, out_dtype, stream);
     char *at = static_cast<char *>(workspace);
     MxPackArgs a{};
     a.x = x; a.q = reinterpret_cast<uint8_t *>(at); a.scales = a.q + linear_codes(n, k);
     a.n = n; a.c = k; a.ld_x = ld_x;
     if (int rc = mx_pack(a, x_dtype, stream)) return rc;
-    MxProductArgs p{};
-    p.a = a.q; p.a_scales = a.scales; p.b = w; p.b_scales = w_scales; p.bias = bias; p.out = out;
+    p.a = a.q; p.a_scales = a.scales;
     p.part = reinterpret_cast<float *>(at + linear_codes(n, k) + linear_scales(n, k));
-    p.n = n; p.m = m; p.k = k; p.act = act;
     return mx_product(p, out_dtype, stream);
 }
 

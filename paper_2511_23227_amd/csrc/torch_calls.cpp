@@ -713,9 +713,11 @@ PyObject *mx_linear(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         const int64_t n = x.size(0);
         if (given) need_rows(*given, n, w.n, "out is [n, m], contiguous");
         const Tensor out = given ? *given : empty({n, w.n}, wanted < 0 ? x.scalar_type() : type_of(wanted), x);
-        const Tensor ws = workspace_of(lib.mx_linear_workspace_bytes(n, w.n, w.c), workspace, x);
+        const size_t bytes = lib.mx_linear_workspace_bytes(n, w.n, w.c);
+        Tensor ws;
+        if (bytes) ws = workspace_of(bytes, workspace, x);
         const int rc = lib.mx_linear(x.data_ptr(), pitch(x), code_of(x.scalar_type()), w.q, w.scales, bias_at(bias, w.n), act, n, w.n, w.c, out.data_ptr(),
-                                     code_of(out.scalar_type()), ws.data_ptr(), ws.nbytes(), stream);
+                                     code_of(out.scalar_type()), bytes ? ws.data_ptr() : nullptr, bytes ? ws.nbytes() : 0, stream);
         written(given);
         return result(rc, out);
     });
