@@ -15,11 +15,11 @@ typedef float v4f_anywhere __attribute__((ext_vector_type(4), aligned(4)));
 typedef v2u32 v2u32_anywhere __attribute__((aligned(2)));
 
 
-// BYTE: which byte of the scales
-template <int BYTE> __device__ inline v4f multiply(const v4u &b, const v4u &a, v4f sum, uint32_t b_scale, uint32_t a_scale)
+// which bytes of the scales
+template <int B_BYTE, int A_BYTE = B_BYTE> __device__ inline v4f multiply(const v4u &b, const v4u &a, v4f sum, uint32_t b_scale, uint32_t a_scale)
 {
     const v8i x = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0}, y = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, sum, 4, 4, BYTE, (int)b_scale, BYTE, (int)a_scale);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, sum, 4, 4, B_BYTE, (int)b_scale, A_BYTE, (int)a_scale);
 }
 
 // N neighbouring columns of a row of out, of which `left` are there
@@ -55,14 +55,22 @@ template <typename F> __device__ inline void as_act(int act, F f)
 }
 
 // ---- tiles through LDS --------------------------------------------------------------------------------------------------------------
-// A block of WA x WB waves takes 16 WA FA rows of a and 16 WB FB of b, a wave 16 FA and 16 FB of them.  A stage is 256 elements: of every row 128 bytes of
-// codes and two words of scales, moved straight into LDS, the next stage while the matrix cores work on this one.
+// A block of WA x WB waves takes 16 WA FA rows of a and 16 WB FB of b, a wave 16 FA and 16 FB of them.  A stage is 256 elements: 128 bytes of every row's
+// codes, a whole cache line, moved straight into LDS, and with every second one the sixteen scales of two (a request of eight takes the caches as long as one of a line: 153 us
+// for 130).  (Stages of 128 elements, three of them ahead: 8192 x 8192 x 8192
+// in 401 us for 337.)
 //
-// A row's eight 16-byte pieces (blocks) lie in LDS at piece ^ s, s a function of the row that makes sixteen lanes reading one piece of an instruction's sixteen rows
-// meet all banks.  b's rows go to two instructions in turn, four by four, so that a lane ends with eight neighbouring columns of a row of out.
+// What a wave does meanwhile is laid out by hand.  A stage is two instructions deep.  While the first one's products run the operands of the second are read; then all waves
+// meet, the stage's place in LDS is free, and the stage after the next is requested, two requests at a time between the products (a compute unit takes as long for the requests
+// as for the products).  Half way through the second one's products the next stage, requested one and a half stages ago, is waited for, and the operands of its first are
+// read.
+//
+// A row's eight 16-byte pieces (blocks) lie in LDS at piece ^ s, s a function of the row.  The sixteen lanes whose reads share a cycle are 0-3, 12-15 and 20-27 (or 4-11,
+// 16-19 and 28-31; the same again 32 further on), so of an instruction's rows r 0-3 and 12-15 with one piece and 4-11 with the piece two on: with bit 2 of s set for rows 4-11
+// and its other bits from bits 3 and 1 of r they meet all banks (s = r / 2 mod 8, made for neighbouring lanes, doubled the cycles of every read).  b's rows go to two instructions in turn, four by four, so that a lane ends with eight neighbouring columns of a row of out.
 // Lane (r, l) of an instruction has row r; over the stage's two instructions it takes the blocks 2 l and 2 l + 1, whose scales are one 16-bit read (the order in
 // which blocks are summed is free).
-constexpr int STAGE = 256, STAGE_BYTES = 128, STAGE_BLOCKS = 8;
+constexpr int STAGE = 256, STAGE_BYTES = 128, STAGE_BLOCKS = 8, SCALE_BYTES = 16;         // (a row's scales of two stages)
 
 // rows of a tensor as a descriptor in scalar registers, for inline assembly
 __device__ inline v4u scalar_rows(const uint8_t *p, int64_t first, int64_t n, int64_t pitch, int rows)
@@ -86,9 +94,9 @@ __device__ inline void rows_to_lds_b32(const v4u &rows, uint32_t offset, uint32_
 
 template <int WA, int WB, int FA, int FB> struct Tile {
     static constexpr int A = 16 * WA * FA, B = 16 * WB * FB, WAVES = WA * WB, ROWS = A + B;
-    static constexpr int SCALES_AT = ROWS * STAGE_BYTES, BYTES = ROWS * (STAGE_BYTES + STAGE_BLOCKS);
-    static constexpr int CODE_LOADS = ROWS / 8 / WAVES, SCALE_LOADS = ROWS / 32 / WAVES;     // of a wave for a stage
-    static_assert(A % (16 * WAVES) == 0 && B % (16 * WAVES) == 0 && A % (32 * WAVES) == 0 && B % (32 * WAVES) == 0, "whole loads");
+    static constexpr int CODES = ROWS * STAGE_BYTES, SCALES = ROWS * SCALE_BYTES, BYTES = CODES + SCALES;
+    static constexpr int LOADS = ROWS / 8 / WAVES, SCALE_LOADS = ROWS / 64 / WAVES;          // of a wave for a stage's codes, for two stages' scales
+    static_assert(A % 64 == 0 && ROWS % (64 * WAVES) == 0 && A % (8 * WAVES) == 0 && WAVES % 4 == 0 && LOADS == 2 * FB && FA % 2 == 0 && FB % 2 == 0, "whole loads");
 };
 
 // Which tile a block takes: the blocks of a chiplet (every eighth) take neighbouring tiles, bands of eight rows of tiles column by column, so that its cache
@@ -102,8 +110,9 @@ __device__ inline void tile_of(uint32_t id, uint32_t rows, uint32_t columns, uin
     y = 8u * band + in - x * high;
 }
 
-template <typename T, bool PARTS, int WA, int WB, int FA, int FB>
-__global__ __launch_bounds__(64 * WA * WB, WA *WB == 8 ? 2 : 1) void tile_kernel(const MxProductArgs p, uint32_t tile_rows, uint32_t tile_columns, int64_t stages, int64_t of_part)
+// PARTS: blockIdx.y's part of the sum.  ONE: the sum has one stage
+template <typename T, bool PARTS, bool ONE, int WA, int WB, int FA, int FB>
+__global__ __launch_bounds__(64 * WA * WB, ONE ? 4 : (FA == 8 ? 1 : 2)) void tile_kernel(const MxProductArgs p, uint32_t tile_rows, uint32_t tile_columns, int64_t stages, int64_t of_part)
 {
     typedef Tile<WA, WB, FA, FB> S;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -111,70 +120,130 @@ __global__ __launch_bounds__(64 * WA * WB, WA *WB == 8 ? 2 : 1) void tile_kernel
     uint32_t ty, tx;
     tile_of(blockIdx.x, tile_rows, tile_columns, ty, tx);
     const int64_t i0 = (int64_t)ty * S::A, j0 = (int64_t)tx * S::B;
-    const uint32_t pitch = (uint32_t)mx_row_bytes(p.k), scale_pitch = (uint32_t)mx_scale_bytes(p.k), blocks = (uint32_t)mx_blocks(p.k), words = scale_pitch / 4u;
+    const uint32_t pitch = (uint32_t)mx_row_bytes(p.k), scale_pitch = (uint32_t)mx_scale_bytes(p.k), blocks = (uint32_t)mx_blocks(p.k);
+    const int64_t from = PARTS ? blockIdx.y * of_part : 0, to = PARTS && from + of_part < stages ? from + of_part : stages;
     const v4u aq = scalar_rows(p.a, i0, p.n, pitch, S::A), as = scalar_rows(p.a_scales, i0, p.n, scale_pitch, S::A);
     const v4u bq = scalar_rows(p.b, j0, p.m, pitch, S::B), bs = scalar_rows(p.b_scales, j0, p.m, scale_pitch, S::B);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    // what the lane moves: piece `piece` of rows 8 (wave + i WAVES) + lane / 8, word lane % 2 of rows 32 (wave + i WAVES) + lane / 2
-    const uint32_t a_piece = (uint32_t)(lane & 7) ^ ((4u * (uint32_t)wave + (uint32_t)(lane >> 4)) & 7u);          // s = row / 2 mod 8
-    const uint32_t b_piece = (uint32_t)(lane & 7) ^ (2u * ((uint32_t)wave & 3u) + ((uint32_t)(lane >> 4) & 1u));     // s = 2 (row / 8 mod 4) + row / 2 mod 2
-    const uint32_t code_at = (8u * (uint32_t)wave + (uint32_t)(lane >> 3)) * pitch, word_at = (32u * (uint32_t)wave + (uint32_t)(lane >> 1)) * scale_pitch + 4u * (uint32_t)(lane & 1);
-    auto request = [&](int64_t stage, uint32_t buffer) {
-        const uint32_t to = lds0 + buffer * S::BYTES, block0 = STAGE_BLOCKS * (uint32_t)stage, word = 2u * (uint32_t)stage + (uint32_t)(lane & 1);
-        const uint32_t a_at = block0 + a_piece < blocks ? code_at + 16u * (block0 + a_piece) : OOB_OFFSET, b_at = block0 + b_piece < blocks ? code_at + 16u * (block0 + b_piece) : OOB_OFFSET;
-#pragma unroll
-        for (int i = 0; i < S::CODE_LOADS; ++i) {
-            const bool of_a = 8 * i * S::WAVES < S::A;
-            const uint32_t row = 8u * (uint32_t)i * S::WAVES - (of_a ? 0u : (uint32_t)S::A);
-            const uint32_t at = of_a ? a_at : b_at;
-            rows_to_lds_b128(of_a ? aq : bq, at == OOB_OFFSET ? at : at + row * pitch, to + (uint32_t)(8 * (wave + i * S::WAVES)) * STAGE_BYTES);
-        }
+    // what the lane moves: a piece of rows 8 (wave + i WAVES) + lane / 8, the scales of row 64 wave + lane
+    auto spread = [](uint32_t bit3, uint32_t bit2, uint32_t bit1) { return ((bit2 ^ bit3) & 1u) << 2 | (bit3 & 1u) << 1 | (bit1 & 1u); };
+    const uint32_t wv = (uint32_t)wave, ln = (uint32_t)lane;
+    const uint32_t a_piece = (ln & 7u) ^ spread(wv, ln >> 5, ln >> 4), b_piece = (ln & 7u) ^ spread(wv >> 1, wv, ln >> 4);
+    const uint32_t a_code_at = (8u * wv + (ln >> 3)) * pitch + 16u * a_piece, b_code_at = (8u * wv + (ln >> 3)) * pitch + 16u * b_piece;
+    const uint32_t scale_at = (64u * wv + ln) * scale_pitch;
+    const uint32_t some_blocks = (uint64_t)blocks < 8u * (uint64_t)to ? blocks : 8u * (uint32_t)to;
+    // the i-th of a wave's requests for a stage (past the part's last one: of nothing)
+    auto request = [&](uint32_t stage, uint32_t to_lds, int i) {
+        const bool of_a = 8 * i * S::WAVES < S::A;
+        const uint32_t row = 8u * (uint32_t)i * S::WAVES - (of_a ? 0u : (uint32_t)S::A), at = row * pitch + STAGE_BYTES * stage;
+        rows_to_lds_b128(of_a ? aq : bq, STAGE_BLOCKS * stage + (of_a ? a_piece : b_piece) < some_blocks ? at + (of_a ? a_code_at : b_code_at) : OOB_OFFSET,
+                         to_lds + (uint32_t)(8 * (wave + i * S::WAVES)) * STAGE_BYTES);
+    };
+    // of two stages from an even one of the part on (behind a row's last scales the next row's, which count for nothing)
+    auto request_scales = [&](uint32_t stage, uint32_t to_lds) {
 #pragma unroll
         for (int i = 0; i < S::SCALE_LOADS; ++i) {
-            const bool of_a = 32 * i * S::WAVES < S::A;
-            const uint32_t row = 32u * (uint32_t)i * S::WAVES - (of_a ? 0u : (uint32_t)S::A);
-            rows_to_lds_b32(of_a ? as : bs, word < words ? word_at + row * scale_pitch + 8u * (uint32_t)stage : OOB_OFFSET,
-                            to + S::SCALES_AT + (uint32_t)(32 * (wave + i * S::WAVES)) * STAGE_BLOCKS);
+            const bool of_a = S::SCALE_LOADS > 1 ? 64 * i * S::WAVES < S::A : wave < S::A / 64;
+            const uint32_t row = 64u * (uint32_t)i * S::WAVES - (of_a ? 0u : (uint32_t)S::A);
+            rows_to_lds_b128(of_a ? as : bs, STAGE_BLOCKS * stage < some_blocks ? scale_at + row * scale_pitch + STAGE_BLOCKS * stage : OOB_OFFSET,
+                             to_lds + 1024u * (wv + (uint32_t)i * S::WAVES));
         }
     };
     const int wa = wave / WB, wb = wave % WB;
     const int b_row = 8 * (r >> 2) + (r & 3);                     // of the even one of two instructions; the odd one's are four further on, with the same s
-    const uint32_t read_a = (uint32_t)r * STAGE_BYTES + 16u * ((2u * (uint32_t)l) ^ ((uint32_t)r >> 1 & 7u));
-    const uint32_t read_b = (uint32_t)b_row * STAGE_BYTES + 16u * ((2u * (uint32_t)l) ^ (2u * ((uint32_t)r >> 2) + ((uint32_t)r >> 1 & 1u)));
+    const uint32_t own_s = spread((uint32_t)r >> 3, (uint32_t)r >> 2, (uint32_t)r >> 1), in_row = 16u * ((2u * (uint32_t)l) ^ own_s);
+    const uint32_t read_a = (uint32_t)r * STAGE_BYTES + in_row, read_b = (uint32_t)b_row * STAGE_BYTES + in_row;
     v4f sum[FA][FB];
 #pragma unroll
     for (int y = 0; y < FA; ++y)
 #pragma unroll
         for (int x = 0; x < FB; ++x) sum[y][x] = v4f{0.f, 0.f, 0.f, 0.f};
-    const int64_t from = PARTS ? blockIdx.y * of_part : 0, to = PARTS && from + of_part < stages ? from + of_part : stages;
-    request(from, 0u);
-    for (int64_t s = from; s < to; ++s) {
-        const uint32_t buffer = (uint32_t)(s - from) & 1u;
-        // this stage has arrived, and all waves are done with the one before, whose place the next one takes
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < to) request(s + 1, buffer ^ 1u);
-        const uint8_t *codes = lds + buffer * S::BYTES, *scales = codes + S::SCALES_AT;
-        const uint32_t left = blocks - STAGE_BLOCKS * (uint32_t)s, own = 2u * (uint32_t)l;   // (scales behind a row's last block may be anything)
-        const uint32_t mask = (own < left ? 0xffu : 0u) | (own + 1u < left ? 0xff00u : 0u);
-        uint32_t sa[FA], sb[FB];
+    v4u va[2][FA], vb[2][FB];
+    uint32_t sa[FA / 2], sb[FB / 2];                              // two rows' scales of a stage in a word
+    auto read_a_rows = [&](const uint8_t *codes, int t) {
 #pragma unroll
-        for (int y = 0; y < FA; ++y) sa[y] = *reinterpret_cast<const uint16_t *>(scales + (16 * (wa * FA + y) + r) * STAGE_BLOCKS + 2 * l) & mask;
+        for (int y = 0; y < FA; ++y) va[t][y] = *reinterpret_cast<const v4u *>(codes + (read_a ^ (16u * t)) + 16 * (wa * FA + y) * STAGE_BYTES);
+    };
+    auto read_b_row = [&](const uint8_t *codes, int t, int x) {
+        vb[t][x] = *reinterpret_cast<const v4u *>(codes + S::A * STAGE_BYTES + (read_b ^ (16u * t)) + (16 * (wb * FB + (x & ~1)) + 4 * (x & 1)) * STAGE_BYTES);
+    };
+    auto read_scales = [&](const uint8_t *from_lds, uint32_t stage) {
+        const uint8_t *scales = from_lds + 2 * l;
+        auto half = [&](int row) { return (uint32_t)*reinterpret_cast<const uint16_t *>(scales + row * SCALE_BYTES); };
+        const uint32_t own = STAGE_BLOCKS * stage + 2u * (uint32_t)l;    // (scales behind a row's last block may be anything)
+        const uint32_t mask = ((own < blocks ? 0xffu : 0u) | (own + 1u < blocks ? 0xff00u : 0u)) * 0x10001u;
 #pragma unroll
-        for (int x = 0; x < FB; ++x) sb[x] = *reinterpret_cast<const uint16_t *>(scales + (S::A + 16 * (wb * FB + (x & ~1)) + 4 * (x & 1) + b_row) * STAGE_BLOCKS + 2 * l) & mask;
+        for (int y = 0; y < FA; y += 2) sa[y / 2] = (half(16 * (wa * FA + y) + r) | half(16 * (wa * FA + y + 1) + r) << 16) & mask;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint8_t *at_a = codes + (read_a ^ (16u * t)), *at_b = codes + S::A * STAGE_BYTES + (read_b ^ (16u * t));
-            v4u va[FA], vb[FB];
+        for (int x = 0; x < FB; x += 2) sb[x / 2] = (half(S::A + 16 * (wb * FB + x) + b_row) | half(S::A + 16 * (wb * FB + x) + 4 + b_row) << 16) & mask;
+    };
+    auto products = [&](auto t, int x) {
+        constexpr int D = decltype(t)::value;
 #pragma unroll
-            for (int x = 0; x < FB; ++x) vb[x] = *reinterpret_cast<const v4u *>(at_b + (16 * (wb * FB + (x & ~1)) + 4 * (x & 1)) * STAGE_BYTES);
-#pragma unroll
-            for (int y = 0; y < FA; ++y) va[y] = *reinterpret_cast<const v4u *>(at_a + 16 * (wa * FA + y) * STAGE_BYTES);
-#pragma unroll
-            for (int y = 0; y < FA; ++y)
-#pragma unroll
-                for (int x = 0; x < FB; ++x) sum[y][x] = t == 0 ? multiply<0>(vb[x], va[y], sum[y][x], sb[x], sa[y]) : multiply<1>(vb[x], va[y], sum[y][x], sb[x], sa[y]);
+        for (int y = 0; y < FA; ++y) {
+            const v4u &b = vb[D][x], &a = va[D][y];
+            if (x % 2 == 0) sum[y][x] = y % 2 == 0 ? multiply<D, D>(b, a, sum[y][x], sb[x / 2], sa[y / 2]) : multiply<D, 2 + D>(b, a, sum[y][x], sb[x / 2], sa[y / 2]);
+            else sum[y][x] = y % 2 == 0 ? multiply<2 + D, D>(b, a, sum[y][x], sb[x / 2], sa[y / 2]) : multiply<2 + D, 2 + D>(b, a, sum[y][x], sb[x / 2], sa[y / 2]);
         }
+    };
+    // in LDS: the codes of an even and an odd stage of the part, the scales of an even and an odd pair of stages
+    constexpr uint32_t SCALES_AT = (ONE ? 1 : 2) * S::CODES;
+    const uint32_t first = (uint32_t)from, last = (uint32_t)to;
+    request_scales(first, lds0 + SCALES_AT);
+#pragma unroll
+    for (int j = 0; j < (ONE ? 1 : 2); ++j)
+#pragma unroll
+        for (int i = 0; i < S::LOADS; ++i) request(first + j, lds0 + j * S::CODES, i);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(ONE ? 0 : S::LOADS) : "memory");
+    read_a_rows(lds, 0);
+    read_scales(lds + SCALES_AT, first);
+#pragma unroll
+    for (int x = 0; x < FB; ++x) read_b_row(lds, 0, x);
+    uint32_t at = 0u;                                             // of the stage's codes in LDS
+    for (uint32_t s = first; ONE ? s == first : s < last; ++s) {
+        const uint32_t nth = s - first, next = S::CODES - at;
+        auto scales_at = [&](uint32_t nth) { return SCALES_AT + (nth >> 1 & 1u) * S::SCALES; };
+        if (!ONE && nth % 2u == 0u) request_scales(s + 2u, lds0 + scales_at(nth + 2u));
+        // (no branches from here on: the compiler would move the products behind them)
+        read_a_rows(lds + at, 1);
+#pragma unroll
+        for (int x = 0; x < FB / 2; ++x) {
+            read_b_row(lds + at, 1, 2 * x);
+            read_b_row(lds + at, 1, 2 * x + 1);
+            products(Int<0>{}, x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!ONE) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        auto go_on = [&](auto t, int x, int i) {
+            if constexpr (!ONE) {
+                request(s + 2u, lds0 + at, i);
+                request(s + 2u, lds0 + at, i + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            products(t, x);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+#pragma unroll
+        for (int x = 0; x < FB / 2; ++x) go_on(Int<0>{}, FB / 2 + x, 2 * x);
+#pragma unroll
+        for (int x = 0; x < FB / 2; ++x) go_on(Int<1>{}, x, FB + 2 * x);
+        if constexpr (!ONE) {
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(S::LOADS) : "memory");
+            read_a_rows(lds + next, 0);
+        }
+#pragma unroll
+        for (int x = FB / 2; x < FB; ++x) {
+            if constexpr (!ONE) {
+                read_b_row(lds + next, 0, 2 * x - FB);
+                read_b_row(lds + next, 0, 2 * x - FB + 1);
+            }
+            products(Int<1>{}, x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!ONE) read_scales(lds + scales_at(nth + 1u) + (nth + 1u) % 2u * STAGE_BLOCKS, s + 1u);
+        at = next;
     }
+    if constexpr (!ONE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (nothing of this wave is still on its way into LDS)
     as_act(PARTS ? PCPP_ACT_NONE : p.act, [&](auto act) {
 #pragma unroll
         for (int x = 0; x < FB; x += 2) {
@@ -340,12 +409,12 @@ Shape shape_of(int64_t n, int64_t m, int64_t k)
     return s;
 }
 
-template <typename T, bool PARTS, int WA, int WB, int FA, int FB> int launch_tiles(const MxProductArgs &p, const Shape &s, hipStream_t stream)
+template <typename T, bool PARTS, bool ONE, int WA, int WB, int FA, int FB> int launch_tiles(const MxProductArgs &p, const Shape &s, hipStream_t stream)
 {
     typedef Tile<WA, WB, FA, FB> L;
-    const auto kernel = tile_kernel<T, PARTS, WA, WB, FA, FB>;
-    const size_t bytes = (size_t)(s.of_part > 1 ? 2 : 1) * L::BYTES;
-    if (int rc = raise_lds_limit(reinterpret_cast<const void *>(kernel), 2 * L::BYTES)) return rc;
+    const auto kernel = tile_kernel<T, PARTS, ONE, WA, WB, FA, FB>;
+    constexpr size_t bytes = (ONE ? 1 : 2) * (size_t)L::BYTES;
+    if (int rc = raise_lds_limit(reinterpret_cast<const void *>(kernel), bytes)) return rc;
     // pieces of whole bands whose blocks a grid holds
     const int64_t most = s.columns > (1 << 22) ? 1 : (1 << 22) / s.columns;
     for (int64_t y = 0; y < s.rows; y += most) {
@@ -397,11 +466,12 @@ int mx_product(const MxProductArgs &p, int out_dtype, hipStream_t stream)
             return PCPP_OK;
         }
         if (s.parts > 1) {
-            if (int rc = launch_tiles<float, true, 2, 2, 4, 4>(p, s, stream)) return rc;
+            if (int rc = launch_tiles<float, true, false, 2, 2, 4, 4>(p, s, stream)) return rc;
             join_kernel<T><<<(unsigned)ceil_div(p.n * p.m, 256), 1024, 0, stream>>>(p, (int)s.parts, make_divisor((uint32_t)p.m));
             return PCPP_OK;
         }
-        return s.large ? launch_tiles<T, false, 4, 2, 4, 8>(p, s, stream) : launch_tiles<T, false, 2, 2, 4, 4>(p, s, stream);
+        if (s.large) return launch_tiles<T, false, false, 2, 2, 8, 8>(p, s, stream);
+        return s.stages == 1 ? launch_tiles<T, false, true, 2, 2, 4, 4>(p, s, stream) : launch_tiles<T, false, false, 2, 2, 4, 4>(p, s, stream);
     };
     if (int rc = out_dtype == PCPP_F32 ? with(float{}) : with(bf16_t{})) return rc;
     PCPP_HIP_CHECK(hipGetLastError());
