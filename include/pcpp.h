@@ -434,7 +434,7 @@ PCPP_API int pcpp_dropout_bwd(const void *dy, const int64_t *random, uint32_t si
  *   workspace  pcpp_group_norm_workspace_bytes(n, c, n_clouds, groups, 1) bytes
  * Arithmetic is fp32, each output is rounded once; sums have one order: the same result each time.  Outputs may not overlap inputs.
  * Errors: INVALID_ARG (also: groups do not divide c, eps not finite or below 2^-126, p outside 0 .. 1), WORKSPACE, UNSUPPORTED (c
- * outside 1..1024, n >= 2^31, pitch >= 2^24, dtype, too many random numbers).
+ * outside 1..1024, n >= 2^31, pitch >= 2^22, dtype, too many random numbers).
  * ------------------------------------------------------------------------------------------- */
 #define PCPP_ACT_NONE  0
 #define PCPP_ACT_RELU  1

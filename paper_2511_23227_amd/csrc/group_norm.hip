@@ -20,7 +20,7 @@ namespace {
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int64_t SMALL = 16384;                                  // elements that one block goes through alone
 
-// A lane's channels and weights
+// A lane's channels.  ALIKE: the groups are of whole eights, so a lane's eight channels are of one group and have one mean.
 template <int LPR, int G, int MODE> struct Lane {
     int c0[G];
     Span<MODE> own[G];
@@ -31,6 +31,10 @@ template <int LPR, int G, int MODE> struct Lane {
         row = (uint32_t)(lane / LPR);
 #pragma unroll
         for (int g = 0; g < G; ++g) c0[g] = 8 * (lane % LPR) + 8 * LPR * g, own[g] = Span<MODE>(c0[g], c);
+    }
+    template <typename T> __device__ inline uint32_t offset(int g, uint32_t row_at, int64_t pitch) const
+    {
+        return own[g].template offset<sizeof(T)>(row_at * (uint32_t)pitch);
     }
 };
 __device__ inline int wave_of() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
@@ -77,6 +81,27 @@ __device__ inline void keep_bits(const Philox &philox, uint32_t at, int c, uint3
         }
     }
 }
+// Zero for what goes (not scaled)
+template <int LPR, int G, int MODE>
+__device__ inline void drop_rows(const Philox &philox, uint32_t at, int c, const Drop &drop, const Lane<LPR, G, MODE> &lane, float (&v)[G][8])
+{
+    if constexpr (MODE == RAGGED) {
+        uint32_t bits[G];
+        keep_bits(philox, at, c, drop.threshold, lane, bits);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[g][e] = bits[g] >> e & 1u ? v[g][e] : 0.f;
+    } else {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            uint32_t x[4];
+            philox.draw(at * (uint32_t)((c + 7) / 8) + (uint32_t)lane.c0[g] / 8u, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[g][e] = half_of(x, e) >= drop.threshold ? v[g][e] : 0.f;
+        }
+    }
+}
 
 template <int ACT> struct Act { static constexpr int value = ACT; };
 // f(activation): a branch that all lanes take alike
@@ -88,6 +113,23 @@ template <typename F> __device__ inline void as_act(int act, F f)
     else f(Act<PCPP_ACT_NONE>{});
 }
 
+// v over the lanes of a wave that hold the same channels of other rows: every LPR-th lane
+template <int LPR> __device__ inline float rows_sum(float v)
+{
+    auto ring = [&](auto by) { v += __uint_as_float(dpp<DPP_ROR + decltype(by)::value>(__float_as_uint(v))); };
+    if constexpr (LPR <= 4) ring(Int<4>{});
+    if constexpr (LPR <= 8) ring(Int<8>{});
+    if constexpr (LPR <= 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (LPR <= 32) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    return v;
+}
+
 // Two sums for every channel over the rows of a wave's lanes, then over the waves: [2][CP] in `total`.  (CP: channels in whole lanes)
 template <int LPR, int G, int MODE, int CP>
 __device__ inline void channel_sums(const float (&p)[G][8], const float (&q)[G][8], const Lane<LPR, G, MODE> &lane, int c, float (*sums)[2][CP], float (*total)[CP])
@@ -97,12 +139,7 @@ __device__ inline void channel_sums(const float (&p)[G][8], const float (&q)[G][
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float a = p[g][e], b = q[g][e];
-#pragma unroll
-            for (int m = LPR; m < 64; m <<= 1) {
-                a += __shfl_xor(a, m);
-                b += __shfl_xor(b, m);
-            }
+            const float a = rows_sum<LPR>(p[g][e]), b = rows_sum<LPR>(q[g][e]);
             if (l < LPR && lane.own[g].own(e)) {
                 sums[wave][0][lane.own[g].at + e] = a;
                 sums[wave][1][lane.own[g].at + e] = b;
@@ -119,11 +156,11 @@ __device__ inline void channel_sums(const float (&p)[G][8], const float (&q)[G][
     __syncthreads();
 }
 
-// For every group f(first channel, lane among `per`, per, sum over those lanes) by neighbouring lanes of a wave
-template <typename F> __device__ inline void for_groups(int groups, F f)
+// For every group f(group, lane among `per`, per, sum over those lanes, whether it is one) by neighbouring lanes of a wave
+template <typename F> __device__ inline void for_groups(int groups, int width, F f)
 {
     int per = 64;
-    while (per > 1 && per * groups > THREADS) per >>= 1;
+    while (per > 1 && (per * groups > THREADS || per >= 2 * width)) per >>= 1;
     const int lane = (int)threadIdx.x % per;
     auto sum = [&](float v) {
         for (int m = 1; m < per; m <<= 1) v += __shfl_xor(v, m);
@@ -140,14 +177,14 @@ template <typename T, int LPR, int G, int MODE, int CP, typename F>
 __device__ inline void range_statistics(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, float (*sums)[2][CP], float (*total)[CP],
                                         float *shift, F f)
 {
-    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
+    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, AT_ONCE = sizeof(T) * G > 4 ? 2 : 4;
     const int c = a.c;
     float k[G][8], s[G][8], q[G][8];
-    const __amdgpu_buffer_rsrc_t ks = rows_from<ES>(a.x, lo, hi, a.ld_x, c, 1);
+    const __amdgpu_buffer_rsrc_t ks = rows_from<sizeof(T)>(a.x, lo, hi, a.ld_x, c, 1);
 #pragma unroll
     for (int g = 0; g < G; ++g) {
         Eight<T> raw;
-        row_load<T>(ks, lane.own[g].template offset<ES>(0u), lane.own[g], raw);
+        row_load<T>(ks, lane.template offset<T>(g, 0u, 0), lane.own[g], raw);
         to_floats(raw, k[g]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -155,22 +192,32 @@ __device__ inline void range_statistics(const GroupNormArgs &a, int64_t lo, int6
             if ((int)threadIdx.x < LPR && lane.own[g].own(e)) shift[lane.own[g].at + e] = k[g][e];
         }
     }
-    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += WAVES * ROWS) {
-        const __amdgpu_buffer_rsrc_t xs = rows_from<ES>(a.x, first, hi, a.ld_x, c, ROWS);
-        const bool live = first + lane.row < hi;
+    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += AT_ONCE * STEP) {
+        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, c, AT_ONCE * STEP);
+        Eight<T> raw[AT_ONCE][G];
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            Eight<T> raw;
-            float v[8];
-            row_load<T>(xs, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.ld_x), lane.own[g], raw);
-            to_floats(raw, v);
+        for (int u = 0; u < AT_ONCE; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = live ? v[e] - k[g][e] : 0.f;
-                s[g][e] += d;
-                q[g][e] = __builtin_fmaf(d, d, q[g][e]);
+            for (int g = 0; g < G; ++g) row_load<T>(xs, lane.template offset<T>(g, (uint32_t)(u * STEP) + lane.row, a.ld_x), lane.own[g], raw[u][g]);
+        auto add = [&](auto all) {
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const bool live = decltype(all)::value || first + u * STEP + lane.row < hi;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    float v[8];
+                    to_floats(raw[u][g], v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float d = live ? v[e] - k[g][e] : 0.f;
+                        s[g][e] += d;
+                        q[g][e] = __builtin_fmaf(d, d, q[g][e]);
+                    }
+                }
             }
-        }
+        };
+        if (first + (AT_ONCE - 1) * STEP + ROWS <= hi) add(Int<1>{});
+        else add(Int<0>{});
     }
     channel_sums<LPR, G, MODE, CP>(s, q, lane, c, sums, total);
     const float rows = (float)(hi - lo), inv = 1.f / rows;
@@ -181,12 +228,11 @@ __device__ inline void range_statistics(const GroupNormArgs &a, int64_t lo, int6
     }
     __syncthreads();
     const int width = c / a.groups;
-    for_groups(a.groups, [&](int group, int l, int per, auto sum, bool write) {
+    for_groups(a.groups, width, [&](int group, int l, int per, auto sum, bool write) {
         float mean = 0.f, m2 = 0.f, about = 0.f;
         const float pivot = total[0][group * width];
         for (int i = l; i < width; i += per) {
-            const float d = total[0][group * width + i] - pivot;
-            mean += d;
+            mean += total[0][group * width + i] - pivot;
             m2 += total[1][group * width + i];
         }
         mean = sum(mean) / (float)width;
@@ -200,111 +246,164 @@ __device__ inline void range_statistics(const GroupNormArgs &a, int64_t lo, int6
     __syncthreads();                                              // (the sums are free again)
 }
 
-// The lane's channels' mean and rstd; stats: [groups][2] of the cloud
-template <int LPR, int G, int MODE>
-__device__ inline void lane_statistics(const float *stats, const Divisor &width, const Lane<LPR, G, MODE> &lane, float (&mean)[G][8], float (&rstd)[G][8])
+// One of the two numbers of a group for each of the lane's channels; pairs: [groups][2] of a cloud
+template <bool ALIKE, int LPR, int G, int MODE>
+__device__ inline void lane_pairs(const float *pairs, const Divisor &width, const Lane<LPR, G, MODE> &lane, float (&first)[G][ALIKE ? 1 : 8], float (&second)[G][ALIKE ? 1 : 8])
 {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < (ALIKE ? 1 : 8); ++e) {
+            const bool there = lane.own[g].any() && (MODE != NARROW || e < lane.own[g].n);
+            const uint32_t group = there ? width.quotient((uint32_t)(lane.own[g].at + e)) : 0u;
+            first[g][e] = pairs[2u * group];
+            second[g][e] = pairs[2u * group + 1u];
+        }
+}
+
+// y of rows [lo, hi): z = x by + off
+template <bool ALIKE, typename T, int LPR, int G, int MODE>
+__device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width,
+                                   const Philox &philox)
+{
+    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, AT_ONCE = sizeof(T) * G > 4 ? 1 : 2;
+    const int c = a.c;
+    float by[G][8], off[G][8], mean[G][ALIKE ? 1 : 8], rstd[G][ALIKE ? 1 : 8];
+    load_affine(a.w, 1.f, lane.own, a.c, by);
+    load_affine(a.b, 0.f, lane.own, a.c, off);
+    lane_pairs<ALIKE>(stats, width, lane, mean, rstd);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const bool there = lane.own[g].any() && (MODE != NARROW || e < lane.own[g].n);
-            const uint32_t group = there ? width.quotient((uint32_t)(lane.own[g].at + e)) : 0u;
-            mean[g][e] = stats[2u * group];
-            rstd[g][e] = stats[2u * group + 1u];
+            by[g][e] *= rstd[g][ALIKE ? 0 : e];
+            off[g][e] = __builtin_fmaf(-mean[g][ALIKE ? 0 : e], by[g][e], off[g][e]);
         }
-}
-
-// y of rows [lo, hi)
-template <typename T, int LPR, int G, int MODE>
-__device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8], const float (&b)[G][8],
-                                   const float *stats, const Divisor &width, const Philox &philox)
-{
-    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
-    const int c = a.c;
-    float mean[G][8], rstd[G][8];
-    lane_statistics(stats, width, lane, mean, rstd);
-    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += WAVES * ROWS) {
-        const __amdgpu_buffer_rsrc_t xs = rows_from<ES>(a.x, first, hi, a.ld_x, c, ROWS), ys = rows_from<ES>(a.y, first, hi, c, c, ROWS);
-        Eight<T> raw[G];
+    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += AT_ONCE * STEP) {
+        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, c, AT_ONCE * STEP), ys = rows_from<sizeof(T)>(a.y, first, hi, c, c, AT_ONCE * STEP);
+        Eight<T> raw[AT_ONCE][G];
 #pragma unroll
-        for (int g = 0; g < G; ++g) row_load<T>(xs, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.ld_x), lane.own[g], raw[g]);
-        uint32_t bits[G];
-        if (a.drop.threshold) keep_bits(philox, (uint32_t)first + lane.row, c, a.drop.threshold, lane, bits);
+        for (int u = 0; u < AT_ONCE; ++u)
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            float v[8];
-            to_floats(raw[g], v);
+            for (int g = 0; g < G; ++g) row_load<T>(xs, lane.template offset<T>(g, (uint32_t)(u * STEP) + lane.row, a.ld_x), lane.own[g], raw[u][g]);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const uint32_t row = (uint32_t)(u * STEP) + lane.row;
+            float v[G][8];
+#pragma unroll
+            for (int g = 0; g < G; ++g) to_floats(raw[u][g], v[g]);
             as_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = activate<decltype(act)::value>(__builtin_fmaf(w[g][e], (v[e] - mean[g][e]) * rstd[g][e], b[g][e]));
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[g][e] = activate<decltype(act)::value>(__builtin_fmaf(v[g][e], by[g][e], off[g][e]));
             });
             if (a.drop.threshold) {
+                drop_rows(philox, (uint32_t)first + row, c, a.drop, lane, v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = bits[g] >> e & 1u ? v[e] * a.drop.scale : 0.f;
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[g][e] *= a.drop.scale;
             }
-            row_store<T>(ys, lane.own[g].template offset<ES>(lane.row * (uint32_t)c), lane.own[g], v);
+#pragma unroll
+            for (int g = 0; g < G; ++g) row_store<T>(ys, lane.template offset<T>(g, row, c), lane.own[g], v[g]);
         }
     }
 }
 
-// What flows to z, and v, of a wave's rows from `first` on: f(element, dz, v) for all of the lane's, zeros in rows past the last
-template <typename T, int LPR, int G, int MODE, typename F>
-__device__ inline void gradient_rows(const GroupNormArgs &a, int64_t first, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8],
-                                     const float (&b)[G][8], const float (&mean)[G][8], const float (&rstd)[G][8], const Philox &philox, F f)
-{
-    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
-    const int c = a.c;
-    const __amdgpu_buffer_rsrc_t xs = rows_from<ES>(a.x, first, hi, a.ld_x, c, ROWS), ds = rows_from<ES>(a.dy, first, hi, c, c, ROWS);
-    const bool live = first + lane.row < hi;
-    Eight<T> xr[G], dr[G];
+// What the gradients' two passes know of a lane's channels.  v = x rstd + shift, z = x by + off
+template <bool ALIKE, int G> struct Known {
+    float rstd[G][ALIKE ? 1 : 8], shift[G][ALIKE ? 1 : 8], by[G][8], off[G][8];
+    template <int LPR, int MODE>
+    __device__ inline void load(const GroupNormArgs &a, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width)
+    {
+        load_affine(a.w, 1.f, lane.own, a.c, by);
+        load_affine(a.b, 0.f, lane.own, a.c, off);
+        lane_pairs<ALIKE>(stats, width, lane, shift, rstd);
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        row_load<T>(xs, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.ld_x), lane.own[g], xr[g]);
-        row_load<T>(ds, lane.own[g].template offset<ES>(lane.row * (uint32_t)c), lane.own[g], dr[g]);
-    }
-    uint32_t bits[G];
-    if (a.drop.threshold) keep_bits(philox, (uint32_t)first + lane.row, c, a.drop.threshold, lane, bits);
+        for (int g = 0; g < G; ++g) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        float v[8], d[8];
-        to_floats(xr[g], v);
-        to_floats(dr[g], d);
+            for (int e = 0; e < 8; ++e) {
+                by[g][e] *= rstd[g][ALIKE ? 0 : e];
+                off[g][e] = __builtin_fmaf(-shift[g][ALIKE ? 0 : e], by[g][e], off[g][e]);
+            }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = live ? (v[e] - mean[g][e]) * rstd[g][e] : 0.f;
-        if (a.drop.threshold) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d[e] = bits[g] >> e & 1u ? d[e] * a.drop.scale : 0.f;
+            for (int e = 0; e < (ALIKE ? 1 : 8); ++e) shift[g][e] *= -rstd[g][e];
         }
+    }
+};
+
+// Rows of x and dy on their way
+template <typename T, int G> struct Rows {
+    Eight<T> x[G], dy[G];
+    template <int LPR, int MODE>
+    __device__ inline void load(const GroupNormArgs &a, const __amdgpu_buffer_rsrc_t &xs, const __amdgpu_buffer_rsrc_t &ds, uint32_t row, const Lane<LPR, G, MODE> &lane)
+    {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            row_load<T>(xs, lane.template offset<T>(g, row, a.ld_x), lane.own[g], x[g]);
+            row_load<T>(ds, lane.template offset<T>(g, row, a.c), lane.own[g], dy[g]);
+        }
+    }
+    // x and what flows to z, without the scale of the dropout; zeros in rows past the last
+    template <bool ALIKE, int LPR, int MODE>
+    __device__ inline void gradient(const GroupNormArgs &a, const Known<ALIKE, G> &known, uint32_t at, const Lane<LPR, G, MODE> &lane, const Philox &philox, float (&xv)[G][8],
+                                    float (&d)[G][8]) const
+    {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            to_floats(x[g], xv[g]);
+            to_floats(dy[g], d[g]);
+        }
+        if (a.drop.threshold) drop_rows(philox, at, a.c, a.drop, lane, d);
         as_act(a.act, [&](auto act) {
             if constexpr (decltype(act)::value != PCPP_ACT_NONE) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] *= slope<decltype(act)::value>(__builtin_fmaf(w[g][e], v[e], b[g][e]));
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[g][e] *= slope<decltype(act)::value>(__builtin_fmaf(xv[g][e], known.by[g][e], known.off[g][e]));
             }
         });
-        f(g, d, v);
     }
-}
+};
 
 // Sums of dz and dz v of every channel over rows [lo, hi), not empty: [2][CP] in `total`
-template <typename T, int LPR, int G, int MODE, int CP>
-__device__ inline void range_gradients(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8], const float (&b)[G][8],
-                                       const float *stats, const Divisor &width, const Philox &philox, float (*sums)[2][CP], float (*total)[CP])
+template <bool ALIKE, typename T, int LPR, int G, int MODE, int CP>
+__device__ inline void range_gradients(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width,
+                                       const Philox &philox, float (*sums)[2][CP], float (*total)[CP])
 {
-    float mean[G][8], rstd[G][8], s[G][8], q[G][8];
-    lane_statistics(stats, width, lane, mean, rstd);
+    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, AT_ONCE = sizeof(T) * G > 4 ? 1 : 2;
+    Known<ALIKE, G> known;
+    known.load(a, lane, stats, width);
+    float s[G][8], q[G][8];
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[g][e] = q[g][e] = 0.f;
-    for (int64_t first = lo + (int64_t)wave_of() * (64 / LPR); first < hi; first += WAVES * (64 / LPR))
-        gradient_rows<T>(a, first, hi, lane, w, b, mean, rstd, philox, [&](int g, const float (&d)[8], const float (&v)[8]) {
+    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += AT_ONCE * STEP) {
+        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, a.c, AT_ONCE * STEP), ds = rows_from<sizeof(T)>(a.dy, first, hi, a.c, a.c, AT_ONCE * STEP);
+        Rows<T, G> rows[AT_ONCE];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                s[g][e] += d[e];
-                q[g][e] = __builtin_fmaf(d[e], v[e], q[g][e]);
-            }
-        });
+        for (int u = 0; u < AT_ONCE; ++u) rows[u].load(a, xs, ds, (uint32_t)(u * STEP) + lane.row, lane);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            float x[G][8], d[G][8];
+            rows[u].gradient(a, known, (uint32_t)(first + u * STEP) + lane.row, lane, philox, x, d);
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[g][e] += d[g][e];
+                    q[g][e] = __builtin_fmaf(d[g][e], __builtin_fmaf(x[g][e], known.rstd[g][ALIKE ? 0 : e], known.shift[g][ALIKE ? 0 : e]), q[g][e]);
+                }
+        }
+    }
+    if (a.drop.threshold) {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[g][e] *= a.drop.scale, q[g][e] *= a.drop.scale;
+    }
     channel_sums<LPR, G, MODE, CP>(s, q, lane, a.c, sums, total);
 }
 
@@ -313,7 +412,7 @@ template <int CP> __device__ inline void group_means(const GroupNormArgs &a, con
 {
     const int width = a.c / a.groups;
     const float inv = (float)(1.0 / (rows * (double)width));
-    for_groups(a.groups, [&](int group, int l, int per, auto sum, bool write) {
+    for_groups(a.groups, width, [&](int group, int l, int per, auto sum, bool write) {
         float m1 = 0.f, m2 = 0.f;
         for (int i = group * width + l; i < (group + 1) * width; i += per) {
             const float w = a.w ? a.w[i] : 1.f;
@@ -327,23 +426,45 @@ template <int CP> __device__ inline void group_means(const GroupNormArgs &a, con
     __syncthreads();
 }
 
-// dx of rows [lo, hi)
-template <typename T, int LPR, int G, int MODE>
-__device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float (&w)[G][8],
-                                      const float (&b)[G][8], const float *stats, const float *coef, const Divisor &width, const Philox &philox)
+// dx of rows [lo, hi):  rstd (w dz - m1 - v m2) = dz (w rstd) + x (-rstd^2 m2) - rstd (m1 + shift m2)
+template <bool ALIKE, typename T, int LPR, int G, int MODE>
+__device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const float *coef,
+                                      const Divisor &width, const Philox &philox)
 {
-    constexpr int ROWS = 64 / LPR, ES = sizeof(T);
-    float mean[G][8], rstd[G][8], m1[G][8], m2[G][8];
-    lane_statistics(stats, width, lane, mean, rstd);
-    lane_statistics(coef, width, lane, m1, m2);
-    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += WAVES * ROWS) {
-        const __amdgpu_buffer_rsrc_t os = rows_from<ES>(a.dx, first, hi, a.c, a.c, ROWS);
-        gradient_rows<T>(a, first, hi, lane, w, b, mean, rstd, philox, [&](int g, const float (&d)[8], const float (&v)[8]) {
-            float o[8];
+    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, AT_ONCE = sizeof(T) * G > 4 ? 1 : 2, N = ALIKE ? 1 : 8;
+    Known<ALIKE, G> known;
+    known.load(a, lane, stats, width);
+    float m1[G][N], m2[G][N], of_d[G][8];
+    lane_pairs<ALIKE>(coef, width, lane, m1, m2);
+    const float scale = a.drop.threshold ? a.drop.scale : 1.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = rstd[g][e] * (__builtin_fmaf(w[g][e], d[e], -m1[g][e]) - v[e] * m2[g][e]);
-            row_store<T>(os, lane.own[g].template offset<ES>(lane.row * (uint32_t)a.c), lane.own[g], o);
-        });
+    for (int g = 0; g < G; ++g) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            m1[g][e] = -known.rstd[g][e] * __builtin_fmaf(known.shift[g][e], m2[g][e], m1[g][e]);
+            m2[g][e] *= -known.rstd[g][e] * known.rstd[g][e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) of_d[g][e] = known.by[g][e] * scale;
+    }
+    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += AT_ONCE * STEP) {
+        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, a.c, AT_ONCE * STEP), ds = rows_from<sizeof(T)>(a.dy, first, hi, a.c, a.c, AT_ONCE * STEP);
+        const __amdgpu_buffer_rsrc_t os = rows_from<sizeof(T)>(a.dx, first, hi, a.c, a.c, AT_ONCE * STEP);
+        Rows<T, G> rows[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) rows[u].load(a, xs, ds, (uint32_t)(u * STEP) + lane.row, lane);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const uint32_t row = (uint32_t)(u * STEP) + lane.row;
+            float x[G][8], d[G][8];
+            rows[u].gradient(a, known, (uint32_t)first + row, lane, philox, x, d);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[g][e] = __builtin_fmaf(d[g][e], of_d[g][e], __builtin_fmaf(x[g][e], m2[g][ALIKE ? 0 : e], m1[g][ALIKE ? 0 : e]));
+                row_store<T>(os, lane.template offset<T>(g, row, a.c), lane.own[g], d[g]);
+            }
+        }
     }
 }
 
@@ -355,8 +476,8 @@ struct Chunk {
     {
         lo = (int64_t)i * rows;
         hi = lo + rows < clouds.n ? lo + rows : clouds.n;
-        first = clouds.at(lo);
-        last = hi < clouds.n ? clouds.at(hi) : clouds.count - 1;
+        first = clouds.at_for_all(lo);
+        last = clouds.at_for_all(hi - 1);
         if (first >= clouds.count) first = clouds.count - 1;      // (rows behind the last cloud: it has none of them)
         if (last >= clouds.count) last = clouds.count - 1;
     }
@@ -384,6 +505,26 @@ template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THR
     }
 }
 
+// Sums of a cloud's chunks' means and squares about a pivot
+struct Joined {
+    float s, q, m;
+    __device__ inline void add(const GroupNormArgs &a, int64_t rows, int64_t lo, int64_t hi, const float *part, float pivot, int i)
+    {
+        const int64_t from = (int64_t)i * rows > lo ? (int64_t)i * rows : lo, to = (int64_t)(i + 1) * rows < hi ? (int64_t)(i + 1) * rows : hi;
+        const float *at = part + (size_t)i * 2 * a.groups;
+        const float cnt = (float)(to - from), d = at[0] - pivot;
+        s = __builtin_fmaf(cnt, d, s);
+        q = __builtin_fmaf(cnt * d, d, q);
+        m += at[1];
+    }
+    __device__ inline void finish(const GroupNormArgs &a, int64_t rows_of_cloud, float pivot, float &mean, float &rstd) const
+    {
+        const float n = (float)rows_of_cloud, width = (float)(a.c / a.groups), off = s / n, between = q - s * off, m2 = m + width * (between < 0.f ? 0.f : between);
+        mean = pivot + off;
+        rstd = 1.f / sqrtf(m2 / (n * width) + a.eps);
+    }
+};
+
 // The chunks of a cloud joined: a block takes sixteen groups, a thread every 64th chunk of one.
 __global__ __launch_bounds__(1024) void cloud_statistics_kernel(const GroupNormArgs a, int64_t rows)
 {
@@ -398,22 +539,16 @@ __global__ __launch_bounds__(1024) void cloud_statistics_kernel(const GroupNormA
     }
     const int i0 = (int)(lo / rows), i1 = (int)((hi - 1) / rows);
     const float *part = a.part + ((size_t)b * a.groups + group) * 2;
-    const size_t pitch = (size_t)a.groups * 2;
-    float s = 0.f, q = 0.f, m = 0.f, pivot = 0.f;
+    Joined v{0.f, 0.f, 0.f};
+    float pivot = 0.f;
     if (group < a.groups) {
-        pivot = part[(size_t)i0 * pitch];
+        pivot = part[(size_t)i0 * 2 * a.groups];
 #pragma unroll 4
-        for (int i = i0 + sl; i <= i1; i += 64) {
-            const int64_t from = (int64_t)i * rows > lo ? (int64_t)i * rows : lo, to_ = (int64_t)(i + 1) * rows < hi ? (int64_t)(i + 1) * rows : hi;
-            const float cnt = (float)(to_ - from), d = part[(size_t)i * pitch] - pivot;
-            s = __builtin_fmaf(cnt, d, s);
-            q = __builtin_fmaf(cnt * d, d, q);
-            m += part[(size_t)i * pitch + 1];
-        }
+        for (int i = i0 + sl; i <= i1; i += 64) v.add(a, rows, lo, hi, part, pivot, i);
     }
-    sums[sl][gl][0] = s;
-    sums[sl][gl][1] = q;
-    sums[sl][gl][2] = m;
+    sums[sl][gl][0] = v.s;
+    sums[sl][gl][1] = v.q;
+    sums[sl][gl][2] = v.m;
     for (int step = 32; step > 0; step >>= 1) {
         __syncthreads();
         if (sl < step) {
@@ -422,26 +557,53 @@ __global__ __launch_bounds__(1024) void cloud_statistics_kernel(const GroupNormA
         }
     }
     if (sl != 0 || group >= a.groups) return;
-    const float n = (float)(hi - lo), width = (float)(a.c / a.groups);
-    s = sums[0][gl][0], q = sums[0][gl][1], m = sums[0][gl][2];
-    const float off = s / n, between = q - s * off, m2 = m + width * (between < 0.f ? 0.f : between);
-    to[0] = pivot + off;
-    to[1] = 1.f / sqrtf(m2 / (n * width) + a.eps);
+    float mean, rstd;
+    Joined{sums[0][gl][0], sums[0][gl][1], sums[0][gl][2]}.finish(a, hi - lo, pivot, mean, rstd);
+    to[0] = mean, to[1] = rstd;
 }
 
-template <typename T, int LPR, int G, int MODE>
+// JOIN: every block joins the chunks of its clouds for itself, the first of a cloud writes the result
+template <bool JOIN, bool ALIKE, typename T, int LPR, int G, int MODE>
 __global__ __launch_bounds__(THREADS) void apply_kernel(const GroupNormArgs a, int64_t rows, const Divisor width)
 {
+    constexpr int CP = 8 * LPR * G;
+    __shared__ float stats[JOIN ? 2 * CP : 1];
     const Clouds clouds{a.offsets, a.n_clouds, a.n};
     const Chunk chunk(clouds, rows, (int)(gridDim.x - 1 - blockIdx.x));         // (from the end on: what was read last is still in the caches)
     const Lane<LPR, G, MODE> lane(a.c);
     const Philox philox(a.drop.random);
-    float w[G][8], b[G][8];
-    load_affine(a.w, 1.f, lane.own, a.c, w);
-    load_affine(a.b, 0.f, lane.own, a.c, b);
+    if constexpr (JOIN) {
+        if (blockIdx.x == 0 && a.stats)                           // clouds without rows, which no chunk has
+            for (int i = threadIdx.x; i < a.n_clouds; i += THREADS)
+                if (clouds.first(i) >= clouds.end(i))
+                    for (int k = 0; k < 2 * a.groups; ++k) a.stats[(size_t)i * 2 * a.groups + k] = 0.f;
+    }
     for (int i = chunk.first; i <= chunk.last; ++i) {
         int64_t lo, hi;
-        if (chunk.range(clouds, i, lo, hi)) apply_range<T>(a, lo, hi, lane, w, b, a.stats + (size_t)i * a.groups * 2, width, philox);
+        if (!chunk.range(clouds, i, lo, hi)) continue;
+        if constexpr (JOIN) {
+            const int64_t first = clouds.first(i), end = clouds.end(i);
+            const int i0 = (int)(first / rows), i1 = (int)((end - 1) / rows);
+            __syncthreads();                                      // (the last cloud's are in use no more)
+            for_groups(a.groups, i1 - i0 + 1, [&](int group, int l, int per, auto sum, bool write) {
+                const float *part = a.part + ((size_t)i * a.groups + group) * 2;
+                const float pivot = part[(size_t)i0 * 2 * a.groups];
+                Joined v{0.f, 0.f, 0.f};
+#pragma unroll 4
+                for (int k = i0 + l; k <= i1; k += per) v.add(a, rows, first, end, part, pivot, k);
+                v.s = sum(v.s), v.q = sum(v.q), v.m = sum(v.m);
+                float mean, rstd;
+                v.finish(a, end - first, pivot, mean, rstd);
+                if (write && l == 0) {
+                    stats[2 * group] = mean, stats[2 * group + 1] = rstd;
+                    if (a.stats && lo == first) a.stats[((size_t)i * a.groups + group) * 2] = mean, a.stats[((size_t)i * a.groups + group) * 2 + 1] = rstd;
+                }
+            });
+            __syncthreads();
+            apply_range<ALIKE, T>(a, lo, hi, lane, stats, width, philox);
+        } else {
+            apply_range<ALIKE, T>(a, lo, hi, lane, a.stats + (size_t)i * a.groups * 2, width, philox);
+        }
     }
 }
 
@@ -466,13 +628,10 @@ template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THR
         stats[2 * g] = mean, stats[2 * g + 1] = rstd;
         if (to) to[2 * g] = mean, to[2 * g + 1] = rstd;
     });
-    float w[G][8], b[G][8];
-    load_affine(a.w, 1.f, lane.own, a.c, w);
-    load_affine(a.b, 0.f, lane.own, a.c, b);
-    apply_range<T>(a, lo, hi, lane, w, b, stats, width, philox);
+    apply_range<false, T>(a, lo, hi, lane, stats, width, philox);
 }
 
-template <typename T, int LPR, int G, int MODE>
+template <bool ALIKE, typename T, int LPR, int G, int MODE>
 __global__ __launch_bounds__(THREADS) void chunk_gradients_kernel(const GroupNormArgs a, int64_t rows, const Divisor width)
 {
     constexpr int CP = 8 * LPR * G;
@@ -481,13 +640,10 @@ __global__ __launch_bounds__(THREADS) void chunk_gradients_kernel(const GroupNor
     const Chunk chunk(clouds, rows, (int)blockIdx.x);
     const Lane<LPR, G, MODE> lane(a.c);
     const Philox philox(a.drop.random);
-    float w[G][8], b[G][8];
-    load_affine(a.w, 1.f, lane.own, a.c, w);
-    load_affine(a.b, 0.f, lane.own, a.c, b);
     for (int i = chunk.first; i <= chunk.last; ++i) {
         int64_t lo, hi;
         if (!chunk.range(clouds, i, lo, hi)) continue;            // (nothing reads the slot)
-        range_gradients<T, LPR, G, MODE, CP>(a, lo, hi, lane, w, b, a.stats + (size_t)i * a.groups * 2, width, philox, sums, total);
+        range_gradients<ALIKE, T, LPR, G, MODE, CP>(a, lo, hi, lane, a.stats + (size_t)i * a.groups * 2, width, philox, sums, total);
         float *to = a.part + ((size_t)blockIdx.x + (size_t)i) * 2 * a.c;
         for (int k = threadIdx.x; k < 2 * a.c; k += THREADS) to[k] = total[k >= a.c][k >= a.c ? k - a.c : k];
         __syncthreads();
@@ -517,11 +673,11 @@ __global__ __launch_bounds__(1024) void cloud_gradients_kernel(const GroupNormAr
 }
 
 // dx, and in blocks behind the chunks' the weights' gradients: the clouds' sums joined, sixteen columns a block
-template <typename T, int LPR, int G, int MODE>
+template <bool ALIKE, typename T, int LPR, int G, int MODE>
 __global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a, int64_t rows, int chunks, const Divisor width)
 {
     constexpr int CP = 8 * LPR * G;
-    __shared__ float total[2][CP], coef[2 * CP];
+    __shared__ float total[2][CP], coef[2 * CP], parts[16][16];
     const Clouds clouds{a.offsets, a.n_clouds, a.n};
     if ((int)blockIdx.x >= chunks) {
         const int column = ((int)blockIdx.x - chunks) * 16 + (threadIdx.x & 15), sl = threadIdx.x >> 4;
@@ -530,7 +686,6 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a
 #pragma unroll 4
             for (int b = sl; b < a.n_clouds; b += 16) v += a.coef[(size_t)b * 2 * a.c + column];
         }
-        __shared__ float parts[16][16];
         parts[sl][threadIdx.x & 15] = v;
         __syncthreads();
         if (sl != 0 || column >= 2 * a.c) return;
@@ -542,9 +697,6 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a
     const Chunk chunk(clouds, rows, chunks - 1 - (int)blockIdx.x);
     const Lane<LPR, G, MODE> lane(a.c);
     const Philox philox(a.drop.random);
-    float w[G][8], b[G][8];
-    load_affine(a.w, 1.f, lane.own, a.c, w);
-    load_affine(a.b, 0.f, lane.own, a.c, b);
     for (int i = chunk.first; i <= chunk.last; ++i) {
         int64_t lo, hi;
         if (!chunk.range(clouds, i, lo, hi)) continue;
@@ -552,7 +704,7 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a
         for (int k = threadIdx.x; k < 2 * a.c; k += THREADS) total[k >= a.c][k >= a.c ? k - a.c : k] = from[k];
         __syncthreads();
         group_means<CP>(a, total, (double)(clouds.end(i) - clouds.first(i)), coef);
-        gradient_range<T>(a, lo, hi, lane, w, b, a.stats + (size_t)i * a.groups * 2, coef, width, philox);
+        gradient_range<ALIKE, T>(a, lo, hi, lane, a.stats + (size_t)i * a.groups * 2, coef, width, philox);
         __syncthreads();
     }
 }
@@ -565,19 +717,16 @@ template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THR
     const Clouds clouds{a.offsets, a.n_clouds, a.n};
     const Lane<LPR, G, MODE> lane(a.c);
     const Philox philox(a.drop.random);
-    float w[G][8], b[G][8];
-    load_affine(a.w, 1.f, lane.own, a.c, w);
-    load_affine(a.b, 0.f, lane.own, a.c, b);
     for (int k = threadIdx.x; k < CP; k += THREADS) all[0][k] = all[1][k] = 0.f;
     for (int i = 0; i < a.n_clouds; ++i) {
         const int64_t lo = clouds.first(i), hi = clouds.end(i);
         if (lo >= hi) continue;
         const float *stats = a.stats + (size_t)i * a.groups * 2;
-        range_gradients<T, LPR, G, MODE, CP>(a, lo, hi, lane, w, b, stats, width, philox, sums, total);
+        range_gradients<false, T, LPR, G, MODE, CP>(a, lo, hi, lane, stats, width, philox, sums, total);
         for (int k = threadIdx.x; k < a.c; k += THREADS) all[0][k] += total[0][k], all[1][k] += total[1][k];
         if (a.dx) {
             group_means<CP>(a, total, (double)(hi - lo), coef);
-            gradient_range<T>(a, lo, hi, lane, w, b, stats, coef, width, philox);
+            gradient_range<false, T>(a, lo, hi, lane, stats, coef, width, philox);
         }
         __syncthreads();
     }
@@ -591,8 +740,20 @@ template <typename F> void with_kernel(int dtype, int c, F f)
 {
     with_rows(c, [&](auto lpr, auto g, auto mode) { dtype == PCPP_F32 ? f(float{}, lpr, g, mode) : f(bf16_t{}, lpr, g, mode); });
 }
+// ... and whether a lane's channels are of one group
+template <typename F> void with_kernel(int dtype, int c, int groups, F f)
+{
+    with_kernel(dtype, c, [&](auto t, auto lpr, auto g, auto mode) {
+        if constexpr (decltype(mode)::value == WHOLE) {
+            if (c / groups % 8 == 0) return f(t, lpr, g, mode, Int<1>{});
+        }
+        f(t, lpr, g, mode, Int<0>{});
+    });
+}
 
 bool one_block(int64_t n, int c, int n_clouds) { return n * c <= SMALL && n_clouds <= 64; }
+// Whether the blocks that write y join the chunks' statistics for themselves, which saves a launch (4 us) and costs each a read of at most 64 KB
+bool join_in_place(const GroupNormSizes &s, int groups) { return (int64_t)s.chunks * groups <= 8192; }
 
 }  // namespace
 
@@ -602,12 +763,12 @@ GroupNormSizes group_norm_sizes(int64_t n, int c, int n_clouds, int groups, bool
     GroupNormSizes s{};
     const int64_t step = WAVES * 64 / row_lanes(c);               // rows that a block takes at a time
     int64_t rows = ceil_div(ceil_div(n, 1024), step) * step;
-    if (rows < 2 * step) rows = 2 * step;
+    if (rows < 4 * step) rows = 4 * step;
     s.rows = rows;
     s.chunks = (int)ceil_div(n > 0 ? n : 1, rows);
     s.slots = (size_t)s.chunks + (size_t)n_clouds - 1;
     s.part = one_block(n, c, n_clouds) ? 0 : align_up(s.slots * 2 * (size_t)(backward ? c : groups) * sizeof(float));
-    s.extra = backward ? (s.part ? align_up((size_t)n_clouds * 2 * c * sizeof(float)) : 0) : (s.part ? align_up((size_t)n_clouds * groups * 2 * sizeof(float)) : 0);
+    s.extra = !s.part ? 0 : align_up((size_t)n_clouds * 2 * (size_t)(backward ? c : groups) * sizeof(float));
     s.bytes = s.part + s.extra;
     return s;
 }
@@ -623,16 +784,21 @@ int group_norm_fwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
         return PCPP_OK;
     }
     const GroupNormSizes s = group_norm_sizes(a.n, a.c, a.n_clouds, a.groups, false);
+    const bool join = join_in_place(s, a.groups);
     with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
         chunk_statistics_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
             <<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows);
     });
     PCPP_HIP_CHECK(hipGetLastError());
-    cloud_statistics_kernel<<<dim3((unsigned)a.n_clouds, (unsigned)ceil_div(a.groups, 16)), 1024, 0, stream>>>(a, s.rows);
-    PCPP_HIP_CHECK(hipGetLastError());
-    with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
-        apply_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
-            <<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
+    if (!join) {
+        cloud_statistics_kernel<<<dim3((unsigned)a.n_clouds, (unsigned)ceil_div(a.groups, 16)), 1024, 0, stream>>>(a, s.rows);
+        PCPP_HIP_CHECK(hipGetLastError());
+    }
+    with_kernel(dtype, a.c, a.groups, [&](auto t, auto lpr, auto g, auto mode, auto alike) {
+        constexpr int LPR = decltype(lpr)::value, G = decltype(g)::value, MODE = decltype(mode)::value;
+        constexpr bool ALIKE = decltype(alike)::value;
+        if (join) apply_kernel<true, ALIKE, decltype(t), LPR, G, MODE><<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
+        else apply_kernel<false, ALIKE, decltype(t), LPR, G, MODE><<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
     });
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;
@@ -649,17 +815,16 @@ int group_norm_bwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
         return PCPP_OK;
     }
     const GroupNormSizes s = group_norm_sizes(a.n, a.c, a.n_clouds, a.groups, true);
-    with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
-        chunk_gradients_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
+    with_kernel(dtype, a.c, a.groups, [&](auto t, auto lpr, auto g, auto mode, auto alike) {
+        chunk_gradients_kernel<(bool)decltype(alike)::value, decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
             <<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
     });
     PCPP_HIP_CHECK(hipGetLastError());
     cloud_gradients_kernel<<<dim3((unsigned)a.n_clouds, (unsigned)ceil_div(2 * a.c, 16)), 1024, 0, stream>>>(a, s.rows);
     PCPP_HIP_CHECK(hipGetLastError());
     const int sums = a.dw || a.db ? (int)ceil_div(2 * a.c, 16) : 0, chunks = a.dx ? s.chunks : 0;
-    if (sums + chunks == 0) return PCPP_OK;
-    with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
-        gradient_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
+    with_kernel(dtype, a.c, a.groups, [&](auto t, auto lpr, auto g, auto mode, auto alike) {
+        gradient_kernel<(bool)decltype(alike)::value, decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
             <<<(unsigned)(chunks + sums), THREADS, 0, stream>>>(a, s.rows, chunks, width);
     });
     PCPP_HIP_CHECK(hipGetLastError());

@@ -34,9 +34,9 @@ struct Philox {                                                   // what a kern
         for (int r = 0; r < 10; ++r) {
             const uint64_t a = (uint64_t)0xD2511F53u * x[0], b = (uint64_t)0xCD9E8D57u * x[2];
             const uint32_t x1 = x[1], x3 = x[3];
-            x[0] = (uint32_t)(b >> 32) ^ x1 ^ k0;
+            x[0] = __builtin_amdgcn_bitop3_b32((uint32_t)(b >> 32), x1, k0, 0x96);                // (0x96: exclusive or of the three)
             x[1] = (uint32_t)b;
-            x[2] = (uint32_t)(a >> 32) ^ x3 ^ k1;
+            x[2] = __builtin_amdgcn_bitop3_b32((uint32_t)(a >> 32), x3, k1, 0x96);
             x[3] = (uint32_t)a;
             k0 += 0x9E3779B9u;
             k1 += 0xBB67AE85u;

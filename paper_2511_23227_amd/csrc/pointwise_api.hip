@@ -10,7 +10,7 @@ namespace pcpp {
 namespace {
 
 constexpr int MAX_CHANNELS = 1024, MAX_DROP_CHANNELS = 65536, MAX_CLOUDS = 65536;
-constexpr int64_t MAX_PITCH = 1 << 24;                            // (a wave's sixteen rows within 32-bit offsets)
+constexpr int64_t MAX_PITCH = 1 << 24, MAX_NORM_PITCH = 1 << 22;  // (the norms: 208 rows within 32-bit offsets)
 constexpr uint64_t MAX_COUNTERS = ((uint64_t)1 << 32) - 65536;
 
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -93,7 +93,7 @@ int check_norm(const char *fn, int64_t ld_x, const float *w, const float *b, con
         if (int rc = check_random(fn, random, n, c)) return rc;
     if (int rc = check_clouds(fn, offsets, n_clouds)) return rc;
     if (ld_x < c) return invalid(fn, "pitch < c");
-    if (ld_x >= MAX_PITCH) return unsupported(fn, "row pitches must be below 2^24");
+    if (ld_x >= MAX_NORM_PITCH) return unsupported(fn, "row pitches must be below 2^22");
     if (!aligned(w, 4) || !aligned(b, 4)) return invalid(fn, "w and b must be 4-byte aligned");
     return PCPP_OK;
 }
