@@ -156,6 +156,21 @@ __device__ inline void channel_sums(const float (&p)[G][8], const float (&q)[G][
     __syncthreads();
 }
 
+// v and that of the lane's partner, N neighbouring lanes having the same
+template <int N> __device__ inline float lanes_sum(float v)
+{
+    if constexpr (N < 16) {
+        constexpr int CTRL = N == 1 ? DPP_XOR1 : (N == 2 ? DPP_XOR2 : (N == 4 ? DPP_HALF_MIRROR : DPP_MIRROR));
+        return v + __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
+    } else if constexpr (N == 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    } else {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+}
+
 // For every group f(group, lane among `per`, per, sum over those lanes, whether it is one) by neighbouring lanes of a wave
 template <typename F> __device__ inline void for_groups(int groups, int width, F f)
 {
@@ -163,8 +178,12 @@ template <typename F> __device__ inline void for_groups(int groups, int width, F
     while (per > 1 && (per * groups > THREADS || per >= 2 * width)) per >>= 1;
     const int lane = (int)threadIdx.x % per;
     auto sum = [&](float v) {
-        for (int m = 1; m < per; m <<= 1) v += __shfl_xor(v, m);
-        return v;
+        if (per >= 2) v = lanes_sum<1>(v);
+        if (per >= 4) v = lanes_sum<2>(v);
+        if (per >= 8) v = lanes_sum<4>(v);
+        if (per >= 16) v = lanes_sum<8>(v);
+        if (per >= 32) v = lanes_sum<16>(v);
+        return per >= 64 ? lanes_sum<32>(v) : v;
     };
     for (int g0 = 0; g0 < groups; g0 += THREADS / per) {
         const int g = g0 + (int)threadIdx.x / per;                // (past the last: as the last, without an effect)
@@ -261,17 +280,28 @@ __device__ inline void lane_pairs(const float *pairs, const Divisor &width, cons
         }
 }
 
-// y of rows [lo, hi): z = x by + off
-template <bool ALIKE, typename T, int LPR, int G, int MODE>
-__device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width,
-                                   const Philox &philox)
+// y of rows [lo, hi), not empty: z = x by + off.  The weights and the first rows are on their way while `statistics` finds the cloud's, the next ones while some are
+// written.
+template <bool ALIKE, typename T, int LPR, int G, int MODE, typename F>
+__device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const Divisor &width, const Philox &philox, F statistics)
 {
     constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, AT_ONCE = sizeof(T) * G > 4 ? 1 : 2;
     const int c = a.c;
+    Eight<T> raw[AT_ONCE][G];
+    auto load = [&](int64_t first, Eight<T> (&to)[AT_ONCE][G]) {
+        if (first >= hi) return;
+        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, c, AT_ONCE * STEP);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+            for (int g = 0; g < G; ++g) row_load<T>(xs, lane.template offset<T>(g, (uint32_t)(u * STEP) + lane.row, a.ld_x), lane.own[g], to[u][g]);
+    };
+    int64_t first = lo + (int64_t)wave_of() * ROWS;
+    load(first, raw);
     float by[G][8], off[G][8], mean[G][ALIKE ? 1 : 8], rstd[G][ALIKE ? 1 : 8];
     load_affine(a.w, 1.f, lane.own, a.c, by);
     load_affine(a.b, 0.f, lane.own, a.c, off);
-    lane_pairs<ALIKE>(stats, width, lane, mean, rstd);
+    lane_pairs<ALIKE>(statistics(), width, lane, mean, rstd);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -279,13 +309,10 @@ __device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t h
             by[g][e] *= rstd[g][ALIKE ? 0 : e];
             off[g][e] = __builtin_fmaf(-mean[g][ALIKE ? 0 : e], by[g][e], off[g][e]);
         }
-    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += AT_ONCE * STEP) {
-        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, c, AT_ONCE * STEP), ys = rows_from<sizeof(T)>(a.y, first, hi, c, c, AT_ONCE * STEP);
-        Eight<T> raw[AT_ONCE][G];
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u)
-#pragma unroll
-            for (int g = 0; g < G; ++g) row_load<T>(xs, lane.template offset<T>(g, (uint32_t)(u * STEP) + lane.row, a.ld_x), lane.own[g], raw[u][g]);
+    for (; first < hi; first += AT_ONCE * STEP) {
+        Eight<T> next[AT_ONCE][G];
+        load(first + AT_ONCE * STEP, next);
+        const __amdgpu_buffer_rsrc_t ys = rows_from<sizeof(T)>(a.y, first, hi, c, c, AT_ONCE * STEP);
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
             const uint32_t row = (uint32_t)(u * STEP) + lane.row;
@@ -308,6 +335,10 @@ __device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t h
 #pragma unroll
             for (int g = 0; g < G; ++g) row_store<T>(ys, lane.template offset<T>(g, row, c), lane.own[g], v[g]);
         }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+            for (int g = 0; g < G; ++g) raw[u][g] = next[u][g];
     }
 }
 
@@ -337,12 +368,14 @@ template <bool ALIKE, int G> struct Known {
 template <typename T, int G> struct Rows {
     Eight<T> x[G], dy[G];
     template <int LPR, int MODE>
-    __device__ inline void load(const GroupNormArgs &a, const __amdgpu_buffer_rsrc_t &xs, const __amdgpu_buffer_rsrc_t &ds, uint32_t row, const Lane<LPR, G, MODE> &lane)
+    __device__ inline void load(const GroupNormArgs &a, int64_t first, int64_t hi, const Lane<LPR, G, MODE> &lane)
     {
+        if (first >= hi) return;
+        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, a.c, 64 / LPR), ds = rows_from<sizeof(T)>(a.dy, first, hi, a.c, a.c, 64 / LPR);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            row_load<T>(xs, lane.template offset<T>(g, row, a.ld_x), lane.own[g], x[g]);
-            row_load<T>(ds, lane.template offset<T>(g, row, a.c), lane.own[g], dy[g]);
+            row_load<T>(xs, lane.template offset<T>(g, lane.row, a.ld_x), lane.own[g], x[g]);
+            row_load<T>(ds, lane.template offset<T>(g, lane.row, a.c), lane.own[g], dy[g]);
         }
     }
     // x and what flows to z, without the scale of the dropout; zeros in rows past the last
@@ -372,7 +405,10 @@ template <bool ALIKE, typename T, int LPR, int G, int MODE, int CP>
 __device__ inline void range_gradients(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width,
                                        const Philox &philox, float (*sums)[2][CP], float (*total)[CP])
 {
-    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, AT_ONCE = sizeof(T) * G > 4 ? 1 : 2;
+    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS;
+    int64_t first = lo + (int64_t)wave_of() * ROWS;
+    Rows<T, G> rows, next;                                        // (one on its way while the other is in use)
+    rows.load(a, first, hi, lane);
     Known<ALIKE, G> known;
     known.load(a, lane, stats, width);
     float s[G][8], q[G][8];
@@ -380,23 +416,18 @@ __device__ inline void range_gradients(const GroupNormArgs &a, int64_t lo, int64
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[g][e] = q[g][e] = 0.f;
-    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += AT_ONCE * STEP) {
-        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, a.c, AT_ONCE * STEP), ds = rows_from<sizeof(T)>(a.dy, first, hi, a.c, a.c, AT_ONCE * STEP);
-        Rows<T, G> rows[AT_ONCE];
+    for (; first < hi; first += STEP) {
+        next.load(a, first + STEP, hi, lane);
+        float x[G][8], d[G][8];
+        rows.gradient(a, known, (uint32_t)first + lane.row, lane, philox, x, d);
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) rows[u].load(a, xs, ds, (uint32_t)(u * STEP) + lane.row, lane);
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            float x[G][8], d[G][8];
-            rows[u].gradient(a, known, (uint32_t)(first + u * STEP) + lane.row, lane, philox, x, d);
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[g][e] += d[g][e];
-                    q[g][e] = __builtin_fmaf(d[g][e], __builtin_fmaf(x[g][e], known.rstd[g][ALIKE ? 0 : e], known.shift[g][ALIKE ? 0 : e]), q[g][e]);
-                }
-        }
+            for (int e = 0; e < 8; ++e) {
+                s[g][e] += d[g][e];
+                q[g][e] = __builtin_fmaf(d[g][e], __builtin_fmaf(x[g][e], known.rstd[g][ALIKE ? 0 : e], known.shift[g][ALIKE ? 0 : e]), q[g][e]);
+            }
+        rows = next;
     }
     if (a.drop.threshold) {
 #pragma unroll
@@ -426,16 +457,19 @@ template <int CP> __device__ inline void group_means(const GroupNormArgs &a, con
     __syncthreads();
 }
 
-// dx of rows [lo, hi):  rstd (w dz - m1 - v m2) = dz (w rstd) + x (-rstd^2 m2) - rstd (m1 + shift m2)
-template <bool ALIKE, typename T, int LPR, int G, int MODE>
-__device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const float *coef,
-                                      const Divisor &width, const Philox &philox)
+// dx of rows [lo, hi), not empty:  rstd (w dz - m1 - v m2) = dz (w rstd) + x (-rstd^2 m2) - rstd (m1 + shift m2).  `means` finds m1 and m2.
+template <bool ALIKE, typename T, int LPR, int G, int MODE, typename F>
+__device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width,
+                                      const Philox &philox, F means)
 {
-    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, AT_ONCE = sizeof(T) * G > 4 ? 1 : 2, N = ALIKE ? 1 : 8;
+    constexpr int ROWS = 64 / LPR, STEP = WAVES * ROWS, N = ALIKE ? 1 : 8;
+    int64_t first = lo + (int64_t)wave_of() * ROWS;
+    Rows<T, G> rows, next;
+    rows.load(a, first, hi, lane);
     Known<ALIKE, G> known;
     known.load(a, lane, stats, width);
     float m1[G][N], m2[G][N], of_d[G][8];
-    lane_pairs<ALIKE>(coef, width, lane, m1, m2);
+    lane_pairs<ALIKE>(means(), width, lane, m1, m2);
     const float scale = a.drop.threshold ? a.drop.scale : 1.f;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
@@ -447,24 +481,18 @@ __device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_
 #pragma unroll
         for (int e = 0; e < 8; ++e) of_d[g][e] = known.by[g][e] * scale;
     }
-    for (int64_t first = lo + (int64_t)wave_of() * ROWS; first < hi; first += AT_ONCE * STEP) {
-        const __amdgpu_buffer_rsrc_t xs = rows_from<sizeof(T)>(a.x, first, hi, a.ld_x, a.c, AT_ONCE * STEP), ds = rows_from<sizeof(T)>(a.dy, first, hi, a.c, a.c, AT_ONCE * STEP);
-        const __amdgpu_buffer_rsrc_t os = rows_from<sizeof(T)>(a.dx, first, hi, a.c, a.c, AT_ONCE * STEP);
-        Rows<T, G> rows[AT_ONCE];
+    for (; first < hi; first += STEP) {
+        next.load(a, first + STEP, hi, lane);
+        const __amdgpu_buffer_rsrc_t os = rows_from<sizeof(T)>(a.dx, first, hi, a.c, a.c, ROWS);
+        float x[G][8], d[G][8];
+        rows.gradient(a, known, (uint32_t)first + lane.row, lane, philox, x, d);
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) rows[u].load(a, xs, ds, (uint32_t)(u * STEP) + lane.row, lane);
+        for (int g = 0; g < G; ++g) {
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const uint32_t row = (uint32_t)(u * STEP) + lane.row;
-            float x[G][8], d[G][8];
-            rows[u].gradient(a, known, (uint32_t)first + row, lane, philox, x, d);
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[g][e] = __builtin_fmaf(d[g][e], of_d[g][e], __builtin_fmaf(x[g][e], m2[g][ALIKE ? 0 : e], m1[g][ALIKE ? 0 : e]));
-                row_store<T>(os, lane.template offset<T>(g, row, a.c), lane.own[g], d[g]);
-            }
+            for (int e = 0; e < 8; ++e) d[g][e] = __builtin_fmaf(d[g][e], of_d[g][e], __builtin_fmaf(x[g][e], m2[g][ALIKE ? 0 : e], m1[g][ALIKE ? 0 : e]));
+            row_store<T>(os, lane.template offset<T>(g, lane.row, a.c), lane.own[g], d[g]);
         }
+        rows = next;
     }
 }
 
@@ -472,16 +500,17 @@ __device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_
 struct Chunk {
     int64_t lo, hi;
     int first, last;
-    __device__ inline Chunk(const Clouds &clouds, int64_t rows, int i)
+    __device__ inline Chunk(const WaveClouds &of, int64_t rows, int i)
     {
+        const int64_t n = of.clouds.n;
         lo = (int64_t)i * rows;
-        hi = lo + rows < clouds.n ? lo + rows : clouds.n;
-        first = clouds.at_for_all(lo);
-        last = clouds.at_for_all(hi - 1);
-        if (first >= clouds.count) first = clouds.count - 1;      // (rows behind the last cloud: it has none of them)
-        if (last >= clouds.count) last = clouds.count - 1;
+        hi = lo + rows < n ? lo + rows : n;
+        const int end = of.clouds.count - 1;                      // (rows behind the last cloud: it has none of them)
+        first = of.at(lo), last = of.at(hi - 1);
+        first = first < end ? first : end;
+        last = last < end ? last : end;
     }
-    __device__ inline bool range(const Clouds &clouds, int b, int64_t &from, int64_t &to) const
+    __device__ inline bool range(const WaveClouds &clouds, int b, int64_t &from, int64_t &to) const
     {
         const int64_t f = clouds.first(b), e = clouds.end(b);
         from = f > lo ? f : lo;
@@ -494,7 +523,7 @@ template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THR
 {
     constexpr int CP = 8 * LPR * G;
     __shared__ float sums[WAVES][2][CP], total[2][CP], shift[CP];
-    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const WaveClouds clouds(Clouds{a.offsets, a.n_clouds, a.n});
     const Chunk chunk(clouds, rows, (int)blockIdx.x);
     const Lane<LPR, G, MODE> lane(a.c);
     for (int b = chunk.first; b <= chunk.last; ++b) {
@@ -564,26 +593,27 @@ __global__ __launch_bounds__(1024) void cloud_statistics_kernel(const GroupNormA
 
 // JOIN: every block joins the chunks of its clouds for itself, the first of a cloud writes the result
 template <bool JOIN, bool ALIKE, typename T, int LPR, int G, int MODE>
-__global__ __launch_bounds__(THREADS) void apply_kernel(const GroupNormArgs a, int64_t rows, const Divisor width)
+__global__ __launch_bounds__(THREADS) void apply_kernel(const GroupNormArgs a, int64_t rows, const Divisor chunk_rows, const Divisor width)
 {
     constexpr int CP = 8 * LPR * G;
     __shared__ float stats[JOIN ? 2 * CP : 1];
-    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const WaveClouds clouds(Clouds{a.offsets, a.n_clouds, a.n});
     const Chunk chunk(clouds, rows, (int)(gridDim.x - 1 - blockIdx.x));         // (from the end on: what was read last is still in the caches)
     const Lane<LPR, G, MODE> lane(a.c);
     const Philox philox(a.drop.random);
     if constexpr (JOIN) {
-        if (blockIdx.x == 0 && a.stats)                           // clouds without rows, which no chunk has
+        if (blockIdx.x == 0)                                      // clouds without rows, which no chunk has
             for (int i = threadIdx.x; i < a.n_clouds; i += THREADS)
-                if (clouds.first(i) >= clouds.end(i))
+                if (clouds.clouds.first(i) >= clouds.clouds.end(i))
                     for (int k = 0; k < 2 * a.groups; ++k) a.stats[(size_t)i * 2 * a.groups + k] = 0.f;
     }
     for (int i = chunk.first; i <= chunk.last; ++i) {
         int64_t lo, hi;
         if (!chunk.range(clouds, i, lo, hi)) continue;
-        if constexpr (JOIN) {
+        apply_range<ALIKE, T>(a, lo, hi, lane, width, philox, [&]() -> const float * {
+            if constexpr (!JOIN) return a.stats + (size_t)i * a.groups * 2;
             const int64_t first = clouds.first(i), end = clouds.end(i);
-            const int i0 = (int)(first / rows), i1 = (int)((end - 1) / rows);
+            const int i0 = (int)chunk_rows.quotient((uint32_t)first), i1 = (int)chunk_rows.quotient((uint32_t)(end - 1));
             __syncthreads();                                      // (the last cloud's are in use no more)
             for_groups(a.groups, i1 - i0 + 1, [&](int group, int l, int per, auto sum, bool write) {
                 const float *part = a.part + ((size_t)i * a.groups + group) * 2;
@@ -596,14 +626,12 @@ __global__ __launch_bounds__(THREADS) void apply_kernel(const GroupNormArgs a, i
                 v.finish(a, end - first, pivot, mean, rstd);
                 if (write && l == 0) {
                     stats[2 * group] = mean, stats[2 * group + 1] = rstd;
-                    if (a.stats && lo == first) a.stats[((size_t)i * a.groups + group) * 2] = mean, a.stats[((size_t)i * a.groups + group) * 2 + 1] = rstd;
+                    if (lo == first) a.stats[((size_t)i * a.groups + group) * 2] = mean, a.stats[((size_t)i * a.groups + group) * 2 + 1] = rstd;
                 }
             });
             __syncthreads();
-            apply_range<ALIKE, T>(a, lo, hi, lane, stats, width, philox);
-        } else {
-            apply_range<ALIKE, T>(a, lo, hi, lane, a.stats + (size_t)i * a.groups * 2, width, philox);
-        }
+            return stats;
+        });
     }
 }
 
@@ -628,7 +656,7 @@ template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THR
         stats[2 * g] = mean, stats[2 * g + 1] = rstd;
         if (to) to[2 * g] = mean, to[2 * g + 1] = rstd;
     });
-    apply_range<false, T>(a, lo, hi, lane, stats, width, philox);
+    apply_range<false, T>(a, lo, hi, lane, width, philox, [&] { return stats; });
 }
 
 template <bool ALIKE, typename T, int LPR, int G, int MODE>
@@ -636,7 +664,7 @@ __global__ __launch_bounds__(THREADS) void chunk_gradients_kernel(const GroupNor
 {
     constexpr int CP = 8 * LPR * G;
     __shared__ float sums[WAVES][2][CP], total[2][CP];
-    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const WaveClouds clouds(Clouds{a.offsets, a.n_clouds, a.n});
     const Chunk chunk(clouds, rows, (int)blockIdx.x);
     const Lane<LPR, G, MODE> lane(a.c);
     const Philox philox(a.drop.random);
@@ -678,7 +706,7 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a
 {
     constexpr int CP = 8 * LPR * G;
     __shared__ float total[2][CP], coef[2 * CP], parts[16][16];
-    const Clouds clouds{a.offsets, a.n_clouds, a.n};
+    const WaveClouds clouds(Clouds{a.offsets, a.n_clouds, a.n});
     if ((int)blockIdx.x >= chunks) {
         const int column = ((int)blockIdx.x - chunks) * 16 + (threadIdx.x & 15), sl = threadIdx.x >> 4;
         float v = 0.f;
@@ -700,11 +728,13 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a
     for (int i = chunk.first; i <= chunk.last; ++i) {
         int64_t lo, hi;
         if (!chunk.range(clouds, i, lo, hi)) continue;
-        const float *from = a.coef + (size_t)i * 2 * a.c;
-        for (int k = threadIdx.x; k < 2 * a.c; k += THREADS) total[k >= a.c][k >= a.c ? k - a.c : k] = from[k];
-        __syncthreads();
-        group_means<CP>(a, total, (double)(clouds.end(i) - clouds.first(i)), coef);
-        gradient_range<ALIKE, T>(a, lo, hi, lane, a.stats + (size_t)i * a.groups * 2, coef, width, philox);
+        gradient_range<ALIKE, T>(a, lo, hi, lane, a.stats + (size_t)i * a.groups * 2, width, philox, [&] {
+            const float *from = a.coef + (size_t)i * 2 * a.c;
+            for (int k = threadIdx.x; k < 2 * a.c; k += THREADS) total[k >= a.c][k >= a.c ? k - a.c : k] = from[k];
+            __syncthreads();
+            group_means<CP>(a, total, (double)(clouds.end(i) - clouds.first(i)), coef);
+            return coef;
+        });
         __syncthreads();
     }
 }
@@ -725,8 +755,10 @@ template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THR
         range_gradients<false, T, LPR, G, MODE, CP>(a, lo, hi, lane, stats, width, philox, sums, total);
         for (int k = threadIdx.x; k < a.c; k += THREADS) all[0][k] += total[0][k], all[1][k] += total[1][k];
         if (a.dx) {
-            group_means<CP>(a, total, (double)(hi - lo), coef);
-            gradient_range<false, T>(a, lo, hi, lane, stats, coef, width, philox);
+            gradient_range<false, T>(a, lo, hi, lane, stats, width, philox, [&] {
+                group_means<CP>(a, total, (double)(hi - lo), coef);
+                return coef;
+            });
         }
         __syncthreads();
     }
@@ -762,10 +794,10 @@ GroupNormSizes group_norm_sizes(int64_t n, int c, int n_clouds, int groups, bool
 {
     GroupNormSizes s{};
     const int64_t step = WAVES * 64 / row_lanes(c);               // rows that a block takes at a time
-    int64_t rows = ceil_div(ceil_div(n, 1024), step) * step;
-    if (rows < 4 * step) rows = 4 * step;
-    s.rows = rows;
-    s.chunks = (int)ceil_div(n > 0 ? n : 1, rows);
+    // (two blocks for each CU; four make 5 of 43 us more of 99 991 x 91, one takes a third more of 1 000 000 x 256)
+    s.rows = ceil_div(ceil_div(n, 512), step) * step;
+    if (s.rows < 4 * step) s.rows = 4 * step;
+    s.chunks = (int)ceil_div(n > 0 ? n : 1, s.rows);
     s.slots = (size_t)s.chunks + (size_t)n_clouds - 1;
     s.part = one_block(n, c, n_clouds) ? 0 : align_up(s.slots * 2 * (size_t)(backward ? c : groups) * sizeof(float));
     s.extra = !s.part ? 0 : align_up((size_t)n_clouds * 2 * (size_t)(backward ? c : groups) * sizeof(float));
@@ -797,8 +829,8 @@ int group_norm_fwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
     with_kernel(dtype, a.c, a.groups, [&](auto t, auto lpr, auto g, auto mode, auto alike) {
         constexpr int LPR = decltype(lpr)::value, G = decltype(g)::value, MODE = decltype(mode)::value;
         constexpr bool ALIKE = decltype(alike)::value;
-        if (join) apply_kernel<true, ALIKE, decltype(t), LPR, G, MODE><<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
-        else apply_kernel<false, ALIKE, decltype(t), LPR, G, MODE><<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, width);
+        if (join) apply_kernel<true, ALIKE, decltype(t), LPR, G, MODE><<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, make_divisor((uint32_t)s.rows), width);
+        else apply_kernel<false, ALIKE, decltype(t), LPR, G, MODE><<<(unsigned)s.chunks, THREADS, 0, stream>>>(a, s.rows, make_divisor((uint32_t)s.rows), width);
     });
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;

@@ -55,6 +55,31 @@ struct Clouds {
         return __builtin_amdgcn_readfirstlane(lo + k < hi ? lo + k : hi);
     }
 };
+// The clouds as a wave asks for them, all lanes the same: up to 63 are held, an offset a lane, so that all its questions cost one load
+struct WaveClouds {
+    Clouds clouds;
+    int own = 0;
+    bool held;
+    __device__ inline explicit WaveClouds(const Clouds &c) : clouds(c), held(c.offsets && c.count < 64)
+    {
+        const int lane = threadIdx.x & 63;
+        if (held) own = (int)c.bound(lane <= c.count ? lane : c.count);
+    }
+    __device__ inline int64_t bound(int b) const { return held ? (int64_t)__builtin_amdgcn_readlane(own, b) : clouds.bound(b); }
+    __device__ inline int64_t first(int b) const { return bound(b); }
+    __device__ inline int64_t end(int b) const
+    {
+        const int64_t a = bound(b), e = bound(b + 1);
+        return e > a ? e : a;
+    }
+    __device__ inline int at(int64_t row) const
+    {
+        if (!held) return clouds.at_for_all(row);
+        const int lane = threadIdx.x & 63;
+        const unsigned long long behind = __ballot(lane >= 1 && lane <= clouds.count && own > row);
+        return behind ? __ffsll((long long)behind) - 2 : clouds.count;
+    }
+};
 
 // ---- activations --------------------------------------------------------------------------------------------------------------
 __device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
