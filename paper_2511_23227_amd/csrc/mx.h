@@ -20,11 +20,10 @@ constexpr int64_t mx_scale_bytes(int64_t c) { return 4 * ceil_div(c, 4 * MX_BLOC
 constexpr uint32_t MX_TOP_CODE = 252u, MX_NAN_CODE = 255u;
 __device__ inline uint32_t mx_code(uint32_t amax, bool random)
 {
-    if (amax >= 0x7f800000u) return MX_NAN_CODE;
-    const int e = (int)((amax + (random ? 0x3fffffu : 0x200000u)) >> 23) - 2;
-    return e < 1 ? 1u : (e < (int)MX_TOP_CODE ? (uint32_t)e : MX_TOP_CODE);
+    const uint32_t e = (amax + (random ? 0x3fffffu : 0x200000u)) >> 23, at_least = e > 3u ? e : 3u, code = (at_least < MX_TOP_CODE + 2u ? at_least : MX_TOP_CODE + 2u) - 2u;
+    return amax >= 0x7f800000u ? MX_NAN_CODE : code;
 }
-__device__ inline float mx_step(uint32_t code) { return __uint_as_float((code < MX_TOP_CODE ? code : MX_TOP_CODE) << 23); }
+__device__ inline float mx_step(uint32_t code) { return __uint_as_float(code << 23); }      // (255: what comes of it is left aside)
 
 // ---- eight numbers as they lie in memory to eight 4-bit codes -----------------------------------------------------------------------
 // The conversions divide by the power of two (exactly) and round to nearest (ties to the even fraction) or at random: a 32-bit fraction is added to what lies below the

@@ -83,29 +83,51 @@ template <> struct Columns<bf16_t> {
     }
 };
 
+// the 32 rows of a wave from row `first` on; nothing where they lie behind the last
+template <int ES> __device__ inline __amdgpu_buffer_rsrc_t tile_rows(const void *p, int64_t first, int64_t n, int64_t pitch, int64_t c)
+{
+    const int64_t left = n - first < 32 ? n - first : 32;
+    return make_rsrc(static_cast<const char *>(p) + first * pitch * ES, left > 0 ? (uint32_t)(((left - 1) * pitch + c) * ES) : 0u);
+}
+
 template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREADS) void pack_columns_kernel(const MxPackArgs a, const Divisor row_tiles)
 {
     __shared__ __attribute__((aligned(16))) uint8_t tile[TILE_CHANNELS][80];    // 64 bytes a channel, and a pitch that spreads the banks
     __shared__ uint32_t words[TILE_CHANNELS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rl = lane / 8, cl = lane % 8;
     const uint32_t tile_y = row_tiles.quotient(blockIdx.x), tile_x = blockIdx.x - tile_y * row_tiles.by;
-    const int64_t row0 = (int64_t)tile_x * TILE_ROWS + 32 * wave + 4 * rl, c0 = (int64_t)tile_y * TILE_CHANNELS + 8 * cl;
+    const int64_t first = (int64_t)tile_x * TILE_ROWS + 32 * wave, c0 = (int64_t)tile_y * TILE_CHANNELS + 8 * cl;      // the wave's first row, the lane's first channel
+    const uint32_t row = 4u * (uint32_t)rl;
     if (threadIdx.x < TILE_CHANNELS) words[threadIdx.x] = 0u;
     Eight<T> v[4];
-    uint32_t u[4][4];
+    if (a.c >= 8) {
+        const __amdgpu_buffer_rsrc_t xs = tile_rows<sizeof(T)>(a.x, first, a.n, a.ld_x, a.c);
+        const int64_t at = c0 + 8 <= a.c ? c0 : a.c - 8;          // (where the row ends inside the eight, its last eight, moved into place)
+        const uint32_t pitch = (uint32_t)a.ld_x, off = c0 < a.c ? row * pitch + (uint32_t)at : 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + i;
-        load_channels(static_cast<const T *>(a.x) + (row < a.n ? row : a.n - 1) * a.ld_x, c0, a.c, v[i]);
-        if (row >= a.n) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < (int)(sizeof(T) / 2); ++k) v[i].a[k] = v4u{0u, 0u, 0u, 0u};
+            for (int k = 0; k < (int)(sizeof(T) / 2); ++k) {
+                const auto r = __builtin_amdgcn_raw_buffer_load_b128(xs, (int)(c0 < a.c ? (off + (uint32_t)i * pitch) * (uint32_t)sizeof(T) + 16u * k : OOB_OFFSET), 0, 0);
+                v[i].a[k] = v4u{r[0], r[1], r[2], r[3]};
+            }
+        if (a.c % 8 != 0 && c0 + 8 > a.c && c0 < a.c) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) move_down(v[i], (int)(c0 - at));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = first + row + i;
+            load_channels(static_cast<const T *>(a.x) + (r < a.n ? r : a.n - 1) * a.ld_x, c0, r < a.n ? a.c : 0, v[i]);
         }
     }
+    uint32_t u[4][4];
     if constexpr (RANDOM) {
         const Philox philox(a.random);
+        const uint32_t per_row = (uint32_t)ceil_div(a.c, 8), from = ((uint32_t)first + row) * per_row + (uint32_t)(c0 / 8);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) philox.draw((uint32_t)(row0 + i) * (uint32_t)ceil_div(a.c, 8) + (uint32_t)(c0 / 8), u[i]);
+        for (int i = 0; i < 4; ++i) philox.draw(from + (uint32_t)i * per_row, u[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -113,20 +135,15 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
             for (int k = 0; k < 4; ++k) u[i][k] = 0u;
     }
     if constexpr (ROWS) {
-        const int64_t block = c0 / MX_BLOCK;
+        const uint32_t q_pitch = (uint32_t)mx_row_bytes(a.c), s_pitch = (uint32_t)mx_scale_bytes(a.c), blocks = (uint32_t)mx_blocks(a.c), block = (uint32_t)(c0 / MX_BLOCK);
+        const __amdgpu_buffer_rsrc_t qs = tile_rows<1>(a.q, first, a.n, q_pitch, q_pitch), ss = tile_rows<1>(a.scales, first, a.n, s_pitch, s_pitch);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t row = row0 + i;
-            const uint32_t code = mx_code(quad_largest(largest(v[i])), RANDOM), bits = mx_quantise<RANDOM>(v[i], code, u[i]);
-            if (row < a.n && block < mx_blocks(a.c)) {
-                reinterpret_cast<uint32_t *>(a.q + row * mx_row_bytes(a.c))[c0 / 8] = bits;
-                if (cl % 4 == 0) {
-                    uint8_t *to = a.scales + row * mx_scale_bytes(a.c);
-                    to[block] = (uint8_t)code;
-                    if (block + 1 == mx_blocks(a.c))
-                        for (int64_t k = block + 1; k < mx_scale_bytes(a.c); ++k) to[k] = 0;
-                }
-            }
+            const uint32_t code = mx_code(quad_largest(largest(v[i])), RANDOM), bits = mx_quantise<RANDOM>(v[i], code, u[i]), r = row + (uint32_t)i;
+            __builtin_amdgcn_raw_buffer_store_b32(bits, qs, (int)(block < blocks ? r * q_pitch + (uint32_t)(c0 / 2) : OOB_OFFSET), 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b8((uint8_t)code, ss, (int)(block < blocks && cl % 4 == 0 ? r * s_pitch + block : OOB_OFFSET), 0, 0);
+            if (blocks % 4u != 0u && block + 1u == blocks && cl % 4 == 0)                       // (the rest of the row's whole words)
+                for (uint32_t k = block + 1u; k < s_pitch; ++k) __builtin_amdgcn_raw_buffer_store_b8((uint8_t)0, ss, (int)(r * s_pitch + k), 0, 0);
         }
     }
     // channel by channel: the largest of the wave's 32 rows, four codes of the lane's rows

@@ -11,6 +11,7 @@ namespace {
 
 constexpr int MAX_CHANNELS = 1024, MAX_DROP_CHANNELS = 65536, MAX_CLOUDS = 65536;
 constexpr int64_t MAX_PITCH = 1 << 24, MAX_NORM_PITCH = 1 << 22;  // (the norms: 208 rows within 32-bit offsets)
+constexpr int64_t MAX_MX_PITCH = 1 << 25;                         // (32 rows)
 constexpr uint64_t MAX_COUNTERS = ((uint64_t)1 << 32) - 65536;
 
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -214,7 +215,7 @@ int pcpp_mx_pack(const void *x, int64_t ld_x, int dtype, int64_t n, int64_t c, c
     const char *fn = "pcpp_mx_pack";
     if (int rc = check_mx(fn, n, c, dtype)) return rc;
     if (ld_x < c) return invalid(fn, "pitch < c");
-    if (ld_x >= INT32_MAX) return unsupported(fn, "row pitches must be below 2^31");
+    if (ld_x >= MAX_MX_PITCH) return unsupported(fn, "row pitches must be below 2^25");
     if (random)
         if (int rc = check_random(fn, random, n, c)) return rc;
     if ((q != nullptr) != (scales != nullptr) || (qt != nullptr) != (scales_t != nullptr)) return invalid(fn, "codes and scales belong together");
@@ -271,7 +272,7 @@ int pcpp_mx_linear(const void *x, int64_t ld_x, int x_dtype, const uint8_t *w, c
     if (int rc = check_product(fn, w, w_scales, bias, act, n, m, k, out, out_dtype)) return rc;
     if (!is_type(x_dtype)) return unsupported(fn, "unsupported dtype");
     if (ld_x < k) return invalid(fn, "pitch < k");
-    if (ld_x >= INT32_MAX) return unsupported(fn, "row pitches must be below 2^31");
+    if (ld_x >= MAX_MX_PITCH) return unsupported(fn, "row pitches must be below 2^25");
     if (n > 0 && !x) return invalid(fn, "null tensor pointer");
     if (!aligned(x, dtype_bytes(x_dtype))) return invalid(fn, "x must be aligned to its elements");
     if (n == 0) return PCPP_OK;
