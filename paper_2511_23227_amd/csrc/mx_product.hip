@@ -296,8 +296,8 @@ template <typename T> __global__ __launch_bounds__(1024) void join_kernel(const 
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------------------
-// Up to sixteen rows of a: what counts is reading b once.  A block takes sixteen rows of b, its waves every WAVES-th stage of the sum; codes go from memory to the
-// registers of the lanes that multiply them.  a comes in 4 bits or, of few elements, as it is: the block rounds it into LDS while its first rows of b are on
+// Up to sixteen rows of a: what counts is reading b once.  A block takes sixteen rows of b, its waves every WAVES-th stage of the sum; codes go from memory to
+// the registers of the lanes that multiply them.  a comes in 4 bits or, of few elements, as it is: the block rounds it into LDS while its first rows of b are on
 // their way.
 constexpr int FEW_ROWS = 16;
 constexpr int64_t FEW_ELEMENTS = 32768;                           // of a that every block rounds for itself (17 KB of LDS)
@@ -383,6 +383,9 @@ template <typename T, typename X, int WAVES> __global__ __launch_bounds__(64 * W
     });
 }
 
+// ... while b has enough rows for the blocks to share, or the sum is short (16 x 64 x 100 000, four blocks of sixteen waves: 123 us, in parts 11)
+bool few_rows(int64_t n, int64_t m, int64_t k) { return n <= FEW_ROWS && (m >= 2048 || k <= 64 * FEW_STAGE); }
+
 // How a product is cut: tiles, and parts of the sum where the tiles do not fill the card.
 struct Shape {
     bool few, large;
@@ -393,16 +396,16 @@ Shape shape_of(int64_t n, int64_t m, int64_t k)
     Shape s{};
     s.stages = ceil_div(k, STAGE);
     s.parts = 1;
-    s.few = n <= FEW_ROWS;
+    s.few = few_rows(n, m, k);
     if (s.few) return s;
     s.large = ceil_div(n, 256) * ceil_div(m, 256) >= 192 && s.stages >= 4;
     const int tile = s.large ? 256 : 128;
     s.rows = ceil_div(n, tile);
     s.columns = ceil_div(m, tile);
     const int64_t tiles = s.rows * s.columns;
-    if (tiles < 256 && s.stages >= 8) {
-        s.parts = ceil_div(512, tiles);
-        if (s.parts > s.stages / 4) s.parts = s.stages / 4;
+    if (tiles < 128 && s.stages >= 8) {                           // (a block for each CU: 256 x 128 x 200 000 in 21 us, two 27; three stages a part at least)
+        s.parts = 256 / tiles;
+        if (s.parts > s.stages / 3) s.parts = s.stages / 3;
     }
     s.of_part = ceil_div(s.stages, s.parts);
     s.parts = ceil_div(s.stages, s.of_part);                      // (none is empty)
@@ -440,7 +443,7 @@ template <typename T, typename X> void launch_few(const MxProductArgs &p, const 
 
 }  // namespace
 
-bool mx_linear_few(int64_t n, int64_t k) { return n <= FEW_ROWS && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
+bool mx_linear_few(int64_t n, int64_t m, int64_t k) { return few_rows(n, m, k) && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
 int mx_linear_few(const MxProductArgs &p, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream)
 {
     auto with = [&](auto t, auto s) { launch_few<decltype(t)>(p, static_cast<const decltype(s) *>(x), ld_x, stream); };
@@ -462,7 +465,8 @@ int mx_product(const MxProductArgs &p, int out_dtype, hipStream_t stream)
     auto with = [&](auto t) -> int {
         typedef decltype(t) T;
         if (s.few) {
-            launch_few<T, uint8_t>(p, nullptr, 0, stream);
+            const uint8_t *none = nullptr;
+            launch_few<T>(p, none, 0, stream);
             return PCPP_OK;
         }
         if (s.parts > 1) {
