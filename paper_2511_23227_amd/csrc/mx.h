@@ -172,7 +172,7 @@ struct MxProductArgs {
 size_t mx_product_workspace_bytes(int64_t n, int64_t m, int64_t k);
 int mx_product(const MxProductArgs &a, int out_dtype, hipStream_t stream);
 // few rows of x [n, k] as they are (a and a_scales are not read)
-bool mx_linear_few(int64_t n, int64_t m, int64_t k);
+bool mx_linear_few(int64_t n, int64_t k);
 int mx_linear_few(const MxProductArgs &a, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream);
 
 }  // namespace pcpp

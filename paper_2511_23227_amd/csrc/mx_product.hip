@@ -300,7 +300,7 @@ template <typename T> __global__ __launch_bounds__(1024) void join_kernel(const 
 // the registers of the lanes that multiply them.  a comes in 4 bits or, of few elements, as it is: the block rounds it into LDS while its first rows of b are on
 // their way.
 constexpr int FEW_ROWS = 16;
-constexpr int64_t FEW_ELEMENTS = 32768;                           // of a that every block rounds for itself (17 KB of LDS)
+constexpr int64_t FEW_ELEMENTS = 16384;                           // of a that every block rounds for itself (9 KB of LDS; 1 x 4096 x 32 768 28 us, rounded first 21)
 
 template <typename T, typename X, int WAVES> __global__ __launch_bounds__(64 * WAVES) void few_kernel(const MxProductArgs p, const X *__restrict__ x, int64_t ld_x)
 {
@@ -383,8 +383,9 @@ template <typename T, typename X, int WAVES> __global__ __launch_bounds__(64 * W
     });
 }
 
-// ... while b has enough rows for the blocks to share, or the sum is short (16 x 64 x 100 000, four blocks of sixteen waves: 123 us, in parts 11)
-bool few_rows(int64_t n, int64_t m, int64_t k) { return n <= FEW_ROWS && (m >= 2048 || k <= 64 * FEW_STAGE); }
+// ... of sums up to 8192 long: the waves of one block walk the whole sum, tiles cut it over the card (16 x 256 x 4096 in 6.2 us, in parts 8.4; 16 x 256 x 16 384
+// in 12.5 and 8.6, 16 x 4096 x 50 000 in 31 and 25)
+bool few_rows(int64_t n, int64_t k) { return n <= FEW_ROWS && k <= 32 * STAGE; }
 
 // How a product is cut: tiles, and parts of the sum where the tiles do not fill the card.
 struct Shape {
@@ -396,7 +397,7 @@ Shape shape_of(int64_t n, int64_t m, int64_t k)
     Shape s{};
     s.stages = ceil_div(k, STAGE);
     s.parts = 1;
-    s.few = few_rows(n, m, k);
+    s.few = few_rows(n, k);
     if (s.few) return s;
     s.large = ceil_div(n, 256) * ceil_div(m, 256) >= 192 && s.stages >= 4;
     const int tile = s.large ? 256 : 128;
@@ -443,7 +444,8 @@ template <typename T, typename X> void launch_few(const MxProductArgs &p, const 
 
 }  // namespace
 
-bool mx_linear_few(int64_t n, int64_t m, int64_t k) { return few_rows(n, m, k) && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
+// (one launch less than rounding first: 1 x 64 x 16 384 in 9.1 us, 12.1)
+bool mx_linear_few(int64_t n, int64_t k) { return n <= FEW_ROWS && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
 int mx_linear_few(const MxProductArgs &p, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream)
 {
     auto with = [&](auto t, auto s) { launch_few<decltype(t)>(p, static_cast<const decltype(s) *>(x), ld_x, stream); };

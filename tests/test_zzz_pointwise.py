@@ -313,7 +313,7 @@ def product_reference(a, b, bias, act):
 PRODUCTS = [  # n, m, k
     (1, 1, 1), (1, 64, 64), (1, 300, 4096), (2, 257, 1000), (16, 128, 256), (17, 130, 129), (100, 91, 91), (128, 128, 128), (129, 255, 513), (300, 200, 31),
     (1000, 64, 32), (33, 1000, 2048), (512, 512, 512), (5, 3, 100_000), (91, 64, 33_333), (700, 520, 1500), (3500, 3601, 1100), (13, 40, 20_000),
-    (16, 2100, 600), (9, 33, 16_384),
+    (16, 2100, 600), (9, 33, 16_384), (9, 33, 8192), (9, 33, 8193), (17, 70, 8000),
 ]
 
 
