@@ -18,7 +18,6 @@ namespace pcpp {
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int64_t SMALL = 16384;                                  // elements that one block goes through alone
 
 // A lane's channels.  ALIKE: the groups are of whole eights, so a lane's eight channels are of one group and have one mean.
 template <int LPR, int G, int MODE> struct Lane {
@@ -739,32 +738,31 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(const GroupNormArgs a
     }
 }
 
-// Few rows: one block, cloud by cloud
+// Few rows: a block takes a cloud.  The weights' gradients are written by the only one or, of several clouds, joined by gradient_kernel's last blocks.
 template <typename T, int LPR, int G, int MODE> __global__ __launch_bounds__(THREADS) void small_backward_kernel(const GroupNormArgs a, const Divisor width)
 {
     constexpr int CP = 8 * LPR * G;
-    __shared__ float sums[WAVES][2][CP], total[2][CP], coef[2 * CP], all[2][CP];
+    __shared__ float sums[WAVES][2][CP], total[2][CP], coef[2 * CP];
     const Clouds clouds{a.offsets, a.n_clouds, a.n};
     const Lane<LPR, G, MODE> lane(a.c);
     const Philox philox(a.drop.random);
-    for (int k = threadIdx.x; k < CP; k += THREADS) all[0][k] = all[1][k] = 0.f;
-    for (int i = 0; i < a.n_clouds; ++i) {
-        const int64_t lo = clouds.first(i), hi = clouds.end(i);
-        if (lo >= hi) continue;
-        const float *stats = a.stats + (size_t)i * a.groups * 2;
+    const int64_t lo = clouds.first((int)blockIdx.x), hi = clouds.end((int)blockIdx.x);
+    const float *stats = a.stats + (size_t)blockIdx.x * a.groups * 2;
+    if (lo < hi) {
         range_gradients<false, T, LPR, G, MODE, CP>(a, lo, hi, lane, stats, width, philox, sums, total);
-        for (int k = threadIdx.x; k < a.c; k += THREADS) all[0][k] += total[0][k], all[1][k] += total[1][k];
         if (a.dx) {
             gradient_range<false, T>(a, lo, hi, lane, stats, width, philox, [&] {
                 group_means<CP>(a, total, (double)(hi - lo), coef);
                 return coef;
             });
         }
-        __syncthreads();
     }
-    for (int k = threadIdx.x; k < a.c; k += THREADS) {
-        if (a.db) a.db[k] = all[0][k];
-        if (a.dw) a.dw[k] = all[1][k];
+    for (int k = threadIdx.x; k < 2 * a.c; k += THREADS) {
+        const int which = k >= a.c, ch = which ? k - a.c : k;
+        const float v = lo < hi ? total[which][ch] : 0.f;
+        float *only = which ? a.dw : a.db;
+        if (a.n_clouds > 1) a.coef[(size_t)blockIdx.x * 2 * a.c + k] = v;
+        else if (only) only[ch] = v;
     }
 }
 
@@ -783,7 +781,14 @@ template <typename F> void with_kernel(int dtype, int c, int groups, F f)
     });
 }
 
-bool one_block(int64_t n, int c, int n_clouds) { return n * c <= SMALL && n_clouds <= 64; }
+int64_t rows_at_once(int c) { return WAVES * 64 / row_lanes(c); }
+// A block to a cloud, from its statistics to its rows, in place of passes over chunks: where a cloud has ten steps of a block or fewer on average.  (256 x 64 of one cloud, eight
+// steps: 8.1 us forward and 12.8 backward, by chunks 10.0 and 14.3; 1000 x 16, sixteen: 11.0 and 19.9, 10.6 and 15.3.  Eighty steps in all at most, for clouds of very different sizes.)
+bool block_a_cloud(int64_t n, int c, int n_clouds)
+{
+    const int64_t steps = ceil_div(n, rows_at_once(c));
+    return steps <= 80 && steps <= 10 * (int64_t)n_clouds;
+}
 // Whether the blocks that write y join the chunks' statistics for themselves, which saves a launch (4 us) and costs each a read of at most 64 KB
 bool join_in_place(const GroupNormSizes &s, int groups) { return (int64_t)s.chunks * groups <= 8192; }
 
@@ -793,14 +798,16 @@ bool join_in_place(const GroupNormSizes &s, int groups) { return (int64_t)s.chun
 GroupNormSizes group_norm_sizes(int64_t n, int c, int n_clouds, int groups, bool backward)
 {
     GroupNormSizes s{};
-    const int64_t step = WAVES * 64 / row_lanes(c);               // rows that a block takes at a time
-    // (two blocks for each CU; four make 5 of 43 us more of 99 991 x 91, one takes a third more of 1 000 000 x 256)
-    s.rows = ceil_div(ceil_div(n, 512), step) * step;
-    if (s.rows < 4 * step) s.rows = 4 * step;
+    const int64_t step = rows_at_once(c);
+    // (two blocks for each CU; four make 5 of 43 us more of 99 991 x 91, one takes a third more of 1 000 000 x 256.  More for very many clouds, which a block takes one by one.)
+    const int64_t most = n_clouds > 512 ? n_clouds : 512, of_cloud = ceil_div(ceil_div(n, n_clouds), step), least = of_cloud < 4 ? (of_cloud > 1 ? of_cloud : 1) : 4;
+    s.rows = ceil_div(ceil_div(n, most), step) * step;
+    if (s.rows < least * step) s.rows = least * step;
     s.chunks = (int)ceil_div(n > 0 ? n : 1, s.rows);
     s.slots = (size_t)s.chunks + (size_t)n_clouds - 1;
-    s.part = one_block(n, c, n_clouds) ? 0 : align_up(s.slots * 2 * (size_t)(backward ? c : groups) * sizeof(float));
-    s.extra = !s.part ? 0 : align_up((size_t)n_clouds * 2 * (size_t)(backward ? c : groups) * sizeof(float));
+    const bool small = block_a_cloud(n, c, n_clouds);
+    s.part = small ? 0 : align_up(s.slots * 2 * (size_t)(backward ? c : groups) * sizeof(float));
+    s.extra = small && !(backward && n_clouds > 1) ? 0 : align_up((size_t)n_clouds * 2 * (size_t)(backward ? c : groups) * sizeof(float));
     s.bytes = s.part + s.extra;
     return s;
 }
@@ -808,7 +815,7 @@ GroupNormSizes group_norm_sizes(int64_t n, int c, int n_clouds, int groups, bool
 int group_norm_fwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
 {
     const Divisor width = make_divisor((uint32_t)(a.c / a.groups));
-    if (one_block(a.n, a.c, a.n_clouds)) {
+    if (block_a_cloud(a.n, a.c, a.n_clouds)) {
         with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
             small_forward_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value><<<(unsigned)a.n_clouds, THREADS, 0, stream>>>(a, width);
         });
@@ -839,11 +846,18 @@ int group_norm_fwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
 int group_norm_bwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
 {
     const Divisor width = make_divisor((uint32_t)(a.c / a.groups));
-    if (one_block(a.n, a.c, a.n_clouds)) {
+    const int sums = a.dw || a.db ? (int)ceil_div(2 * a.c, 16) : 0;
+    if (block_a_cloud(a.n, a.c, a.n_clouds)) {
         with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
-            small_backward_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value><<<1, THREADS, 0, stream>>>(a, width);
+            small_backward_kernel<decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value><<<(unsigned)a.n_clouds, THREADS, 0, stream>>>(a, width);
         });
         PCPP_HIP_CHECK(hipGetLastError());
+        if (sums && a.n_clouds > 1) {
+            with_kernel(dtype, a.c, [&](auto t, auto lpr, auto g, auto mode) {
+                gradient_kernel<false, decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value><<<(unsigned)sums, THREADS, 0, stream>>>(a, 0, 0, width);
+            });
+            PCPP_HIP_CHECK(hipGetLastError());
+        }
         return PCPP_OK;
     }
     const GroupNormSizes s = group_norm_sizes(a.n, a.c, a.n_clouds, a.groups, true);
@@ -854,7 +868,7 @@ int group_norm_bwd(const GroupNormArgs &a, int dtype, hipStream_t stream)
     PCPP_HIP_CHECK(hipGetLastError());
     cloud_gradients_kernel<<<dim3((unsigned)a.n_clouds, (unsigned)ceil_div(2 * a.c, 16)), 1024, 0, stream>>>(a, s.rows);
     PCPP_HIP_CHECK(hipGetLastError());
-    const int sums = a.dw || a.db ? (int)ceil_div(2 * a.c, 16) : 0, chunks = a.dx ? s.chunks : 0;
+    const int chunks = a.dx ? s.chunks : 0;
     with_kernel(dtype, a.c, a.groups, [&](auto t, auto lpr, auto g, auto mode, auto alike) {
         gradient_kernel<(bool)decltype(alike)::value, decltype(t), decltype(lpr)::value, decltype(g)::value, decltype(mode)::value>
             <<<(unsigned)(chunks + sums), THREADS, 0, stream>>>(a, s.rows, chunks, width);

@@ -126,6 +126,8 @@ NORMS = [  # n, c, groups, offsets, act, p, pitch
     (700, 1021, 1, None, "gelu", 0.1, 0), (600, 1024, 1024, [0, 599, 600], "none", 0.0, 0), (1300, 33, 11, [0, 1300], "silu", 0.1, 0),
     (2500, 16, 2, [0] + list(range(0, 2500, 31)) + [2500], "gelu", 0.1, 0), (5000, 3, 1, None, "relu", 0.0, 0),
     (400, 32, 4, [100, 100, 100], "silu", 0.0, 0),     # no cloud has a row
+    (130, 256, 32, [0, 0, 5, 60, 130], "gelu", 0.1, 0), (900, 40, 5, [0] + list(range(2, 900, 9)), "silu", 0.1, 3),    # a block to a cloud
+    (3000, 40, 5, [1] + list(range(4, 3000, 11)) + [2999], "gelu", 0.2, 0),    # short chunks for short clouds
 ]
 
 
@@ -209,6 +211,26 @@ def test_group_norm_keeps_infinities_to_their_group(pcpp):
     dy = rows_of(1000, 32, F32, 32)
     d = pcpp.pcpp_group_norm_bwd(dy, x, y.mean_rstd, None, None, off)
     assert torch.isnan(d.dx.cpu()[bad]).all() and torch.isfinite(d.dx.cpu()[~bad]).all()
+
+
+@gpu
+def test_group_norm_of_thousands_of_clouds(pcpp):
+    """... found by three loads of 64 offsets, and of no rows at all."""
+    n, c, offsets = 9000, 6, [0, 0] + list(range(1, 8998, 2)) + [8997, 8999]
+    x, dy, off = rows_of(n, c, F32, 35), rows_of(n, c, F32, 36), torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    y_ref, stats, off_y, off_stats = group_norm(x, 3, None, None, offsets, "silu", 1e-3, None)
+    y = pcpp.pcpp_group_norm_fwd(x, 3, None, None, off, act=pcpp.ACT_SILU, eps=1e-3)
+    within(y.mean_rstd, stats, off_stats, "mean_rstd")
+    within(y.y[:8999], y_ref[:8999], off_y[:8999], "y")
+    d = pcpp.pcpp_group_norm_bwd(dy, x, y.mean_rstd, None, None, off, act=pcpp.ACT_SILU)
+    dx, dw, db = group_norm_grads(dy, x, y.mean_rstd, None, None, offsets, "silu", None)
+    within(d.dx[:8999], dx[0][:8999], dx[1][:8999], "dx")
+    within(d.dw, *dw, "dw")
+    within(d.db, *db, "db")
+    none = torch.zeros(len(offsets), dtype=torch.int32, device="cuda")
+    y = pcpp.pcpp_group_norm_fwd(x[:0], 3, None, None, none)
+    d = pcpp.pcpp_group_norm_bwd(dy[:0], x[:0], y.mean_rstd, None, None, none)
+    assert y.y.shape == (0, 6) and not y.mean_rstd.any() and not d.dw.any() and not d.db.any()
 
 
 @gpu
