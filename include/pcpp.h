@@ -465,12 +465,12 @@ PCPP_API int pcpp_group_norm_bwd(const void *dy, const void *x, int64_t ld_x, co
  *   q, scales    the rows; both NULL: not wanted
  *   qt, scales_t the columns: the same form of x transposed, [c] rows of n elements; both NULL: not wanted
  * q and qt are 16-byte aligned, scales 4-byte.  pcpp_mx_unpack writes the values, [n, c] dtype, contiguous; they are bf16 numbers exactly.
- * Errors: INVALID_ARG, UNSUPPORTED (c >= 2^24, n >= 2^31, with columns n >= 2^24, pitch >= 2^25, dtype, too many random numbers).
+ * Outputs may not overlap inputs.  Errors: INVALID_ARG, UNSUPPORTED (c >= 2^24, n >= 2^31, with columns n >= 2^24, pitch >= 2^25, dtype, too many random numbers).
  *
  * Products of such rows, out[i, j] = act(sum_l a[i, l] * b[j, l] + bias[j]) with a [n, k], b [m, k], bias [m] fp32 (NULL: none), out [n, m] out_dtype,
  * contiguous, aligned to an element.  Products and sums are fp32, rounded once.  A linear layer y = x W^T and its gradients dx = dy W, dW = dy^T x are
  * this call on rows of x and W; rows of dy and columns of W; columns of dy and of x.
- * pcpp_mx_linear takes a as x [n, k] x_dtype, row pitch ld_x, and rounds it to 4 bits to nearest on the way.
+ * pcpp_mx_linear takes a as x [n, k] x_dtype, row pitch ld_x, and rounds it to 4 bits to nearest on the way.  Outputs may not overlap inputs.
  *   workspace  pcpp_mx_product_workspace_bytes / pcpp_mx_linear_workspace_bytes(n, m, k) bytes, 256-byte aligned (may be NULL if that is 0)
  * Errors: INVALID_ARG (also: m or k < 1), WORKSPACE, UNSUPPORTED (k or m >= 2^24, n >= 2^31, pitch >= 2^25, dtype).
  * ------------------------------------------------------------------------------------------- */

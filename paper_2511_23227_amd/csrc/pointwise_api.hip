@@ -224,6 +224,7 @@ int pcpp_mx_pack(const void *x, int64_t ld_x, int dtype, int64_t n, int64_t c, c
     if (!x || (!q && !qt)) return invalid(fn, "null tensor pointer");
     if (!aligned(x, dtype_bytes(dtype)) || !aligned(q, 16) || !aligned(qt, 16) || !aligned(scales, 4) || !aligned(scales_t, 4))
         return invalid(fn, "x must be aligned to its elements, codes to 16 bytes, scales to 4");
+    if (x == q || x == qt || x == scales || x == scales_t) return invalid(fn, "the output may not be an input");
     MxPackArgs a{};
     a.x = x; a.q = q; a.scales = scales; a.qt = qt; a.scales_t = scales_t;
     a.n = n; a.c = c; a.ld_x = ld_x;
@@ -238,6 +239,7 @@ int pcpp_mx_unpack(const uint8_t *q, const uint8_t *scales, int64_t n, int64_t c
     if (n == 0) return PCPP_OK;
     if (!x || !q || !scales) return invalid(fn, "null tensor pointer");
     if (!aligned(x, dtype_bytes(dtype)) || !aligned(q, 16) || !aligned(scales, 4)) return invalid(fn, "x must be aligned to its elements, codes to 16 bytes, scales to 4");
+    if (x == q || x == scales) return invalid(fn, "the output may not be an input");
     return mx_unpack(q, scales, n, c, x, dtype, static_cast<hipStream_t>(stream));
 }
 
@@ -251,6 +253,7 @@ int pcpp_mx_product(const uint8_t *a, const uint8_t *a_scales, const uint8_t *b,
     if (n > 0 && (!a || !a_scales)) return invalid(fn, "null tensor pointer");
     if (!aligned(a, 16) || !aligned(a_scales, 4)) return invalid(fn, "codes must be 16-byte aligned, scales 4-byte");
     if (n == 0) return PCPP_OK;
+    if (out == a || out == b || out == a_scales || out == b_scales || out == bias) return invalid(fn, "the output may not be an input");
     if (int rc = check_workspace(fn, workspace, workspace_bytes, mx_product_workspace_bytes(n, m, k))) return rc;
     MxProductArgs p{};
     p.a = a; p.a_scales = a_scales; p.b = b; p.b_scales = b_scales; p.bias = bias; p.out = out; p.part = static_cast<float *>(workspace);
@@ -276,6 +279,7 @@ int pcpp_mx_linear(const void *x, int64_t ld_x, int x_dtype, const uint8_t *w, c
     if (n > 0 && !x) return invalid(fn, "null tensor pointer");
     if (!aligned(x, dtype_bytes(x_dtype))) return invalid(fn, "x must be aligned to its elements");
     if (n == 0) return PCPP_OK;
+    if (out == x || out == w || out == w_scales || out == bias) return invalid(fn, "the output may not be an input");
     if (int rc = check_workspace(fn, workspace, workspace_bytes, pcpp_mx_linear_workspace_bytes(n, m, k))) return rc;
     MxProductArgs p{};
     p.b = w; p.b_scales = w_scales; p.bias = bias; p.out = out;

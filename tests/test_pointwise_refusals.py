@@ -90,7 +90,9 @@ def test_rows_in_four_bits(lib, p):
     assert [lib.pcpp_mx_row_bytes(c) for c in (0, 1, 32, 33, 128, 2 ** 24 - 1, 2 ** 24)] == [0, 16, 16, 32, 64, 2 ** 23, 0]
     assert [lib.pcpp_mx_scale_bytes(c) for c in (-1, 1, 128, 129, 4096, 2 ** 24)] == [0, 4, 4, 8, 128, 0]
 
-    def pack(x=a, ld=64, dtype=F32, n=4, c=64, rng=None, q=a, s=a, qt=None, st=None):
+    other = vp(p + 1024)
+
+    def pack(x=other, ld=64, dtype=F32, n=4, c=64, rng=None, q=a, s=a, qt=None, st=None):
         return lib.pcpp_mx_pack(x, ld, dtype, n, c, rng, 1, q, s, qt, st, None)
 
     assert pack(n=-1) == INVALID and pack(c=0) == INVALID and pack(c=2 ** 24, ld=2 ** 24) == UNSUPPORTED and pack(n=2 ** 31) == UNSUPPORTED
@@ -98,18 +100,20 @@ def test_rows_in_four_bits(lib, p):
     assert pack(x=None) == INVALID and pack(q=None) == INVALID and pack(s=None) == INVALID and pack(q=None, s=None) == INVALID and pack(qt=a) == INVALID
     assert pack(q=vp(p + 8)) == INVALID and pack(s=vp(p + 2)) == INVALID and pack(x=vp(p + 2)) == INVALID and pack(qt=vp(p + 4), st=a) == INVALID
     assert pack(qt=a, st=a, n=2 ** 24) == UNSUPPORTED and pack(rng=vp(p + 4)) == INVALID and pack(rng=a, n=2 ** 30) == UNSUPPORTED
+    assert pack(x=a) == INVALID and pack(x=a, q=None, s=None, qt=a, st=other) == INVALID and pack(s=other) == INVALID
     assert pack(n=0, x=None, q=None, s=None) == 0
 
-    def unpack(q=a, s=a, n=4, c=64, x=a, dtype=F32):
+    def unpack(q=a, s=a, n=4, c=64, x=other, dtype=F32):
         return lib.pcpp_mx_unpack(q, s, n, c, x, dtype, None)
 
     assert unpack(q=None) == INVALID and unpack(s=None) == INVALID and unpack(x=None) == INVALID and unpack(n=-1) == INVALID and unpack(c=0) == INVALID
     assert unpack(dtype=3) == UNSUPPORTED and unpack(q=vp(p + 8)) == INVALID and unpack(s=vp(p + 1)) == INVALID and unpack(x=vp(p + 2)) == INVALID
+    assert unpack(x=a) == INVALID and unpack(s=other) == INVALID
     assert unpack(n=0, q=None) == 0
 
 
 def test_products(lib, p):
-    a = vp(p)
+    a, y = vp(p), vp(p + 1024)
     size, linear_size = lib.pcpp_mx_product_workspace_bytes, lib.pcpp_mx_linear_workspace_bytes
     for f in (size, linear_size):
         assert [f(*s) for s in ((-1, 8, 8), (8, 0, 8), (8, 8, 0), (8, 2 ** 24, 8), (8, 8, 2 ** 24), (2 ** 31, 8, 8))] == [0] * 6
@@ -117,10 +121,10 @@ def test_products(lib, p):
     need, linear_need = size(*parts), linear_size(*parts)
     assert need >= 2 * 64 * 64 * 4 and linear_need >= need + 64 * 50_000 and size(4096, 4096, 64) == 0
 
-    def product(q=a, s=a, wq=a, ws_=a, bias=None, act=0, n=64, m=64, k=100_000, out=a, dtype=F32, ws=(a, need)):
+    def product(q=a, s=a, wq=a, ws_=a, bias=None, act=0, n=64, m=64, k=100_000, out=y, dtype=F32, ws=(a, need)):
         return lib.pcpp_mx_product(q, s, wq, ws_, bias, act, n, m, k, out, dtype, *ws, None)
 
-    def linear(x=a, ld=100_000, xdtype=F32, wq=a, ws_=a, bias=None, act=0, n=64, m=64, k=100_000, out=a, dtype=F32, ws=(a, linear_need)):
+    def linear(x=a, ld=100_000, xdtype=F32, wq=a, ws_=a, bias=None, act=0, n=64, m=64, k=100_000, out=y, dtype=F32, ws=(a, linear_need)):
         return lib.pcpp_mx_linear(x, ld, xdtype, wq, ws_, bias, act, n, m, k, out, dtype, *ws, None)
 
     for call, room in ((product, need), (linear, linear_need)):
@@ -129,6 +133,8 @@ def test_products(lib, p):
         assert call(wq=None) == INVALID and call(ws_=None) == INVALID and call(out=None) == INVALID
         assert call(wq=vp(p + 8)) == INVALID and call(ws_=vp(p + 2)) == INVALID and call(bias=vp(p + 2)) == INVALID and call(out=vp(p + 2)) == INVALID
         assert call(ws=(None, room)) == WORKSPACE and call(ws=(a, room - 1)) == WORKSPACE and call(ws=(vp(p + 8), room)) == WORKSPACE
+        assert call(out=a) == INVALID and call(wq=y) == INVALID and call(ws_=y) == INVALID and call(bias=y) == INVALID
         assert call(n=0, ws=(None, 0)) == 0
     assert product(q=None) == INVALID and product(s=None) == INVALID and product(q=vp(p + 4)) == INVALID
+    assert product(q=y) == INVALID and product(s=y) == INVALID and linear(x=y) == INVALID
     assert linear(x=None) == INVALID and linear(ld=99_999) == INVALID and linear(xdtype=4) == UNSUPPORTED and linear(x=vp(p + 2)) == INVALID

@@ -336,6 +336,7 @@ PRODUCTS = [  # n, m, k
     (1, 1, 1), (1, 64, 64), (1, 300, 4096), (2, 257, 1000), (16, 128, 256), (17, 130, 129), (100, 91, 91), (128, 128, 128), (129, 255, 513), (300, 200, 31),
     (1000, 64, 32), (33, 1000, 2048), (512, 512, 512), (5, 3, 100_000), (91, 64, 33_333), (700, 520, 1500), (3500, 3601, 1100), (13, 40, 20_000),
     (16, 2100, 600), (9, 33, 16_384), (9, 33, 8192), (9, 33, 8193), (17, 70, 8000),
+    (1, 40, 16_384), (1, 33, 16_400), (8, 24, 2048), (9, 24, 2048),
 ]
 
 
@@ -409,7 +410,8 @@ def test_what_the_calls_refuse(pcpp):
                  lambda: pcpp.pcpp_group_norm_bwd(x, x, torch.zeros(2, 4, 2, device="cuda")), lambda: pcpp.pcpp_group_norm_bwd(x, x.bfloat16(), torch.zeros(1, 4, 2, device="cuda")),
                  lambda: pcpp.pcpp_mx_pack(x, rows=False), lambda: pcpp.pcpp_mx_pack(x.double()), lambda: pcpp.pcpp_mx_unpack(pcpp.MxRows(w.q, w.scales, 65)),
                  lambda: pcpp.pcpp_mx_linear(x[:, :63], w), lambda: pcpp.pcpp_mx_linear(x, w, x[0]), lambda: pcpp.pcpp_mx_linear(x, w, act=9),
-                 lambda: pcpp.pcpp_mx_product(w, pcpp.pcpp_mx_pack(x[:, :32]).rows), lambda: pcpp.pcpp_mx_product(w, w, out=x)):
+                 lambda: pcpp.pcpp_mx_product(w, pcpp.pcpp_mx_pack(x[:, :32]).rows), lambda: pcpp.pcpp_mx_product(w, w, out=x), lambda: pcpp.pcpp_mx_linear(x[:16, :16], pcpp.pcpp_mx_pack(x[:16, :16]).rows, out=x.view(-1)[:256].view(16, 16)),
+                 lambda: pcpp.pcpp_mx_linear(x[:1], pcpp.pcpp_mx_pack(rows_of(64, 64, F32)).rows, out=x[:1])):
         with pytest.raises(refused):
             call()
 
