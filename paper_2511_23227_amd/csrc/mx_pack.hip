@@ -93,12 +93,11 @@ template <int ES> __device__ inline __amdgpu_buffer_rsrc_t tile_rows(const void 
 template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREADS) void pack_columns_kernel(const MxPackArgs a, const Divisor row_tiles)
 {
     __shared__ __attribute__((aligned(16))) uint8_t tile[TILE_CHANNELS][80];    // 64 bytes a channel, and a pitch that spreads the banks
-    __shared__ uint32_t words[TILE_CHANNELS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rl = lane / 8, cl = lane % 8;
+    __shared__ __attribute__((aligned(8))) uint8_t codes[4][TILE_CHANNELS];    // of the waves' rows
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), rl = lane / 8, cl = lane % 8;
     const uint32_t tile_y = row_tiles.quotient(blockIdx.x), tile_x = blockIdx.x - tile_y * row_tiles.by;
     const int64_t first = (int64_t)tile_x * TILE_ROWS + 32 * wave, c0 = (int64_t)tile_y * TILE_CHANNELS + 8 * cl;      // the wave's first row, the lane's first channel
     const uint32_t row = 4u * (uint32_t)rl;
-    if (threadIdx.x < TILE_CHANNELS) words[threadIdx.x] = 0u;
     Eight<T> v[4];
     if (a.c >= 8) {
         const __amdgpu_buffer_rsrc_t xs = tile_rows<sizeof(T)>(a.x, first, a.n, a.ld_x, a.c);
@@ -148,7 +147,7 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
     }
     // channel by channel: the largest of the wave's 32 rows, four codes of the lane's rows
     const Columns<T> columns(v);
-    __syncthreads();
+    uint32_t scales[2] = {0u, 0u};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const uint32_t code = mx_code(columns.largest_of(e), RANDOM);
@@ -163,14 +162,15 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
         }
         if (code == MX_NAN_CODE) bits = 0u;
         *reinterpret_cast<uint16_t *>(&tile[8 * cl + e][16 * wave + 2 * rl]) = (uint16_t)bits;
-        if (rl == 0 && (int64_t)tile_x * TILE_ROWS + 32 * wave < a.n) reinterpret_cast<uint8_t *>(&words[8 * cl + e])[wave] = (uint8_t)code;
+        scales[e / 4] |= code << 8 * (e % 4);
     }
+    if (rl == 0) *reinterpret_cast<v2u32 *>(&codes[wave][8 * cl]) = first < a.n ? v2u32{scales[0], scales[1]} : v2u32{0u, 0u};
     __syncthreads();
     const int ch = threadIdx.x / 4, part = threadIdx.x % 4;
     const int64_t channel = (int64_t)tile_y * TILE_CHANNELS + ch, block = 4 * (int64_t)tile_x + part;
     if (channel >= a.c) return;
     if (block < mx_blocks(a.n)) *reinterpret_cast<v4u *>(a.qt + channel * mx_row_bytes(a.n) + 16 * block) = *reinterpret_cast<const v4u *>(&tile[ch][16 * part]);
-    if (part == 0) reinterpret_cast<uint32_t *>(a.scales_t + channel * mx_scale_bytes(a.n))[tile_x] = words[ch];
+    if (part == 0) reinterpret_cast<uint32_t *>(a.scales_t + channel * mx_scale_bytes(a.n))[tile_x] = codes[0][ch] | (uint32_t)codes[1][ch] << 8 | (uint32_t)codes[2][ch] << 16 | (uint32_t)codes[3][ch] << 24;
 }
 
 template <typename T> __device__ inline void store_up_to_eight(T *row, int64_t c0, int64_t c, const float (&v)[8])
