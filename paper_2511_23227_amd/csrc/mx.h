@@ -126,20 +126,19 @@ __device__ inline void move_down(Eight<bf16_t> &r, int by)
     for (int i = 0; i < 4; ++i) w[i] = by & 1 ? w[i] >> 16 | (i < 3 ? w[i < 3 ? i + 1 : 3] << 16 : 0u) : w[i];
     r.a[0] = v4u{w[0], w[1], w[2], w[3]};
 }
+template <typename T> __device__ inline void load_within(const T *row, int64_t c0, int64_t c, Eight<T> &r) { load_eight<false>(row + (c0 + 8 <= c ? c0 : c - 8), r); }
+template <typename T> __device__ inline void into_place(int64_t c0, int64_t c, Eight<T> &r)
+{
+    if (c0 + 8 <= c) return;
+    if (c0 < c) return move_down(r, (int)(c0 + 8 - c));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.a[i] = v4u{0u, 0u, 0u, 0u};
+}
 template <typename T> __device__ inline void load_channels(const T *row, int64_t c0, int64_t c, Eight<T> &r)
 {
     if (c >= 8) {
-        const int64_t at = c0 + 8 <= c ? c0 : c - 8;
-        load_eight<false>(row + at, r);
-        if (at != c0) {
-            const int64_t by = c0 - at;
-            if (by < 8) {
-                move_down(r, (int)by);
-            } else {
-#pragma unroll
-                for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.a[i] = v4u{0u, 0u, 0u, 0u};
-            }
-        }
+        load_within(row, c0, c, r);
+        into_place(c0, c, r);
         return;
     }
 #pragma unroll
@@ -171,8 +170,8 @@ struct MxProductArgs {
 };
 size_t mx_product_workspace_bytes(int64_t n, int64_t m, int64_t k);
 int mx_product(const MxProductArgs &a, int out_dtype, hipStream_t stream);
-// few rows of x [n, k] as they are (a and a_scales are not read)
-bool mx_linear_few(int64_t n, int64_t k);
-int mx_linear_few(const MxProductArgs &a, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream);
+// rows of x [n, k] as they are, rounded where they are multiplied (a and a_scales are not read)
+bool mx_linear_alone(int64_t n, int64_t m, int64_t k);
+int mx_linear_alone(const MxProductArgs &a, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream);
 
 }  // namespace pcpp

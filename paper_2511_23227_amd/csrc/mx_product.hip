@@ -110,10 +110,13 @@ __device__ inline void tile_of(uint32_t id, uint32_t rows, uint32_t columns, uin
     y = 8u * band + in - x * high;
 }
 
-// PARTS: blockIdx.y's part of the sum.  ONE: the sum has one stage
-template <typename T, bool PARTS, bool ONE, int WA, int WB, int FA, int FB>
-__global__ __launch_bounds__(64 * WA * WB, ONE ? 4 : (FA == 8 ? 1 : 2)) void tile_kernel(const MxProductArgs p, uint32_t tile_rows, uint32_t tile_columns, int64_t stages, int64_t of_part)
+// PARTS: blockIdx.y's part of the sum.  ONE: the sum has one stage.  X: a's rows come as they are, in that type (uint8_t: in 4 bits), and the block rounds its own.
+template <typename T, typename X, bool PARTS, bool ONE, int WA, int WB, int FA, int FB>
+__global__ __launch_bounds__(64 * WA * WB, ONE ? 4 : (FA == 8 ? 1 : 2)) void tile_kernel(const MxProductArgs p, const X *__restrict__ rows, int64_t ld_rows, uint32_t tile_rows,
+                                                                                         uint32_t tile_columns, int64_t stages, int64_t of_part, const Divisor per_row)
 {
+    constexpr bool ROUND = sizeof(X) > 1;
+    static_assert(!ROUND || ONE, "rounded rows are short");
     typedef Tile<WA, WB, FA, FB> S;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r = lane & 15, l = lane >> 4;
@@ -144,6 +147,7 @@ __global__ __launch_bounds__(64 * WA * WB, ONE ? 4 : (FA == 8 ? 1 : 2)) void til
 #pragma unroll
         for (int i = 0; i < S::SCALE_LOADS; ++i) {
             const bool of_a = S::SCALE_LOADS > 1 ? 64 * i * S::WAVES < S::A : wave < S::A / 64;
+            if (ROUND && of_a) continue;
             const uint32_t row = 64u * (uint32_t)i * S::WAVES - (of_a ? 0u : (uint32_t)S::A);
             rows_to_lds_b128(of_a ? as : bs, STAGE_BLOCKS * stage < some_blocks ? scale_at + row * scale_pitch + STAGE_BLOCKS * stage : OOB_OFFSET,
                              to_lds + 1024u * (wv + (uint32_t)i * S::WAVES));
@@ -193,7 +197,39 @@ __global__ __launch_bounds__(64 * WA * WB, ONE ? 4 : (FA == 8 ? 1 : 2)) void til
 #pragma unroll
     for (int j = 0; j < (ONE ? 1 : 2); ++j)
 #pragma unroll
-        for (int i = 0; i < S::LOADS; ++i) request(first + j, lds0 + j * S::CODES, i);
+        for (int i = ROUND ? S::A / 8 / S::WAVES : 0; i < S::LOADS; ++i) request(first + j, lds0 + j * S::CODES, i);
+    if constexpr (ROUND) {
+        // (what lies behind a row's last block, and rows behind the last: any codes, with scales that are masked and b's zeros, or not stored)
+        const uint32_t total = (p.n - i0 < S::A ? (uint32_t)(p.n - i0) : (uint32_t)S::A) * per_row.by;
+        constexpr uint32_t AT_ONCE = 4, STEP = 64 * S::WAVES;
+        for (uint32_t id0 = threadIdx.x; id0 < total; id0 += AT_ONCE * STEP) {
+            Eight<X> v[AT_ONCE];
+            uint32_t row[AT_ONCE], j[AT_ONCE];
+#pragma unroll
+            for (uint32_t u = 0; u < AT_ONCE; ++u) {              // (past the last as the first, which is left)
+                const uint32_t id = id0 + u * STEP < total ? id0 + u * STEP : id0;
+                row[u] = per_row.quotient(id), j[u] = id - row[u] * per_row.by;
+            }
+            const X *x = rows + i0 * ld_rows;
+            if (p.k >= 8) {
+#pragma unroll
+                for (uint32_t u = 0; u < AT_ONCE; ++u) load_within(x + row[u] * ld_rows, 8 * (int64_t)j[u], p.k, v[u]);
+#pragma unroll
+                for (uint32_t u = 0; u < AT_ONCE; ++u) into_place(8 * (int64_t)j[u], p.k, v[u]);
+            } else {
+#pragma unroll
+                for (uint32_t u = 0; u < AT_ONCE; ++u) load_channels(x + row[u] * ld_rows, 8 * (int64_t)j[u], p.k, v[u]);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < AT_ONCE; ++u) {
+                if (id0 + u * STEP >= total) break;               // (quads stay whole)
+                const uint32_t block = j[u] / 4u, none[4] = {0u, 0u, 0u, 0u}, code = mx_code(quad_largest(largest(v[u])), false), q = mx_quantise<false>(v[u], code, none);
+                *reinterpret_cast<uint32_t *>(lds + row[u] * STAGE_BYTES + 16u * (block ^ spread(row[u] >> 3, row[u] >> 2, row[u] >> 1)) + 4u * (j[u] % 4u)) = q;
+                if (j[u] % 4u == 0u) lds[SCALES_AT + row[u] * SCALE_BYTES + block] = (uint8_t)code;
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(ONE ? 0 : S::LOADS) : "memory");
     read_a_rows(lds, 0);
     read_scales(lds + SCALES_AT, first);
@@ -413,10 +449,11 @@ Shape shape_of(int64_t n, int64_t m, int64_t k)
     return s;
 }
 
-template <typename T, bool PARTS, bool ONE, int WA, int WB, int FA, int FB> int launch_tiles(const MxProductArgs &p, const Shape &s, hipStream_t stream)
+template <typename T, bool PARTS, bool ONE, int WA, int WB, int FA, int FB, typename X = uint8_t>
+int launch_tiles(const MxProductArgs &p, const Shape &s, hipStream_t stream, const X *x = nullptr, int64_t ld_x = 0)
 {
     typedef Tile<WA, WB, FA, FB> L;
-    const auto kernel = tile_kernel<T, PARTS, ONE, WA, WB, FA, FB>;
+    const auto kernel = tile_kernel<T, X, PARTS, ONE, WA, WB, FA, FB>;
     constexpr size_t bytes = (ONE ? 1 : 2) * (size_t)L::BYTES;
     if (int rc = raise_lds_limit(reinterpret_cast<const void *>(kernel), bytes)) return rc;
     // pieces of whole bands whose blocks a grid holds
@@ -424,11 +461,11 @@ template <typename T, bool PARTS, bool ONE, int WA, int WB, int FA, int FB> int 
     for (int64_t y = 0; y < s.rows; y += most) {
         MxProductArgs q = p;
         const int64_t i = y * L::A, rows = s.rows - y < most ? s.rows - y : most;
-        q.a += i * mx_row_bytes(p.k);
-        q.a_scales += i * mx_scale_bytes(p.k);
+        if (!x) q.a += i * mx_row_bytes(p.k), q.a_scales += i * mx_scale_bytes(p.k);
         q.out = static_cast<T *>(p.out) + i * p.m;
         q.n = p.n - i < rows * L::A ? p.n - i : rows * L::A;
-        kernel<<<dim3((unsigned)(rows * s.columns), (unsigned)s.parts), 64 * L::WAVES, bytes, stream>>>(q, (uint32_t)rows, (uint32_t)s.columns, s.stages, s.of_part);
+        kernel<<<dim3((unsigned)(rows * s.columns), (unsigned)s.parts), 64 * L::WAVES, bytes, stream>>>(
+            q, x ? x + i * ld_x : nullptr, ld_x, (uint32_t)rows, (uint32_t)s.columns, s.stages, s.of_part, make_divisor((uint32_t)(4 * mx_blocks(p.k))));
     }
     return PCPP_OK;
 }
@@ -444,13 +481,23 @@ template <typename T, typename X> void launch_few(const MxProductArgs &p, const 
 
 }  // namespace
 
-// (one launch less than rounding first: 1 x 64 x 16 384 in 9.1 us, 12.1)
-bool mx_linear_few(int64_t n, int64_t k) { return n <= FEW_ROWS && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
-int mx_linear_few(const MxProductArgs &p, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream)
+// Which products take rows as they are, one launch less than rounding first.  Few: 1 x 64 x 16 384 in 9.1 us, 12.1.  Sums of one stage with one or two columns of tiles, each of which
+// rounds the rows (115 200 x 64 -> 64 9.9 us, 13.9; 200 000 x 128 -> 256 33, 39, but -> 512 with gelu 87, 82; 100 x 256 -> 256 7.2, 6.6).
+bool few_of_x(int64_t n, int64_t k) { return n <= FEW_ROWS && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
+bool mx_linear_alone(int64_t n, int64_t m, int64_t k) { return few_of_x(n, k) || (k <= STAGE && m <= 256); }
+int mx_linear_alone(const MxProductArgs &p, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream)
 {
-    auto with = [&](auto t, auto s) { launch_few<decltype(t)>(p, static_cast<const decltype(s) *>(x), ld_x, stream); };
-    if (x_dtype == PCPP_F32) out_dtype == PCPP_F32 ? with(float{}, float{}) : with(bf16_t{}, float{});
-    else out_dtype == PCPP_F32 ? with(float{}, bf16_t{}) : with(bf16_t{}, bf16_t{});
+    auto with = [&](auto t, auto s) -> int {
+        typedef decltype(t) T;
+        typedef decltype(s) X;
+        const X *rows = static_cast<const X *>(x);
+        if (!few_of_x(p.n, p.k)) return launch_tiles<T, false, true, 2, 2, 4, 4>(p, shape_of(p.n, p.m, p.k), stream, rows, ld_x);
+        launch_few<T>(p, rows, ld_x, stream);
+        return PCPP_OK;
+    };
+    const int rc = x_dtype == PCPP_F32 ? (out_dtype == PCPP_F32 ? with(float{}, float{}) : with(bf16_t{}, float{}))
+                                       : (out_dtype == PCPP_F32 ? with(float{}, bf16_t{}) : with(bf16_t{}, bf16_t{}));
+    if (rc != PCPP_OK) return rc;
     PCPP_HIP_CHECK(hipGetLastError());
     return PCPP_OK;
 }

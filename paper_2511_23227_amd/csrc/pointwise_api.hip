@@ -263,7 +263,7 @@ int pcpp_mx_product(const uint8_t *a, const uint8_t *a_scales, const uint8_t *b,
 
 size_t pcpp_mx_linear_workspace_bytes(int64_t n, int64_t m, int64_t k)
 {
-    if (!sizes(n, m, k) || mx_linear_few(n, k)) return 0;
+    if (!sizes(n, m, k) || mx_linear_alone(n, m, k)) return 0;
     return linear_codes(n, k) + linear_scales(n, k) + mx_product_workspace_bytes(n, m, k);
 }
 
@@ -284,7 +284,7 @@ int pcpp_mx_linear(const void *x, int64_t ld_x, int x_dtype, const uint8_t *w, c
     MxProductArgs p{};
     p.b = w; p.b_scales = w_scales; p.bias = bias; p.out = out;
     p.n = n; p.m = m; p.k = k; p.act = act;
-    if (mx_linear_few(n, k)) return mx_linear_few(p, x, x_dtype, ld_x, out_dtype, stream);
+    if (mx_linear_alone(n, m, k)) return mx_linear_alone(p, x, x_dtype, ld_x, out_dtype, stream);
     char *at = static_cast<char *>(workspace);
     MxPackArgs a{};
     a.x = x; a.q = reinterpret_cast<uint8_t *>(at); a.scales = a.q + linear_codes(n, k);

@@ -337,6 +337,7 @@ PRODUCTS = [  # n, m, k
     (1000, 64, 32), (33, 1000, 2048), (512, 512, 512), (5, 3, 100_000), (91, 64, 33_333), (700, 520, 1500), (3500, 3601, 1100), (13, 40, 20_000),
     (16, 2100, 600), (9, 33, 16_384), (9, 33, 8192), (9, 33, 8193), (17, 70, 8000),
     (1, 40, 16_384), (1, 33, 16_400), (8, 24, 2048), (9, 24, 2048),
+    (130, 256, 256), (130, 257, 256), (300, 100, 7), (129, 200, 257), (1000, 72, 91), (17, 9, 1),
 ]
 
 
