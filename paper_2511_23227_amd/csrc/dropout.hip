@@ -6,6 +6,9 @@
 // The bits come from a counter (philox.h) and are formed again where they are needed: no mask is stored.  A thread takes eight
 // neighbouring channels, which share a counter.  Where a row ends inside a thread's eight channels it takes the row's last eight instead,
 // some of which are the thread before's too: their bits come from that thread, and both write the same.
+//
+// Memory bounds it: 1 000 000 x 256 bf16 in 166 us, 6.2 TB/s; 99 991 x 91 bf16 onto an fp32 residual in 15.1 us, 6.0 TB/s.  The ten rounds of the
+// generator hide behind it (138 vector instructions a wave in all).
 #include "pointwise.h"
 
 namespace pcpp {

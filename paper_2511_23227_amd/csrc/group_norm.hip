@@ -11,6 +11,13 @@
 //
 // Statistics: a lane sums x - k and (x - k)^2, k the range's first row, which cannot lose what the variance is made of unless that row lies
 // thousands of deviations off; channels, chunks and clouds are joined by their means and sums of squares about them.
+//
+// Forward x is read twice, backward x and dy are, since nothing can be written before the last row of a cloud is known; the second pass goes from the
+// end on, where the caches still have rows.  1 000 000 x 256 bf16 takes 310 us forward (1.5 GB moved at 5.0 TB/s) and 511 backward with dropout (2.6
+// GB, 5.0 TB/s: memory, with the generator's and the activation's 42 000 vector instructions a wave for each pass beside it); 99 991 x 91 fp32 44
+// backward (4.1 TB/s; three launches).  115 200 x 64 takes 26.6 forward where its bytes take 9: two kernels of 10 and 18, each a chain of the first
+// loads, the statistics joined over 56 chunks, and gelu and dropout at two waves a SIMD (blocks of half and a quarter of the rows for the second
+// kernel: as long, and 2 us more).
 #include "pointwise.h"
 
 namespace pcpp {
@@ -100,16 +107,6 @@ __device__ inline void drop_rows(const Philox &philox, uint32_t at, int c, const
             for (int e = 0; e < 8; ++e) v[g][e] = half_of(x, e) >= drop.threshold ? v[g][e] : 0.f;
         }
     }
-}
-
-template <int ACT> struct Act { static constexpr int value = ACT; };
-// f(activation): a branch that all lanes take alike
-template <typename F> __device__ inline void as_act(int act, F f)
-{
-    if (act == PCPP_ACT_SILU) f(Act<PCPP_ACT_SILU>{});
-    else if (act == PCPP_ACT_GELU) f(Act<PCPP_ACT_GELU>{});
-    else if (act == PCPP_ACT_RELU) f(Act<PCPP_ACT_RELU>{});
-    else f(Act<PCPP_ACT_NONE>{});
 }
 
 // v over the lanes of a wave that hold the same channels of other rows: every LPR-th lane
@@ -782,15 +779,16 @@ template <typename F> void with_kernel(int dtype, int c, int groups, F f)
 }
 
 int64_t rows_at_once(int c) { return WAVES * 64 / row_lanes(c); }
-// A block to a cloud, from its statistics to its rows, in place of passes over chunks: where a cloud has ten steps of a block or fewer on average.  (256 x 64 of one cloud, eight
-// steps: 8.1 us forward and 12.8 backward, by chunks 10.0 and 14.3; 1000 x 16, sixteen: 11.0 and 19.9, 10.6 and 15.3.  Eighty steps in all at most, for clouds of very different sizes.)
+// A block to a cloud, from its statistics to its rows, in place of passes over chunks: where a cloud has ten steps of a block or fewer on average.
+// (256 x 64 of one cloud, eight steps: 8.1 us forward and 12.8 backward, by chunks 10.0 and 14.3; 1000 x 16, sixteen: 11.0 and 19.9, 10.6 and 15.3.
+// Eighty steps in all at most, for clouds of very different sizes.)
 bool block_a_cloud(int64_t n, int c, int n_clouds)
 {
     const int64_t steps = ceil_div(n, rows_at_once(c));
     return steps <= 80 && steps <= 10 * (int64_t)n_clouds;
 }
-// Whether the blocks that write y join the chunks' statistics for themselves: that saves a launch and costs each a read of their clouds' (8 groups, 115 200 x 64 of one cloud: 19.4 us
-// for 20.7; 16 groups 23.7 for 21.6; 30 000 x 64, 235 chunks of 16 groups: 13.6 for 15.0)
+// Whether the blocks that write y join the chunks' statistics for themselves: that saves a launch and costs each a read of their clouds' (8 groups,
+// 115 200 x 64 of one cloud: 19.4 us for 20.7; 16 groups 23.7 for 21.6; 30 000 x 64, 235 chunks of 16 groups: 13.6 for 15.0)
 bool join_in_place(const GroupNormSizes &s, int groups) { return (int64_t)s.chunks * groups <= 4096; }
 
 }  // namespace
@@ -800,7 +798,8 @@ GroupNormSizes group_norm_sizes(int64_t n, int c, int n_clouds, int groups, bool
 {
     GroupNormSizes s{};
     const int64_t step = rows_at_once(c);
-    // (two blocks for each CU; four make 5 of 43 us more of 99 991 x 91, one takes a third more of 1 000 000 x 256.  More for very many clouds, which a block takes one by one.)
+    // (two blocks for each CU; four make 5 of 43 us more of 99 991 x 91, one takes a third more of 1 000 000 x 256.  More for very many clouds, which
+    // a block takes one by one.)
     const int64_t most = n_clouds > 512 ? n_clouds : 512, of_cloud = ceil_div(ceil_div(n, n_clouds), step), least = of_cloud < 4 ? (of_cloud > 1 ? of_cloud : 1) : 4;
     s.rows = ceil_div(ceil_div(n, most), step) * step;
     if (s.rows < least * step) s.rows = least * step;

@@ -26,10 +26,10 @@ __device__ inline uint32_t mx_code(uint32_t amax, bool random)
 __device__ inline float mx_step(uint32_t code) { return __uint_as_float(code << 23); }      // (255: what comes of it is left aside)
 
 // ---- eight numbers as they lie in memory to eight 4-bit codes -----------------------------------------------------------------------
-// The conversions divide by the power of two (exactly) and round to nearest (ties to the even fraction) or at random: a 32-bit fraction is added to what lies below the
-// last place, here an element's sixteen bits in the upper half, so up if the remainder's first sixteen bits and they make a whole step.  Past 6 they give 6.  A pair of numbers
-// shares a conversion; at random each takes its own, of which only its half is used (the second of a pair takes the fraction one place lower; the compiler does not hand the destination's other bytes on, so they are
-// put together here).
+// The conversions divide by the power of two (exactly) and round to nearest (ties to the even fraction) or at random: a 32-bit fraction is added to
+// what lies below the last place, here an element's sixteen bits in the upper half, so up if the remainder's first sixteen bits and they make a whole
+// step.  Past 6 they give 6.  A pair of numbers shares a conversion; at random each takes its own, of which only its half is used (the second of a
+// pair takes the fraction one place lower; the compiler does not hand the destination's other bytes on, so they are put together here).
 typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
 template <typename T> struct Pair;
 template <> struct Pair<float> {

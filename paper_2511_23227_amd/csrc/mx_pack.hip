@@ -4,6 +4,10 @@
 // the transposed matrix, for products that sum over the rows): a wave takes 32 rows of 64 channels, a lane four rows of eight channels, so that the maximum goes
 // over eight lanes; a block's 128 rows go through LDS and leave in pieces of 64 bytes of a channel.  Both forms come of one pass where both are wanted.
 // Scaling by a power of two is exact, so the codes are the same in any implementation.
+//
+// To nearest memory bounds it: rows of 199 993 x 128 bf16 in 12.7 us (5.1 TB/s), columns of 200 000 x 128 in 17.5 (3.7), back to bf16 16.7 (3.9).  At
+// random vector instructions do: 580 a wave for 2048 elements of columns (100 000 x 91 fp32 14.8 us, 2.8 TB/s), 750 for rows and columns (200 000 x
+// 256 bf16 47 us, 3.3 TB/s), 20 wide multiplications of the generator for eight elements and a conversion for each element and form among them.
 #include "mx.h"
 
 namespace pcpp {

@@ -3,6 +3,10 @@
 // The scaled matrix instruction takes 16 x 128 elements of either side, a lane 32 of one row, which is a block, with the block's power of
 // two; products and sums are fp32.  b's rows go to the instruction's rows, so that a lane ends with four neighbouring columns of one row of out.
 // Where there are few tiles and many elements to sum, the sum is cut into parts, which are joined in order by a second kernel.
+//
+// 8192 x 8192 x 8192 takes 290 to 335 us by the numbers and the card, 3.8 to 3.3 PFLOP/s (the matrix instructions alone reach 8.5 on constant numbers and 6 to 7 on random ones, with their
+// operands from LDS but no requests 4.3 to 4.8). 115 200 x 64 -> 256 with gelu takes 28 us with the rounding of x (bytes 15): the vector instructions
+// of 29 million activations.  256 x 128 x 200 000 takes 21 (bytes 8), a block for each CU and a join of 4.7.
 #include "mx.h"
 
 namespace pcpp {
@@ -13,7 +17,6 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_anywhere __attribute__((ext_vector_type(4), aligned(4)));
 typedef v2u32 v2u32_anywhere __attribute__((aligned(2)));
-
 
 // which bytes of the scales
 template <int B_BYTE, int A_BYTE = B_BYTE> __device__ inline v4f multiply(const v4u &b, const v4u &a, v4f sum, uint32_t b_scale, uint32_t a_scale)
@@ -45,31 +48,24 @@ template <int N> __device__ inline void load_bias(const float *bias, int64_t j, 
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = bias && j + e < m ? bias[j + e] : 0.f;
 }
-// f(activation): a branch that all lanes take alike
-template <typename F> __device__ inline void as_act(int act, F f)
-{
-    if (act == PCPP_ACT_NONE) f(Int<PCPP_ACT_NONE>{});
-    else if (act == PCPP_ACT_SILU) f(Int<PCPP_ACT_SILU>{});
-    else if (act == PCPP_ACT_GELU) f(Int<PCPP_ACT_GELU>{});
-    else f(Int<PCPP_ACT_RELU>{});
-}
 
 // ---- tiles through LDS --------------------------------------------------------------------------------------------------------------
-// A block of WA x WB waves takes 16 WA FA rows of a and 16 WB FB of b, a wave 16 FA and 16 FB of them.  A stage is 256 elements: 128 bytes of every row's
-// codes, a whole cache line, moved straight into LDS, and with every second one the sixteen scales of two (a request of eight takes the caches as long as one of a line: 153 us
-// for 130).  (Stages of 128 elements, three of them ahead: 8192 x 8192 x 8192
-// in 401 us for 337.)
+// A block of WA x WB waves takes 16 WA FA rows of a and 16 WB FB of b, a wave 16 FA and 16 FB of them.  A stage is 256 elements: 128 bytes of every
+// row's codes, a whole cache line, moved straight into LDS, and with every second one the sixteen scales of two (a request of eight takes the caches
+// as long as one of a line: 153 us for 130).  (Stages of 128 elements, three of them ahead: 8192 x 8192 x 8192 in 401 us where these took 337, before
+// the order below.)
 //
-// What a wave does meanwhile is laid out by hand.  A stage is two instructions deep.  While the first one's products run the operands of the second are read; then all waves
-// meet, the stage's place in LDS is free, and the stage after the next is requested, two requests at a time between the products (a compute unit takes as long for the requests
-// as for the products).  Half way through the second one's products the next stage, requested one and a half stages ago, is waited for, and the operands of its first are
-// read.
+// What a wave does meanwhile is laid out by hand.  A stage is two instructions deep.  While the first one's products run the operands of the second
+// are read; then all waves meet, the stage's place in LDS is free, and the stage after the next is requested, two requests at a time between the
+// products (a compute unit takes as long for the requests as for the products).  Half way through the second one's products the next stage, requested
+// one and a half stages ago, is waited for, and the operands of its first are read.
 //
-// A row's eight 16-byte pieces (blocks) lie in LDS at piece ^ s, s a function of the row.  The sixteen lanes whose reads share a cycle are 0-3, 12-15 and 20-27 (or 4-11,
-// 16-19 and 28-31; the same again 32 further on), so of an instruction's rows r 0-3 and 12-15 with one piece and 4-11 with the piece two on: with bit 2 of s set for rows 4-11
-// and its other bits from bits 3 and 1 of r they meet all banks (s = r / 2 mod 8, made for neighbouring lanes, doubled the cycles of every read).  b's rows go to two instructions in turn, four by four, so that a lane ends with eight neighbouring columns of a row of out.
-// Lane (r, l) of an instruction has row r; over the stage's two instructions it takes the blocks 2 l and 2 l + 1, whose scales are one 16-bit read (the order in
-// which blocks are summed is free).
+// A row's eight 16-byte pieces (blocks) lie in LDS at piece ^ s, s a function of the row.  The sixteen lanes whose reads share a cycle are 0-3, 12-15
+// and 20-27 (or 4-11, 16-19 and 28-31; the same again 32 further on), so of an instruction's rows r 0-3 and 12-15 with one piece and 4-11 with the
+// piece two on: with bit 2 of s set for rows 4-11 and its other bits from bits 3 and 1 of r they meet all banks (s = r / 2 mod 8, made for
+// neighbouring lanes, doubled the cycles of every read).  b's rows go to two instructions in turn, four by four, so that a lane ends with eight
+// neighbouring columns of a row of out. Lane (r, l) of an instruction has row r; over the stage's two instructions it takes the blocks 2 l and 2 l +
+// 1, whose scales are one 16-bit read (the order in which blocks are summed is free).
 constexpr int STAGE = 256, STAGE_BYTES = 128, STAGE_BLOCKS = 8, SCALE_BYTES = 16;         // (a row's scales of two stages)
 
 // rows of a tensor as a descriptor in scalar registers, for inline assembly
@@ -81,15 +77,11 @@ __device__ inline v4u scalar_rows(const uint8_t *p, int64_t first, int64_t n, in
     return v4u{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)),
                (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
-// 16 (4) bytes a lane from its offset behind the descriptor's start to LDS byte address `lds` + 16 (4) lane; zeros past the descriptor.  (The address travels in
+// 16 bytes a lane from its offset behind the descriptor's start to LDS byte address `lds` + 16 lane; zeros past the descriptor.  (The address travels in
 // M0, which the compiler reserves and nothing else here uses.)
 __device__ inline void rows_to_lds_b128(const v4u &rows, uint32_t offset, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(rows), "s"(lds) : "memory");
-}
-__device__ inline void rows_to_lds_b32(const v4u &rows, uint32_t offset, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(rows), "s"(lds) : "memory");
 }
 
 template <int WA, int WB, int FA, int FB> struct Tile {
@@ -332,9 +324,9 @@ template <typename T> __global__ __launch_bounds__(1024) void join_kernel(const 
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------------------
-// Up to sixteen rows of a: what counts is reading b once.  A block takes sixteen rows of b, its waves every WAVES-th stage of the sum; codes go from memory to
-// the registers of the lanes that multiply them.  a comes in 4 bits or, of few elements, as it is: the block rounds it into LDS while its first rows of b are on
-// their way.
+// Up to sixteen rows of a: what counts is reading b once (1 x 16 384 x 4096: 9.8 us with the rounding of a, 3.6 TB/s; an empty kernel takes 2.3).  A
+// block takes sixteen rows of b, its waves every WAVES-th stage of the sum; codes go from memory to the registers of the lanes that multiply them.  a
+// comes in 4 bits or, of few elements, as it is: the block rounds it into LDS while its first rows of b are on their way.
 constexpr int FEW_ROWS = 16;
 constexpr int64_t FEW_ELEMENTS = 16384;                           // of a that every block rounds for itself (9 KB of LDS; 1 x 4096 x 32 768 28 us, rounded first 21)
 
@@ -481,8 +473,9 @@ template <typename T, typename X> void launch_few(const MxProductArgs &p, const 
 
 }  // namespace
 
-// Which products take rows as they are, one launch less than rounding first.  Few: 1 x 64 x 16 384 in 9.1 us, 12.1.  Sums of one stage with one or two columns of tiles, each of which
-// rounds the rows (115 200 x 64 -> 64 9.9 us, 13.9; 200 000 x 128 -> 256 33, 39, but -> 512 with gelu 87, 82; 100 x 256 -> 256 7.2, 6.6).
+// Which products take rows as they are, one launch less than rounding first.  Few: 1 x 64 x 16 384 in 9.1 us, 12.1.  Sums of one stage with one or
+// two columns of tiles, each of which rounds the rows (115 200 x 64 -> 64 9.9 us, 13.9; 200 000 x 128 -> 256 33, 39, but -> 512 with gelu 87, 82; 100
+// x 256 -> 256 7.2, 6.6).
 bool few_of_x(int64_t n, int64_t k) { return n <= FEW_ROWS && n * MX_BLOCK * mx_blocks(k) <= FEW_ELEMENTS; }
 bool mx_linear_alone(int64_t n, int64_t m, int64_t k) { return few_of_x(n, k) || (k <= STAGE && m <= 256); }
 int mx_linear_alone(const MxProductArgs &p, const void *x, int x_dtype, int64_t ld_x, int out_dtype, hipStream_t stream)

@@ -83,9 +83,10 @@ struct WaveClouds {
 
 // ---- activations --------------------------------------------------------------------------------------------------------------
 __device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
-// The normal distribution below -a, a >= 0: 2 to a polynomial of degree 10, fitted to the logarithm over 0 .. 8 by least squares for the absolute error (and a
-// hundredth of it for the relative), reweighted until it was level; behind 8 it goes on falling.  In fp32 off by 1.1e-7 at most, a times it by 5e-8, and by 3e-5 of itself below 6.
-// One exponential and no division: with the library's erff a 115 200 x 256 output took 20 us longer than without an activation, with exp(-a^2) t P(t), t = 1 / (1 + k a), 12.
+// The normal distribution below -a, a >= 0: 2 to a polynomial of degree 10, fitted to the logarithm over 0 .. 8 by least squares for the absolute
+// error (and a hundredth of it for the relative), reweighted until it was level; behind 8 it goes on falling.  In fp32 off by 1.1e-7 at most, a times
+// it by 5e-8, and by 3e-5 of itself below 6. One exponential and no division: with the library's erff a 115 200 x 256 output took 20 us longer than
+// without an activation, with exp(-a^2) t P(t), t = 1 / (1 + k a), 12.
 __device__ inline float normal_tail(float a)
 {
     float p = -8.52743387e-09f;
@@ -122,14 +123,13 @@ template <int ACT> __device__ inline float slope(float z)         // the derivat
         return z > 0.f ? 1.f - below : below;
     } else return 1.f;
 }
-template <typename F> void with_act(int act, F f)
+// f(activation): a branch that all lanes take alike
+template <typename F> __device__ inline void as_act(int act, F f)
 {
-    switch (act) {
-    case PCPP_ACT_RELU: return f(Int<PCPP_ACT_RELU>{});
-    case PCPP_ACT_SILU: return f(Int<PCPP_ACT_SILU>{});
-    case PCPP_ACT_GELU: return f(Int<PCPP_ACT_GELU>{});
-    default: return f(Int<PCPP_ACT_NONE>{});
-    }
+    if (act == PCPP_ACT_NONE) f(Int<PCPP_ACT_NONE>{});
+    else if (act == PCPP_ACT_SILU) f(Int<PCPP_ACT_SILU>{});
+    else if (act == PCPP_ACT_GELU) f(Int<PCPP_ACT_GELU>{});
+    else f(Int<PCPP_ACT_RELU>{});
 }
 
 // ---- x / d by a multiplication (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994) ---------------
