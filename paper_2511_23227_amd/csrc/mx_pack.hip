@@ -5,7 +5,8 @@
 // over eight lanes; a block's 128 rows go through LDS and leave in pieces of 64 bytes of a channel.  Both forms come of one pass where both are wanted.
 // Scaling by a power of two is exact, so the codes are the same in any implementation.
 //
-// To nearest memory bounds it: rows of 199 993 x 128 bf16 in 12.7 us (5.1 TB/s), columns of 200 000 x 128 in 17.5 (3.7), back to bf16 16.7 (3.9).  At
+// To nearest memory bounds it: rows of 199 993 x 128 bf16 in 12.7 us (5.1 TB/s), columns of 200 000 x 128 in 17.5 (3.7), back to bf16
+// 11.1 (5.9; with the values formed by hand, where the conversions take a third of the instructions, 17).  At
 // random vector instructions do: 580 a wave for 2048 elements of columns (100 000 x 91 fp32 14.8 us, 2.8 TB/s), 750 for rows and columns (200 000 x
 // 256 bf16 47 us, 3.3 TB/s), 20 wide multiplications of the generator for eight elements and a conversion for each element and form among them.
 #include "mx.h"
@@ -177,12 +178,33 @@ template <typename T, bool RANDOM, bool ROWS> __global__ __launch_bounds__(THREA
     if (part == 0) reinterpret_cast<uint32_t *>(a.scales_t + channel * mx_scale_bytes(a.n))[tile_x] = codes[0][ch] | (uint32_t)codes[1][ch] << 8 | (uint32_t)codes[2][ch] << 16 | (uint32_t)codes[3][ch] << 24;
 }
 
-template <typename T> __device__ inline void store_up_to_eight(T *row, int64_t c0, int64_t c, const float (&v)[8])
+// The values of eight codes, which the conversions multiply by the power of two, to a row's channels c0 .. up to the last
+__device__ inline void store_values(float *row, int64_t c0, int64_t c, uint32_t bits, uint32_t code)
 {
+    const float step = mx_step(code);
+    const v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(bits, step, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(bits, step, 1),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(bits, step, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(bits, step, 3)};
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = code == MX_NAN_CODE ? __builtin_nanf("") : p[e >> 1][e & 1];
     if (c0 + 8 <= c) return store_eight<false>(row + c0, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (c0 + e < c) row[c0 + e] = one_of<T>(v[e]);
+    for (int e = 0; e < 7; ++e)
+        if (c0 + e < c) row[c0 + e] = v[e];
+}
+__device__ inline void store_values(bf16_t *row, int64_t c0, int64_t c, uint32_t bits, uint32_t code)
+{
+    const float step = mx_step(code);
+    v4u w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(bits, step, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(bits, step, 1)),
+             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(bits, step, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(bits, step, 3))};
+    if (code == MX_NAN_CODE) w = v4u{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    if (c0 + 8 <= c) {
+        *reinterpret_cast<v4u_anywhere *>(row + c0) = w;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (c0 + e < c) row[c0 + e] = (bf16_t)(w[e >> 1] >> 16 * (e & 1));
 }
 
 template <typename T>
@@ -194,16 +216,7 @@ __global__ __launch_bounds__(THREADS) void unpack_kernel(const uint8_t *__restri
     const uint32_t r = per_row.quotient(id), j = id - r * per_row.by;
     const int64_t row = first + r;
     const uint32_t bits = reinterpret_cast<const uint32_t *>(q + row * mx_row_bytes(c))[j], code = scales[row * mx_scale_bytes(c) + j / 4];
-    const float step = __uint_as_float(code << 23), half_step = code ? 0.5f * step : 0x1p-128f;           // (code 0: 2^-127, subnormal)
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t k = bits >> (4 * e) & 7u;
-        const float twice = (float)(k < 4u ? k : (k & 1u ? (k == 5u ? 6u : 12u) : (k == 4u ? 4u : 8u)));
-        v[e] = code == MX_NAN_CODE ? __builtin_nanf("") : twice * half_step;
-        v[e] = bits >> (4 * e) & 8u ? -v[e] : v[e];
-    }
-    store_up_to_eight(x + row * c, 8 * (int64_t)j, c, v);
+    store_values(x + row * c, 8 * (int64_t)j, c, bits, code);
 }
 
 template <typename F> void with_type(int dtype, F f)
