@@ -472,7 +472,7 @@ PCPP_API int pcpp_group_norm_bwd(const void *dy, const void *x, int64_t ld_x, co
  * this call on rows of x and W; rows of dy and columns of W; columns of dy and of x.
  * pcpp_mx_linear takes a as x [n, k] x_dtype, row pitch ld_x, and rounds it to 4 bits to nearest on the way.  Outputs may not overlap inputs.
  *   workspace  pcpp_mx_product_workspace_bytes / pcpp_mx_linear_workspace_bytes(n, m, k) bytes, 256-byte aligned (may be NULL if that is 0)
- * Errors: INVALID_ARG (also: m or k < 1), WORKSPACE, UNSUPPORTED (k or m >= 2^24, n >= 2^31, pitch >= 2^25, dtype).
+ * Errors: INVALID_ARG (also: m or k < 1; the gradient of a batch without rows, zeros, is the caller's to write), WORKSPACE, UNSUPPORTED (k or m >= 2^24, n >= 2^31, pitch >= 2^25, dtype).
  * ------------------------------------------------------------------------------------------- */
 PCPP_API size_t pcpp_mx_row_bytes(int64_t c);    /* 0 if c is outside 1 .. 2^24 - 1 */
 PCPP_API size_t pcpp_mx_scale_bytes(int64_t c);

@@ -688,7 +688,8 @@ def pcpp_mx_unpack(m: MxRows, dtype: torch.dtype = torch.bfloat16, out: torch.Te
 
 def pcpp_mx_product(a: MxRows, b: MxRows, bias: torch.Tensor | None = None, *, act: int = ACT_NONE, dtype: torch.dtype = torch.bfloat16,
                     out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """act(a b^T + bias): every row of a with every row of b, summed in fp32, bias float32 [rows of b]."""
+    """act(a b^T + bias): every row of a with every row of b, summed in fp32, bias float32 [rows of b].  Columns of a batch without rows
+    are rows of no elements: act(bias), so zeros for its weights' gradient."""
     return _outputs(_compiled().mx_product(a.q, a.scales, a.c, b.q, b.scales, b.c, bias, act, _code_or(dtype), out, workspace, *_where()))[0]
 
 

@@ -12,6 +12,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/zeros.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "pcpp.h"
@@ -610,6 +611,7 @@ PyObject *group_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 
 int64_t mx_row_bytes(int64_t c) { return (c + 31) / 32 * 16; }
 int64_t mx_scale_bytes(int64_t c) { return (c + 127) / 128 * 4; }
+// Rows of no elements (c = 0) are the columns of a batch without rows.
 struct Rows4 {
     const uint8_t *q, *scales;
     int64_t n, c;
@@ -617,7 +619,7 @@ struct Rows4 {
     {
         const Tensor &codes = args.tensor(), &exponents = args.tensor();
         c = args.integer();
-        need(c >= 1 && c < (1 << 24), "channels outside 1 .. 2^24 - 1");
+        need(c >= 0 && c < (1 << 24), "channels outside 0 .. 2^24 - 1");
         n = codes.dim() == 2 ? codes.size(0) : -1;
         need(codes.scalar_type() == at::kByte && exponents.scalar_type() == at::kByte && codes.is_contiguous() && exponents.is_contiguous() &&
                  shape(codes, n, mx_row_bytes(c)) && shape(exponents, n, mx_scale_bytes(c)),
@@ -660,7 +662,8 @@ PyObject *mx_unpack(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         void *stream = args.stream();
         if (given) need_rows(*given, rows.n, rows.c, "out has another shape than the rows, or is not contiguous");
         const Tensor out = given ? *given : empty({rows.n, rows.c}, type_of(code), like);
-        const int rc = lib.mx_unpack(rows.q, rows.scales, rows.n, rows.c, out.data_ptr(), code_of(out.scalar_type()), stream);
+        const int type = code_of(out.scalar_type());
+        const int rc = rows.c == 0 ? PCPP_OK : lib.mx_unpack(rows.q, rows.scales, rows.n, rows.c, out.data_ptr(), type, stream);
         written(given);
         return result(rc, out);
     });
@@ -677,9 +680,9 @@ const float *bias_at(const Tensor *t, int64_t m)
 PyObject *mx_product(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     return guarded(a, n_args, [](Args &args) {
-        const Rows4 x(args);
+        Rows4 x(args);
         const Tensor &like = THPVariable_Unpack(args.a[0]);
-        const Rows4 w(args);
+        Rows4 w(args);
         const Tensor *bias = args.optional();
         const int act = args.small();
         const int64_t wanted = args.integer();
@@ -688,6 +691,12 @@ PyObject *mx_product(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         need(x.c == w.c, "both sides have the same number of channels");
         if (given) need_rows(*given, x.n, w.n, "out is [n, m], contiguous");
         const Tensor out = given ? *given : empty({x.n, w.n}, type_of(wanted), like);
+        Tensor none;
+        if (x.c == 0) {                                           // (sums of nothing: those of one block of zeros on either side)
+            none = at::zeros({x.n > w.n ? x.n : w.n, mx_row_bytes(1)}, like.options());
+            x.q = w.q = x.scales = w.scales = static_cast<const uint8_t *>(none.data_ptr());
+            x.c = w.c = 1;
+        }
         const size_t bytes = lib.mx_product_workspace_bytes(x.n, w.n, x.c);
         Tensor ws;
         if (bytes) ws = workspace_of(bytes, workspace, like);
