@@ -85,7 +85,7 @@ struct WaveClouds {
 __device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
 // The normal distribution below -a, a >= 0: 2 to a polynomial of degree 10, fitted to the logarithm over 0 .. 8 by least squares for the absolute
 // error (and a hundredth of it for the relative), reweighted until it was level; behind 8 it goes on falling.  In fp32 off by 1.1e-7 at most, a times
-// it by 5e-8, and by 3e-5 of itself below 6. One exponential and no division: with the library's erff a 115 200 x 256 output took 20 us longer than
+// it by 5e-8, and by 3.5e-5 of itself below 6. One exponential and no division: with the library's erff a 115 200 x 256 output took 20 us longer than
 // without an activation, with exp(-a^2) t P(t), t = 1 / (1 + k a), 12.
 __device__ inline float normal_tail(float a)
 {
