@@ -422,10 +422,10 @@ PCPP_API int pcpp_dropout_bwd(const void *dy, const int64_t *random, uint32_t si
  *   x          [n, c] dtype, row pitch ld_x elements, aligned to an element
  *   w, b       [c] fp32; NULL: ones, zeros
  *   random, site, p   dropout of the elements as in pcpp_dropout_fwd; p = 0: none (random may be NULL)
- *   y          [n, c] dtype, contiguous
- *   mean_rstd  [n_clouds, groups, 2] fp32, for the gradient (NULL: not wanted); (0, 0) for an empty cloud
+ *   y          [n, c] dtype, contiguous, 16-byte aligned, as are dy and dx
+ *   mean_rstd  [n_clouds, groups, 2] fp32, 8-byte aligned, for the gradient (NULL: not wanted); (0, 0) for an empty cloud
  *   workspace  pcpp_group_norm_workspace_bytes(n, c, n_clouds, groups, 0) bytes, 256-byte aligned (may be NULL if that is 0)
- * An Inf or NaN makes its cloud's group NaN, and no other.
+ * An Inf or NaN makes its cloud's group NaN, and no other.  Squares are summed in fp32: where the sum passes its range (deviations of 2^60) rstd is 0.
  *
  * Gradients, from dy [n, c] dtype, contiguous, and the forward pass's mean_rstd:
  *   dz = drop(dy) * act'(z),  dx = rstd * (w * dz - m1 - v * m2),  m1, m2 = means of w * dz and of w * dz * v over the cloud and group,
@@ -469,7 +469,8 @@ PCPP_API int pcpp_group_norm_bwd(const void *dy, const void *x, int64_t ld_x, co
  *
  * Products of such rows, out[i, j] = act(sum_l a[i, l] * b[j, l] + bias[j]) with a [n, k], b [m, k], bias [m] fp32 (NULL: none), out [n, m] out_dtype,
  * contiguous, aligned to an element.  Products and sums are fp32, rounded once.  A linear layer y = x W^T and its gradients dx = dy W, dW = dy^T x are
- * this call on rows of x and W; rows of dy and columns of W; columns of dy and of x.
+ * this call on rows of x and W; rows of dy and columns of W; columns of dy and of x.  What flows back through act and into bias (act'(z) dy, for
+ * which z has to be kept or formed again, and its sums over the rows) is the caller's.
  * pcpp_mx_linear takes a as x [n, k] x_dtype, row pitch ld_x, and rounds it to 4 bits to nearest on the way.  Outputs may not overlap inputs.
  *   workspace  pcpp_mx_product_workspace_bytes / pcpp_mx_linear_workspace_bytes(n, m, k) bytes, 256-byte aligned (may be NULL if that is 0)
  * Errors: INVALID_ARG (also: m or k < 1; the gradient of a batch without rows, zeros, is the caller's to write), WORKSPACE, UNSUPPORTED (k or m >= 2^24, n >= 2^31, pitch >= 2^25, dtype).

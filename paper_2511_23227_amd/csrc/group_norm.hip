@@ -15,9 +15,9 @@
 // Forward x is read twice, backward x and dy are, since nothing can be written before the last row of a cloud is known; the second pass goes from the
 // end on, where the caches still have rows.  1 000 000 x 256 bf16 takes 310 us forward (1.5 GB moved at 5.0 TB/s) and 511 backward with dropout (2.6
 // GB, 5.0 TB/s: memory, with the generator's and the activation's 42 000 vector instructions a wave for each pass beside it); 99 991 x 91 fp32 44
-// backward (4.1 TB/s; three launches).  115 200 x 64 takes 26.6 forward where its bytes take 9: two kernels of 10 and 18, each a chain of the first
-// loads, the statistics joined over 56 chunks, and gelu and dropout at two waves a SIMD (blocks of half and a quarter of the rows for the second
-// kernel: as long, and 2 us more).
+// backward (4.1 TB/s; three launches).  115 200 x 64 takes 26.8 forward where its bytes take 9: two kernels of 10 and 18.  Of the second about 8 are
+// the vector instructions of gelu and dropout (2400 a wave), the rest a chain of the first loads and the statistics joined over 56 chunks, which two
+// waves a SIMD do not hide (blocks of half and a quarter of the rows for it: as long, and 2 us more).
 #include "pointwise.h"
 
 namespace pcpp {
@@ -338,7 +338,8 @@ __device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t h
     }
 }
 
-// What the gradients' two passes know of a lane's channels.  v = x rstd + shift, z = x by + off
+// What the gradients' two passes know of a lane's channels.  v = x rstd + shift, z = x by + off: one operation each, and two roundings the size of
+// mean rstd where (x - mean) rstd has that of the mean itself alone (gradients of 99 991 x 91 fp32: 1.2e-7 of their length off, plain operations in fp32 0.8e-7).
 template <bool ALIKE, int G> struct Known {
     float rstd[G][ALIKE ? 1 : 8], shift[G][ALIKE ? 1 : 8], by[G][8], off[G][8];
     template <int LPR, int MODE>
@@ -788,7 +789,8 @@ bool block_a_cloud(int64_t n, int c, int n_clouds)
     return steps <= 80 && steps <= 10 * (int64_t)n_clouds;
 }
 // Whether the blocks that write y join the chunks' statistics for themselves: that saves a launch and costs each a read of their clouds' (8 groups,
-// 115 200 x 64 of one cloud: 19.4 us for 20.7; 16 groups 23.7 for 21.6; 30 000 x 64, 235 chunks of 16 groups: 13.6 for 15.0)
+// 115 200 x 64 of one cloud: 19.4 us for 20.7; 16 groups 23.7 for 21.6; 30 000 x 64, 235 chunks of 16 groups: 13.6 for 15.0).  All chunks count, as if
+// one cloud had them; of several clouds, whose blocks read less, some take the launch that need not.
 bool join_in_place(const GroupNormSizes &s, int groups) { return (int64_t)s.chunks * groups <= 4096; }
 
 }  // namespace

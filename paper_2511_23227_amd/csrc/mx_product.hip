@@ -102,6 +102,8 @@ __device__ inline void tile_of(uint32_t id, uint32_t rows, uint32_t columns, uin
     y = 8u * band + in - x * high;
 }
 
+// A wave of the 256 x 256 tile has a SIMD and its 512 registers to itself.  With fp32 results two registers go to scratch behind the loop, where they
+// are stored; none of the waits that count requests has scratch accesses beside it (8192 x 8192 x 8192 to fp32 315 us, to bf16 325).
 // PARTS: blockIdx.y's part of the sum.  ONE: the sum has one stage.  X: a's rows come as they are, in that type (uint8_t: in 4 bits), and the block rounds its own.
 template <typename T, typename X, bool PARTS, bool ONE, int WA, int WB, int FA, int FB>
 __global__ __launch_bounds__(64 * WA * WB, ONE ? 4 : (FA == 8 ? 1 : 2)) void tile_kernel(const MxProductArgs p, const X *__restrict__ rows, int64_t ld_rows, uint32_t tile_rows,
