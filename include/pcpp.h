@@ -425,7 +425,7 @@ PCPP_API int pcpp_dropout_bwd(const void *dy, const int64_t *random, uint32_t si
  *   y          [n, c] dtype, contiguous, 16-byte aligned, as are dy and dx
  *   mean_rstd  [n_clouds, groups, 2] fp32, 8-byte aligned, for the gradient (NULL: not wanted); (0, 0) for an empty cloud
  *   workspace  pcpp_group_norm_workspace_bytes(n, c, n_clouds, groups, 0) bytes, 256-byte aligned (may be NULL if that is 0)
- * An Inf or NaN makes its cloud's group NaN, and no other.  Squares are summed in fp32: where the sum passes its range (deviations of 2^60) rstd is 0.
+ * An Inf or NaN makes its cloud's group NaN, and no other.  Squares are summed in fp32: where the sum passes its range (deviations of 2^60) rstd is 0 or NaN.
  *
  * Gradients, from dy [n, c] dtype, contiguous, and the forward pass's mean_rstd:
  *   dz = drop(dy) * act'(z),  dx = rstd * (w * dz - m1 - v * m2),  m1, m2 = means of w * dz and of w * dz * v over the cloud and group,

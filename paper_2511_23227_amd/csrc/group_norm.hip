@@ -10,7 +10,9 @@
 // nothing of the clouds but their number, and every sum has one order.
 //
 // Statistics: a lane sums x - k and (x - k)^2, k the range's first row, which cannot lose what the variance is made of unless that row lies
-// thousands of deviations off; channels, chunks and clouds are joined by their means and sums of squares about them.
+// thousands of deviations off; channels, chunks and clouds are joined by their means and sums of squares about them.  x - mean is formed before anything
+// is multiplied by it: a channel that is constant in its cloud has v = 0 whatever its size (with z = x (w rstd) + (b - mean w rstd) it was off by 2^-24
+// mean rstd, with x = 1e5 and eps = 1e-5 by 2).
 //
 // Forward x is read twice, backward x and dy are, since nothing can be written before the last row of a cloud is known; the second pass goes from the
 // end on, where the caches still have rows.  1 000 000 x 256 bf16 takes 310 us forward (1.5 GB moved at 5.0 TB/s) and 511 backward with dropout (2.6
@@ -276,7 +278,7 @@ __device__ inline void lane_pairs(const float *pairs, const Divisor &width, cons
         }
 }
 
-// y of rows [lo, hi), not empty: z = x by + off.  The weights and the first rows are on their way while `statistics` finds the cloud's, the next ones while some are
+// y of rows [lo, hi), not empty: z = (x - mean) by + b.  The weights and the first rows are on their way while `statistics` finds the cloud's, the next ones while some are
 // written.
 template <bool ALIKE, typename T, int LPR, int G, int MODE, typename F>
 __device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const Divisor &width, const Philox &philox, F statistics)
@@ -294,17 +296,14 @@ __device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t h
     };
     int64_t first = lo + (int64_t)wave_of() * ROWS;
     load(first, raw);
-    float by[G][8], off[G][8], mean[G][ALIKE ? 1 : 8], rstd[G][ALIKE ? 1 : 8];
+    float by[G][8], b[G][8], mean[G][ALIKE ? 1 : 8], rstd[G][ALIKE ? 1 : 8];
     load_affine(a.w, 1.f, lane.own, a.c, by);
-    load_affine(a.b, 0.f, lane.own, a.c, off);
+    load_affine(a.b, 0.f, lane.own, a.c, b);
     lane_pairs<ALIKE>(statistics(), width, lane, mean, rstd);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            by[g][e] *= rstd[g][ALIKE ? 0 : e];
-            off[g][e] = __builtin_fmaf(-mean[g][ALIKE ? 0 : e], by[g][e], off[g][e]);
-        }
+        for (int e = 0; e < 8; ++e) by[g][e] *= rstd[g][ALIKE ? 0 : e];
     for (; first < hi; first += AT_ONCE * STEP) {
         Eight<T> next[AT_ONCE][G];
         load(first + AT_ONCE * STEP, next);
@@ -319,7 +318,7 @@ __device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t h
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[g][e] = activate<decltype(act)::value>(__builtin_fmaf(v[g][e], by[g][e], off[g][e]));
+                    for (int e = 0; e < 8; ++e) v[g][e] = activate<decltype(act)::value>(__builtin_fmaf(v[g][e] - mean[g][ALIKE ? 0 : e], by[g][e], b[g][e]));
             });
             if (a.drop.threshold) {
                 drop_rows(philox, (uint32_t)first + row, c, a.drop, lane, v);
@@ -338,26 +337,19 @@ __device__ inline void apply_range(const GroupNormArgs &a, int64_t lo, int64_t h
     }
 }
 
-// What the gradients' two passes know of a lane's channels.  v = x rstd + shift, z = x by + off: one operation each, and two roundings the size of
-// mean rstd where (x - mean) rstd has that of the mean itself alone (gradients of 99 991 x 91 fp32: 1.2e-7 of their length off, plain operations in fp32 0.8e-7).
+// What the gradients' two passes know of a lane's channels.  v = (x - mean) rstd, z = (x - mean) by + b
 template <bool ALIKE, int G> struct Known {
-    float rstd[G][ALIKE ? 1 : 8], shift[G][ALIKE ? 1 : 8], by[G][8], off[G][8];
+    float mean[G][ALIKE ? 1 : 8], rstd[G][ALIKE ? 1 : 8], by[G][8], b[G][8];
     template <int LPR, int MODE>
     __device__ inline void load(const GroupNormArgs &a, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width)
     {
         load_affine(a.w, 1.f, lane.own, a.c, by);
-        load_affine(a.b, 0.f, lane.own, a.c, off);
-        lane_pairs<ALIKE>(stats, width, lane, shift, rstd);
+        load_affine(a.b, 0.f, lane.own, a.c, b);
+        lane_pairs<ALIKE>(stats, width, lane, mean, rstd);
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                by[g][e] *= rstd[g][ALIKE ? 0 : e];
-                off[g][e] = __builtin_fmaf(-shift[g][ALIKE ? 0 : e], by[g][e], off[g][e]);
-            }
-#pragma unroll
-            for (int e = 0; e < (ALIKE ? 1 : 8); ++e) shift[g][e] *= -rstd[g][e];
-        }
+            for (int e = 0; e < 8; ++e) by[g][e] *= rstd[g][ALIKE ? 0 : e];
     }
 };
 
@@ -375,7 +367,7 @@ template <typename T, int G> struct Rows {
             row_load<T>(ds, lane.template offset<T>(g, lane.row, a.c), lane.own[g], dy[g]);
         }
     }
-    // x and what flows to z, without the scale of the dropout; zeros in rows past the last
+    // x - mean and what flows to z, without the scale of the dropout, which is zero in rows past the last
     template <bool ALIKE, int LPR, int MODE>
     __device__ inline void gradient(const GroupNormArgs &a, const Known<ALIKE, G> &known, uint32_t at, const Lane<LPR, G, MODE> &lane, const Philox &philox, float (&xv)[G][8],
                                     float (&d)[G][8]) const
@@ -387,12 +379,13 @@ template <typename T, int G> struct Rows {
         }
         if (a.drop.threshold) drop_rows(philox, at, a.c, a.drop, lane, d);
         as_act(a.act, [&](auto act) {
-            if constexpr (decltype(act)::value != PCPP_ACT_NONE) {
 #pragma unroll
-                for (int g = 0; g < G; ++g)
+            for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) d[g][e] *= slope<decltype(act)::value>(__builtin_fmaf(xv[g][e], known.by[g][e], known.off[g][e]));
-            }
+                for (int e = 0; e < 8; ++e) {
+                    xv[g][e] -= known.mean[g][ALIKE ? 0 : e];
+                    if constexpr (decltype(act)::value != PCPP_ACT_NONE) d[g][e] *= slope<decltype(act)::value>(__builtin_fmaf(xv[g][e], known.by[g][e], known.b[g][e]));
+                }
         });
     }
 };
@@ -422,16 +415,15 @@ __device__ inline void range_gradients(const GroupNormArgs &a, int64_t lo, int64
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 s[g][e] += d[g][e];
-                q[g][e] = __builtin_fmaf(d[g][e], __builtin_fmaf(x[g][e], known.rstd[g][ALIKE ? 0 : e], known.shift[g][ALIKE ? 0 : e]), q[g][e]);
+                q[g][e] = __builtin_fmaf(d[g][e], x[g][e], q[g][e]);
             }
         rows = next;
     }
-    if (a.drop.threshold) {
+    const float scale = a.drop.threshold ? a.drop.scale : 1.f;
 #pragma unroll
-        for (int g = 0; g < G; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[g][e] *= a.drop.scale, q[g][e] *= a.drop.scale;
-    }
+        for (int e = 0; e < 8; ++e) s[g][e] *= scale, q[g][e] *= scale * known.rstd[g][ALIKE ? 0 : e];
     channel_sums<LPR, G, MODE, CP>(s, q, lane, a.c, sums, total);
 }
 
@@ -454,7 +446,7 @@ template <int CP> __device__ inline void group_means(const GroupNormArgs &a, con
     __syncthreads();
 }
 
-// dx of rows [lo, hi), not empty:  rstd (w dz - m1 - v m2) = dz (w rstd) + x (-rstd^2 m2) - rstd (m1 + shift m2).  `means` finds m1 and m2.
+// dx of rows [lo, hi), not empty:  rstd (w dz - m1 - v m2) = dz (w rstd) + (x - mean) (-rstd^2 m2) - rstd m1.  `means` finds m1 and m2.
 template <bool ALIKE, typename T, int LPR, int G, int MODE, typename F>
 __device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_t hi, const Lane<LPR, G, MODE> &lane, const float *stats, const Divisor &width,
                                       const Philox &philox, F means)
@@ -472,7 +464,7 @@ __device__ inline void gradient_range(const GroupNormArgs &a, int64_t lo, int64_
     for (int g = 0; g < G; ++g) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            m1[g][e] = -known.rstd[g][e] * __builtin_fmaf(known.shift[g][e], m2[g][e], m1[g][e]);
+            m1[g][e] *= -known.rstd[g][e];
             m2[g][e] *= -known.rstd[g][e] * known.rstd[g][e];
         }
 #pragma unroll

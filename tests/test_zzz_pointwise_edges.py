@@ -1,4 +1,4 @@
-"""The pointwise layers' operators where a batch has no rows, offsets make no sense, a single row lies anywhere; and which of the group norm's ways
+"""The pointwise layers' operators where a batch has no rows, offsets make no sense, a single row lies anywhere, a channel is constant; and which of the group norm's ways
 through the rows each size takes.
 
 The forward pass needs no workspace where a block takes a cloud from its statistics to its rows; by chunks it needs two numbers for every
@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 import torch
 
-from pointwise_reference import BF16, F32, U, activate, group_norm, group_norm_grads
+from pointwise_reference import BF16, F32, U, activate, group_norm, group_norm_grads, slope
 from test_zzz_pointwise import pcpp, rng, rows_of, within  # noqa: F401  (pcpp: the fixture)
 
 gpu = pytest.mark.gpu
@@ -216,3 +216,36 @@ def test_by_chunks_clouds_without_a_row(pcpp, n, c, groups, clouds, launch):
     assert not stats.any() and not dw.any() and not db.any()
     for t in (y, dx):
         assert (t.view(torch.uint8) == 0x5A).all()
+
+
+# ---- channels that are the same in every row ---------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("n,c,offsets", [(40, 24, [0, 1, 2, 17, 40]), (60, 5, None), (9000, 16, [0, 4000, 9000]), (9000, 91, [0, 1, 9000]), (900, 1023, [0, 300, 900]),
+                                         (70_000, 64, [0, 35_000, 70_000])])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_constant_channels(pcpp, n, c, offsets, dtype, act):
+    """Groups of one channel that a cloud's rows all share, from 1 to 3e5: x - mean is zero without a rounding, so y is act(b), dw is zero and dx has no
+    share of v, however small eps is beside the numbers."""
+    g = torch.Generator().manual_seed(91)
+    w, b = (1 + 0.3 * torch.randn(c, generator=g)).cuda(), (0.3 * torch.randn(c, generator=g)).cuda()
+    ranges = [(0, n)] if offsets is None else list(zip(offsets[:-1], offsets[1:]))
+    x, dy = torch.empty(n, c, dtype=dtype), rows_of(n, c, dtype, 92)
+    for lo, hi in ranges:
+        x[lo:hi] = (torch.exp(12.6 * torch.rand(1, c, generator=g)) * torch.sign(torch.randn(1, c, generator=g))).to(dtype)
+    off = None if offsets is None else torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    code = {"none": pcpp.ACT_NONE, "silu": pcpp.ACT_SILU}[act]
+    eps, rstd = 1e-5, float(np.float32(1e-5)) ** -0.5
+    y = pcpp.pcpp_group_norm_fwd(x.cuda(), c, w, b, off, act=code, eps=eps)
+    z = b.double().cpu()
+    ref = activate(z, act).expand(n, c)
+    within(y.y, ref, 16 * U * (z.abs() + ref.abs()), "y")
+    d = pcpp.pcpp_group_norm_bwd(dy, x.cuda(), y.mean_rstd, w, b, off, act=code)
+    assert not d.dw.any()
+    dz = dy.double().cpu() * slope(z, act)
+    for lo, hi in ranges:
+        depth, t = 64 + (hi - lo) / 32, w.double().cpu() * dz[lo:hi]
+        m1 = t.mean(0)
+        bound = rstd * (16 * U * (t.abs() + m1.abs() + (w.double().cpu() * dy[lo:hi].double().cpu()).abs()) + (depth + 16) * U * t.abs().mean(0))
+        within(d.dx[lo:hi], rstd * (t - m1), bound, "dx")
