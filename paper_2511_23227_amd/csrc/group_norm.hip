@@ -15,10 +15,10 @@
 // mean rstd, with x = 1e5 and eps = 1e-5 by 2).
 //
 // Forward x is read twice, backward x and dy are, since nothing can be written before the last row of a cloud is known; the second pass goes from the
-// end on, where the caches still have rows.  1 000 000 x 256 bf16 takes 310 us forward (1.5 GB moved at 5.0 TB/s) and 511 backward with dropout (2.6
-// GB, 5.0 TB/s: memory, with the generator's and the activation's 42 000 vector instructions a wave for each pass beside it); 99 991 x 91 fp32 44
-// backward (4.1 TB/s; three launches).  115 200 x 64 takes 26.8 forward where its bytes take 9: two kernels of 10 and 18.  Of the second about 8 are
-// the vector instructions of gelu and dropout (2400 a wave), the rest a chain of the first loads and the statistics joined over 56 chunks, which two
+// end on, where the caches still have rows.  1 000 000 x 256 bf16 takes 316 us forward (1.5 GB moved at 4.9 TB/s) and 511 backward with dropout (2.6
+// GB, 5.0 TB/s: memory, with the generator's and the activation's 43 000 vector instructions a wave for each pass beside it); 99 991 x 91 fp32 44
+// backward (4.1 TB/s; three launches).  115 200 x 64 takes 27 forward where its bytes take 9: two kernels of 9.5 and 19.  Of the second about 8 are
+// the vector instructions of gelu and dropout (2500 a wave), the rest a chain of the first loads and the statistics joined over 56 chunks, which two
 // waves a SIMD do not hide (blocks of half and a quarter of the rows for it: as long, and 2 us more).
 #include "pointwise.h"
 
